@@ -20,6 +20,12 @@
  *                     attention-state merge (App. F)
  *   hk_append_kv      append-only dense-tier write of one decode step (Sec. 3.1 Step 1)
  *   hk_alloc_init     a fresh device page allocator
+ * Several new tokens per sequence (prompts filled chunk by chunk, drafted tokens):
+ *   hk_reserve_slots  tables, masks and slot maps of the chunks, from their lengths
+ *   hk_write_kv       K and V rows into the pool through a slot map
+ *   hk_chunk_attn     causal attention of the chunks over the paged cache
+ *   hk_verify_draft   drafted tokens against the target's probabilities
+ *   hk_trim_slots     the newest slots of every head back to the pool
  * Step 4 (Sec. 3.1, hard budget; Sec. 3.3.1 budget thresholds L_lower / L_upper):
  *   hk_score_rows     each window row's own attention probabilities over the candidates
  *   hk_vote_topp      Cautious Update: every row's own Top-p set, counted as votes
@@ -80,9 +86,12 @@ enum {
 };
 /* bits OR-ed into the device status word */
 enum {
-  HK_FLAG_NOSPACE = 1,   /* hk_compact / hk_append_kv: free list too short; cache left unchanged */
+  HK_FLAG_NOSPACE = 1,   /* hk_compact / hk_append_kv / hk_reserve_slots: free list too short or
+                            a row full; cache left unchanged                           */
   HK_FLAG_NAN = 2,       /* a NaN probability was met and given weight 0               */
-  HK_FLAG_RANGE = 4      /* a probability outside [0,1] was clamped                    */
+  HK_FLAG_RANGE = 4,     /* a probability outside [0,1] was clamped                    */
+  HK_FLAG_CHUNK = 8      /* hk_reserve_slots: chunk starts not ascending or outside the
+                            token rows, or a chunk over max_len; cache left unchanged  */
 };
 
 typedef enum { HK_F32 = 0, HK_BF16 = 1 } hk_dtype;
@@ -115,7 +124,7 @@ typedef struct {
 } hk_dims;
 
 enum { HK_OP_SCORE = 0, HK_OP_COMPACT = 1, HK_OP_DECODE = 2, HK_OP_APPEND = 3, HK_OP_COMPRESS = 4,
-       HK_OP_SELECT = 5 };
+       HK_OP_SELECT = 5, HK_OP_RESERVE = 6, HK_OP_TRIM = 7 };
 
 /* Bytes of workspace entry point `op` needs for these dims and table width (HK_OP_SELECT:
  * hk_select_workspace_size(dims->NS * dims->Hkv, 16 * max_pages)). */
@@ -392,6 +401,122 @@ hk_status hk_append_kv(const hk_dims* dims, const hk_paged_kv* kv, const void* k
                        const void* v_new, const hk_allocator* alloc, int32_t* status,
                        void* workspace, size_t ws_bytes, hipStream_t stream);
 
+/* ------------------------------------------------------------------ a7: chunks of new tokens
+ * The append-only write (Sec. 3.1 Step 1) and the decode attention (App. F) for any number of
+ * new tokens per sequence in one call: prompts filled chunk by chunk, drafted tokens tested
+ * together, single tokens beside them.  A step of one layer is
+ *   hk_reserve_slots -> hk_write_kv -> hk_chunk_attn,
+ * and after a draft hk_verify_draft -> hk_trim_slots; hk_reserve_slots and hk_trim_slots may take
+ * every layer of the cache at once.
+ *
+ * The new tokens of the batch lie behind one another in token rows; sequence s has the rows
+ * [start[s], start[s + 1]), possibly none.  Rows outside every chunk are padding: no call reads
+ * or writes them, but for their slot map entries (-1).  max_len bounds the launches: it need not
+ * be met.  Only the fields' sizes are seen by the host, so one captured graph serves every
+ * mixture of lengths within them.
+ */
+typedef struct {
+  const int32_t* start;  /* [n_seq + 1] device, ascending, within [0, n_tokens]         */
+  int32_t n_seq;         /* sequences of the batch                                      */
+  int32_t n_tokens;      /* rows of the token tensors                                   */
+  int32_t max_len;       /* no chunk is longer                                          */
+} hk_chunks;
+
+/* Slots for the chunks at the rows' ends.  Token i of a chunk of len goes to logical slot
+ * end + i, where end is one past the highest valid slot of the row's newest page (that page's
+ * first slot if none is valid; 0 for an empty row), in every KV head and layer of its sequence:
+ *   need = max(0, ceil((end + len) / 16) - n_pages)  pages are popped for a head, in head order
+ *   and ascending page order (the pops are free_ids[top - sum need ...]), n_pages grows by
+ *   them, and the mask bits of [end, end + len) are set.
+ * dims->NS may be any multiple of chunks->n_seq: sequence s of the cache then has the chunk of
+ * s % n_seq (layers one after the other).
+ *   slot_map [NS / n_seq][n_tokens][Hkv] int64 or NULL: 16 * page + slot of every row, -1 for
+ *            padding; K row r of the pool as [16 * num_pages][D] is then slot_map's.
+ * All or nothing: if the free list is too short or a row would pass max_pages (HK_FLAG_NOSPACE),
+ * or the chunks are not as promised (HK_FLAG_CHUNK), the cache is left as it was and slot_map is
+ * all -1, so that hk_write_kv writes nothing; hk_chunk_attn then reads the rows as they are, and
+ * hk_trim_slots must not be called for the slots that were never given.
+ * Until hk_write_kv has run the new slots hold what the pool held.
+ * workspace: >= hk_workspace_size(HK_OP_RESERVE) bytes, 256-byte aligned.
+ * HK_ERR_ARG for null pointers or sizes below 1, HK_ERR_SHAPE unless NS % n_seq == 0, n_tokens and
+ * max_len <= 2^24, and heads x pages touched + slot map entries < 2^31; alloc->capacity >= 1.
+ */
+hk_status hk_reserve_slots(const hk_dims* dims, const hk_paged_kv* kv, const hk_chunks* chunks,
+                           const hk_allocator* alloc, int64_t* slot_map, int32_t* status,
+                           void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* K and V rows into the pool: row (layer l, token t, KV head h) of k_new and v_new goes to pool
+ * row slot_map[l][t][h]; rows whose entry lies outside [0, 16 * num_pages) are skipped.
+ *   k_new    element (l, t, h, d) at k_new[l * k_layer_stride + t * k_row_stride + h * D + d], in
+ *            kv->dtype (e.g. a slice of a projection that holds Q, K and V side by side);
+ *            v_new likewise.  Strides in elements, their bytes multiples of 16; row strides of at
+ *            least Hkv * D; pointers 16-byte aligned (HK_ERR_ALIGN).
+ * Two rows with one slot race.  Of kv only the pools, num_pages and dtype are used.
+ * HK_ERR_SHAPE when n_layers * n_tokens * Hkv * (pieces of 16 bytes in a row) reaches 2^31.
+ */
+hk_status hk_write_kv(const hk_dims* dims, const hk_paged_kv* kv, int32_t n_layers,
+                      int32_t n_tokens, const int64_t* slot_map, const void* k_new,
+                      int64_t k_layer_stride, int64_t k_row_stride, const void* v_new,
+                      int64_t v_layer_stride, int64_t v_row_stride, hipStream_t stream);
+
+/* Causal attention of every chunk over its sequence's row (App. F), the chunk's own tokens being
+ * the row's newest slots: with end as above and len the chunk's length, query i of the chunk sees
+ * the valid slots j <= end - len + i of each KV head h:
+ *   o = sum_j Softmax_j(sm_scale q.k_j) v_j,   lse = log sum_j exp(sm_scale q.k_j).
+ * A query that sees no valid slot gives o = 0, lse = -inf.  K and V of masked slots and of slots
+ * past the row's end are not read into the result, whatever they hold.
+ *   q    row t, head g at q[t * q_row_stride + g * D], in kv->dtype; q_row_stride >= Hq * D, its
+ *        bytes a multiple of 16; 16-byte aligned
+ *   o    [n_tokens][Hq][D] in kv->dtype, 16-byte aligned
+ *   lse  [n_tokens][Hq] fp32 or NULL
+ * dims->NS == chunks->n_seq; Hq / Hkv at most 64.  Scores, sums and outputs are accumulated in
+ * fp32; a bf16 cache's probabilities enter the product with V in bf16.
+ * workspace: >= hk_chunk_attn_workspace_size(dims, chunks, kv->max_pages) bytes, 256-byte aligned
+ * (0 for some sizes: it may then be NULL); calls that overlap on one workspace race.
+ */
+size_t hk_chunk_attn_workspace_size(const hk_dims* dims, const hk_chunks* chunks,
+                                    int32_t max_pages);
+hk_status hk_chunk_attn(const hk_dims* dims, const hk_paged_kv* kv, const hk_chunks* chunks,
+                        const void* q, int64_t q_row_stride, float sm_scale, void* o, float* lse,
+                        void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* Drafted tokens against the target's probabilities.  The chunk of a sequence is the last token
+ * that stands followed by its drafts: with a = start[s], tokens[a + i], i >= 1, are the drafts,
+ * row t of p is the target's distribution of the token after row t, and row t of q the one that
+ * tokens[t] was drafted from (q NULL: drafts without a choice, probability 1).  With
+ *   F(x) = floor(2^40 clamp(x, 0, 1)) (NaN counts as 0),   m(u) = floor(2^24 clamp(u, 0, 1 - 2^-24))
+ * draft t is kept while m(u[t]) F(q[t][x]) < 2^24 F(p[t - 1][x]), x = tokens[t]: probability
+ * min(1, p / q).  A draft outside [0, V) is not kept.  n_accept[s] = r drafts are kept, n_drop[s] =
+ * len - 1 - r are not, and
+ *   next_token[s] = min{ v : sum_{w <= v} weight > floor(m(u[a]) * sum weight / 2^24) },
+ *   weight[v] = max(0, F(p[a + r][v]) - F(q[a + r + 1][v])) where a draft was rejected (with q NULL:
+ *   F(p) without the rejected token), F(p[a + r][v]) where none was or where the former sum is 0;
+ * -1 if every weight is 0.  Whole numbers throughout: the same inputs give the same tokens whatever
+ * the batch.  An empty chunk gives 0, -1, 0.
+ *   tokens [n_tokens] int32; u [n_tokens] fp32; p row t at p + t * p_row_stride, q likewise, in
+ *   `dtype` (HK_F32 or HK_BF16), strides in elements, >= V, any alignment of the type
+ *   n_accept, next_token, n_drop [n_seq] int32; n_drop is what hk_trim_slots takes
+ *   status  int32 or NULL: HK_FLAG_NAN / HK_FLAG_RANGE of the rows next_token was drawn from
+ * V in [1, 2^20]; workspace: >= hk_verify_workspace_size(n_seq, V) bytes, 256-byte aligned.
+ */
+size_t hk_verify_workspace_size(int32_t n_seq, int32_t V);
+hk_status hk_verify_draft(const hk_chunks* chunks, int32_t V, hk_dtype dtype, const int32_t* tokens,
+                          const void* p, int64_t p_row_stride, const void* q, int64_t q_row_stride,
+                          const float* u, int32_t* n_accept, int32_t* next_token, int32_t* n_drop,
+                          int32_t* status, void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* The newest slots back to the pool: of every head of sequence s (s % n_seq, layers one after the
+ * other, as for hk_reserve_slots) the last drop = max(0, n_drop[s % n_seq]) logical slots,
+ *   end' = max(0, end - drop): mask bits from end' on are cleared, pages from ceil(end' / 16) on are
+ *   pushed, in head order and ascending page order, their table entries set to -1.
+ * Undoes hk_reserve_slots of the same lengths, free list included.  A head with drop = 0 is left as
+ * it is.  alloc->capacity >= kv->num_pages (HK_ERR_ARG otherwise).
+ * workspace: >= hk_workspace_size(HK_OP_TRIM) bytes, 256-byte aligned.
+ */
+hk_status hk_trim_slots(const hk_dims* dims, const hk_paged_kv* kv, int32_t n_seq,
+                        const int32_t* n_drop, const hk_allocator* alloc, void* workspace,
+                        size_t ws_bytes, hipStream_t stream);
+
 /* ------------------------------------------------------------------ Step 4: hard budget
  * The hard budget of the continuous compression pipeline (Sec. 3.1 Step 4 and the Condensed
  * tier; Sec. 3.3.1 budget thresholds): a head whose memory exceeds L_upper is rewritten under
@@ -499,7 +624,13 @@ enum {
   HK_TK_VOTE_COUNT = 14,   /* hk_vote_topp: column counts of the row bitmaps             */
   HK_TK_BUDGET_PLAN = 15,  /* hk_budget_plan                                             */
   HK_TK_BUDGET_SELECT = 16,/* hk_budget_select                                           */
-  HK_TK_COUNT = 17
+  HK_TK_RESERVE = 17,      /* hk_reserve_slots: count + write, timed together            */
+  HK_TK_WRITE_KV = 18,     /* hk_write_kv                                                */
+  HK_TK_CHUNK_ATTN = 19,   /* hk_chunk_attn: attention of rows and splits                */
+  HK_TK_CHUNK_MERGE = 20,  /* hk_chunk_attn: merge of the splits' states                 */
+  HK_TK_VERIFY = 21,       /* hk_verify_draft: sums + pick, timed together               */
+  HK_TK_TRIM = 22,         /* hk_trim_slots: count + write, timed together               */
+  HK_TK_COUNT = 23
 };
 hk_status hk_timing_enable(uint32_t kernel_mask);
 hk_status hk_timing_read(int32_t kernel, double* total_ms, int64_t* launches);

@@ -24,13 +24,16 @@ __all__ = ["HardKVError", "lib", "PagedKV", "Allocator", "hk_score", "hk_calibra
            "PROBE_MFMA4", "hk_decode_plan",
            "hk_decode_attn_noalloc", "hk_decode_noalloc_scratch_bytes", "ERR_SCRATCH",
            "OP_SELECT", "hk_select_workspace_size", "select_workspace", "hk_topp_select_ws",
-           "hk_calibrate_topp_ws"]
+           "hk_calibrate_topp_ws", "Chunks", "OP_RESERVE", "OP_TRIM", "FLAG_CHUNK", "hk_reserve_slots",
+           "hk_write_kv", "hk_chunk_attn_workspace_size", "chunk_attn_workspace", "hk_chunk_attn",
+           "hk_verify_workspace_size", "verify_workspace", "hk_verify_draft", "hk_trim_slots"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libhardkv.so")
 
 HK_F32, HK_BF16 = 0, 1
 OP_SCORE, OP_COMPACT, OP_DECODE, OP_APPEND, OP_COMPRESS, OP_SELECT = 0, 1, 2, 3, 4, 5
-FLAG_NOSPACE, FLAG_NAN, FLAG_RANGE = 1, 2, 4
+OP_RESERVE, OP_TRIM = 6, 7
+FLAG_NOSPACE, FLAG_NAN, FLAG_RANGE, FLAG_CHUNK = 1, 2, 4, 8
 ERR_SCRATCH = 7
 BUDGET_KEEP, BUDGET_SPARSE, BUDGET_REWRITE = 0, 1, 2
 PROBE_EXP, PROBE_MFMA, PROBE_MIX, PROBE_SPLIT, PROBE_VALU, PROBE_MFMA4 = 0, 1, 2, 3, 4, 5
@@ -40,11 +43,14 @@ EXPORTED = ["hk_score", "hk_calibrate", "hk_calibrate_solve_T", "hk_topp_select"
             "hk_score_rows", "hk_vote_topp", "hk_budget_plan", "hk_budget_select",
             "hk_compact_modes", "hk_calibrate_solve_T_gd", "hk_alloc_init", "hk_compress",
             "hk_probe", "hk_decode_plan", "hk_decode_attn_noalloc", "hk_decode_noalloc_scratch_bytes",
-            "hk_select_workspace_size", "hk_topp_select_ws", "hk_calibrate_topp_ws"]
+            "hk_select_workspace_size", "hk_topp_select_ws", "hk_calibrate_topp_ws",
+            "hk_reserve_slots", "hk_write_kv", "hk_chunk_attn_workspace_size", "hk_chunk_attn",
+            "hk_verify_workspace_size", "hk_verify_draft", "hk_trim_slots"]
 # kernel ids of hk_timing_read, in header order
 TIMED_KERNELS = ["score_pass1", "score_merge", "score_pass2", "calibrate", "topp", "solve_T",
                  "compact_gather", "compact_meta", "decode_split", "decode_merge", "append",
-                 "calib_topp", "score_rows", "vote", "vote_count", "budget_plan", "budget_select"]
+                 "calib_topp", "score_rows", "vote", "vote_count", "budget_plan", "budget_select",
+                 "reserve", "write_kv", "chunk_attn", "chunk_merge", "verify", "trim"]
 
 
 class HardKVError(RuntimeError):
@@ -64,6 +70,11 @@ class hk_paged_kv(C.Structure):
 
 class hk_allocator(C.Structure):
     _fields_ = [("free_ids", C.c_void_p), ("free_top", C.c_void_p), ("capacity", C.c_int32)]
+
+
+class hk_chunks(C.Structure):
+    _fields_ = [("start", C.c_void_p), ("n_seq", C.c_int32), ("n_tokens", C.c_int32),
+                ("max_len", C.c_int32)]
 
 
 _lib = None
@@ -140,6 +151,26 @@ def lib():
         L.hk_decode_noalloc_scratch_bytes.argtypes = [C.POINTER(hk_dims), I32]
         L.hk_decode_plan.restype = I32
         L.hk_decode_plan.argtypes = [C.POINTER(hk_dims), I32, C.POINTER(I32), C.POINTER(I32)]
+        I64 = C.c_int64
+        L.hk_reserve_slots.restype = I32
+        L.hk_reserve_slots.argtypes = [C.POINTER(hk_dims), C.POINTER(hk_paged_kv),
+                                       C.POINTER(hk_chunks), C.POINTER(hk_allocator), P, P, P, SZ, P]
+        L.hk_write_kv.restype = I32
+        L.hk_write_kv.argtypes = [C.POINTER(hk_dims), C.POINTER(hk_paged_kv), I32, I32, P, P, I64,
+                                  I64, P, I64, I64, P]
+        L.hk_chunk_attn_workspace_size.restype = SZ
+        L.hk_chunk_attn_workspace_size.argtypes = [C.POINTER(hk_dims), C.POINTER(hk_chunks), I32]
+        L.hk_chunk_attn.restype = I32
+        L.hk_chunk_attn.argtypes = [C.POINTER(hk_dims), C.POINTER(hk_paged_kv), C.POINTER(hk_chunks),
+                                    P, I64, F, P, P, P, SZ, P]
+        L.hk_verify_workspace_size.restype = SZ
+        L.hk_verify_workspace_size.argtypes = [I32, I32]
+        L.hk_verify_draft.restype = I32
+        L.hk_verify_draft.argtypes = [C.POINTER(hk_chunks), I32, I32, P, P, I64, P, I64, P, P, P, P,
+                                      P, P, SZ, P]
+        L.hk_trim_slots.restype = I32
+        L.hk_trim_slots.argtypes = [C.POINTER(hk_dims), C.POINTER(hk_paged_kv), I32, P,
+                                    C.POINTER(hk_allocator), P, SZ, P]
         L.hk_probe.restype = I32
         L.hk_probe.argtypes = [I32, I32, I32, P, P]
         L.hk_timing_enable.restype = I32
@@ -409,6 +440,131 @@ def hk_compact_modes(d: hk_dims, kv: PagedKV, sel_bits, L_dense: int, head_mode,
     _check(lib().hk_compact_modes(C.byref(d), C.byref(kv.desc), _ptr(sel_bits), int(L_dense),
                                   _ptr(head_mode), C.byref(alloc.desc), _ptr(status), _ptr(ws),
                                   ws.numel(), _stream(stream)), "hk_compact_modes")
+
+
+# ---------------------------------------------------------------- chunks of new tokens
+# The wrappers below compare the tensors with the sizes given (a row too few would be read past
+# its end) and run on the tensors' own device, on its current stream unless one is given.
+class Chunks:
+    """The new tokens of a batch: sequence s has the token rows start[s] .. start[s + 1] of
+    n_tokens (start: int32 device tensor of n_seq + 1 entries), at most max_len of them."""
+
+    def __init__(self, start, n_tokens: int, max_len: int):
+        if start.dtype != torch.int32 or start.dim() != 1 or not start.is_contiguous():
+            raise HardKVError("chunk starts must be a contiguous int32 vector")
+        self.start, self.n_tokens, self.max_len = start, int(n_tokens), int(max_len)
+        self.n_seq = start.numel() - 1
+        self.desc = hk_chunks(start.data_ptr(), self.n_seq, self.n_tokens, self.max_len)
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise HardKVError(what)
+
+
+def _kv_dtype(kv: PagedKV):
+    return kv.k_pool.dtype
+
+
+def _run(name: str, t, stream, *args):
+    """Call an entry point on the device that holds t."""
+    with torch.cuda.device(t.device):
+        s = torch.cuda.current_stream() if stream is None else stream
+        _check(getattr(lib(), name)(*args, C.c_void_p(s.cuda_stream)), name)
+
+
+def _vector(t, n: int, dtype, what: str):
+    _need(t.dtype == dtype and t.is_contiguous() and t.numel() >= n,
+          f"{what} must be a contiguous {dtype} tensor of at least {n} entries")
+    return _ptr(t)
+
+
+def _token_rows(t, n_tokens: int, heads: int, D: int, dtype, what: str):
+    """(pointer, row stride) of a [..., tokens, heads, D] tensor whose rows are contiguous."""
+    _need(t.dtype == dtype and t.dim() >= 3 and tuple(t.shape[-2:]) == (heads, D)
+          and t.shape[-3] >= n_tokens, f"{what} must be [tokens, {heads}, {D}] in {dtype}")
+    _need(t.stride(-1) == 1 and (heads == 1 or t.stride(-2) == D),
+          f"{what}: the heads of a token must be contiguous")
+    return C.c_void_p(t.data_ptr()), t.stride(-3) if n_tokens > 1 else max(t.stride(-3), heads * D)
+
+
+def hk_reserve_slots(d: hk_dims, kv: PagedKV, chunks: Chunks, alloc: Allocator, ws, slot_map=None,
+                     status=None, stream=None):
+    heads = d.NS * d.Hkv
+    _need(kv.page_table.shape[0] >= heads, "the cache has fewer rows than NS * Hkv")
+    n = d.NS // max(chunks.n_seq, 1) * chunks.n_tokens * d.Hkv
+    _run("hk_reserve_slots", kv.page_table, stream, C.byref(d), C.byref(kv.desc),
+         C.byref(chunks.desc), C.byref(alloc.desc),
+         None if slot_map is None else _vector(slot_map, n, torch.int64, "slot_map"), _ptr(status),
+         _ptr(ws), ws.numel())
+
+
+def hk_write_kv(d: hk_dims, kv: PagedKV, n_tokens: int, slot_map, k_new, v_new, stream=None):
+    """k_new, v_new: [tokens, Hkv, D], or [layers, tokens, Hkv, D] with the slot map of as many
+    layers; views into larger tensors are fine as long as a token's heads are contiguous."""
+    _need(k_new.dim() == v_new.dim() and k_new.dim() in (3, 4), "k_new and v_new must be 3- or 4-d")
+    layers = k_new.shape[0] if k_new.dim() == 4 else 1
+    _need(v_new.dim() == 3 or v_new.shape[0] == layers, "k_new and v_new differ in layers")
+    kp, kr = _token_rows(k_new, n_tokens, d.Hkv, d.D, _kv_dtype(kv), "k_new")
+    vp, vr = _token_rows(v_new, n_tokens, d.Hkv, d.D, _kv_dtype(kv), "v_new")
+    _run("hk_write_kv", kv.k_pool, stream, C.byref(d), C.byref(kv.desc), layers, int(n_tokens),
+         _vector(slot_map, layers * n_tokens * d.Hkv, torch.int64, "slot_map"), kp,
+         k_new.stride(0) if layers > 1 else 0, kr, vp, v_new.stride(0) if layers > 1 else 0, vr)
+
+
+def hk_chunk_attn_workspace_size(d: hk_dims, chunks: Chunks, max_pages: int) -> int:
+    return int(lib().hk_chunk_attn_workspace_size(C.byref(d), C.byref(chunks.desc), int(max_pages)))
+
+
+def chunk_attn_workspace(d: hk_dims, chunks: Chunks, max_pages: int, device) -> torch.Tensor:
+    n = max(256, hk_chunk_attn_workspace_size(d, chunks, max_pages))
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def hk_chunk_attn(d: hk_dims, kv: PagedKV, chunks: Chunks, q, sm_scale: float, o, ws, lse=None,
+                  stream=None):
+    T = chunks.n_tokens
+    _need(kv.page_table.shape[0] >= d.NS * d.Hkv, "the cache has fewer rows than NS * Hkv")
+    qp, qr = _token_rows(q, T, d.Hq, d.D, _kv_dtype(kv), "q")
+    _need(q.dim() == 3, "q must be 3-d")
+    op = _vector(o, T * d.Hq * d.D, _kv_dtype(kv), "o")
+    lp = None if lse is None else _vector(lse, T * d.Hq, torch.float32, "lse")
+    _run("hk_chunk_attn", kv.k_pool, stream, C.byref(d), C.byref(kv.desc), C.byref(chunks.desc), qp,
+         qr, float(sm_scale), op, lp, _ptr(ws), 0 if ws is None else ws.numel())
+
+
+def hk_verify_workspace_size(n_seq: int, V: int) -> int:
+    return int(lib().hk_verify_workspace_size(int(n_seq), int(V)))
+
+
+def verify_workspace(n_seq: int, V: int, device) -> torch.Tensor:
+    n = max(256, hk_verify_workspace_size(n_seq, V))
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def hk_verify_draft(chunks: Chunks, V: int, tokens, p, u, n_accept, next_token, n_drop, ws, q=None,
+                    status=None, stream=None):
+    T, B, i32 = chunks.n_tokens, chunks.n_seq, torch.int32
+    dt = {torch.float32: HK_F32, torch.bfloat16: HK_BF16}.get(p.dtype)
+    _need(dt is not None, "probabilities must be float32 or bfloat16")
+    for t, what in ((p, "p"), (q, "q")):
+        _need(t is None or (t.dtype == p.dtype and t.dim() == 2 and t.shape[0] >= T
+                            and t.shape[1] >= V and (t.stride(1) == 1 or V == 1)),
+              f"{what} must be [tokens, V] with contiguous rows, both in one type")
+    row = lambda t: 0 if t is None else (t.stride(0) if T > 1 else max(t.stride(0), V))  # noqa: E731
+    _run("hk_verify_draft", p, stream, C.byref(chunks.desc), int(V), dt,
+         _vector(tokens, T, i32, "tokens"), C.c_void_p(p.data_ptr()), row(p),
+         None if q is None else C.c_void_p(q.data_ptr()), row(q),
+         _vector(u, T, torch.float32, "u"), _vector(n_accept, B, i32, "n_accept"),
+         _vector(next_token, B, i32, "next_token"), _vector(n_drop, B, i32, "n_drop"), _ptr(status),
+         _ptr(ws), ws.numel())
+
+
+def hk_trim_slots(d: hk_dims, kv: PagedKV, n_drop, alloc: Allocator, ws, stream=None):
+    _need(kv.page_table.shape[0] >= d.NS * d.Hkv, "the cache has fewer rows than NS * Hkv")
+    n = n_drop.numel()
+    _run("hk_trim_slots", kv.page_table, stream, C.byref(d), C.byref(kv.desc), n,
+         _vector(n_drop, n, torch.int32, "n_drop"), C.byref(alloc.desc), _ptr(ws), ws.numel())
 
 
 def hk_timing_enable(kernels=None):

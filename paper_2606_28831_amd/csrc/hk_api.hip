@@ -4,6 +4,7 @@
 #include <cmath>
 #include <cstdint>
 
+#include "hk_chunk.h"
 #include "hk_internal.h"
 
 bool hk_decode_supports_group(int G);
@@ -27,14 +28,19 @@ hk_status check_dims(const hk_dims* d, bool need_w) {
   return HK_OK;
 }
 
-hk_status check_kv(const hk_paged_kv* kv, bool need_v) {
+// The tables' pointers are read 16 bytes at a time where `wide`, an entry at a time otherwise (any
+// run of rows of a cache, such as one layer's, then begins at a legal address).
+hk_status check_kv(const hk_paged_kv* kv, bool need_v, bool wide = true) {
   if (!kv || !kv->k_pool || !kv->page_table || !kv->page_mask || !kv->n_pages) return HK_ERR_ARG;
   if (need_v && !kv->v_pool) return HK_ERR_ARG;
   if (kv->dtype != HK_F32 && kv->dtype != HK_BF16) return HK_ERR_DTYPE;
   if (kv->num_pages <= 0 || kv->max_pages <= 0) return HK_ERR_ARG;
   if (kv->max_pages % 2 != 0) return HK_ERR_SHAPE;                 // S_max multiple of 32
   if (!aligned16(kv->k_pool) || (need_v && !aligned16(kv->v_pool))) return HK_ERR_ALIGN;
-  if (!aligned16(kv->page_table) || !aligned16(kv->page_mask) || !aligned16(kv->n_pages))
+  if (wide && (!aligned16(kv->page_table) || !aligned16(kv->page_mask) || !aligned16(kv->n_pages)))
+    return HK_ERR_ALIGN;
+  if ((reinterpret_cast<uintptr_t>(kv->page_table) | reinterpret_cast<uintptr_t>(kv->n_pages)) % 4 ||
+      reinterpret_cast<uintptr_t>(kv->page_mask) % 2)
     return HK_ERR_ALIGN;
   return HK_OK;
 }
@@ -53,6 +59,24 @@ hk_status check_rows_wide(int n_heads, int S_max, const int32_t* cand_len) {
 hk_status launched(hipError_t e) { return e == hipSuccess ? HK_OK : HK_ERR_HIP; }
 
 size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+constexpr int kMaxRows = 1 << 24;        // token rows of a call
+constexpr int kMaxVocab = 1 << 20;
+constexpr int kMaxGroup = 64;            // query heads per KV head of the chunk attention
+
+hk_status check_chunks(const hk_chunks* c) {
+  if (!c || !c->start) return HK_ERR_ARG;
+  if (c->n_seq <= 0 || c->n_tokens <= 0 || c->max_len <= 0) return HK_ERR_ARG;
+  if (c->n_seq > 65535 || c->n_tokens > kMaxRows || c->max_len > kMaxRows) return HK_ERR_SHAPE;
+  return HK_OK;
+}
+
+// token rows of `row` elements of `es` bytes, `stride` elements apart
+hk_status check_rows_at(const void* p, int64_t stride, int64_t row, int es) {
+  if (!p || stride < row) return HK_ERR_ARG;
+  if (!aligned16(p) || stride % (16 / es) != 0) return HK_ERR_ALIGN;
+  return HK_OK;
+}
 
 // Workspace of hk_compress: scores, candidate counts, row LSEs, selection, then the score,
 // selection and compaction scratch (the stages run one after the other; they share one
@@ -88,6 +112,8 @@ size_t hk_workspace_size(int32_t op, const hk_dims* d, int32_t max_pages) {
     case HK_OP_APPEND: return hk_append_ws(d->NS, d->Hkv);
     case HK_OP_COMPRESS: return compress_ws(d, max_pages).total;
     case HK_OP_SELECT: return hk_select_wide_ws(d->NS * d->Hkv, max_pages * HK_PAGE);
+    case HK_OP_RESERVE: return hk_reserve_ws(d->NS * d->Hkv);
+    case HK_OP_TRIM: return hk_trim_ws(d->NS * d->Hkv);
     default: return 0;
   }
 }
@@ -98,6 +124,7 @@ const char* hk_status_string(int32_t code, int32_t flags) {
       case HK_FLAG_NOSPACE: return "HK_FLAG_NOSPACE: page pool exhausted, cache left unchanged";
       case HK_FLAG_NAN: return "HK_FLAG_NAN: NaN probability given weight 0";
       case HK_FLAG_RANGE: return "HK_FLAG_RANGE: probability outside [0,1] clamped";
+      case HK_FLAG_CHUNK: return "HK_FLAG_CHUNK: chunk starts or lengths out of bounds, cache left unchanged";
       default: return "unknown flag";
     }
   }
@@ -503,6 +530,110 @@ hk_status hk_append_kv(const hk_dims* dims, const hk_paged_kv* kv, const void* k
   if (!aligned256(workspace)) return HK_ERR_ALIGN;
   return launched(hk_launch_append(dims->NS, dims->Hkv, dims->D, kv, k_new, v_new, alloc, status,
                                    workspace, stream));
+}
+
+hk_status hk_reserve_slots(const hk_dims* dims, const hk_paged_kv* kv, const hk_chunks* chunks,
+                           const hk_allocator* alloc, int64_t* slot_map, int32_t* status,
+                           void* workspace, size_t ws_bytes, hipStream_t stream) {
+  hk_status e = check_dims(dims, false);
+  if (e) return e;
+  if ((e = check_kv(kv, false, false))) return e;
+  if ((e = check_chunks(chunks))) return e;
+  if (!alloc || !alloc->free_ids || !alloc->free_top || alloc->capacity <= 0) return HK_ERR_ARG;
+  if (dims->NS % chunks->n_seq != 0) return HK_ERR_SHAPE;
+  const long long n_heads = (long long)dims->NS * dims->Hkv;
+  const long long touched = (chunks->max_len + 2 * HK_PAGE - 2) / HK_PAGE;
+  const long long map = (n_heads / chunks->n_seq) * chunks->n_tokens;
+  if (n_heads * touched + map >= 1ll << 31) return HK_ERR_SHAPE;
+  if (!workspace || ws_bytes < hk_reserve_ws((int)n_heads)) return HK_ERR_WORKSPACE;
+  if (!aligned256(workspace)) return HK_ERR_ALIGN;
+  return launched(hk_launch_reserve((int)n_heads, dims->Hkv, kv, chunks, alloc, slot_map, status, workspace,
+                                    stream));
+}
+
+hk_status hk_write_kv(const hk_dims* dims, const hk_paged_kv* kv, int32_t n_layers, int32_t n_tokens,
+                      const int64_t* slot_map, const void* k_new, int64_t k_layer_stride,
+                      int64_t k_row_stride, const void* v_new, int64_t v_layer_stride,
+                      int64_t v_row_stride, hipStream_t stream) {
+  hk_status e = check_dims(dims, false);
+  if (e) return e;
+  if ((e = check_kv(kv, true, false))) return e;
+  if (n_layers <= 0 || n_tokens <= 0 || !slot_map) return HK_ERR_ARG;
+  const int es = kv->dtype == HK_BF16 ? 2 : 4;
+  const int64_t row = (int64_t)dims->Hkv * dims->D;
+  if ((e = check_rows_at(k_new, k_row_stride, row, es))) return e;
+  if ((e = check_rows_at(v_new, v_row_stride, row, es))) return e;
+  if (n_layers > 1 && (k_layer_stride % (16 / es) || v_layer_stride % (16 / es))) return HK_ERR_ALIGN;
+  if (n_layers > kMaxRows || n_tokens > kMaxRows) return HK_ERR_SHAPE;
+  if ((double)n_layers * n_tokens * row * es / 16 >= 2147483648.0) return HK_ERR_SHAPE;
+  return launched(hk_launch_write_kv(dims->Hkv, dims->D, kv, n_layers, n_tokens, slot_map, k_new,
+                                     n_layers > 1 ? k_layer_stride : 0, k_row_stride, v_new,
+                                     n_layers > 1 ? v_layer_stride : 0, v_row_stride, stream));
+}
+
+size_t hk_chunk_attn_workspace_size(const hk_dims* dims, const hk_chunks* chunks, int32_t max_pages) {
+  if (check_dims(dims, false) || !chunks || chunks->n_tokens <= 0 || chunks->max_len <= 0 || max_pages <= 0) return 0;
+  if (chunks->n_tokens > kMaxRows || chunks->max_len > kMaxRows) return 0;
+  return hk_chunk_attn_ws(dims->NS, dims->Hq, dims->Hkv, dims->D, chunks->n_tokens, chunks->max_len, max_pages);
+}
+
+hk_status hk_chunk_attn(const hk_dims* dims, const hk_paged_kv* kv, const hk_chunks* chunks, const void* q,
+                        int64_t q_row_stride, float sm_scale, void* o, float* lse, void* workspace,
+                        size_t ws_bytes, hipStream_t stream) {
+  hk_status e = check_dims(dims, false);
+  if (e) return e;
+  if ((e = check_kv(kv, true, false))) return e;
+  if ((e = check_chunks(chunks))) return e;
+  if (!o || !(sm_scale > 0.f) || !std::isfinite(sm_scale)) return HK_ERR_ARG;
+  if (dims->NS != chunks->n_seq || dims->Hq / dims->Hkv > kMaxGroup) return HK_ERR_SHAPE;
+  const int es = kv->dtype == HK_BF16 ? 2 : 4;
+  if ((e = check_rows_at(q, q_row_stride, (int64_t)dims->Hq * dims->D, es))) return e;
+  if (!aligned16(o)) return HK_ERR_ALIGN;
+  const size_t need = hk_chunk_attn_ws(dims->NS, dims->Hq, dims->Hkv, dims->D, chunks->n_tokens, chunks->max_len,
+                                       kv->max_pages);
+  if (need) {
+    if (!workspace || ws_bytes < need) return HK_ERR_WORKSPACE;
+    if (!aligned256(workspace)) return HK_ERR_ALIGN;
+  }
+  return launched(hk_launch_chunk_attn(dims->NS, dims->Hq, dims->Hkv, dims->D, kv, chunks, q, q_row_stride, sm_scale,
+                                       o, lse, workspace, stream));
+}
+
+size_t hk_verify_workspace_size(int32_t n_seq, int32_t V) {
+  if (n_seq <= 0 || V <= 0 || V > kMaxVocab) return 0;
+  return hk_verify_ws(n_seq, V);
+}
+
+hk_status hk_verify_draft(const hk_chunks* chunks, int32_t V, hk_dtype dtype, const int32_t* tokens,
+                          const void* p, int64_t p_row_stride, const void* q, int64_t q_row_stride,
+                          const float* u, int32_t* n_accept, int32_t* next_token, int32_t* n_drop,
+                          int32_t* status, void* workspace, size_t ws_bytes, hipStream_t stream) {
+  hk_status e = check_chunks(chunks);
+  if (e) return e;
+  if (V <= 0 || !tokens || !p || !u || !n_accept || !next_token || !n_drop) return HK_ERR_ARG;
+  if (V > kMaxVocab) return HK_ERR_SHAPE;
+  if (dtype != HK_F32 && dtype != HK_BF16) return HK_ERR_DTYPE;
+  if (p_row_stride < V || (q && q_row_stride < V)) return HK_ERR_ARG;
+  const uintptr_t es = dtype == HK_BF16 ? 2 : 4;
+  if (reinterpret_cast<uintptr_t>(p) % es || reinterpret_cast<uintptr_t>(q) % es) return HK_ERR_ALIGN;
+  if (!workspace || ws_bytes < hk_verify_ws(chunks->n_seq, V)) return HK_ERR_WORKSPACE;
+  if (!aligned256(workspace)) return HK_ERR_ALIGN;
+  return launched(hk_launch_verify(chunks->n_seq, V, dtype, chunks, tokens, p, p_row_stride, q, q_row_stride, u,
+                                   n_accept, next_token, n_drop, status, workspace, stream));
+}
+
+hk_status hk_trim_slots(const hk_dims* dims, const hk_paged_kv* kv, int32_t n_seq, const int32_t* n_drop,
+                        const hk_allocator* alloc, void* workspace, size_t ws_bytes, hipStream_t stream) {
+  hk_status e = check_dims(dims, false);
+  if (e) return e;
+  if ((e = check_kv(kv, false, false))) return e;
+  if (n_seq <= 0 || !n_drop || !alloc || !alloc->free_ids || !alloc->free_top) return HK_ERR_ARG;
+  if (alloc->capacity < kv->num_pages) return HK_ERR_ARG;        // every page can be pushed
+  if (dims->NS % n_seq != 0) return HK_ERR_SHAPE;
+  const int n_heads = dims->NS * dims->Hkv;
+  if (!workspace || ws_bytes < hk_trim_ws(n_heads)) return HK_ERR_WORKSPACE;
+  if (!aligned256(workspace)) return HK_ERR_ALIGN;
+  return launched(hk_launch_trim(n_heads, dims->Hkv, kv, n_seq, n_drop, alloc, workspace, stream));
 }
 
 hk_status hk_probe(int32_t kind, int32_t blocks, int32_t iters, float* out, hipStream_t stream) {

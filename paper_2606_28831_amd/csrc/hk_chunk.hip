@@ -1,0 +1,737 @@
+// a7: causal attention of chunks of new tokens over the paged cache (gfx950).
+//
+// The query rows of one KV head are folded: row r of a chunk is query head r % G of token r / G,
+// and all of them read the same K and V.  Two kernels share the work by the folded rows of a
+// sequence:
+//   tile   more than SHORT_ROWS rows: a workgroup takes TM rows, its four waves 64 (fp32: 32) rows
+//          each, all against the same K and V tiles in LDS;
+//   short  up to SHORT_ROWS rows (drafts, single tokens): a workgroup takes the 32 rows, its four
+//          waves take the pages in turn, every page read once by one wave, and meet at the end.
+// Both may split a row's pages over workgroups; merge_kernel joins the splits' states with the
+// operator of App. F.  Work and split of a workgroup follow from the chunk starts and page counts
+// in device memory.
+//
+// Arithmetic of a wave, per block of 32 keys: C[key][query] = K Q^T on MFMA, so that a lane holds
+// 16 keys of one query and the softmax needs no cross-lane step but for a new reference; then
+// O^T[dim][query] += V^T P^T, P going in as it lies: contraction order is free, so the keys keep the
+// order of the score tile's registers, and V's columns come from LDS by transposing reads (bf16)
+// or one value a lane (fp32).
+//
+// Softmax: one pass with a running reference m per query, a whole number that moves only when a
+// score exceeds it by 2^CH_SLACK, so most blocks need no rescaling.  Probabilities are formed as
+// exp2(z - m - bias), where 2^bias is at least 2^CH_SLACK times the keys of the row: sums of P V
+// and their merge cannot leave the fp32 range where the result does not.
+// Precision: scores, sums and outputs in fp32.  P enters the bf16 product rounded to nearest bf16:
+// an error of 2^-9 of each term, of the size of the output's own rounding; the row sum is taken
+// from the unrounded values, for the LSE.
+#include <algorithm>
+#include <type_traits>
+
+#include "hk_chunk.h"
+
+namespace hk {
+
+constexpr int CH_NT = 256;
+constexpr int CH_NW = CH_NT / 64;
+constexpr float CH_SLACK = 12.f;
+constexpr int SHORT_ROWS = 32;
+constexpr int MIN_PAGES = 16;                 // fewest pages of a split
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// ------------------------------------------------------------------ LDS tiles
+// A tile row is one key's K or V row, its 16-byte pieces permuted within the row by the key so that
+// the MFMA fragments' reads spread over the banks.
+template <typename T, int D>
+struct TileLayout {
+  static constexpr int ES = sizeof(T);
+  static constexpr int ROW = D * ES;          // bytes
+  static constexpr int PIECES = ROW / 16;
+  static constexpr int PAGE = HK_PAGE * ROW;
+  static constexpr int LOADS = PAGE / 1024;   // 16-byte loads per lane of a wave for a page
+  __device__ static __forceinline__ int turn(int key) {
+    if (ES == 4) return (key & 7) | ((key & 4) << 1);
+    if (D == 128) return ((key & 3) << 2) | ((key >> 2) & 3);
+    return ((key & 2) << 1) | ((key >> 2) & 3);
+  }
+  __device__ static __forceinline__ int at(int key, int piece) { return key * ROW + ((piece ^ turn(key)) * 16); }
+};
+
+// One page's K or V rows on their way from memory to LDS: piece i * 64 + lane of the page.
+template <typename T, int D>
+struct PageRegs {
+  using L = TileLayout<T, D>;
+  u32x4 r[L::LOADS];
+  __device__ __forceinline__ void load(const char* pool, int page) {
+    const u32x4* src = reinterpret_cast<const u32x4*>(pool + (size_t)page * L::PAGE) + (threadIdx.x & 63);
+#pragma unroll
+    for (int i = 0; i < L::LOADS; ++i) r[i] = src[i * 64];
+  }
+  // rows whose mask bit is 0 become zeros: nothing they hold may meet a probability of 0
+  __device__ __forceinline__ void clear(uint32_t mask) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < L::LOADS; ++i)
+      if (!((mask >> ((i * 64 + lane) / L::PIECES)) & 1u)) r[i] = u32x4{0u, 0u, 0u, 0u};
+  }
+  // the page's rows that hold an infinite value or NaN, bit per row
+  __device__ __forceinline__ uint32_t odd_rows() const {
+    uint32_t rows = 0;
+#pragma unroll
+    for (int i = 0; i < L::LOADS; ++i) {
+      bool odd = false;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t x = r[i][w];
+        odd |= L::ES == 4 ? (x & 0x7f800000u) == 0x7f800000u
+                          : (x & 0x7f800000u) == 0x7f800000u || (x & 0x7f80u) == 0x7f80u;
+      }
+      const unsigned long long b = __ballot(odd);
+      if (b)
+        for (int k = 0; k < 64 / L::PIECES; ++k)
+          if ((b >> (k * L::PIECES)) & ((1ull << L::PIECES) - 1)) rows |= 1u << (i * (64 / L::PIECES) + k);
+    }
+    return rows;
+  }
+  __device__ __forceinline__ void store(char* tile, int key0) const {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < L::LOADS; ++i) {
+      const int e = i * 64 + lane;
+      *reinterpret_cast<u32x4*>(tile + L::at(key0 + e / L::PIECES, e % L::PIECES)) = r[i];
+    }
+  }
+};
+
+// ------------------------------------------------------------------ matrix products of a wave
+// Fragment order: lane l holds query (or key, or dim) l % 32 and half hi = l / 32 of the contraction.
+// Register r of a score tile is key (r & 3) + 8 (r >> 2) + 4 hi.
+template <typename T, int D>
+struct Mma;
+
+template <int D>
+struct Mma<uint16_t, D> {
+  using L = TileLayout<uint16_t, D>;
+  struct Query {
+    bf16x8 f[D / 16];
+  };
+  __device__ static __forceinline__ void load_q(Query& q, const uint16_t* row) {
+    const int hi = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+      q.f[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(row + (2 * s + hi) * 8));
+  }
+  template <int NB>
+  __device__ static __forceinline__ void scores(f32x16 (&z)[NB], const Query (&q)[NB], const char* k) {
+    const int lane = threadIdx.x & 63, key = lane & 31, hi = lane >> 5;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) z[b][r] = 0.f;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      const bf16x8 a = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(k + L::at(key, 2 * s + hi)));
+#pragma unroll
+      for (int b = 0; b < NB; ++b) z[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[b].f[s], z[b], 0, 0, 0);
+    }
+  }
+  template <int NB>
+  __device__ static __forceinline__ void values(f32x16 (&acc)[NB][D / 32], const f32x16 (&p)[NB], const char* v) {
+    const int lane = threadIdx.x & 63, hi = lane >> 5, g1 = (lane >> 4) & 1, i16 = lane & 15;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      bf16x8 bp[NB];
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+          const bf16x2 t = __builtin_convertvector((f32x2{p[b][8 * s + j], p[b][8 * s + j + 1]}), bf16x2);
+          bp[b][j] = t[0];
+          bp[b][j + 1] = t[1];
+        }
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt) {
+        s16x4 a[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          // sixteen lanes turn four keys x 16 dims: lane i supplies 4 dims of key i / 4
+          const int key = 16 * s + 8 * h + 4 * hi + (i16 >> 2), piece = 4 * dt + 2 * g1 + ((i16 & 3) >> 1);
+          const char* at = v + L::at(key, piece) + (i16 & 1) * 8;
+          a[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (__attribute__((address_space(3))) s16x4*)(uintptr_t)(__attribute__((address_space(3))) const char*)at);
+        }
+        const bf16x8 av = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a[0], a[1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+          acc[b][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, bp[b], acc[b][dt], 0, 0, 0);
+      }
+    }
+  }
+  __device__ static __forceinline__ float value(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+  __device__ static __forceinline__ void put4(uint16_t* to, float x, float y, float z, float w) {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    const uint32_t a = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x, y}), bf16x2));
+    const uint32_t b = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{z, w}), bf16x2));
+    *reinterpret_cast<u32x2*>(to) = u32x2{a, b};
+  }
+  __device__ static __forceinline__ void put2(uint16_t* to, float x, float y) {
+    *reinterpret_cast<uint32_t*>(to) = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x, y}), bf16x2));
+  }
+};
+
+template <int D>
+struct Mma<float, D> {
+  using L = TileLayout<float, D>;
+  struct Query {
+    f32x4 f[D / 8];
+  };
+  __device__ static __forceinline__ void load_q(Query& q, const float* row) {
+    const int hi = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int s = 0; s < D / 8; ++s) q.f[s] = *reinterpret_cast<const f32x4*>(row + (2 * s + hi) * 4);
+  }
+  template <int NB>
+  __device__ static __forceinline__ void scores(f32x16 (&z)[NB], const Query (&q)[NB], const char* k) {
+    const int lane = threadIdx.x & 63, key = lane & 31, hi = lane >> 5;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) z[b][r] = 0.f;
+#pragma unroll
+    for (int s = 0; s < D / 8; ++s) {
+      const f32x4 a = *reinterpret_cast<const f32x4*>(k + L::at(key, 2 * s + hi));
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) z[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], q[b].f[s][j], z[b], 0, 0, 0);
+    }
+  }
+  template <int NB>
+  __device__ static __forceinline__ void values(f32x16 (&acc)[NB][D / 32], const f32x16 (&p)[NB], const char* v) {
+    const int lane = threadIdx.x & 63, hi = lane >> 5, dim = lane & 31;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int key = (r & 3) + 8 * (r >> 2) + 4 * hi;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt) {
+        const float a = *reinterpret_cast<const float*>(v + L::at(key, 8 * dt + (dim >> 2)) + (dim & 3) * 4);
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+          acc[b][dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p[b][r], acc[b][dt], 0, 0, 0);
+      }
+    }
+  }
+  __device__ static __forceinline__ float value(float x) { return x; }
+  __device__ static __forceinline__ void put4(float* to, float x, float y, float z, float w) {
+    *reinterpret_cast<f32x4*>(to) = f32x4{x, y, z, w};
+  }
+  __device__ static __forceinline__ void put2(float* to, float x, float y) {
+    *reinterpret_cast<f32x2*>(to) = f32x2{x, y};
+  }
+};
+
+// ------------------------------------------------------------------ the softmax state of a wave
+// NB blocks of 32 queries; lane l holds query l % 32 of each, and half of its keys.
+template <typename T, int D, int NB>
+struct State {
+  using M = Mma<T, D>;
+  f32x16 acc[NB][D / 32];                     // O^T: register r is dim 32 dt + (r & 3) + 8 (r >> 2) + 4 hi
+  float m[NB], mb[NB], l[NB];                 // reference, reference + bias (0 while there is none), sum
+  __device__ __forceinline__ void init() {
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      m[b] = -INFINITY;
+      mb[b] = 0.f;
+      l[b] = 0.f;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[b][dt][r] = 0.f;
+    }
+  }
+  // 32 keys from LDS; vis[b]: bit k, key k of them is seen by the lane's query (all: every bit of
+  // every lane is 1).  odd: keys whose V row holds infinite values and is not seen by every query;
+  // it is zeros in LDS and added here, at row(key), to the queries that see it: for the others
+  // its product with a probability of 0 would be NaN.
+  template <typename F>
+  __device__ __forceinline__ void block(const typename M::Query (&q)[NB], const char* k, const char* v,
+                                        const uint32_t (&vis)[NB], bool all, float c2, float bias, uint32_t odd,
+                                        F row) {
+    const int hi = (threadIdx.x & 63) >> 5;
+    f32x16 z[NB];
+    M::template scores<NB>(z, q, k);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      if (!all) {
+        const uint32_t w = vis[b] >> (4 * hi);
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (!((w >> ((r & 3) + 8 * (r >> 2))) & 1u)) z[b][r] = -INFINITY;
+      }
+      float zm = z[b][0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) zm = fmaxf(zm, z[b][r]);
+      zm *= c2;
+      if (__any(zm > m[b] + CH_SLACK)) {
+        zm = fmaxf(zm, __shfl_xor(zm, 32, 64));
+        const float mn = fmaxf(m[b], ceilf(zm));
+        const float alpha = m[b] == -INFINITY ? 0.f : fast_exp2(m[b] - mn);
+        m[b] = mn;
+        mb[b] = mn == -INFINITY ? 0.f : mn + bias;
+        l[b] *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[b][dt][r] *= alpha;
+      }
+      float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        z[b][r] = fast_exp2(fmaf(z[b][r], c2, -mb[b]));
+        s[r & 3] += z[b][r];
+      }
+      l[b] += (s[0] + s[1]) + (s[2] + s[3]);
+    }
+    M::template values<NB>(acc, z, v);
+    while (odd) {
+      const int key = __builtin_ctz(odd), reg = (key & 3) + 4 * (key >> 3), lane = threadIdx.x & 63;
+      odd &= odd - 1;
+      const T* vr = row(key);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        float p = z[b][0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) p = reg == r ? z[b][r] : p;
+        p = __shfl(p, (lane & 31) + 32 * ((key >> 2) & 1), 64);
+        const bool sees = (vis[b] >> key) & 1u;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float x = M::value(vr[32 * dt + (r & 3) + 8 * (r >> 2) + 4 * hi]);
+            acc[b][dt][r] = sees ? fmaf(p, x, acc[b][dt][r]) : acc[b][dt][r];
+          }
+      }
+    }
+  }
+};
+
+// What a workgroup works on: rows of one sequence and KV head, and a range of its pages.
+struct Work {
+  int first, len, rows;                       // the chunk, and its folded rows len * G
+  int end;                                    // one past the row's newest valid slot
+  int pages;                                  // pages that the workgroup's last token sees
+  int share;                                  // of them per split
+};
+__device__ __forceinline__ int tile_pages(int n, int end, int len, int last_token) {
+  const int seen = max(end - len + last_token + 1, 0);
+  return min(n, (seen + HK_PAGE - 1) / HK_PAGE);
+}
+__device__ __forceinline__ int split_share(int pages, int n_split) {
+  return max((pages + n_split - 1) / n_split, MIN_PAGES);
+}
+__device__ __forceinline__ float bias_of(int pages) { return (float)(32 - __clz(pages * HK_PAGE)) + CH_SLACK; }
+
+struct Args {
+  const char *q, *k_pool, *v_pool;
+  const int32_t *table, *n_pages, *start;
+  const uint16_t* masks;
+  int64_t q_row;                              // elements
+  char* o;
+  float *lse, *part_o, *part_ml;
+  int Hq, Hkv, G, max_pages, num_pages, n_seq, n_tokens, max_len, n_split;
+  float c2;
+};
+
+// One query's result (lane: half of the dims): normalised into o, or the split's state.
+template <typename T, int D>
+__device__ __forceinline__ void put_state(const Args& a, int64_t row, int split, const f32x16 (&acc)[D / 32], float mb,
+                                          float l) {
+  const int hi = (threadIdx.x & 63) >> 5;
+  if (a.n_split > 1) {
+    float* to = a.part_o + (row * a.n_split + split) * D;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<f32x4*>(to + 32 * dt + 8 * j + 4 * hi) =
+            f32x4{acc[dt][4 * j], acc[dt][4 * j + 1], acc[dt][4 * j + 2], acc[dt][4 * j + 3]};
+    if (hi == 0) *reinterpret_cast<f32x2*>(a.part_ml + (row * a.n_split + split) * 2) = f32x2{l == 0.f ? -INFINITY : mb, l};
+    return;
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;   // (a NaN stays one)
+  T* to = reinterpret_cast<T*>(a.o) + row * D;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      Mma<T, D>::put4(to + 32 * dt + 8 * j + 4 * hi, acc[dt][4 * j] * inv, acc[dt][4 * j + 1] * inv,
+                      acc[dt][4 * j + 2] * inv, acc[dt][4 * j + 3] * inv);
+  if (hi == 0 && a.lse) a.lse[row] = l == 0.f ? -INFINITY : (mb + __log2f(l)) * kLn2;
+}
+
+// ------------------------------------------------------------------ tile kernel
+template <typename T, int D, int NB>
+__global__ __launch_bounds__(CH_NT, 1) void chunk_tile_kernel(Args a) {
+  using L = TileLayout<T, D>;
+  using M = Mma<T, D>;
+  constexpr int TM = CH_NW * NB * 32, TP = 4, TK = TP * HK_PAGE;   // rows, pages and keys of a tile
+  __shared__ __align__(16) char s_k[2][TK * L::ROW], s_v[2][TK * L::ROW];
+  __shared__ uint16_t s_odd[2][TP];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  // the largest tiles of a sequence first: tile u of the launch counts down
+  const int kv = blockIdx.x % a.Hkv, u = (int)(gridDim.x / a.Hkv) - 1 - (int)(blockIdx.x / a.Hkv), split = blockIdx.y;
+  auto tiles_before = [&](int s) { return min(max(a.start[s], 0), a.n_tokens) * a.G / TM + s; };
+  int s = 0;
+  for (int hi = a.n_seq; hi - s > 1;) {
+    const int mid = (s + hi) / 2;
+    if (tiles_before(mid) <= u) s = mid;
+    else hi = mid;
+  }
+  const Chunk c = chunk_of(a.start, s, a.n_tokens, a.max_len);
+  const int rows = c.len * a.G, r0 = (u - tiles_before(s)) * TM;
+  if (rows <= SHORT_ROWS || r0 < 0 || r0 >= rows) return;
+  const int h = s * a.Hkv + kv, n = min(max(a.n_pages[h], 0), a.max_pages);
+  const int32_t* trow = a.table + (size_t)h * a.max_pages;
+  const uint16_t* mrow = a.masks + (size_t)h * a.max_pages;
+  const int end = row_end(n, n > 0 ? mrow[n - 1] : 0u);
+  const int pages = tile_pages(n, end, c.len, (min(r0 + TM, rows) - 1) / a.G);
+  const int share = split_share(pages, a.n_split);
+  const int p0 = split * share, p1 = min(p0 + share, pages);
+  if (split > 0 && p0 >= pages) return;
+
+  // rows past the chunk repeat its last one; they are not stored
+  typename M::Query q[NB];
+  int64_t row[NB];
+  int seen[NB];                               // keys before this one are seen by the lane's query
+  const int w0 = r0 + wave * NB * 32;
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    const int r = min(w0 + b * 32 + (lane & 31), rows - 1), tok = r / a.G;
+    row[b] = (int64_t)(c.first + tok) * a.Hq + kv * a.G + (r - tok * a.G);
+    seen[b] = end - c.len + tok + 1;
+    M::load_q(q[b], reinterpret_cast<const T*>(a.q) + (int64_t)(c.first + tok) * a.q_row + (kv * a.G + (r - tok * a.G)) * D);
+  }
+  const int seen_all = end - c.len + min(w0, rows - 1) / a.G + 1;
+  const float bias = bias_of(pages);
+  State<T, D, NB> st;
+  st.init();
+  const bool active = w0 < rows;
+  const int tiles = p1 > p0 ? (p1 - p0 + TP - 1) / TP : 0;
+  PageRegs<T, D> rk, rv;
+  uint32_t mask = 0;
+  const int tile_seen = end - c.len + r0 / a.G + 1;             // keys that every query of the tile sees
+  auto load = [&](int t) {
+    const int p = p0 + t * TP + wave;
+    mask = p < p1 ? mrow[p] : 0u;
+    const int id = min(max(trow[min(p, p1 - 1)], 0), a.num_pages - 1);
+    rk.load(a.k_pool, id);
+    rv.load(a.v_pool, id);
+  };
+  auto at_edge = [&](int p) { return (p + 1) * HK_PAGE > tile_seen; };
+  // V row of key k of the 32 from page p on
+  auto row_at = [&](int p) {
+    return [&, p](int k) {
+      const int id = min(max(trow[min(p + k / HK_PAGE, p1 - 1)], 0), a.num_pages - 1);
+      return reinterpret_cast<const T*>(a.v_pool) + ((size_t)id * HK_PAGE + k % HK_PAGE) * D;
+    };
+  };
+  if (tiles > 0) load(0);
+  for (int t = 0; t < tiles; ++t) {
+    if (at_edge(p0 + t * TP + wave)) {
+      const uint32_t odd = rv.odd_rows() & mask;
+      mask &= ~odd;
+      if (lane == 0) s_odd[t & 1][wave] = (uint16_t)odd;
+    }
+    if (mask != 0xffffu) rv.clear(mask);
+    rk.store(s_k[t & 1], wave * HK_PAGE);
+    rv.store(s_v[t & 1], wave * HK_PAGE);
+    __syncthreads();
+    if (t + 1 < tiles) load(t + 1);
+    if (active)
+#pragma unroll
+      for (int hb = 0; hb < TK / 32; ++hb) {
+        const int p = p0 + t * TP + 2 * hb, key = p * HK_PAGE;
+        const uint32_t valid = (p < p1 ? (uint32_t)mrow[p] : 0u) | (p + 1 < p1 ? (uint32_t)mrow[p + 1] << 16 : 0u);
+        const bool all = valid == 0xffffffffu && key + 32 <= seen_all;
+        uint32_t vis[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          const int k = seen[b] - key;
+          vis[b] = valid & (k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u);
+        }
+        const uint32_t odd = (at_edge(p) ? (uint32_t)s_odd[t & 1][2 * hb] : 0u) |
+                             (at_edge(p + 1) ? (uint32_t)s_odd[t & 1][2 * hb + 1] << 16 : 0u);
+        st.block(q, s_k[t & 1] + hb * 32 * L::ROW, s_v[t & 1] + hb * 32 * L::ROW, vis, all, a.c2, bias,
+                 __builtin_amdgcn_readfirstlane(odd), row_at(p));
+      }
+  }
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    const float l = st.l[b] + __shfl_xor(st.l[b], 32, 64);
+    if (w0 + b * 32 + (lane & 31) < rows) put_state<T, D>(a, row[b], split, st.acc[b], st.mb[b], l);
+  }
+}
+
+// ------------------------------------------------------------------ short kernel
+template <typename T, int D>
+__global__ __launch_bounds__(CH_NT, 1) void chunk_short_kernel(Args a) {
+  using L = TileLayout<T, D>;
+  using M = Mma<T, D>;
+  constexpr int WP = 2, TP = CH_NW * WP;      // pages of a wave and of the workgroup per step
+  constexpr int OP = D + 4;                   // floats of a query's sums in LDS, padded
+  constexpr int STAGE = CH_NW * 2 * 32 * L::ROW, JOIN = CH_NW * 32 * OP * 4;
+  __shared__ __align__(16) char s_buf[STAGE > JOIN ? STAGE : JOIN];
+  __shared__ float s_m[CH_NW][32], s_l[CH_NW][32];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hi = lane >> 5;
+  const int h = blockIdx.x, s = h / a.Hkv, kv = h % a.Hkv, split = blockIdx.y;
+  const Chunk c = chunk_of(a.start, s, a.n_tokens, a.max_len);
+  const int rows = c.len * a.G;
+  if (rows <= 0 || rows > SHORT_ROWS) return;
+  const int n = min(max(a.n_pages[h], 0), a.max_pages);
+  const int32_t* trow = a.table + (size_t)h * a.max_pages;
+  const uint16_t* mrow = a.masks + (size_t)h * a.max_pages;
+  const int end = row_end(n, n > 0 ? mrow[n - 1] : 0u);
+  const int pages = tile_pages(n, end, c.len, c.len - 1);
+  const int share = split_share(pages, a.n_split);
+  const int p0 = split * share, p1 = min(p0 + share, pages);
+  if (split > 0 && p0 >= pages) return;
+
+  const int r = min(lane & 31, rows - 1), tok = r / a.G;
+  const int seen = end - c.len + tok + 1, seen_all = end - c.len + 1;
+  typename M::Query q[1];
+  M::load_q(q[0], reinterpret_cast<const T*>(a.q) + (int64_t)(c.first + tok) * a.q_row + (kv * a.G + (r - tok * a.G)) * D);
+  const float bias = bias_of(pages);
+  State<T, D, 1> st;
+  st.init();
+  char* my_k = s_buf + wave * 2 * 32 * L::ROW;
+  char* my_v = my_k + 32 * L::ROW;
+  const int steps = p1 > p0 ? (p1 - p0 + TP - 1) / TP : 0;
+  PageRegs<T, D> rk[WP], rv[WP];
+  uint32_t mask[WP];
+  auto load = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < WP; ++i) {
+      const int p = p0 + t * TP + wave * WP + i;
+      mask[i] = p < p1 ? mrow[p] : 0u;
+      const int id = min(max(trow[min(p, p1 - 1)], 0), a.num_pages - 1);
+      rk[i].load(a.k_pool, id);
+      rv[i].load(a.v_pool, id);
+    }
+  };
+  if (steps > 0) load(0);
+  for (int t = 0; t < steps; ++t) {
+    // the wave's own region of LDS: its reads of the last step are done before these writes, in
+    // the order of its instructions
+    uint32_t odd = 0;
+#pragma unroll
+    for (int i = 0; i < WP; ++i) {
+      if ((p0 + t * TP + wave * WP + i + 1) * HK_PAGE > seen_all) {
+        const uint32_t o = rv[i].odd_rows() & mask[i];
+        mask[i] &= ~o;
+        odd |= o << (16 * i);
+      }
+      if (mask[i] != 0xffffu) rv[i].clear(mask[i]);
+      rk[i].store(my_k, i * HK_PAGE);
+      rv[i].store(my_v, i * HK_PAGE);
+    }
+    if (t + 1 < steps) load(t + 1);
+    const int p = p0 + t * TP + wave * WP, key = p * HK_PAGE;
+    const uint32_t valid = (p < p1 ? (uint32_t)mrow[p] : 0u) | (p + 1 < p1 ? (uint32_t)mrow[p + 1] << 16 : 0u);
+    const bool all = valid == 0xffffffffu && key + 32 <= seen_all;
+    const int k = seen - key;
+    const uint32_t vis[1] = {valid & (k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u)};
+    __builtin_amdgcn_wave_barrier();
+    st.block(q, my_k, my_v, vis, all, a.c2, bias, __builtin_amdgcn_readfirstlane(odd), [&](int j) {
+      const int id = min(max(trow[min(p + j / HK_PAGE, p1 - 1)], 0), a.num_pages - 1);
+      return reinterpret_cast<const T*>(a.v_pool) + ((size_t)id * HK_PAGE + j % HK_PAGE) * D;
+    });
+    __builtin_amdgcn_wave_barrier();
+  }
+  // the waves' states: one reference for all, then sums
+  float l = st.l[0] + __shfl_xor(st.l[0], 32, 64);
+  if (hi == 0) {
+    s_m[wave][lane] = l == 0.f ? -INFINITY : st.mb[0];
+    s_l[wave][lane] = l;
+  }
+  __syncthreads();
+  float mb = -INFINITY;
+  l = 0.f;
+#pragma unroll
+  for (int w = 0; w < CH_NW; ++w) mb = fmaxf(mb, s_m[w][lane & 31]);
+  if (mb != -INFINITY)
+#pragma unroll
+    for (int w = 0; w < CH_NW; ++w) l += s_l[w][lane & 31] * fast_exp2(s_m[w][lane & 31] - mb);
+  const float own = mb == -INFINITY ? 0.f : fast_exp2(s_m[wave][lane & 31] - mb);
+  float* s_o = reinterpret_cast<float*>(s_buf);
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *reinterpret_cast<f32x4*>(s_o + (wave * 32 + (lane & 31)) * OP + 32 * dt + 8 * j + 4 * hi) =
+          f32x4{st.acc[0][dt][4 * j] * own, st.acc[0][dt][4 * j + 1] * own, st.acc[0][dt][4 * j + 2] * own,
+                st.acc[0][dt][4 * j + 3] * own};
+  __syncthreads();
+  // eight threads of a query's dims each
+  constexpr int PER = D / 8;
+  const int qr = threadIdx.x >> 3, d0 = (threadIdx.x & 7) * PER;
+  if (qr >= rows) return;
+  float M_ = -INFINITY, L_ = 0.f;
+#pragma unroll
+  for (int w = 0; w < CH_NW; ++w) M_ = fmaxf(M_, s_m[w][qr]);
+  if (M_ != -INFINITY)
+#pragma unroll
+    for (int w = 0; w < CH_NW; ++w) L_ += s_l[w][qr] * fast_exp2(s_m[w][qr] - M_);
+  const int tq = qr / a.G;
+  const int64_t orow = (int64_t)(c.first + tq) * a.Hq + kv * a.G + (qr - tq * a.G);
+  const float inv = a.n_split > 1 ? 1.f : L_ == 0.f ? 0.f : 1.f / L_;
+#pragma unroll
+  for (int d = 0; d < PER; d += 4) {
+    f32x4 t = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < CH_NW; ++w) t += *reinterpret_cast<const f32x4*>(s_o + (w * 32 + qr) * OP + d0 + d);
+    t *= inv;
+    if (a.n_split > 1) *reinterpret_cast<f32x4*>(a.part_o + (orow * a.n_split + split) * D + d0 + d) = t;
+    else M::put4(reinterpret_cast<T*>(a.o) + orow * D + d0 + d, t[0], t[1], t[2], t[3]);
+  }
+  if ((threadIdx.x & 7) == 0) {
+    if (a.n_split > 1) *reinterpret_cast<f32x2*>(a.part_ml + (orow * a.n_split + split) * 2) = f32x2{M_, L_};
+    else if (a.lse) a.lse[orow] = L_ == 0.f ? -INFINITY : (M_ + __log2f(L_)) * kLn2;
+  }
+}
+
+// ------------------------------------------------------------------ merge
+// One wave per (token, query head): the states of the splits that held pages.
+template <typename T, int D, int TM>
+__global__ __launch_bounds__(CH_NT) void chunk_merge_kernel(Args a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)blockIdx.x * CH_NW + (threadIdx.x >> 6);
+  if (row >= (int64_t)a.n_tokens * a.Hq) return;
+  const int t = (int)(row / a.Hq), hq = (int)(row % a.Hq), kv = hq / a.G, g = hq % a.G;
+  int s = 0;
+  for (int hi = a.n_seq; hi - s > 1;) {
+    const int mid = (s + hi) / 2;
+    if (a.start[mid] <= t) s = mid;
+    else hi = mid;
+  }
+  const Chunk c = chunk_of(a.start, s, a.n_tokens, a.max_len);
+  const int i = t - c.first;
+  if (i < 0 || i >= c.len) return;            // padding
+  const int h = s * a.Hkv + kv, n = min(max(a.n_pages[h], 0), a.max_pages);
+  const int end = row_end(n, n > 0 ? a.masks[(size_t)h * a.max_pages + n - 1] : 0u);
+  const int rows = c.len * a.G;
+  const int last = rows <= SHORT_ROWS ? c.len - 1 : (min(((i * a.G + g) / TM + 1) * TM, rows) - 1) / a.G;
+  const int pages = tile_pages(n, end, c.len, last), share = split_share(pages, a.n_split);
+  const int used = max((pages + share - 1) / share, 1);
+  const float* ml = a.part_ml + row * a.n_split * 2;
+  const float* po = a.part_o + row * a.n_split * D;
+  float M_ = -INFINITY;
+  for (int j = 0; j < used; ++j) M_ = fmaxf(M_, ml[2 * j]);
+  constexpr int PER = D / 64;
+  float l = 0.f, o[PER];
+#pragma unroll
+  for (int e = 0; e < PER; ++e) o[e] = 0.f;
+  if (M_ != -INFINITY)
+    for (int j = 0; j < used; ++j) {
+      const float f = fast_exp2(ml[2 * j] - M_);
+      l += ml[2 * j + 1] * f;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) o[e] += po[(size_t)j * D + lane * PER + e] * f;
+    }
+  const float inv = l == 0.f ? 0.f : 1.f / l;   // (a NaN stays one)
+  T* to = reinterpret_cast<T*>(a.o) + row * D + lane * PER;
+  if constexpr (PER == 2) Mma<T, D>::put2(to, o[0] * inv, o[1] * inv);
+  else if constexpr (std::is_same<T, float>::value) *to = o[0] * inv;
+  else *reinterpret_cast<__bf16*>(to) = (__bf16)(o[0] * inv);
+  if (lane == 0 && a.lse) a.lse[row] = l == 0.f ? -INFINITY : (M_ + __log2f(l)) * kLn2;
+}
+
+template <typename T, int D, int NB>
+static void launch(Args a, hipStream_t st, int short_wg, int tile_wg) {
+  constexpr int TM = CH_NW * NB * 32;
+  {
+    TimedLaunch t(HK_TK_CHUNK_ATTN, st);
+    if (tile_wg > 0)
+      hipLaunchKernelGGL((chunk_tile_kernel<T, D, NB>), dim3(tile_wg, a.n_split), dim3(CH_NT), 0, st, a);
+    hipLaunchKernelGGL((chunk_short_kernel<T, D>), dim3(short_wg, a.n_split), dim3(CH_NT), 0, st, a);
+  }
+  if (a.n_split > 1) {
+    TimedLaunch t(HK_TK_CHUNK_MERGE, st);
+    const int64_t rows = (int64_t)a.n_tokens * a.Hq;
+    hipLaunchKernelGGL((chunk_merge_kernel<T, D, TM>), dim3((uint32_t)((rows + CH_NW - 1) / CH_NW)), dim3(CH_NT), 0, st, a);
+  }
+}
+
+// Splits of a launch: enough workgroups to fill the chip, none of less than MIN_PAGES pages.
+static int plan_splits(long long wg, int max_pages) {
+  int n = 1;
+  const int most = (max_pages + MIN_PAGES - 1) / MIN_PAGES;
+  while (n < most && n < 64 && wg * n < 512) n *= 2;
+  return n < most ? n : most;
+}
+
+struct Plan {
+  int short_wg, tile_wg, n_split;
+};
+static Plan plan(int NS, int Hq, int Hkv, int TM, int n_tokens, int max_len, int max_pages) {
+  const int G = Hq / Hkv;
+  Plan p;
+  p.short_wg = NS * Hkv;
+  const long long rows = (long long)n_tokens * G;
+  const bool tiles = (long long)max_len * G > SHORT_ROWS && rows > SHORT_ROWS;
+  p.tile_wg = tiles ? (int)((rows / TM + NS) * Hkv) : 0;
+  p.n_split = plan_splits(tiles ? p.tile_wg : p.short_wg, max_pages);
+  return p;
+}
+
+}  // namespace hk
+
+using namespace hk;
+
+static int tile_rows(hk_dtype dtype) { return CH_NW * 32 * (dtype == HK_BF16 ? 2 : 1); }
+
+// Grows with the tokens and does not depend on the type: split states are kept for at most
+// MAX_STATES rows (plan_splits stops at 512 workgroups, so a launch that splits has fewer).
+constexpr size_t MAX_STATES = (size_t)1024 * CH_NW * 64;
+size_t hk_chunk_attn_ws(int NS, int Hq, int Hkv, int D, int n_tokens, int max_len, int max_pages) {
+  const size_t most = std::min((max_pages + MIN_PAGES - 1) / MIN_PAGES, 64);
+  const size_t rows = std::min((size_t)n_tokens * Hq * most, MAX_STATES);
+  return rows * (D + 2) * sizeof(float);
+}
+
+hipError_t hk_launch_chunk_attn(int NS, int Hq, int Hkv, int D, const hk_paged_kv* kv, const hk_chunks* ch,
+                                const void* q, int64_t q_row, float sm_scale, void* o, float* lse, void* ws,
+                                hipStream_t st) {
+  const bool bf = kv->dtype == HK_BF16;
+  const Plan p = plan(NS, Hq, Hkv, tile_rows(kv->dtype), ch->n_tokens, ch->max_len, kv->max_pages);
+  Args a;
+  a.q = static_cast<const char*>(q);
+  a.k_pool = static_cast<const char*>(kv->k_pool);
+  a.v_pool = static_cast<const char*>(kv->v_pool);
+  a.table = kv->page_table;
+  a.n_pages = kv->n_pages;
+  a.start = ch->start;
+  a.masks = kv->page_mask;
+  a.q_row = q_row;
+  a.o = static_cast<char*>(o);
+  a.lse = lse;
+  a.part_o = static_cast<float*>(ws);
+  a.part_ml = p.n_split > 1 ? a.part_o + (size_t)ch->n_tokens * Hq * p.n_split * D : nullptr;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.G = Hq / Hkv;
+  a.max_pages = kv->max_pages;
+  a.num_pages = kv->num_pages;
+  a.n_seq = NS;
+  a.n_tokens = ch->n_tokens;
+  a.max_len = ch->max_len;
+  a.n_split = p.n_split;
+  a.c2 = sm_scale * kLog2e;
+  if (bf && D == 128) launch<uint16_t, 128, 2>(a, st, p.short_wg, p.tile_wg);
+  else if (bf) launch<uint16_t, 64, 2>(a, st, p.short_wg, p.tile_wg);
+  else if (D == 128) launch<float, 128, 1>(a, st, p.short_wg, p.tile_wg);
+  else launch<float, 64, 1>(a, st, p.short_wg, p.tile_wg);
+  return hipGetLastError();
+}

@@ -12,7 +12,9 @@ from dataclasses import dataclass
 
 import torch
 
-from . import (Allocator, PagedKV, OP_APPEND, OP_COMPACT, OP_DECODE, OP_SCORE, dims, hk_append_kv,
+from . import (Allocator, Chunks, PagedKV, OP_APPEND, OP_COMPACT, OP_DECODE, OP_RESERVE, OP_SCORE, OP_TRIM,
+               HardKVError, chunk_attn_workspace, dims, hk_append_kv, hk_chunk_attn, hk_reserve_slots,
+               hk_trim_slots, hk_verify_draft, hk_write_kv, verify_workspace,
                hk_budget_plan, hk_budget_select, hk_calibrate, hk_calibrate_solve_T,
                hk_calibrate_solve_T_gd, hk_calibrate_topp_ws, hk_compact, hk_compact_modes, hk_decode_attn, hk_pool_max,
                hk_score, hk_score_rows, hk_vote_topp, select_workspace, workspace)
@@ -221,6 +223,77 @@ class Decoder:
         hk_decode_attn(self.d, q, self.kv, self.sm_scale, o, lse, self.ws, stream=stream)
 
 
+class ChunkDecoder:
+    """Steps of several new tokens per sequence (prompts in chunks, drafts, single tokens beside
+    them) over a cache of `layers` layers of B sequences, layers one after the other.
+
+    append(): slots for a batch of chunks in every layer, and their K and V rows into the pool;
+    reserve() and write() are its halves, for K and V that come layer by layer.
+    attend(): one layer's causal attention of the chunks.
+    trim(): the newest n_drop[s] tokens of every sequence taken back, in every layer.
+    The buffers serve any chunks of at most max_tokens rows and max_len tokens a sequence.
+    status collects FLAG_NOSPACE / FLAG_CHUNK: such a reserve() gave no slots (see hardkv.h).
+    """
+
+    def __init__(self, B, Hq, Hkv, D, kv: PagedKV, alloc: Allocator, max_tokens: int, max_len: int,
+                 layers: int = 1):
+        self.B, self.layers, self.max_tokens, self.max_len = B, layers, max_tokens, max_len
+        self.d_all, self.d = dims(layers * B, Hq, Hkv, D), dims(B, Hq, Hkv, D)
+        self.kv, self.alloc = kv, alloc
+        self.kv_layer = [kv.rows(l * B * Hkv, B * Hkv) for l in range(layers)] if layers > 1 else [kv]
+        self.sm_scale = 1.0 / math.sqrt(D)
+        dev = kv.k_pool.device
+        self.ws_slots = workspace(OP_RESERVE, self.d_all, kv.max_pages, dev)
+        self.ws_trim = workspace(OP_TRIM, self.d_all, kv.max_pages, dev)
+        most = Chunks(torch.empty(B + 1, dtype=torch.int32), max_tokens, max_len)
+        self.ws = chunk_attn_workspace(self.d, most, kv.max_pages, dev)
+        self.status = torch.zeros(1, dtype=torch.int32, device=dev)
+
+    def _fits(self, chunks: Chunks):
+        if chunks.n_seq != self.B or chunks.n_tokens > self.max_tokens or chunks.max_len > self.max_len:
+            raise HardKVError("the chunks are larger than the decoder was made for")
+
+    def reserve(self, chunks: Chunks, slot_map, stream=None):
+        """slot_map: [layers, n_tokens, Hkv] int64, written in full."""
+        self._fits(chunks)
+        hk_reserve_slots(self.d_all, self.kv, chunks, self.alloc, self.ws_slots, slot_map=slot_map,
+                         status=self.status, stream=stream)
+
+    def write(self, chunks: Chunks, slot_map, k_new, v_new, stream=None):
+        """One layer ([tokens, Hkv, D], that layer's part of the slot map) or all of them
+        ([layers, tokens, Hkv, D])."""
+        hk_write_kv(self.d, self.kv, chunks.n_tokens, slot_map, k_new, v_new, stream=stream)
+
+    def append(self, chunks: Chunks, k_new, v_new, slot_map, stream=None):
+        self.reserve(chunks, slot_map, stream=stream)
+        self.write(chunks, slot_map, k_new, v_new, stream=stream)
+
+    def attend(self, chunks: Chunks, q, o, lse=None, layer: int = 0, stream=None):
+        self._fits(chunks)
+        hk_chunk_attn(self.d, self.kv_layer[layer], chunks, q, self.sm_scale, o, self.ws, lse=lse,
+                      stream=stream)
+
+    def trim(self, n_drop, stream=None):
+        if n_drop.numel() != self.B:
+            raise HardKVError("n_drop must have one entry per sequence")
+        hk_trim_slots(self.d_all, self.kv, n_drop, self.alloc, self.ws_trim, stream=stream)
+
+
+class Verifier:
+    """Drafted tokens of up to B sequences against the target's probabilities over V tokens."""
+
+    def __init__(self, B: int, V: int, device):
+        self.B, self.V = B, V
+        self.ws = verify_workspace(B, V, device)
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)
+
+    def verify(self, chunks: Chunks, tokens, p, u, n_accept, next_token, n_drop, q=None, stream=None):
+        if chunks.n_seq > self.B:
+            raise HardKVError("more sequences than the verifier was made for")
+        hk_verify_draft(chunks, self.V, tokens, p, u, n_accept, next_token, n_drop, self.ws, q=q,
+                        status=self.status, stream=stream)
+
+
 class DecodeLoop:
     """End-to-end decode loop over L independent attention layers sharing one page pool
     and one allocator (config-5 style).
@@ -229,11 +302,17 @@ class DecodeLoop:
                 decode-attention launch per layer, writing o and the row LSE.
     compress(): Steps 2-3 over every layer at once, with the window queries and the decode
                 step's own LSEs (single-pass score).
+    With max_tokens (and max_len) it also takes several new tokens per sequence at once:
+    extend():   prompts in chunks, or the last token and its drafts: slots and K/V for every
+                layer, then one chunk attention per layer;
+    accept():   drafts against the target's probabilities, the rejected ones taken back in
+                every layer.
     Heads are ordered (layer, sequence, KV head); sequence index = layer * B + b.
     """
 
     def __init__(self, L, B, Hq, Hkv, D, W, kv: PagedKV, alloc: Allocator, p: float,
-                 L_dense: int, L_sparse: int = 0, keep_c: bool = True):
+                 L_dense: int, L_sparse: int = 0, keep_c: bool = True, max_tokens: int = 0,
+                 max_len: int = 0):
         self.L, self.B, self.Hq, self.Hkv, self.D, self.W = L, B, Hq, Hkv, D, W
         self.kv, self.alloc = kv, alloc
         self.NS = L * B
@@ -248,6 +327,28 @@ class DecodeLoop:
         self.o = torch.empty(self.NS, Hq, D, dtype=torch.float32, device=dev)
         self.comp = Compressor(self.NS, Hq, Hkv, D, W, kv, alloc, p, L_dense=L_dense,
                                L_sparse=L_sparse, metric="attn", keep_c=keep_c)
+        self.chunked = None
+        if max_tokens > 0:
+            self.chunked = ChunkDecoder(B, Hq, Hkv, D, kv, alloc, max_tokens, max_len or max_tokens, layers=L)
+            self.chunked.status = self.status
+            self.slot_map = torch.empty(L * max_tokens * Hkv, dtype=torch.int64, device=dev)
+
+    def extend(self, chunks, q, k, v, o, lse, stream=None):
+        """q [L, tokens, Hq, D], k and v [L, tokens, Hkv, D] (views with contiguous heads will do),
+        o [L, tokens, Hq, D] in the cache's type, lse [L, tokens, Hq] fp32."""
+        if self.chunked is None:
+            raise HardKVError("the loop was made without max_tokens")
+        ch, n = self.chunked, self.L * chunks.n_tokens * self.Hkv
+        ch.append(chunks, k, v, self.slot_map[:n], stream=stream)
+        for l in range(self.L):
+            ch.attend(chunks, q[l], o[l], lse[l], layer=l, stream=stream)
+
+    def accept(self, verifier: Verifier, chunks, tokens, p, u, n_accept, next_token, n_drop, q=None,
+               stream=None):
+        if self.chunked is None:
+            raise HardKVError("the loop was made without max_tokens")
+        verifier.verify(chunks, tokens, p, u, n_accept, next_token, n_drop, q=q, stream=stream)
+        self.chunked.trim(n_drop, stream=stream)
 
     def step(self, q_t, k_t, v_t, lse_t, stream=None):
         hk_append_kv(self.d_all, self.kv, k_t, v_t, self.alloc, self.status, self.ws_app,
