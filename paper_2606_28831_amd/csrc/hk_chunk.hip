@@ -373,13 +373,16 @@ __device__ __forceinline__ void put_state(const Args& a, int64_t row, int split,
 }
 
 // ------------------------------------------------------------------ tile kernel
-template <typename T, int D, int NB>
-__global__ __launch_bounds__(CH_NT, 1) void chunk_tile_kernel(Args a) {
+constexpr int TILE_NW = 8, TILE_NT = 64 * TILE_NW;              // waves and threads of a workgroup
+constexpr int TILE_ROWS = 32 * TILE_NW;
+
+template <typename T, int D>
+__global__ __launch_bounds__(TILE_NT, 2) void chunk_tile_kernel(Args a) {
   using L = TileLayout<T, D>;
   using M = Mma<T, D>;
-  constexpr int TM = CH_NW * NB * 32, TP = 4, TK = TP * HK_PAGE;   // rows, pages and keys of a tile
-  __shared__ __align__(16) char s_k[2][TK * L::ROW], s_v[2][TK * L::ROW];
-  __shared__ uint16_t s_odd[2][TP];
+  constexpr int TM = TILE_ROWS, TP = 4, TK = TP * HK_PAGE;       // rows, pages and keys of a tile
+  __shared__ __align__(16) char s_kv[2][2][TK * L::ROW];
+  __shared__ __align__(8) uint16_t s_mask[2][TP], s_odd[2][TP];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   // the largest tiles of a sequence first: tile u of the launch counts down
   const int kv = blockIdx.x % a.Hkv, u = (int)(gridDim.x / a.Hkv) - 1 - (int)(blockIdx.x / a.Hkv), split = blockIdx.y;
@@ -403,76 +406,84 @@ __global__ __launch_bounds__(CH_NT, 1) void chunk_tile_kernel(Args a) {
   if (split > 0 && p0 >= pages) return;
 
   // rows past the chunk repeat its last one; they are not stored
-  typename M::Query q[NB];
-  int64_t row[NB];
-  int seen[NB];                               // keys before this one are seen by the lane's query
-  const int w0 = r0 + wave * NB * 32;
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    const int r = min(w0 + b * 32 + (lane & 31), rows - 1), tok = r / a.G;
-    row[b] = (int64_t)(c.first + tok) * a.Hq + kv * a.G + (r - tok * a.G);
-    seen[b] = end - c.len + tok + 1;
-    M::load_q(q[b], reinterpret_cast<const T*>(a.q) + (int64_t)(c.first + tok) * a.q_row + (kv * a.G + (r - tok * a.G)) * D);
-  }
+  const int w0 = r0 + wave * 32;
+  const int r = min(w0 + (lane & 31), rows - 1), tok = r / a.G, g = r - tok * a.G;
+  const int64_t row = (int64_t)(c.first + tok) * a.Hq + kv * a.G + g;
+  const int seen = end - c.len + tok + 1;                        // keys before this one are seen by the lane's query
   const int seen_all = end - c.len + min(w0, rows - 1) / a.G + 1;
+  const int tile_seen = end - c.len + r0 / a.G + 1;              // by every query of the workgroup
+  typename M::Query q[1];
+  M::load_q(q[0], reinterpret_cast<const T*>(a.q) + (int64_t)(c.first + tok) * a.q_row + (kv * a.G + g) * D);
   const float bias = bias_of(pages);
-  State<T, D, NB> st;
+  State<T, D, 1> st;
   st.init();
-  const bool active = w0 < rows;
   const int tiles = p1 > p0 ? (p1 - p0 + TP - 1) / TP : 0;
-  PageRegs<T, D> rk, rv;
-  uint32_t mask = 0;
-  const int tile_seen = end - c.len + r0 / a.G + 1;             // keys that every query of the tile sees
-  auto load = [&](int t) {
-    const int p = p0 + t * TP + wave;
-    mask = p < p1 ? mrow[p] : 0u;
-    const int id = min(max(trow[min(p, p1 - 1)], 0), a.num_pages - 1);
-    rk.load(a.k_pool, id);
-    rv.load(a.v_pool, id);
+  // waves 0 to 3 bring a page of K each, waves 4 to 7 the same pages of V; a page's id and mask are
+  // loaded a tile before the page
+  const int my = wave & 3;
+  const bool is_v = wave >= 4;
+  const char* pool = is_v ? a.v_pool : a.k_pool;
+  PageRegs<T, D> rp;
+  int id = 0;
+  uint32_t mask = 0, next_mask = 0;
+  auto load_id = [&](int t) {
+    const int p = p0 + t * TP + my;
+    next_mask = p < p1 ? mrow[p] : 0u;
+    id = trow[min(p, p1 - 1)];
   };
-  auto at_edge = [&](int p) { return (p + 1) * HK_PAGE > tile_seen; };
-  // V row of key k of the 32 from page p on
-  auto row_at = [&](int p) {
+  auto load = [&] {
+    mask = next_mask;
+    rp.load(pool, min(max(id, 0), a.num_pages - 1));
+  };
+  auto row_at = [&](int p) {                                     // V row of key k of the 32 from page p on
     return [&, p](int k) {
-      const int id = min(max(trow[min(p + k / HK_PAGE, p1 - 1)], 0), a.num_pages - 1);
-      return reinterpret_cast<const T*>(a.v_pool) + ((size_t)id * HK_PAGE + k % HK_PAGE) * D;
+      const int at = min(max(trow[min(p + k / HK_PAGE, p1 - 1)], 0), a.num_pages - 1);
+      return reinterpret_cast<const T*>(a.v_pool) + ((size_t)at * HK_PAGE + k % HK_PAGE) * D;
     };
   };
-  if (tiles > 0) load(0);
+  if (tiles > 0) {
+    load_id(0);
+    load();
+    load_id(1);
+  }
   for (int t = 0; t < tiles; ++t) {
-    if (at_edge(p0 + t * TP + wave)) {
-      const uint32_t odd = rv.odd_rows() & mask;
-      mask &= ~odd;
-      if (lane == 0) s_odd[t & 1][wave] = (uint16_t)odd;
+    const int p = p0 + t * TP, buf = t & 1;
+    if (is_v) {
+      uint32_t keep = mask, odd = 0;
+      if ((p + my + 1) * HK_PAGE > tile_seen) {
+        odd = rp.odd_rows() & mask;
+        keep &= ~odd;
+      }
+      if (keep != 0xffffu) rp.clear(keep);
+      if (lane == 0) {
+        s_mask[buf][my] = (uint16_t)mask;
+        s_odd[buf][my] = (uint16_t)odd;
+      }
     }
-    if (mask != 0xffffu) rv.clear(mask);
-    rk.store(s_k[t & 1], wave * HK_PAGE);
-    rv.store(s_v[t & 1], wave * HK_PAGE);
+    rp.store(s_kv[buf][is_v], my * HK_PAGE);
     __syncthreads();
-    if (t + 1 < tiles) load(t + 1);
-    if (active)
+    if (t + 1 < tiles) {
+      load();
+      load_id(t + 2);
+    }
+    if (w0 < rows) {
+      const uint64_t m64 = *reinterpret_cast<const uint64_t*>(s_mask[buf]);
+      const uint64_t o64 = *reinterpret_cast<const uint64_t*>(s_odd[buf]);
 #pragma unroll
       for (int hb = 0; hb < TK / 32; ++hb) {
-        const int p = p0 + t * TP + 2 * hb, key = p * HK_PAGE;
-        const uint32_t valid = (p < p1 ? (uint32_t)mrow[p] : 0u) | (p + 1 < p1 ? (uint32_t)mrow[p + 1] << 16 : 0u);
+        const int key = (p + 2 * hb) * HK_PAGE;
+        const uint32_t valid = __builtin_amdgcn_readfirstlane((uint32_t)(m64 >> (32 * hb)));
+        const uint32_t odd = __builtin_amdgcn_readfirstlane((uint32_t)(o64 >> (32 * hb)));
         const bool all = valid == 0xffffffffu && key + 32 <= seen_all;
-        uint32_t vis[NB];
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          const int k = seen[b] - key;
-          vis[b] = valid & (k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u);
-        }
-        const uint32_t odd = (at_edge(p) ? (uint32_t)s_odd[t & 1][2 * hb] : 0u) |
-                             (at_edge(p + 1) ? (uint32_t)s_odd[t & 1][2 * hb + 1] << 16 : 0u);
-        st.block(q, s_k[t & 1] + hb * 32 * L::ROW, s_v[t & 1] + hb * 32 * L::ROW, vis, all, a.c2, bias,
-                 __builtin_amdgcn_readfirstlane(odd), row_at(p));
+        const int k = seen - key;
+        const uint32_t vis[1] = {valid & (k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u)};
+        st.block(q, s_kv[buf][0] + hb * 32 * L::ROW, s_kv[buf][1] + hb * 32 * L::ROW, vis, all, a.c2, bias, odd,
+                 row_at(p + 2 * hb));
       }
+    }
   }
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    const float l = st.l[b] + __shfl_xor(st.l[b], 32, 64);
-    if (w0 + b * 32 + (lane & 31) < rows) put_state<T, D>(a, row[b], split, st.acc[b], st.mb[b], l);
-  }
+  const float l = st.l[0] + __shfl_xor(st.l[0], 32, 64);
+  if (w0 + (lane & 31) < rows) put_state<T, D>(a, row, split, st.acc[0], st.mb[0], l);
 }
 
 // ------------------------------------------------------------------ short kernel
@@ -648,13 +659,13 @@ __global__ __launch_bounds__(CH_NT) void chunk_merge_kernel(Args a) {
   if (lane == 0 && a.lse) a.lse[row] = l == 0.f ? -INFINITY : (M_ + __log2f(l)) * kLn2;
 }
 
-template <typename T, int D, int NB>
+template <typename T, int D>
 static void launch(Args a, hipStream_t st, int short_wg, int tile_wg) {
-  constexpr int TM = CH_NW * NB * 32;
+  constexpr int TM = TILE_ROWS;
   {
     TimedLaunch t(HK_TK_CHUNK_ATTN, st);
     if (tile_wg > 0)
-      hipLaunchKernelGGL((chunk_tile_kernel<T, D, NB>), dim3(tile_wg, a.n_split), dim3(CH_NT), 0, st, a);
+      hipLaunchKernelGGL((chunk_tile_kernel<T, D>), dim3(tile_wg, a.n_split), dim3(TILE_NT), 0, st, a);
     hipLaunchKernelGGL((chunk_short_kernel<T, D>), dim3(short_wg, a.n_split), dim3(CH_NT), 0, st, a);
   }
   if (a.n_split > 1) {
@@ -690,8 +701,6 @@ static Plan plan(int NS, int Hq, int Hkv, int TM, int n_tokens, int max_len, int
 
 using namespace hk;
 
-static int tile_rows(hk_dtype dtype) { return CH_NW * 32 * (dtype == HK_BF16 ? 2 : 1); }
-
 // Grows with the tokens and does not depend on the type: split states are kept for at most
 // MAX_STATES rows (plan_splits stops at 512 workgroups, so a launch that splits has fewer).
 constexpr size_t MAX_STATES = (size_t)1024 * CH_NW * 64;
@@ -705,7 +714,7 @@ hipError_t hk_launch_chunk_attn(int NS, int Hq, int Hkv, int D, const hk_paged_k
                                 const void* q, int64_t q_row, float sm_scale, void* o, float* lse, void* ws,
                                 hipStream_t st) {
   const bool bf = kv->dtype == HK_BF16;
-  const Plan p = plan(NS, Hq, Hkv, tile_rows(kv->dtype), ch->n_tokens, ch->max_len, kv->max_pages);
+  const Plan p = plan(NS, Hq, Hkv, TILE_ROWS, ch->n_tokens, ch->max_len, kv->max_pages);
   Args a;
   a.q = static_cast<const char*>(q);
   a.k_pool = static_cast<const char*>(kv->k_pool);
@@ -729,9 +738,9 @@ hipError_t hk_launch_chunk_attn(int NS, int Hq, int Hkv, int D, const hk_paged_k
   a.max_len = ch->max_len;
   a.n_split = p.n_split;
   a.c2 = sm_scale * kLog2e;
-  if (bf && D == 128) launch<uint16_t, 128, 2>(a, st, p.short_wg, p.tile_wg);
-  else if (bf) launch<uint16_t, 64, 2>(a, st, p.short_wg, p.tile_wg);
-  else if (D == 128) launch<float, 128, 1>(a, st, p.short_wg, p.tile_wg);
-  else launch<float, 64, 1>(a, st, p.short_wg, p.tile_wg);
+  if (bf && D == 128) launch<uint16_t, 128>(a, st, p.short_wg, p.tile_wg);
+  else if (bf) launch<uint16_t, 64>(a, st, p.short_wg, p.tile_wg);
+  else if (D == 128) launch<float, 128>(a, st, p.short_wg, p.tile_wg);
+  else launch<float, 64>(a, st, p.short_wg, p.tile_wg);
   return hipGetLastError();
 }
