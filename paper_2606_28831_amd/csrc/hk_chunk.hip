@@ -42,8 +42,10 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 // ------------------------------------------------------------------ LDS tiles
-// A tile row is one key's K or V row, its 16-byte pieces permuted within the row by the key so that
-// the MFMA fragments' reads spread over the banks.
+// A tile row is one key's K or V row.  Rows are padded so that the fragments' reads spread over the
+// 64 banks, at offsets that are constants: K, 16 bytes of eight consecutive keys, by 16 bytes; V by
+// 64 (bf16: 64 bytes of eight keys, two to a bank group at best) or 32 (fp32: 128 bytes of keys k
+// and k + 4).
 template <typename T, int D>
 struct TileLayout {
   static constexpr int ES = sizeof(T);
@@ -51,12 +53,7 @@ struct TileLayout {
   static constexpr int PIECES = ROW / 16;
   static constexpr int PAGE = HK_PAGE * ROW;
   static constexpr int LOADS = PAGE / 1024;   // 16-byte loads per lane of a wave for a page
-  __device__ static __forceinline__ int turn(int key) {
-    if (ES == 4) return (key & 7) | ((key & 4) << 1);
-    if (D == 128) return ((key & 3) << 2) | ((key >> 2) & 3);
-    return ((key & 2) << 1) | ((key >> 2) & 3);
-  }
-  __device__ static __forceinline__ int at(int key, int piece) { return key * ROW + ((piece ^ turn(key)) * 16); }
+  static constexpr int K_ROW = ROW + 16, V_ROW = ROW + (ES == 2 ? 64 : 32);
 };
 
 // One page's K or V rows on their way from memory to LDS: piece i * 64 + lane of the page.
@@ -95,13 +92,12 @@ struct PageRegs {
     }
     return rows;
   }
-  __device__ __forceinline__ void store(char* tile, int key0) const {
+  // into rows of `stride` bytes from `to` on
+  __device__ __forceinline__ void store(char* to, int stride) const {
     const int lane = threadIdx.x & 63;
+    to += lane / L::PIECES * stride + lane % L::PIECES * 16;
 #pragma unroll
-    for (int i = 0; i < L::LOADS; ++i) {
-      const int e = i * 64 + lane;
-      *reinterpret_cast<u32x4*>(tile + L::at(key0 + e / L::PIECES, e % L::PIECES)) = r[i];
-    }
+    for (int i = 0; i < L::LOADS; ++i) *reinterpret_cast<u32x4*>(to + i * (64 / L::PIECES) * stride) = r[i];
   }
 };
 
@@ -132,7 +128,7 @@ struct Mma<uint16_t, D> {
       for (int r = 0; r < 16; ++r) z[b][r] = 0.f;
 #pragma unroll
     for (int s = 0; s < D / 16; ++s) {
-      const bf16x8 a = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(k + L::at(key, 2 * s + hi)));
+      const bf16x8 a = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(k + key * L::K_ROW + (2 * s + hi) * 16));
 #pragma unroll
       for (int b = 0; b < NB; ++b) z[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[b].f[s], z[b], 0, 0, 0);
     }
@@ -157,8 +153,7 @@ struct Mma<uint16_t, D> {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           // sixteen lanes turn four keys x 16 dims: lane i supplies 4 dims of key i / 4
-          const int key = 16 * s + 8 * h + 4 * hi + (i16 >> 2), piece = 4 * dt + 2 * g1 + ((i16 & 3) >> 1);
-          const char* at = v + L::at(key, piece) + (i16 & 1) * 8;
+          const char* at = v + (16 * s + 8 * h + 4 * hi + (i16 >> 2)) * L::V_ROW + dt * 64 + g1 * 32 + (i16 & 3) * 8;
           a[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
               (__attribute__((address_space(3))) s16x4*)(uintptr_t)(__attribute__((address_space(3))) const char*)at);
         }
@@ -201,7 +196,7 @@ struct Mma<float, D> {
       for (int r = 0; r < 16; ++r) z[b][r] = 0.f;
 #pragma unroll
     for (int s = 0; s < D / 8; ++s) {
-      const f32x4 a = *reinterpret_cast<const f32x4*>(k + L::at(key, 2 * s + hi));
+      const f32x4 a = *reinterpret_cast<const f32x4*>(k + key * L::K_ROW + (2 * s + hi) * 16);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -216,7 +211,7 @@ struct Mma<float, D> {
       const int key = (r & 3) + 8 * (r >> 2) + 4 * hi;
 #pragma unroll
       for (int dt = 0; dt < D / 32; ++dt) {
-        const float a = *reinterpret_cast<const float*>(v + L::at(key, 8 * dt + (dim >> 2)) + (dim & 3) * 4);
+        const float a = *reinterpret_cast<const float*>(v + key * L::V_ROW + (32 * dt + dim) * 4);
 #pragma unroll
         for (int b = 0; b < NB; ++b)
           acc[b][dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p[b][r], acc[b][dt], 0, 0, 0);
@@ -372,20 +367,25 @@ __device__ __forceinline__ void put_state(const Args& a, int64_t row, int split,
   if (hi == 0 && a.lse) a.lse[row] = l == 0.f ? -INFINITY : (mb + __log2f(l)) * kLn2;
 }
 
-// ------------------------------------------------------------------ tile kernel
-constexpr int TILE_NW = 8, TILE_NT = 64 * TILE_NW;              // waves and threads of a workgroup
-constexpr int TILE_ROWS = 32 * TILE_NW;
+// ------------------------------------------------------------------ tile kernels
+constexpr int TILE_PAGES = 4, TILE_KEYS = TILE_PAGES * HK_PAGE;
 
-template <typename T, int D>
-__global__ __launch_bounds__(TILE_NT, 2) void chunk_tile_kernel(Args a) {
-  using L = TileLayout<T, D>;
-  using M = Mma<T, D>;
-  constexpr int TM = TILE_ROWS, TP = 4, TK = TP * HK_PAGE;       // rows, pages and keys of a tile
-  __shared__ __align__(16) char s_kv[2][2][TK * L::ROW];
-  __shared__ __align__(8) uint16_t s_mask[2][TP], s_odd[2][TP];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// What a workgroup of a tile kernel works on: TM folded rows of one sequence and KV head, and a
+// range of its pages.  None: nothing (p1 < 0).
+struct TileWork {
+  Chunk c;
+  int kv, split, rows, r0, end, pages, p0, p1;
+  const int32_t* trow;
+  const uint16_t* mrow;
+};
+template <int TM>
+__device__ __forceinline__ TileWork tile_work(const Args& a) {
+  TileWork w;
   // the largest tiles of a sequence first: tile u of the launch counts down
-  const int kv = blockIdx.x % a.Hkv, u = (int)(gridDim.x / a.Hkv) - 1 - (int)(blockIdx.x / a.Hkv), split = blockIdx.y;
+  const int u = (int)(gridDim.x / a.Hkv) - 1 - (int)(blockIdx.x / a.Hkv);
+  w.kv = blockIdx.x % a.Hkv;
+  w.split = blockIdx.y;
+  w.p1 = -1;
   auto tiles_before = [&](int s) { return min(max(a.start[s], 0), a.n_tokens) * a.G / TM + s; };
   int s = 0;
   for (int hi = a.n_seq; hi - s > 1;) {
@@ -393,52 +393,68 @@ __global__ __launch_bounds__(TILE_NT, 2) void chunk_tile_kernel(Args a) {
     if (tiles_before(mid) <= u) s = mid;
     else hi = mid;
   }
-  const Chunk c = chunk_of(a.start, s, a.n_tokens, a.max_len);
-  const int rows = c.len * a.G, r0 = (u - tiles_before(s)) * TM;
-  if (rows <= SHORT_ROWS || r0 < 0 || r0 >= rows) return;
-  const int h = s * a.Hkv + kv, n = min(max(a.n_pages[h], 0), a.max_pages);
-  const int32_t* trow = a.table + (size_t)h * a.max_pages;
-  const uint16_t* mrow = a.masks + (size_t)h * a.max_pages;
-  const int end = row_end(n, n > 0 ? mrow[n - 1] : 0u);
-  const int pages = tile_pages(n, end, c.len, (min(r0 + TM, rows) - 1) / a.G);
-  const int share = split_share(pages, a.n_split);
-  const int p0 = split * share, p1 = min(p0 + share, pages);
-  if (split > 0 && p0 >= pages) return;
+  w.c = chunk_of(a.start, s, a.n_tokens, a.max_len);
+  w.rows = w.c.len * a.G;
+  w.r0 = (u - tiles_before(s)) * TM;
+  if (w.rows <= SHORT_ROWS || w.r0 < 0 || w.r0 >= w.rows) return w;
+  const int h = s * a.Hkv + w.kv, n = min(max(a.n_pages[h], 0), a.max_pages);
+  w.trow = a.table + (size_t)h * a.max_pages;
+  w.mrow = a.masks + (size_t)h * a.max_pages;
+  w.end = row_end(n, n > 0 ? w.mrow[n - 1] : 0u);
+  w.pages = tile_pages(n, w.end, w.c.len, (min(w.r0 + TM, w.rows) - 1) / a.G);
+  const int share = split_share(w.pages, a.n_split);
+  w.p0 = w.split * share;
+  w.p1 = w.split > 0 && w.p0 >= w.pages ? -1 : min(w.p0 + share, w.pages);
+  return w;
+}
 
+// fp32: a wave takes 32 rows; the next tile's pages load while a tile is computed.  Bound by the
+// fp32 matrix rate, which is a sixteenth of bf16's.
+template <int D, int NW>
+__global__ __launch_bounds__(64 * NW, 1) void chunk_tile_f32_kernel(Args a) {
+  using L = TileLayout<float, D>;
+  using M = Mma<float, D>;
+  constexpr int TP = TILE_PAGES, PPW = 2 * TP / NW;               // pages that a wave brings
+  __shared__ __align__(16) char s_k[2][TILE_KEYS * L::K_ROW], s_v[2][TILE_KEYS * L::V_ROW];
+  __shared__ __align__(8) uint16_t s_mask[2][TP], s_odd[2][TP];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const TileWork w = tile_work<32 * NW>(a);
+  if (w.p1 < 0) return;
   // rows past the chunk repeat its last one; they are not stored
-  const int w0 = r0 + wave * 32;
-  const int r = min(w0 + (lane & 31), rows - 1), tok = r / a.G, g = r - tok * a.G;
-  const int64_t row = (int64_t)(c.first + tok) * a.Hq + kv * a.G + g;
-  const int seen = end - c.len + tok + 1;                        // keys before this one are seen by the lane's query
-  const int seen_all = end - c.len + min(w0, rows - 1) / a.G + 1;
-  const int tile_seen = end - c.len + r0 / a.G + 1;              // by every query of the workgroup
+  const int w0 = w.r0 + wave * 32, off = w.end - w.c.len + 1;
+  const int r = min(w0 + (lane & 31), w.rows - 1), tok = r / a.G, g = r - tok * a.G;
+  const int64_t row = (int64_t)(w.c.first + tok) * a.Hq + w.kv * a.G + g;
+  const int seen = off + tok;                                    // keys before this one are seen by the lane's query,
+  const int seen_all = off + min(w0, w.rows - 1) / a.G;          // by every query of the wave,
+  const int tile_seen = off + w.r0 / a.G;                        // of the workgroup
   typename M::Query q[1];
-  M::load_q(q[0], reinterpret_cast<const T*>(a.q) + (int64_t)(c.first + tok) * a.q_row + (kv * a.G + g) * D);
-  const float bias = bias_of(pages);
-  State<T, D, 1> st;
+  M::load_q(q[0], reinterpret_cast<const float*>(a.q) + (int64_t)(w.c.first + tok) * a.q_row + (w.kv * a.G + g) * D);
+  const float bias = bias_of(w.pages);
+  State<float, D, 1> st;
   st.init();
-  const int tiles = p1 > p0 ? (p1 - p0 + TP - 1) / TP : 0;
-  // waves 0 to 3 bring a page of K each, waves 4 to 7 the same pages of V; a page's id and mask are
-  // loaded a tile before the page
-  const int my = wave & 3;
-  const bool is_v = wave >= 4;
-  const char* pool = is_v ? a.v_pool : a.k_pool;
-  PageRegs<T, D> rp;
-  int id = 0;
-  uint32_t mask = 0, next_mask = 0;
+  const int tiles = w.p1 > w.p0 ? (w.p1 - w.p0 + TP - 1) / TP : 0;
+  PageRegs<float, D> rp[PPW];
+  int id[PPW];
+  uint32_t mask[PPW], next_mask[PPW];
   auto load_id = [&](int t) {
-    const int p = p0 + t * TP + my;
-    next_mask = p < p1 ? mrow[p] : 0u;
-    id = trow[min(p, p1 - 1)];
+#pragma unroll
+    for (int i = 0; i < PPW; ++i) {
+      const int p = w.p0 + t * TP + (wave * PPW + i) % TP;
+      next_mask[i] = p < w.p1 ? w.mrow[p] : 0u;
+      id[i] = w.trow[min(p, w.p1 - 1)];
+    }
   };
   auto load = [&] {
-    mask = next_mask;
-    rp.load(pool, min(max(id, 0), a.num_pages - 1));
+#pragma unroll
+    for (int i = 0; i < PPW; ++i) {
+      mask[i] = next_mask[i];
+      rp[i].load((wave * PPW + i) / TP ? a.v_pool : a.k_pool, min(max(id[i], 0), a.num_pages - 1));
+    }
   };
   auto row_at = [&](int p) {                                     // V row of key k of the 32 from page p on
     return [&, p](int k) {
-      const int at = min(max(trow[min(p + k / HK_PAGE, p1 - 1)], 0), a.num_pages - 1);
-      return reinterpret_cast<const T*>(a.v_pool) + ((size_t)at * HK_PAGE + k % HK_PAGE) * D;
+      const int at = min(max(w.trow[min(p + k / HK_PAGE, w.p1 - 1)], 0), a.num_pages - 1);
+      return reinterpret_cast<const float*>(a.v_pool) + ((size_t)at * HK_PAGE + k % HK_PAGE) * D;
     };
   };
   if (tiles > 0) {
@@ -447,10 +463,99 @@ __global__ __launch_bounds__(TILE_NT, 2) void chunk_tile_kernel(Args a) {
     load_id(1);
   }
   for (int t = 0; t < tiles; ++t) {
-    const int p = p0 + t * TP, buf = t & 1;
+    const int p = w.p0 + t * TP, buf = t & 1;
+#pragma unroll
+    for (int i = 0; i < PPW; ++i) {
+      const int my = (wave * PPW + i) % TP, is_v = (wave * PPW + i) / TP;
+      if (is_v) {
+        uint32_t keep = mask[i], odd = 0;
+        if ((p + my + 1) * HK_PAGE > tile_seen) {
+          odd = rp[i].odd_rows() & keep;
+          keep &= ~odd;
+        }
+        if (keep != 0xffffu) rp[i].clear(keep);
+        if (lane == 0) {
+          s_mask[buf][my] = (uint16_t)mask[i];
+          s_odd[buf][my] = (uint16_t)odd;
+        }
+      }
+      if (is_v) rp[i].store(s_v[buf] + my * HK_PAGE * L::V_ROW, L::V_ROW);
+      else rp[i].store(s_k[buf] + my * HK_PAGE * L::K_ROW, L::K_ROW);
+    }
+    __syncthreads();
+    if (t + 1 < tiles) {
+      load();
+      load_id(t + 2);
+    }
+    if (w0 < w.rows) {
+      const uint64_t m64 = *reinterpret_cast<const uint64_t*>(s_mask[buf]);
+      const uint64_t o64 = *reinterpret_cast<const uint64_t*>(s_odd[buf]);
+#pragma unroll
+      for (int hb = 0; hb < TILE_KEYS / 32; ++hb) {
+        const int key = (p + 2 * hb) * HK_PAGE;
+        const uint32_t valid = __builtin_amdgcn_readfirstlane((uint32_t)(m64 >> (32 * hb)));
+        const uint32_t odd = __builtin_amdgcn_readfirstlane((uint32_t)(o64 >> (32 * hb)));
+        const bool all = valid == 0xffffffffu && key + 32 <= seen_all;
+        const int k = seen - key;
+        const uint32_t vis[1] = {valid & (k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u)};
+        st.block(q, s_k[buf] + hb * 32 * L::K_ROW, s_v[buf] + hb * 32 * L::V_ROW, vis, all, a.c2, bias, odd,
+                 row_at(p + 2 * hb));
+      }
+    }
+  }
+  const float l = st.l[0] + __shfl_xor(st.l[0], 32, 64);
+  if (w0 + (lane & 31) < w.rows) put_state<float, D>(a, row, w.split, st.acc[0], st.mb[0], l);
+}
+
+// bf16.  Eight waves, two a SIMD, take 32 rows each against tiles of 64 keys.  A wave's steps of 32
+// keys are a pipeline: the scores of the next block run beside the exponentials of this one, its
+// P V beside the next one's maximum; MFMAs and the vector work between them are laid out by hand.
+// Three tiles in LDS: while one is computed the next is stored, and a wave that is a barrier ahead
+// stores over none that another still reads.
+template <int D>
+__global__ __launch_bounds__(512, 2) void chunk_tile_bf16_kernel(Args a) {
+  using L = TileLayout<uint16_t, D>;
+  using M = Mma<uint16_t, D>;
+  constexpr int TP = TILE_PAGES, KS = D / 16, DT = D / 32, VS = 2 * DT, AHEAD = 3;
+  __shared__ __align__(16) char s_k[3][TILE_KEYS * L::K_ROW], s_v[3][TILE_KEYS * L::V_ROW];
+  __shared__ __align__(8) uint16_t s_mask[3][TP], s_odd[3][TP];
+  const int lane = threadIdx.x & 63, hi = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // (conditions on it are scalar)
+  const TileWork w = tile_work<256>(a);
+  if (w.p1 < 0) return;
+  // rows past the chunk repeat its last one; they are not stored
+  const int w0 = w.r0 + wave * 32, off = w.end - w.c.len + 1;
+  const int r = min(w0 + (lane & 31), w.rows - 1), tok = r / a.G, g = r - tok * a.G;
+  const int64_t row = (int64_t)(w.c.first + tok) * a.Hq + w.kv * a.G + g;
+  const int seen = off + tok;                                    // keys before this one are seen by the lane's query,
+  const int seen_all = off + min(w0, w.rows - 1) / a.G;          // by every query of the wave,
+  const int tile_seen = off + w.r0 / a.G;                        // of the workgroup
+  typename M::Query q;
+  M::load_q(q, reinterpret_cast<const uint16_t*>(a.q) + (int64_t)(w.c.first + tok) * a.q_row + (w.kv * a.G + g) * D);
+  const float bias = bias_of(w.pages), c2 = a.c2;
+  const int tiles = w.p1 > w.p0 ? (w.p1 - w.p0 + TP - 1) / TP : 0;
+
+  // waves 0 to 3 bring a page of K each, waves 4 to 7 the same pages of V; a page's id and mask are
+  // loaded a tile before the page
+  const int my = wave & 3;
+  const bool is_v = wave >= 4;
+  const char* pool = is_v ? a.v_pool : a.k_pool;
+  PageRegs<uint16_t, D> rp;
+  int id = 0;
+  uint32_t mask = 0, next_mask = 0;
+  auto load_id = [&](int t) {
+    const int p = w.p0 + t * TP + my;
+    next_mask = p < w.p1 ? w.mrow[p] : 0u;
+    id = w.trow[min(p, w.p1 - 1)];
+  };
+  auto load = [&] {
+    mask = next_mask;
+    rp.load(pool, min(max(id, 0), a.num_pages - 1));
+  };
+  auto store = [&](int t, int buf) {
     if (is_v) {
       uint32_t keep = mask, odd = 0;
-      if ((p + my + 1) * HK_PAGE > tile_seen) {
+      if ((w.p0 + t * TP + my + 1) * HK_PAGE > tile_seen) {
         odd = rp.odd_rows() & mask;
         keep &= ~odd;
       }
@@ -460,30 +565,206 @@ __global__ __launch_bounds__(TILE_NT, 2) void chunk_tile_kernel(Args a) {
         s_odd[buf][my] = (uint16_t)odd;
       }
     }
-    rp.store(s_kv[buf][is_v], my * HK_PAGE);
+    if (is_v) rp.store(s_v[buf] + my * HK_PAGE * L::V_ROW, L::V_ROW);
+    else rp.store(s_k[buf] + my * HK_PAGE * L::K_ROW, L::K_ROW);
+  };
+
+  f32x16 acc[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[dt][e] = 0.f;
+  float m = -INFINITY, mb = 0.f, l = 0.f;
+
+  // LDS addresses of the lane's fragments within 32 keys: K by 16-byte pieces of key l % 32, V by
+  // transposing reads of 4 keys x 16 dims (two a fragment)
+  const int i16 = lane & 15, k_at = (lane & 31) * L::K_ROW + hi * 16;
+  const int v_at = (4 * hi + (i16 >> 2)) * L::V_ROW + ((lane >> 4) & 1) * 32 + (i16 & 3) * 8;
+  auto k_frag = [&](const char* k, int s) {
+    return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(k + k_at + 32 * s));
+  };
+  auto v_frag = [&](const char* v, int i) {                      // i = s * DT + dt
+    const int s = i / DT, dt = i % DT;
+    s16x4 x[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const char* at = v + v_at + (16 * s + 8 * h) * L::V_ROW + dt * 64;
+      x[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (__attribute__((address_space(3))) s16x4*)(uintptr_t)(__attribute__((address_space(3))) const char*)at);
+    }
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  bf16x8 kf[AHEAD], vf[AHEAD];
+  uint32_t bp[8];                                                // P of 32 keys, two a word
+  f32x16 z[2];
+  auto first_k = [&](const char* k) {
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) kf[i] = k_frag(k, i);
+  };
+  // scores of the block at k into zn, beside the probabilities of zc (into bp; the block at v is zc's).
+  // The empty asm statements keep what is computed beside an MFMA in its place.
+  auto scores = [&](f32x16& zn, const f32x16& zc, const char* k, const char* v) {
+    float sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      zn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % AHEAD], q.f[i], i ? zn : f32x16{}, 0, 0, 0);
+      if (i + AHEAD < KS) kf[i % AHEAD] = k_frag(k, i + AHEAD);
+      else vf[i + AHEAD - KS] = v_frag(v, i + AHEAD - KS);
+#pragma unroll
+      for (int e = i * 16 / KS; e < (i + 1) * 16 / KS; e += 2) {
+        const float x = fast_exp2(fmaf(zc[e], c2, -mb)), y = fast_exp2(fmaf(zc[e + 1], c2, -mb));
+        sum[0] += x;
+        sum[1] += y;
+        bp[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x, y}), bf16x2));
+        asm volatile("" : "+v"(bp[e / 2]), "+v"(sum[0]), "+v"(sum[1]));
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    l += sum[0] + sum[1];
+  };
+  // acc += P V of the block at v, beside the maximum of zn, which it returns; the first fragments of
+  // the scores after these come from k
+  auto values = [&](const f32x16& zn, const char* v, const char* k) {
+    float zm = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < VS; ++i) {
+      const int s = 4 * (i / DT);
+      const bf16x8 b = __builtin_bit_cast(bf16x8, (u32x4{bp[s], bp[s + 1], bp[s + 2], bp[s + 3]}));
+      acc[i % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % AHEAD], b, acc[i % DT], 0, 0, 0);
+      if (i + AHEAD < VS) vf[i % AHEAD] = v_frag(v, i + AHEAD);
+      else kf[i + AHEAD - VS] = k_frag(k, i + AHEAD - VS);
+#pragma unroll
+      for (int e = i * 16 / VS; e < (i + 1) * 16 / VS; e += 2) {
+        zm = fmaxf(fmaxf(zm, zn[e]), zn[e + 1]);
+        asm volatile("" : "+v"(zm));
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    return zm;
+  };
+  // keys of the 32 from page p on that the lane's query does not see: -inf
+  auto hide = [&](f32x16& zn, int p, uint32_t valid) {
+    const int key = p * HK_PAGE;
+    if (valid == 0xffffffffu && key + 32 <= seen_all) return;
+    const int k = seen - key;
+    uint32_t x = (valid & (k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u)) >> (4 * hi);
+    asm volatile("" : "+v"(x));                                  // (a branch, not selects in every block)
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (!((x >> ((e & 3) + 8 * (e >> 2))) & 1u)) zn[e] = -INFINITY;
+  };
+  // a new reference where a score has outgrown it
+  auto refer = [&](float zm) {
+    zm *= c2;
+    if (__any(zm > m + CH_SLACK)) {
+      zm = fmaxf(zm, __shfl_xor(zm, 32, 64));
+      const float mn = fmaxf(m, ceilf(zm));
+      const float alpha = m == -INFINITY ? 0.f : fast_exp2(m - mn);
+      m = mn;
+      mb = mn == -INFINITY ? 0.f : mn + bias;
+      l *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[dt][e] *= alpha;
+    }
+  };
+  // rows of V with infinite values that not every query of the tile sees (zeros in LDS)
+  auto add_odd = [&](uint32_t odd, int p, uint32_t valid) {
+    while (odd) {
+      const int key = __builtin_ctz(odd), reg = (key & 3) + 4 * (key >> 3);
+      odd &= odd - 1;
+      const int at = min(max(w.trow[min(p + key / HK_PAGE, w.p1 - 1)], 0), a.num_pages - 1);
+      const uint16_t* vr = reinterpret_cast<const uint16_t*>(a.v_pool) + ((size_t)at * HK_PAGE + key % HK_PAGE) * D;
+      uint32_t two = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) two = reg / 2 == e ? bp[e] : two;
+      asm volatile("" : "+v"(two));
+      float pr = __uint_as_float(reg & 1 ? two & 0xffff0000u : two << 16);
+      pr = __shfl(pr, (lane & 31) + 32 * ((key >> 2) & 1), 64);
+      const bool sees = ((valid >> key) & 1u) && p * HK_PAGE + key < seen;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float x = M::value(vr[32 * dt + (e & 3) + 8 * (e >> 2) + 4 * hi]);
+          acc[dt][e] = sees ? fmaf(pr, x, acc[dt][e]) : acc[dt][e];
+        }
+    }
+  };
+  auto flags = [&](const uint16_t* x) {
+    const uint64_t y = *reinterpret_cast<const uint64_t*>(x);
+    return ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(y >> 32)) << 32) |
+           (uint32_t)__builtin_amdgcn_readfirstlane((int)y);
+  };
+
+  if (tiles > 0) {
+    load_id(0);
+    load();
+    load_id(1);
+    store(0, 0);
+    load();
+    load_id(2);
     __syncthreads();
-    if (t + 1 < tiles) {
+  }
+  auto after = [](int buf) { return buf == 2 ? 0 : buf + 1; };
+  auto bring = [&](int t, int buf) {                             // tile t into LDS, tile t + 1 on its way
+    if (t < tiles) {
+      store(t, buf);
       load();
       load_id(t + 2);
     }
-    if (w0 < rows) {
-      const uint64_t m64 = *reinterpret_cast<const uint64_t*>(s_mask[buf]);
-      const uint64_t o64 = *reinterpret_cast<const uint64_t*>(s_odd[buf]);
-#pragma unroll
-      for (int hb = 0; hb < TK / 32; ++hb) {
-        const int key = (p + 2 * hb) * HK_PAGE;
-        const uint32_t valid = __builtin_amdgcn_readfirstlane((uint32_t)(m64 >> (32 * hb)));
-        const uint32_t odd = __builtin_amdgcn_readfirstlane((uint32_t)(o64 >> (32 * hb)));
-        const bool all = valid == 0xffffffffu && key + 32 <= seen_all;
-        const int k = seen - key;
-        const uint32_t vis[1] = {valid & (k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u)};
-        st.block(q, s_kv[buf][0] + hb * 32 * L::ROW, s_kv[buf][1] + hb * 32 * L::ROW, vis, all, a.c2, bias, odd,
-                 row_at(p + 2 * hb));
-      }
+  };
+  if (w0 >= w.rows) {                                            // a wave without rows brings its pages
+    for (int t = 0, buf = 1; t < tiles; ++t, buf = after(buf)) {
+      bring(t + 1, buf);
+      __syncthreads();
     }
+    return;
   }
-  const float l = st.l[0] + __shfl_xor(st.l[0], 32, 64);
-  if (w0 + (lane & 31) < rows) put_state<T, D>(a, row, split, st.acc[0], st.mb[0], l);
+  constexpr int K_HALF = 32 * L::K_ROW, V_HALF = 32 * L::V_ROW;
+  // the queries are here before the loop, where a wait for them would be one for the next tile too
+#pragma unroll
+  for (int i = 0; i < KS; ++i) asm volatile("" : "+v"(q.f[i]));
+  uint64_t valid = 0, odd = 0;
+  if (tiles > 0) {
+    valid = flags(s_mask[0]);
+    odd = flags(s_odd[0]);
+    first_k(s_k[0]);
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      z[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % AHEAD], q.f[i], i ? z[0] : f32x16{}, 0, 0, 0);
+      if (i + AHEAD < KS) kf[i % AHEAD] = k_frag(s_k[0], i + AHEAD);
+    }
+    hide(z[0], w.p0, (uint32_t)valid);
+    float zm = z[0][0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) zm = fmaxf(zm, z[0][e]);
+    refer(zm);
+    first_k(s_k[0] + K_HALF);
+  }
+  for (int t = 0, buf = 0; t < tiles; ++t) {
+    const int p = w.p0 + t * TP, next = after(buf);
+    // past the last tile the scores are of whatever LDS holds, and hidden
+    bring(t + 1, next);
+    scores(z[1], z[0], s_k[buf] + K_HALF, s_v[buf]);
+    __syncthreads();
+    hide(z[1], p + 2, (uint32_t)(valid >> 32));
+    float zm = values(z[1], s_v[buf], s_k[next]);
+    if ((uint32_t)odd) add_odd((uint32_t)odd, p, (uint32_t)valid);
+    refer(zm);
+    const uint64_t valid_next = t + 1 < tiles ? flags(s_mask[next]) : 0;
+    scores(z[0], z[1], s_k[next], s_v[buf] + V_HALF);
+    hide(z[0], p + 4, (uint32_t)valid_next);
+    zm = values(z[0], s_v[buf] + V_HALF, s_k[next] + K_HALF);
+    if (odd >> 32) add_odd((uint32_t)(odd >> 32), p + 2, (uint32_t)(valid >> 32));
+    refer(zm);
+    valid = valid_next;
+    odd = t + 1 < tiles ? flags(s_odd[next]) : 0;
+    buf = next;
+  }
+  l += __shfl_xor(l, 32, 64);
+  if (w0 + (lane & 31) < w.rows) put_state<uint16_t, D>(a, row, w.split, acc, mb, l);
 }
 
 // ------------------------------------------------------------------ short kernel
@@ -493,7 +774,7 @@ __global__ __launch_bounds__(CH_NT, 1) void chunk_short_kernel(Args a) {
   using M = Mma<T, D>;
   constexpr int WP = 2, TP = CH_NW * WP;      // pages of a wave and of the workgroup per step
   constexpr int OP = D + 4;                   // floats of a query's sums in LDS, padded
-  constexpr int STAGE = CH_NW * 2 * 32 * L::ROW, JOIN = CH_NW * 32 * OP * 4;
+  constexpr int STAGE = CH_NW * 32 * (L::K_ROW + L::V_ROW), JOIN = CH_NW * 32 * OP * 4;
   __shared__ __align__(16) char s_buf[STAGE > JOIN ? STAGE : JOIN];
   __shared__ float s_m[CH_NW][32], s_l[CH_NW][32];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hi = lane >> 5;
@@ -517,8 +798,8 @@ __global__ __launch_bounds__(CH_NT, 1) void chunk_short_kernel(Args a) {
   const float bias = bias_of(pages);
   State<T, D, 1> st;
   st.init();
-  char* my_k = s_buf + wave * 2 * 32 * L::ROW;
-  char* my_v = my_k + 32 * L::ROW;
+  char* my_k = s_buf + wave * 32 * (L::K_ROW + L::V_ROW);
+  char* my_v = my_k + 32 * L::K_ROW;
   const int steps = p1 > p0 ? (p1 - p0 + TP - 1) / TP : 0;
   PageRegs<T, D> rk[WP], rv[WP];
   uint32_t mask[WP];
@@ -545,8 +826,8 @@ __global__ __launch_bounds__(CH_NT, 1) void chunk_short_kernel(Args a) {
         odd |= o << (16 * i);
       }
       if (mask[i] != 0xffffu) rv[i].clear(mask[i]);
-      rk[i].store(my_k, i * HK_PAGE);
-      rv[i].store(my_v, i * HK_PAGE);
+      rk[i].store(my_k + i * HK_PAGE * L::K_ROW, L::K_ROW);
+      rv[i].store(my_v + i * HK_PAGE * L::V_ROW, L::V_ROW);
     }
     if (t + 1 < steps) load(t + 1);
     const int p = p0 + t * TP + wave * WP, key = p * HK_PAGE;
@@ -659,13 +940,20 @@ __global__ __launch_bounds__(CH_NT) void chunk_merge_kernel(Args a) {
   if (lane == 0 && a.lse) a.lse[row] = l == 0.f ? -INFINITY : (M_ + __log2f(l)) * kLn2;
 }
 
+// Rows of a tile kernel's workgroup.
+static constexpr int tile_rows(bool bf, int D) { return bf || D == 64 ? 256 : 128; }
+
 template <typename T, int D>
 static void launch(Args a, hipStream_t st, int short_wg, int tile_wg) {
-  constexpr int TM = TILE_ROWS;
+  constexpr bool bf = sizeof(T) == 2;
+  constexpr int TM = tile_rows(bf, D);
   {
     TimedLaunch t(HK_TK_CHUNK_ATTN, st);
-    if (tile_wg > 0)
-      hipLaunchKernelGGL((chunk_tile_kernel<T, D>), dim3(tile_wg, a.n_split), dim3(TILE_NT), 0, st, a);
+    if (tile_wg > 0) {
+      const dim3 grid(tile_wg, a.n_split), block(2 * TM);
+      if constexpr (bf) hipLaunchKernelGGL((chunk_tile_bf16_kernel<D>), grid, block, 0, st, a);
+      else hipLaunchKernelGGL((chunk_tile_f32_kernel<D, TM / 32>), grid, block, 0, st, a);
+    }
     hipLaunchKernelGGL((chunk_short_kernel<T, D>), dim3(short_wg, a.n_split), dim3(CH_NT), 0, st, a);
   }
   if (a.n_split > 1) {
@@ -714,7 +1002,7 @@ hipError_t hk_launch_chunk_attn(int NS, int Hq, int Hkv, int D, const hk_paged_k
                                 const void* q, int64_t q_row, float sm_scale, void* o, float* lse, void* ws,
                                 hipStream_t st) {
   const bool bf = kv->dtype == HK_BF16;
-  const Plan p = plan(NS, Hq, Hkv, TILE_ROWS, ch->n_tokens, ch->max_len, kv->max_pages);
+  const Plan p = plan(NS, Hq, Hkv, tile_rows(bf, D), ch->n_tokens, ch->max_len, kv->max_pages);
   Args a;
   a.q = static_cast<const char*>(q);
   a.k_pool = static_cast<const char*>(kv->k_pool);
