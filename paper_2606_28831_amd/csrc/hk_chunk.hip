@@ -31,11 +31,9 @@
 
 namespace hk {
 
-constexpr int CH_NT = 256;
-constexpr int CH_NW = CH_NT / 64;
 constexpr float CH_SLACK = 12.f;
 constexpr int SHORT_ROWS = 32;
-constexpr int MIN_PAGES = 16;                 // fewest pages of a split
+constexpr int MIN_PAGES = 8;                  // fewest pages of a split
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -254,13 +252,20 @@ struct State {
   __device__ __forceinline__ void block(const typename M::Query (&q)[NB], const char* k, const char* v,
                                         const uint32_t (&vis)[NB], bool all, float c2, float bias, uint32_t odd,
                                         F row) {
-    const int hi = (threadIdx.x & 63) >> 5;
     f32x16 z[NB];
     M::template scores<NB>(z, q, k);
+    weigh(z, v, vis, all, c2, bias, odd, row);
+  }
+  // the same from their scores z
+  template <typename F>
+  __device__ __forceinline__ void weigh(f32x16 (&z)[NB], const char* v, const uint32_t (&vis)[NB], bool all, float c2,
+                                        float bias, uint32_t odd, F row) {
+    const int hi = (threadIdx.x & 63) >> 5;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       if (!all) {
-        const uint32_t w = vis[b] >> (4 * hi);
+        uint32_t w = vis[b] >> (4 * hi);
+        asm volatile("" : "+v"(w));           // (a branch, not selects in every block)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           if (!((w >> ((r & 3) + 8 * (r >> 2))) & 1u)) z[b][r] = -INFINITY;
@@ -329,31 +334,37 @@ __device__ __forceinline__ int split_share(int pages, int n_split) {
 }
 __device__ __forceinline__ float bias_of(int pages) { return (float)(32 - __clz(pages * HK_PAGE)) + CH_SLACK; }
 
+// Split states lie by workgroup: query r of item i (a head of the short kernel, tile and KV head of a
+// tile kernel) of splits states each begins at (i * rows + r) * splits.
 struct Args {
   const char *q, *k_pool, *v_pool;
   const int32_t *table, *n_pages, *start;
   const uint16_t* masks;
   int64_t q_row;                              // elements
   char* o;
-  float *lse, *part_o, *part_ml;
-  int Hq, Hkv, G, max_pages, num_pages, n_seq, n_tokens, max_len, n_split;
+  float *lse;
+  float *short_o, *short_ml, *tile_o, *tile_ml;
+  int Hq, Hkv, G, max_pages, num_pages, n_seq, n_tokens, max_len;
+  int short_splits, tile_splits;              // splits of a row
   float c2;
 };
 
-// One query's result (lane: half of the dims): normalised into o, or the split's state.
+// One query's result of a tile kernel (lane: half of the dims): normalised into o, or the split's
+// state.  at: the query's first state.
 template <typename T, int D>
-__device__ __forceinline__ void put_state(const Args& a, int64_t row, int split, const f32x16 (&acc)[D / 32], float mb,
-                                          float l) {
+__device__ __forceinline__ void put_state(const Args& a, int64_t row, int64_t at, int split, const f32x16 (&acc)[D / 32],
+                                          float mb, float l) {
   const int hi = (threadIdx.x & 63) >> 5;
-  if (a.n_split > 1) {
-    float* to = a.part_o + (row * a.n_split + split) * D;
+  if (a.tile_splits > 1) {
+    at += split;
+    float* to = a.tile_o + at * D;
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         *reinterpret_cast<f32x4*>(to + 32 * dt + 8 * j + 4 * hi) =
             f32x4{acc[dt][4 * j], acc[dt][4 * j + 1], acc[dt][4 * j + 2], acc[dt][4 * j + 3]};
-    if (hi == 0) *reinterpret_cast<f32x2*>(a.part_ml + (row * a.n_split + split) * 2) = f32x2{l == 0.f ? -INFINITY : mb, l};
+    if (hi == 0) *reinterpret_cast<f32x2*>(a.tile_ml + at * 2) = f32x2{l == 0.f ? -INFINITY : mb, l};
     return;
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;   // (a NaN stays one)
@@ -370,11 +381,28 @@ __device__ __forceinline__ void put_state(const Args& a, int64_t row, int split,
 // ------------------------------------------------------------------ tile kernels
 constexpr int TILE_PAGES = 4, TILE_KEYS = TILE_PAGES * HK_PAGE;
 
+// Tiles of TM folded rows are numbered over the batch: a sequence's begin at tiles_before, which
+// leaves at most one of a sequence without rows.
+template <int TM>
+__device__ __forceinline__ int tiles_before(const Args& a, int s) {
+  return min(max(a.start[s], 0), a.n_tokens) * a.G / TM + s;
+}
+template <int TM>
+__device__ __forceinline__ int tile_sequence(const Args& a, int u) {
+  int s = 0;
+  for (int hi = a.n_seq; hi - s > 1;) {
+    const int mid = (s + hi) / 2;
+    if (tiles_before<TM>(a, mid) <= u) s = mid;
+    else hi = mid;
+  }
+  return s;
+}
+
 // What a workgroup of a tile kernel works on: TM folded rows of one sequence and KV head, and a
 // range of its pages.  None: nothing (p1 < 0).
 struct TileWork {
   Chunk c;
-  int kv, split, rows, r0, end, pages, p0, p1;
+  int item, kv, split, rows, r0, end, pages, p0, p1;
   const int32_t* trow;
   const uint16_t* mrow;
 };
@@ -384,25 +412,20 @@ __device__ __forceinline__ TileWork tile_work(const Args& a) {
   // the largest tiles of a sequence first: tile u of the launch counts down
   const int u = (int)(gridDim.x / a.Hkv) - 1 - (int)(blockIdx.x / a.Hkv);
   w.kv = blockIdx.x % a.Hkv;
+  w.item = u * a.Hkv + w.kv;
   w.split = blockIdx.y;
   w.p1 = -1;
-  auto tiles_before = [&](int s) { return min(max(a.start[s], 0), a.n_tokens) * a.G / TM + s; };
-  int s = 0;
-  for (int hi = a.n_seq; hi - s > 1;) {
-    const int mid = (s + hi) / 2;
-    if (tiles_before(mid) <= u) s = mid;
-    else hi = mid;
-  }
+  const int s = tile_sequence<TM>(a, u);
   w.c = chunk_of(a.start, s, a.n_tokens, a.max_len);
   w.rows = w.c.len * a.G;
-  w.r0 = (u - tiles_before(s)) * TM;
+  w.r0 = (u - tiles_before<TM>(a, s)) * TM;
   if (w.rows <= SHORT_ROWS || w.r0 < 0 || w.r0 >= w.rows) return w;
   const int h = s * a.Hkv + w.kv, n = min(max(a.n_pages[h], 0), a.max_pages);
   w.trow = a.table + (size_t)h * a.max_pages;
   w.mrow = a.masks + (size_t)h * a.max_pages;
   w.end = row_end(n, n > 0 ? w.mrow[n - 1] : 0u);
   w.pages = tile_pages(n, w.end, w.c.len, (min(w.r0 + TM, w.rows) - 1) / a.G);
-  const int share = split_share(w.pages, a.n_split);
+  const int share = split_share(w.pages, a.tile_splits);
   w.p0 = w.split * share;
   w.p1 = w.split > 0 && w.p0 >= w.pages ? -1 : min(w.p0 + share, w.pages);
   return w;
@@ -504,7 +527,7 @@ __global__ __launch_bounds__(64 * NW, 1) void chunk_tile_f32_kernel(Args a) {
     }
   }
   const float l = st.l[0] + __shfl_xor(st.l[0], 32, 64);
-  if (w0 + (lane & 31) < w.rows) put_state<float, D>(a, row, w.split, st.acc[0], st.mb[0], l);
+  if (w0 + (lane & 31) < w.rows) put_state<float, D>(a, row, ((int64_t)w.item * 32 * NW + r - w.r0) * a.tile_splits, w.split, st.acc[0], st.mb[0], l);
 }
 
 // bf16.  Eight waves, two a SIMD, take 32 rows each against tiles of 64 keys.  A wave's steps of 32
@@ -764,51 +787,140 @@ __global__ __launch_bounds__(512, 2) void chunk_tile_bf16_kernel(Args a) {
     buf = next;
   }
   l += __shfl_xor(l, 32, 64);
-  if (w0 + (lane & 31) < w.rows) put_state<uint16_t, D>(a, row, w.split, acc, mb, l);
+  if (w0 + (lane & 31) < w.rows) put_state<uint16_t, D>(a, row, ((int64_t)w.item * 256 + r - w.r0) * a.tile_splits, w.split, acc, mb, l);
 }
 
-// ------------------------------------------------------------------ short kernel
-template <typename T, int D>
-__global__ __launch_bounds__(CH_NT, 1) void chunk_short_kernel(Args a) {
-  using L = TileLayout<T, D>;
-  using M = Mma<T, D>;
-  constexpr int WP = 2, TP = CH_NW * WP;      // pages of a wave and of the workgroup per step
-  constexpr int OP = D + 4;                   // floats of a query's sums in LDS, padded
-  constexpr int STAGE = CH_NW * 32 * (L::K_ROW + L::V_ROW), JOIN = CH_NW * 32 * OP * 4;
-  __shared__ __align__(16) char s_buf[STAGE > JOIN ? STAGE : JOIN];
-  __shared__ float s_m[CH_NW][32], s_l[CH_NW][32];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hi = lane >> 5;
-  const int h = blockIdx.x, s = h / a.Hkv, kv = h % a.Hkv, split = blockIdx.y;
-  const Chunk c = chunk_of(a.start, s, a.n_tokens, a.max_len);
-  const int rows = c.len * a.G;
-  if (rows <= 0 || rows > SHORT_ROWS) return;
-  const int n = min(max(a.n_pages[h], 0), a.max_pages);
-  const int32_t* trow = a.table + (size_t)h * a.max_pages;
-  const uint16_t* mrow = a.masks + (size_t)h * a.max_pages;
-  const int end = row_end(n, n > 0 ? mrow[n - 1] : 0u);
-  const int pages = tile_pages(n, end, c.len, c.len - 1);
-  const int share = split_share(pages, a.n_split);
-  const int p0 = split * share, p1 = min(p0 + share, pages);
-  if (split > 0 && p0 >= pages) return;
+// ------------------------------------------------------------------ short kernels
+constexpr int SHORT_NT = 256, SHORT_NW = SHORT_NT / 64;
 
-  const int r = min(lane & 31, rows - 1), tok = r / a.G;
-  const int seen = end - c.len + tok + 1, seen_all = end - c.len + 1;
+// The rows of a sequence and KV head and the pages of a split that a short kernel's workgroup takes.
+// none: p1 < 0.
+struct ShortWork {
+  Chunk c;
+  int kv, split, rows, end, pages, p0, p1;
+  const int32_t* trow;
+  const uint16_t* mrow;
+};
+__device__ __forceinline__ ShortWork short_work(const Args& a) {
+  ShortWork w;
+  const int h = blockIdx.x, s = h / a.Hkv;
+  w.kv = h % a.Hkv;
+  w.split = blockIdx.y;
+  w.p1 = -1;
+  w.c = chunk_of(a.start, s, a.n_tokens, a.max_len);
+  w.rows = w.c.len * a.G;
+  if (w.rows <= 0 || w.rows > SHORT_ROWS) return w;
+  const int n = min(max(a.n_pages[h], 0), a.max_pages);
+  w.trow = a.table + (size_t)h * a.max_pages;
+  w.mrow = a.masks + (size_t)h * a.max_pages;
+  w.end = row_end(n, n > 0 ? w.mrow[n - 1] : 0u);
+  w.pages = tile_pages(n, w.end, w.c.len, w.c.len - 1);
+  const int share = split_share(w.pages, a.short_splits);
+  w.p0 = w.split * share;
+  w.p1 = w.split > 0 && w.p0 >= w.pages ? -1 : min(w.p0 + share, w.pages);
+  return w;
+}
+
+// The four waves' states, summed against one reference, are the workgroup's result.  s_o: 32 x (D / 2
+// + 4) floats a wave, used for one half of the dims after the other.
+template <typename T, int D>
+__device__ __forceinline__ void join_waves(const Args& a, const ShortWork& w, const f32x16 (&acc)[D / 32], float mb,
+                                           float l, float* s_o, float (*s_m)[32], float (*s_l)[32]) {
+  constexpr int HD = D / 2, OP = HD + 4;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hi = lane >> 5;
+  l += __shfl_xor(l, 32, 64);
+  __syncthreads();                            // (s_o may be the waves' tiles)
+  if (hi == 0) {
+    s_m[wave][lane] = l == 0.f ? -INFINITY : mb;
+    s_l[wave][lane] = l;
+  }
+  __syncthreads();
+  auto whole = [&](int q, float& m) {         // reference and sum of query q
+    m = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < SHORT_NW; ++v) m = fmaxf(m, s_m[v][q]);
+    float x = 0.f;
+    if (m != -INFINITY)
+#pragma unroll
+      for (int v = 0; v < SHORT_NW; ++v) x += s_l[v][q] * fast_exp2(s_m[v][q] - m);
+    else
+#pragma unroll
+      for (int v = 0; v < SHORT_NW; ++v) x += s_l[v][q];          // 0, or NaN
+    return x;
+  };
+  float M_;
+  whole(lane & 31, M_);
+  const float own = M_ == -INFINITY ? 0.f : fast_exp2(s_m[wave][lane & 31] - M_);
+  // eight threads of a query's dims each
+  const int qr = threadIdx.x >> 3, d0 = (threadIdx.x & 7) * (HD / 8);
+  const float l_all = whole(qr, M_);
+  const int tq = qr / a.G;
+  const int64_t row = (int64_t)(w.c.first + tq) * a.Hq + w.kv * a.G + (qr - tq * a.G);
+  const bool parts = a.short_splits > 1;
+  const float inv = parts ? 1.f : l_all == 0.f ? 0.f : 1.f / l_all;   // (a NaN stays one)
+  const int64_t state = ((int64_t)blockIdx.x * SHORT_ROWS + qr) * a.short_splits + w.split;
+  float* po = a.short_o + state * D;
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    if (half) __syncthreads();
+#pragma unroll
+    for (int dt = 0; dt < D / 64; ++dt)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f32x16& x = acc[half * (D / 64) + dt];
+        *reinterpret_cast<f32x4*>(s_o + (wave * 32 + (lane & 31)) * OP + 32 * dt + 8 * j + 4 * hi) =
+            f32x4{x[4 * j] * own, x[4 * j + 1] * own, x[4 * j + 2] * own, x[4 * j + 3] * own};
+      }
+    __syncthreads();
+    if (qr < w.rows)
+#pragma unroll
+      for (int d = 0; d < HD / 8; d += 4) {
+        f32x4 t = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int v = 0; v < SHORT_NW; ++v) t += *reinterpret_cast<const f32x4*>(s_o + (v * 32 + qr) * OP + d0 + d);
+        t *= inv;
+        const int at = half * HD + d0 + d;
+        if (parts) *reinterpret_cast<f32x4*>(po + at) = t;
+        else Mma<T, D>::put4(reinterpret_cast<T*>(a.o) + row * D + at, t[0], t[1], t[2], t[3]);
+      }
+  }
+  if (qr < w.rows && (threadIdx.x & 7) == 0) {
+    if (parts) *reinterpret_cast<f32x2*>(a.short_ml + state * 2) = f32x2{M_, l_all};
+    else if (a.lse) a.lse[row] = l_all == 0.f ? -INFINITY : (M_ + __log2f(l_all)) * kLn2;
+  }
+}
+
+// fp32: both tiles of a wave's 32 keys go through its part of LDS.
+template <int D>
+__global__ __launch_bounds__(SHORT_NT, 1) void chunk_short_f32_kernel(Args a) {
+  using L = TileLayout<float, D>;
+  using M = Mma<float, D>;
+  constexpr int WP = 2, TP = SHORT_NW * WP;   // pages of a wave and of the workgroup per step
+  constexpr int WAVE = 32 * (L::K_ROW + L::V_ROW);
+  static_assert(WAVE >= 32 * (D / 2 + 4) * 4, "the join's sums fit the tiles");
+  __shared__ __align__(16) char s_buf[SHORT_NW * WAVE];
+  __shared__ float s_m[SHORT_NW][32], s_l[SHORT_NW][32];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const ShortWork w = short_work(a);
+  if (w.p1 < 0) return;
+  const int r = min(lane & 31, w.rows - 1), tok = r / a.G, off = w.end - w.c.len + 1;
+  const int seen = off + tok, seen_all = off;
   typename M::Query q[1];
-  M::load_q(q[0], reinterpret_cast<const T*>(a.q) + (int64_t)(c.first + tok) * a.q_row + (kv * a.G + (r - tok * a.G)) * D);
-  const float bias = bias_of(pages);
-  State<T, D, 1> st;
+  M::load_q(q[0], reinterpret_cast<const float*>(a.q) + (int64_t)(w.c.first + tok) * a.q_row + (w.kv * a.G + (r - tok * a.G)) * D);
+  const float bias = bias_of(w.pages);
+  State<float, D, 1> st;
   st.init();
-  char* my_k = s_buf + wave * 32 * (L::K_ROW + L::V_ROW);
+  char* my_k = s_buf + wave * WAVE;
   char* my_v = my_k + 32 * L::K_ROW;
-  const int steps = p1 > p0 ? (p1 - p0 + TP - 1) / TP : 0;
-  PageRegs<T, D> rk[WP], rv[WP];
+  const int steps = w.p1 > w.p0 ? (w.p1 - w.p0 + TP - 1) / TP : 0;
+  PageRegs<float, D> rk[WP], rv[WP];
   uint32_t mask[WP];
+  auto page_id = [&](int p) { return min(max(w.trow[min(p, w.p1 - 1)], 0), a.num_pages - 1); };
   auto load = [&](int t) {
 #pragma unroll
     for (int i = 0; i < WP; ++i) {
-      const int p = p0 + t * TP + wave * WP + i;
-      mask[i] = p < p1 ? mrow[p] : 0u;
-      const int id = min(max(trow[min(p, p1 - 1)], 0), a.num_pages - 1);
+      const int p = w.p0 + t * TP + wave * WP + i, id = page_id(p);
+      mask[i] = p < w.p1 ? w.mrow[p] : 0u;
       rk[i].load(a.k_pool, id);
       rv[i].load(a.v_pool, id);
     }
@@ -817,122 +929,185 @@ __global__ __launch_bounds__(CH_NT, 1) void chunk_short_kernel(Args a) {
   for (int t = 0; t < steps; ++t) {
     // the wave's own region of LDS: its reads of the last step are done before these writes, in
     // the order of its instructions
+    const int p = w.p0 + t * TP + wave * WP, key = p * HK_PAGE;
     uint32_t odd = 0;
+    const uint32_t valid = mask[0] | mask[1] << 16;
 #pragma unroll
     for (int i = 0; i < WP; ++i) {
-      if ((p0 + t * TP + wave * WP + i + 1) * HK_PAGE > seen_all) {
-        const uint32_t o = rv[i].odd_rows() & mask[i];
-        mask[i] &= ~o;
+      uint32_t keep = mask[i];
+      if ((p + i + 1) * HK_PAGE > seen_all) {
+        const uint32_t o = rv[i].odd_rows() & keep;
+        keep &= ~o;
         odd |= o << (16 * i);
       }
-      if (mask[i] != 0xffffu) rv[i].clear(mask[i]);
+      if (keep != 0xffffu) rv[i].clear(keep);
       rk[i].store(my_k + i * HK_PAGE * L::K_ROW, L::K_ROW);
       rv[i].store(my_v + i * HK_PAGE * L::V_ROW, L::V_ROW);
     }
     if (t + 1 < steps) load(t + 1);
-    const int p = p0 + t * TP + wave * WP, key = p * HK_PAGE;
-    const uint32_t valid = (p < p1 ? (uint32_t)mrow[p] : 0u) | (p + 1 < p1 ? (uint32_t)mrow[p + 1] << 16 : 0u);
     const bool all = valid == 0xffffffffu && key + 32 <= seen_all;
     const int k = seen - key;
     const uint32_t vis[1] = {valid & (k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u)};
     __builtin_amdgcn_wave_barrier();
     st.block(q, my_k, my_v, vis, all, a.c2, bias, __builtin_amdgcn_readfirstlane(odd), [&](int j) {
-      const int id = min(max(trow[min(p + j / HK_PAGE, p1 - 1)], 0), a.num_pages - 1);
-      return reinterpret_cast<const T*>(a.v_pool) + ((size_t)id * HK_PAGE + j % HK_PAGE) * D;
+      return reinterpret_cast<const float*>(a.v_pool) + ((size_t)page_id(p + j / HK_PAGE) * HK_PAGE + j % HK_PAGE) * D;
     });
     __builtin_amdgcn_wave_barrier();
   }
-  // the waves' states: one reference for all, then sums
-  float l = st.l[0] + __shfl_xor(st.l[0], 32, 64);
-  if (hi == 0) {
-    s_m[wave][lane] = l == 0.f ? -INFINITY : st.mb[0];
-    s_l[wave][lane] = l;
+  join_waves<float, D>(a, w, st.acc[0], st.mb[0], st.l[0], reinterpret_cast<float*>(s_buf), s_m, s_l);
+}
+
+// bf16: K goes from memory to the registers that are the scores' operand, a key a lane, and only V
+// through LDS; both are requested a step ahead.  Two workgroups a CU.  Bound by HBM reads.
+template <int D>
+__global__ __launch_bounds__(SHORT_NT, 2) void chunk_short_bf16_kernel(Args a) {
+  using L = TileLayout<uint16_t, D>;
+  using M = Mma<uint16_t, D>;
+  constexpr int WP = 2, TP = SHORT_NW * WP, KS = D / 16;
+  constexpr int V_TILE = 32 * L::V_ROW, O_TILE = 32 * (D / 2 + 4) * 4, WAVE = V_TILE > O_TILE ? V_TILE : O_TILE;
+  __shared__ __align__(16) char s_buf[SHORT_NW * WAVE];
+  __shared__ float s_m[SHORT_NW][32], s_l[SHORT_NW][32];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hi = lane >> 5;
+  const ShortWork w = short_work(a);
+  if (w.p1 < 0) return;
+  const int r = min(lane & 31, w.rows - 1), tok = r / a.G, off = w.end - w.c.len + 1;
+  const int seen = off + tok, seen_all = off;
+  typename M::Query q[1];
+  M::load_q(q[0], reinterpret_cast<const uint16_t*>(a.q) + (int64_t)(w.c.first + tok) * a.q_row + (w.kv * a.G + (r - tok * a.G)) * D);
+  const float bias = bias_of(w.pages);
+  State<uint16_t, D, 1> st;
+  st.init();
+  char* my_v = s_buf + wave * WAVE;
+  const int steps = w.p1 > w.p0 ? (w.p1 - w.p0 + TP - 1) / TP : 0;
+  u32x4 kf[KS];
+  PageRegs<uint16_t, D> rv[WP];
+  int id[WP];
+  uint32_t mask[WP], next_mask[WP];
+  auto page_id = [&](int p) { return min(max(w.trow[min(p, w.p1 - 1)], 0), a.num_pages - 1); };
+  auto load_id = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < WP; ++i) {
+      const int p = w.p0 + t * TP + wave * WP + i;
+      next_mask[i] = p < w.p1 ? w.mrow[p] : 0u;
+      id[i] = page_id(p);
+    }
+  };
+  auto load_k = [&] {
+    const int my = (lane & 16) ? id[1] : id[0];                   // the page of key lane % 32
+    const char* row = a.k_pool + (size_t)my * L::PAGE + (lane & 15) * L::ROW + hi * 16;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) kf[s] = *reinterpret_cast<const u32x4*>(row + 32 * s);
+  };
+  if (steps > 0) {
+    load_id(0);
+    load_k();
+#pragma unroll
+    for (int i = 0; i < WP; ++i) rv[i].load(a.v_pool, id[i]);
   }
-  __syncthreads();
-  float mb = -INFINITY;
-  l = 0.f;
+  for (int t = 0; t < steps; ++t) {
+    const int p = w.p0 + t * TP + wave * WP, key = p * HK_PAGE;
 #pragma unroll
-  for (int w = 0; w < CH_NW; ++w) mb = fmaxf(mb, s_m[w][lane & 31]);
-  if (mb != -INFINITY)
+    for (int i = 0; i < WP; ++i) mask[i] = next_mask[i];
+    load_id(t + 1);
+    f32x16 z[1];
 #pragma unroll
-    for (int w = 0; w < CH_NW; ++w) l += s_l[w][lane & 31] * fast_exp2(s_m[w][lane & 31] - mb);
-  const float own = mb == -INFINITY ? 0.f : fast_exp2(s_m[wave][lane & 31] - mb);
-  float* s_o = reinterpret_cast<float*>(s_buf);
+    for (int s = 0; s < KS; ++s)
+      z[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[s]), q[0].f[s], s ? z[0] : f32x16{}, 0, 0, 0);
+    // V of this step into the wave's own region of LDS: its reads of the last step are done before
+    // these writes, in the order of its instructions
+    uint32_t odd = 0;
+    const uint32_t valid = mask[0] | mask[1] << 16;
 #pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt)
+    for (int i = 0; i < WP; ++i) {
+      uint32_t keep = mask[i];
+      if ((p + i + 1) * HK_PAGE > seen_all) {
+        const uint32_t o = rv[i].odd_rows() & keep;
+        keep &= ~o;
+        odd |= o << (16 * i);
+      }
+      if (keep != 0xffffu) rv[i].clear(keep);
+      rv[i].store(my_v + i * HK_PAGE * L::V_ROW, L::V_ROW);
+    }
+    // (past the last step its pages once more, with no valid slot)
+    load_k();
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      *reinterpret_cast<f32x4*>(s_o + (wave * 32 + (lane & 31)) * OP + 32 * dt + 8 * j + 4 * hi) =
-          f32x4{st.acc[0][dt][4 * j] * own, st.acc[0][dt][4 * j + 1] * own, st.acc[0][dt][4 * j + 2] * own,
-                st.acc[0][dt][4 * j + 3] * own};
-  __syncthreads();
-  // eight threads of a query's dims each
-  constexpr int PER = D / 8;
-  const int qr = threadIdx.x >> 3, d0 = (threadIdx.x & 7) * PER;
-  if (qr >= rows) return;
-  float M_ = -INFINITY, L_ = 0.f;
-#pragma unroll
-  for (int w = 0; w < CH_NW; ++w) M_ = fmaxf(M_, s_m[w][qr]);
-  if (M_ != -INFINITY)
-#pragma unroll
-    for (int w = 0; w < CH_NW; ++w) L_ += s_l[w][qr] * fast_exp2(s_m[w][qr] - M_);
-  const int tq = qr / a.G;
-  const int64_t orow = (int64_t)(c.first + tq) * a.Hq + kv * a.G + (qr - tq * a.G);
-  const float inv = a.n_split > 1 ? 1.f : L_ == 0.f ? 0.f : 1.f / L_;
-#pragma unroll
-  for (int d = 0; d < PER; d += 4) {
-    f32x4 t = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < CH_NW; ++w) t += *reinterpret_cast<const f32x4*>(s_o + (w * 32 + qr) * OP + d0 + d);
-    t *= inv;
-    if (a.n_split > 1) *reinterpret_cast<f32x4*>(a.part_o + (orow * a.n_split + split) * D + d0 + d) = t;
-    else M::put4(reinterpret_cast<T*>(a.o) + orow * D + d0 + d, t[0], t[1], t[2], t[3]);
+    for (int i = 0; i < WP; ++i) rv[i].load(a.v_pool, id[i]);
+    const bool all = valid == 0xffffffffu && key + 32 <= seen_all;
+    const int k = seen - key;
+    const uint32_t vis[1] = {valid & (k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u)};
+    __builtin_amdgcn_wave_barrier();
+    st.weigh(z, my_v, vis, all, a.c2, bias, __builtin_amdgcn_readfirstlane(odd), [&](int j) {
+      return reinterpret_cast<const uint16_t*>(a.v_pool) + ((size_t)page_id(p + j / HK_PAGE) * HK_PAGE + j % HK_PAGE) * D;
+    });
+    __builtin_amdgcn_wave_barrier();
   }
-  if ((threadIdx.x & 7) == 0) {
-    if (a.n_split > 1) *reinterpret_cast<f32x2*>(a.part_ml + (orow * a.n_split + split) * 2) = f32x2{M_, L_};
-    else if (a.lse) a.lse[orow] = L_ == 0.f ? -INFINITY : (M_ + __log2f(L_)) * kLn2;
-  }
+  join_waves<uint16_t, D>(a, w, st.acc[0], st.mb[0], st.l[0], reinterpret_cast<float*>(s_buf), s_m, s_l);
 }
 
 // ------------------------------------------------------------------ merge
-// One wave per (token, query head): the states of the splits that held pages.
+// One wave per query of a split item: the states of the splits that held pages.  Lanes read the
+// references and sums of all splits at once (at most 64), the outputs four at a time.  The first
+// short_q waves take the short kernel's queries (none when it did not split), the others a tile
+// kernel's.
+constexpr int MERGE_NT = 256, MERGE_NW = MERGE_NT / 64;
+constexpr int MAX_SPLITS = 64;
+
 template <typename T, int D, int TM>
-__global__ __launch_bounds__(CH_NT) void chunk_merge_kernel(Args a) {
+__global__ __launch_bounds__(MERGE_NT) void chunk_merge_kernel(Args a, int64_t short_q, int64_t all_q) {
   const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * CH_NW + (threadIdx.x >> 6);
-  if (row >= (int64_t)a.n_tokens * a.Hq) return;
-  const int t = (int)(row / a.Hq), hq = (int)(row % a.Hq), kv = hq / a.G, g = hq % a.G;
-  int s = 0;
-  for (int hi = a.n_seq; hi - s > 1;) {
-    const int mid = (s + hi) / 2;
-    if (a.start[mid] <= t) s = mid;
-    else hi = mid;
+  int64_t q = (int64_t)blockIdx.x * MERGE_NW + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (q >= all_q) return;
+  const bool is_short = q < short_q;
+  const int splits = is_short ? a.short_splits : a.tile_splits;
+  int s = 0, kv, r;
+  if (!is_short) q -= short_q;
+  const float* ml = (is_short ? a.short_ml : a.tile_ml) + q * splits * 2;
+  const float* po = (is_short ? a.short_o : a.tile_o) + q * splits * D;
+  const f32x2 mine = lane < splits ? *reinterpret_cast<const f32x2*>(ml + 2 * lane) : f32x2{0.f, 0.f};
+  if (is_short) {
+    const int h = (int)(q / SHORT_ROWS);
+    s = h / a.Hkv;
+    kv = h % a.Hkv;
+    r = (int)(q % SHORT_ROWS);
+  } else {
+    const int item = (int)(q / TM), u = item / a.Hkv;
+    s = tile_sequence<TM>(a, u);
+    kv = item % a.Hkv;
+    r = (u - tiles_before<TM>(a, s)) * TM + (int)(q % TM);
   }
   const Chunk c = chunk_of(a.start, s, a.n_tokens, a.max_len);
-  const int i = t - c.first;
-  if (i < 0 || i >= c.len) return;            // padding
+  const int rows = c.len * a.G;
+  if (r < 0 || r >= rows || (rows <= SHORT_ROWS) != is_short) return;
   const int h = s * a.Hkv + kv, n = min(max(a.n_pages[h], 0), a.max_pages);
   const int end = row_end(n, n > 0 ? a.masks[(size_t)h * a.max_pages + n - 1] : 0u);
-  const int rows = c.len * a.G;
-  const int last = rows <= SHORT_ROWS ? c.len - 1 : (min(((i * a.G + g) / TM + 1) * TM, rows) - 1) / a.G;
-  const int pages = tile_pages(n, end, c.len, last), share = split_share(pages, a.n_split);
+  const int last = is_short ? c.len - 1 : (min((r / TM + 1) * TM, rows) - 1) / a.G;
+  const int pages = tile_pages(n, end, c.len, last), share = split_share(pages, splits);
   const int used = max((pages + share - 1) / share, 1);
-  const float* ml = a.part_ml + row * a.n_split * 2;
-  const float* po = a.part_o + row * a.n_split * D;
-  float M_ = -INFINITY;
-  for (int j = 0; j < used; ++j) M_ = fmaxf(M_, ml[2 * j]);
-  constexpr int PER = D / 64;
-  float l = 0.f, o[PER];
+  constexpr int PER = D / 64, U = 4;
+  const float m = lane < used ? mine[0] : -INFINITY;
+  const float M_ = wave_max(m);
+  const float f = M_ == -INFINITY ? 1.f : fast_exp2(m - M_);     // (no valid key anywhere: sums of 0, or NaN)
+  const float l = wave_sum(lane < used ? mine[1] * f : 0.f);
+  float o[PER];
 #pragma unroll
   for (int e = 0; e < PER; ++e) o[e] = 0.f;
-  if (M_ != -INFINITY)
-    for (int j = 0; j < used; ++j) {
-      const float f = fast_exp2(ml[2 * j] - M_);
-      l += ml[2 * j + 1] * f;
+  for (int j0 = 0; j0 < used; j0 += U) {
+    float x[U][PER];
 #pragma unroll
-      for (int e = 0; e < PER; ++e) o[e] += po[(size_t)j * D + lane * PER + e] * f;
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < PER; ++e) x[u][e] = po[(size_t)min(j0 + u, used - 1) * D + lane * PER + e];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float fu = __shfl(f, j0 + u, 64);
+      if (j0 + u < used && fu != 0.f)
+#pragma unroll
+        for (int e = 0; e < PER; ++e) o[e] = fmaf(x[u][e], fu, o[e]);
     }
+  }
   const float inv = l == 0.f ? 0.f : 1.f / l;   // (a NaN stays one)
+  const int tok = r / a.G;
+  const int64_t row = (int64_t)(c.first + tok) * a.Hq + kv * a.G + (r - tok * a.G);
   T* to = reinterpret_cast<T*>(a.o) + row * D + lane * PER;
   if constexpr (PER == 2) Mma<T, D>::put2(to, o[0] * inv, o[1] * inv);
   else if constexpr (std::is_same<T, float>::value) *to = o[0] * inv;
@@ -944,44 +1119,52 @@ __global__ __launch_bounds__(CH_NT) void chunk_merge_kernel(Args a) {
 static constexpr int tile_rows(bool bf, int D) { return bf || D == 64 ? 256 : 128; }
 
 template <typename T, int D>
-static void launch(Args a, hipStream_t st, int short_wg, int tile_wg) {
+static void launch(const Args& a, hipStream_t st, int short_wg, int tile_wg) {
   constexpr bool bf = sizeof(T) == 2;
   constexpr int TM = tile_rows(bf, D);
   {
     TimedLaunch t(HK_TK_CHUNK_ATTN, st);
     if (tile_wg > 0) {
-      const dim3 grid(tile_wg, a.n_split), block(2 * TM);
+      const dim3 grid(tile_wg, a.tile_splits), block(2 * TM);
       if constexpr (bf) hipLaunchKernelGGL((chunk_tile_bf16_kernel<D>), grid, block, 0, st, a);
       else hipLaunchKernelGGL((chunk_tile_f32_kernel<D, TM / 32>), grid, block, 0, st, a);
     }
-    hipLaunchKernelGGL((chunk_short_kernel<T, D>), dim3(short_wg, a.n_split), dim3(CH_NT), 0, st, a);
+    if (short_wg > 0) {
+      const dim3 grid(short_wg, a.short_splits);
+      if constexpr (bf) hipLaunchKernelGGL((chunk_short_bf16_kernel<D>), grid, dim3(SHORT_NT), 0, st, a);
+      else hipLaunchKernelGGL((chunk_short_f32_kernel<D>), grid, dim3(SHORT_NT), 0, st, a);
+    }
   }
-  if (a.n_split > 1) {
+  const int64_t short_q = a.short_splits > 1 ? (int64_t)short_wg * SHORT_ROWS : 0;
+  const int64_t all_q = short_q + (a.tile_splits > 1 ? (int64_t)tile_wg * TM : 0);
+  if (all_q > 0) {
     TimedLaunch t(HK_TK_CHUNK_MERGE, st);
-    const int64_t rows = (int64_t)a.n_tokens * a.Hq;
-    hipLaunchKernelGGL((chunk_merge_kernel<T, D, TM>), dim3((uint32_t)((rows + CH_NW - 1) / CH_NW)), dim3(CH_NT), 0, st, a);
+    hipLaunchKernelGGL((chunk_merge_kernel<T, D, TM>), dim3((uint32_t)((all_q + MERGE_NW - 1) / MERGE_NW)), dim3(MERGE_NT),
+                       0, st, a, short_q, all_q);
   }
 }
 
-// Splits of a launch: enough workgroups to fill the chip, none of less than MIN_PAGES pages.
-static int plan_splits(long long wg, int max_pages) {
-  int n = 1;
-  const int most = (max_pages + MIN_PAGES - 1) / MIN_PAGES;
-  while (n < most && n < 64 && wg * n < 512) n *= 2;
-  return n < most ? n : most;
-}
-
+// Workgroups and splits of a call.  A launch is split until it offers `want` workgroups, no split
+// of a full-width row having less than MIN_PAGES pages: the short kernel 2048 (four for each that
+// runs at once, as the rows' lengths differ), the tile kernel 512.
 struct Plan {
-  int short_wg, tile_wg, n_split;
+  int short_wg, tile_wg, short_splits, tile_splits;
 };
+static int splits_for(long long wg, int want, int max_pages) {
+  const int most = std::min((max_pages + MIN_PAGES - 1) / MIN_PAGES, MAX_SPLITS);
+  int n = 1;
+  while (n < most && wg * n < want) n *= 2;
+  return std::min(n, most);
+}
 static Plan plan(int NS, int Hq, int Hkv, int TM, int n_tokens, int max_len, int max_pages) {
   const int G = Hq / Hkv;
-  Plan p;
-  p.short_wg = NS * Hkv;
   const long long rows = (long long)n_tokens * G;
   const bool tiles = (long long)max_len * G > SHORT_ROWS && rows > SHORT_ROWS;
+  Plan p;
+  p.short_wg = G <= SHORT_ROWS ? NS * Hkv : 0;
   p.tile_wg = tiles ? (int)((rows / TM + NS) * Hkv) : 0;
-  p.n_split = plan_splits(tiles ? p.tile_wg : p.short_wg, max_pages);
+  p.short_splits = p.short_wg ? splits_for(p.short_wg, 2048, max_pages) : 1;
+  p.tile_splits = tiles ? splits_for(p.tile_wg, 512, max_pages) : 1;
   return p;
 }
 
@@ -989,12 +1172,20 @@ static Plan plan(int NS, int Hq, int Hkv, int TM, int n_tokens, int max_len, int
 
 using namespace hk;
 
-// Grows with the tokens and does not depend on the type: split states are kept for at most
-// MAX_STATES rows (plan_splits stops at 512 workgroups, so a launch that splits has fewer).
-constexpr size_t MAX_STATES = (size_t)1024 * CH_NW * 64;
+// Split states of a call: rows of D + 2 floats.
+static size_t short_states(const Plan& p) {
+  return p.short_splits > 1 ? (size_t)p.short_wg * SHORT_ROWS * p.short_splits : 0;
+}
+// Grows with the tokens and does not depend on the type: a launch of tiles that splits has fewer
+// than twice 512 workgroups.
 size_t hk_chunk_attn_ws(int NS, int Hq, int Hkv, int D, int n_tokens, int max_len, int max_pages) {
-  const size_t most = std::min((max_pages + MIN_PAGES - 1) / MIN_PAGES, 64);
-  const size_t rows = std::min((size_t)n_tokens * Hq * most, MAX_STATES);
+  size_t rows = 0;
+  for (int TM : {128, 256}) {
+    const Plan p = plan(NS, Hq, Hkv, TM, n_tokens, max_len, max_pages);
+    const size_t most = std::min((max_pages + MIN_PAGES - 1) / MIN_PAGES, MAX_SPLITS);
+    const size_t tiles = most > 1 ? std::min((size_t)p.tile_wg * most, (size_t)1024) * TM : 0;
+    rows = std::max(rows, short_states(p) + tiles);
+  }
   return rows * (D + 2) * sizeof(float);
 }
 
@@ -1014,8 +1205,13 @@ hipError_t hk_launch_chunk_attn(int NS, int Hq, int Hkv, int D, const hk_paged_k
   a.q_row = q_row;
   a.o = static_cast<char*>(o);
   a.lse = lse;
-  a.part_o = static_cast<float*>(ws);
-  a.part_ml = p.n_split > 1 ? a.part_o + (size_t)ch->n_tokens * Hq * p.n_split * D : nullptr;
+  a.short_splits = p.short_splits;
+  a.tile_splits = p.tile_splits;
+  const size_t ss = short_states(p), ts = p.tile_splits > 1 ? (size_t)p.tile_wg * p.tile_splits * tile_rows(bf, D) : 0;
+  a.short_o = static_cast<float*>(ws);
+  a.tile_o = a.short_o + ss * D;
+  a.short_ml = a.tile_o + ts * D;
+  a.tile_ml = a.short_ml + ss * 2;
   a.Hq = Hq;
   a.Hkv = Hkv;
   a.G = Hq / Hkv;
@@ -1024,7 +1220,6 @@ hipError_t hk_launch_chunk_attn(int NS, int Hq, int Hkv, int D, const hk_paged_k
   a.n_seq = NS;
   a.n_tokens = ch->n_tokens;
   a.max_len = ch->max_len;
-  a.n_split = p.n_split;
   a.c2 = sm_scale * kLog2e;
   if (bf && D == 128) launch<uint16_t, 128>(a, st, p.short_wg, p.tile_wg);
   else if (bf) launch<uint16_t, 64>(a, st, p.short_wg, p.tile_wg);
