@@ -334,8 +334,8 @@ __device__ __forceinline__ int split_share(int pages, int n_split) {
 }
 __device__ __forceinline__ float bias_of(int pages) { return (float)(32 - __clz(pages * HK_PAGE)) + CH_SLACK; }
 
-// Split states lie by workgroup: query r of item i (a head of the short kernel, tile and KV head of a
-// tile kernel) of splits states each begins at (i * rows + r) * splits.
+// Split states lie by workgroup: of the short kernel two each, of a tile kernel query r of item i (tile
+// and KV head) has tile_splits of them from (i * TM + r) * tile_splits on.
 struct Args {
   const char *q, *k_pool, *v_pool;
   const int32_t *table, *n_pages, *start;
@@ -344,8 +344,9 @@ struct Args {
   char* o;
   float *lse;
   float *short_o, *short_ml, *tile_o, *tile_ml;
+  int32_t* short_first;                       // the short rows' first steps, their total, a workgroup's share
   int Hq, Hkv, G, max_pages, num_pages, n_seq, n_tokens, max_len;
-  int short_splits, tile_splits;              // splits of a row
+  int tile_splits;
   float c2;
 };
 
@@ -793,41 +794,131 @@ __global__ __launch_bounds__(512, 2) void chunk_tile_bf16_kernel(Args a) {
 // ------------------------------------------------------------------ short kernels
 constexpr int SHORT_NT = 256, SHORT_NW = SHORT_NT / 64;
 
-// The rows of a sequence and KV head and the pages of a split that a short kernel's workgroup takes.
-// none: p1 < 0.
-struct ShortWork {
+constexpr int SHORT_WG = 512;                 // workgroups of a launch: two a CU
+constexpr int STEP_PAGES = 8;                 // pages of a step, two a wave
+constexpr int MAX_STATES = 64;                // workgroups that share a row at most
+
+// A row of the short kernels: the chunk of head h's sequence, its folded rows (0: not a short one),
+// and the pages and steps that its last token sees.
+struct ShortRow {
   Chunk c;
-  int kv, split, rows, end, pages, p0, p1;
-  const int32_t* trow;
-  const uint16_t* mrow;
+  int rows, end, pages, steps;
 };
-__device__ __forceinline__ ShortWork short_work(const Args& a) {
-  ShortWork w;
-  const int h = blockIdx.x, s = h / a.Hkv;
-  w.kv = h % a.Hkv;
-  w.split = blockIdx.y;
-  w.p1 = -1;
-  w.c = chunk_of(a.start, s, a.n_tokens, a.max_len);
-  w.rows = w.c.len * a.G;
-  if (w.rows <= 0 || w.rows > SHORT_ROWS) return w;
+__device__ __forceinline__ ShortRow short_row(const Args& a, int h) {
+  ShortRow r;
   const int n = min(max(a.n_pages[h], 0), a.max_pages);
-  w.trow = a.table + (size_t)h * a.max_pages;
-  w.mrow = a.masks + (size_t)h * a.max_pages;
-  w.end = row_end(n, n > 0 ? w.mrow[n - 1] : 0u);
-  w.pages = tile_pages(n, w.end, w.c.len, w.c.len - 1);
-  const int share = split_share(w.pages, a.short_splits);
-  w.p0 = w.split * share;
-  w.p1 = w.split > 0 && w.p0 >= w.pages ? -1 : min(w.p0 + share, w.pages);
-  return w;
+  r.c = chunk_of(a.start, h / a.Hkv, a.n_tokens, a.max_len);
+  r.rows = r.c.len * a.G <= SHORT_ROWS ? r.c.len * a.G : 0;
+  r.end = row_end(n, n > 0 ? a.masks[(size_t)h * a.max_pages + n - 1] : 0u);
+  r.pages = tile_pages(n, r.end, r.c.len, r.c.len - 1);
+  // (a row without pages still has its empty result to write)
+  r.steps = r.rows > 0 ? max((r.pages + STEP_PAGES - 1) / STEP_PAGES, 1) : 0;
+  return r;
 }
 
-// The four waves' states, summed against one reference, are the workgroup's result.  s_o: 32 x (D / 2
-// + 4) floats a wave, used for one half of the dims after the other.
+// The steps of all rows lie behind one another, and every workgroup takes an equal run of them:
+// rows of any mixture of lengths fill the chip evenly, and a launch has no idle workgroups.  Each
+// workgroup sums the rows' steps itself.
+struct Runs {
+  int total, share;
+};
+__device__ inline Runs short_runs(const Args& a, int (&s_first)[SHORT_NT + 1]) {
+  __shared__ int s_sum[SHORT_NW], s_most[SHORT_NW];
+  const int heads = a.n_seq * a.Hkv, per = (heads + SHORT_NT - 1) / SHORT_NT;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int sum = 0, most = 0;
+  for (int h = threadIdx.x * per; h < min((int)(threadIdx.x + 1) * per, heads); ++h) {
+    const int k = short_row(a, h).steps;
+    sum += k;
+    most = max(most, k);
+  }
+  int x = sum;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o, 64);
+    if (lane >= o) x += y;
+  }
+  most = (int)wave_reduce_u32((uint32_t)most, 0u, [](uint32_t p, uint32_t q) { return p > q ? p : q; });
+  if (lane == 63) {
+    s_sum[wave] = x;
+    s_most[wave] = most;
+  }
+  __syncthreads();
+  Runs u = {0, 0};
+  int before = x - sum;
+#pragma unroll
+  for (int w = 0; w < SHORT_NW; ++w) {
+    if (w < wave) before += s_sum[w];
+    u.total += s_sum[w];
+    most = max(most, s_most[w]);
+  }
+  // a row is shared by MAX_STATES workgroups at most
+  u.share = max((u.total + SHORT_WG - 1) / SHORT_WG, (most + MAX_STATES - 2) / (MAX_STATES - 1));
+  s_first[threadIdx.x] = before;
+  if (threadIdx.x == 0) s_first[SHORT_NT] = u.total;
+  if (blockIdx.x == 0) {                      // for the merge
+    int32_t* first = a.short_first;
+    for (int h = threadIdx.x * per; h < min((int)(threadIdx.x + 1) * per, heads); ++h) {
+      first[h] = before;
+      before += short_row(a, h).steps;
+    }
+    if (threadIdx.x == 0) {
+      first[heads] = u.total;
+      first[heads + 1] = u.share;
+    }
+  }
+  __syncthreads();
+  return u;
+}
+
+// A workgroup's next piece of a row: head h, its steps [from, to).
+struct Piece {
+  int h, from, to;
+  ShortRow row;
+};
+// The piece that begins at step x of the launch and ends before step `stop` at the latest.  The same
+// in every lane.
+__device__ inline Piece short_piece(const Args& a, const int (&s_first)[SHORT_NT + 1], int x, int stop) {
+  const int heads = a.n_seq * a.Hkv, per = (heads + SHORT_NT - 1) / SHORT_NT, lane = threadIdx.x & 63;
+  int t = 0;                                  // the last thread whose rows begin at or before x
+  for (int hi = SHORT_NT; hi - t > 1;) {
+    const int mid = (t + hi) / 2;
+    if (s_first[mid] <= x) t = mid;
+    else hi = mid;
+  }
+  int first = s_first[t];
+  Piece p;
+  for (int h0 = t * per;; h0 += 64) {
+    const int h = h0 + lane, k = lane < per && h < heads && h < (t + 1) * per ? short_row(a, h).steps : 0;
+    int y = k;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int z = __shfl_up(y, o, 64);
+      if (lane >= o) y += z;
+    }
+    const unsigned long long in = __ballot(first + y > x);
+    if (in || h0 + 64 >= heads) {
+      const int l = in ? __builtin_ctzll(in) : 63;
+      p.h = __builtin_amdgcn_readfirstlane(min(h0 + l, heads - 1));
+      p.from = x - __builtin_amdgcn_readfirstlane(first + __shfl(y - k, l, 64));
+      break;
+    }
+    first += __shfl(y, 63, 64);
+  }
+  p.row = short_row(a, p.h);
+  p.to = min(p.row.steps, p.from + stop - x);
+  return p;
+}
+
+// The four waves' states, summed against one reference, are the workgroup's result: the row's where
+// the piece is all of it, one of the row's states otherwise.  A workgroup has at most two states: of
+// the row that it begins in the middle of (0), and of the one that it begins and does not end (1).
+// s_o: 32 x (D / 2 + 4) floats a wave, used for one half of the dims after the other.
 template <typename T, int D>
-__device__ __forceinline__ void join_waves(const Args& a, const ShortWork& w, const f32x16 (&acc)[D / 32], float mb,
-                                           float l, float* s_o, float (*s_m)[32], float (*s_l)[32]) {
+__device__ __forceinline__ void join_waves(const Args& a, const Piece& w, const f32x16 (&acc)[D / 32], float mb, float l,
+                                           float* s_o, float (*s_m)[32], float (*s_l)[32]) {
   constexpr int HD = D / 2, OP = HD + 4;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hi = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hi = lane >> 5, kv = w.h % a.Hkv;
   l += __shfl_xor(l, 32, 64);
   __syncthreads();                            // (s_o may be the waves' tiles)
   if (hi == 0) {
@@ -840,13 +931,9 @@ __device__ __forceinline__ void join_waves(const Args& a, const ShortWork& w, co
 #pragma unroll
     for (int v = 0; v < SHORT_NW; ++v) m = fmaxf(m, s_m[v][q]);
     float x = 0.f;
-    if (m != -INFINITY)
 #pragma unroll
-      for (int v = 0; v < SHORT_NW; ++v) x += s_l[v][q] * fast_exp2(s_m[v][q] - m);
-    else
-#pragma unroll
-      for (int v = 0; v < SHORT_NW; ++v) x += s_l[v][q];          // 0, or NaN
-    return x;
+    for (int v = 0; v < SHORT_NW; ++v) x += m == -INFINITY ? s_l[v][q] : s_l[v][q] * fast_exp2(s_m[v][q] - m);
+    return x;                                 // (0 or NaN where there is no reference)
   };
   float M_;
   whole(lane & 31, M_);
@@ -855,10 +942,10 @@ __device__ __forceinline__ void join_waves(const Args& a, const ShortWork& w, co
   const int qr = threadIdx.x >> 3, d0 = (threadIdx.x & 7) * (HD / 8);
   const float l_all = whole(qr, M_);
   const int tq = qr / a.G;
-  const int64_t row = (int64_t)(w.c.first + tq) * a.Hq + w.kv * a.G + (qr - tq * a.G);
-  const bool parts = a.short_splits > 1;
-  const float inv = parts ? 1.f : l_all == 0.f ? 0.f : 1.f / l_all;   // (a NaN stays one)
-  const int64_t state = ((int64_t)blockIdx.x * SHORT_ROWS + qr) * a.short_splits + w.split;
+  const int64_t row = (int64_t)(w.row.c.first + tq) * a.Hq + kv * a.G + (qr - tq * a.G);
+  const bool part = w.from > 0 || w.to < w.row.steps;
+  const float inv = part ? 1.f : l_all == 0.f ? 0.f : 1.f / l_all;   // (a NaN stays one)
+  const int64_t state = (int64_t)(2 * blockIdx.x + (w.from > 0 ? 0 : 1)) * SHORT_ROWS + qr;
   float* po = a.short_o + state * D;
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
@@ -872,7 +959,7 @@ __device__ __forceinline__ void join_waves(const Args& a, const ShortWork& w, co
             f32x4{x[4 * j] * own, x[4 * j + 1] * own, x[4 * j + 2] * own, x[4 * j + 3] * own};
       }
     __syncthreads();
-    if (qr < w.rows)
+    if (qr < w.row.rows)
 #pragma unroll
       for (int d = 0; d < HD / 8; d += 4) {
         f32x4 t = {0.f, 0.f, 0.f, 0.f};
@@ -880,210 +967,119 @@ __device__ __forceinline__ void join_waves(const Args& a, const ShortWork& w, co
         for (int v = 0; v < SHORT_NW; ++v) t += *reinterpret_cast<const f32x4*>(s_o + (v * 32 + qr) * OP + d0 + d);
         t *= inv;
         const int at = half * HD + d0 + d;
-        if (parts) *reinterpret_cast<f32x4*>(po + at) = t;
+        if (part) *reinterpret_cast<f32x4*>(po + at) = t;
         else Mma<T, D>::put4(reinterpret_cast<T*>(a.o) + row * D + at, t[0], t[1], t[2], t[3]);
       }
   }
-  if (qr < w.rows && (threadIdx.x & 7) == 0) {
-    if (parts) *reinterpret_cast<f32x2*>(a.short_ml + state * 2) = f32x2{M_, l_all};
+  if (qr < w.row.rows && (threadIdx.x & 7) == 0) {
+    if (part) *reinterpret_cast<f32x2*>(a.short_ml + state * 2) = f32x2{M_, l_all};
     else if (a.lse) a.lse[row] = l_all == 0.f ? -INFINITY : (M_ + __log2f(l_all)) * kLn2;
   }
+  __syncthreads();                            // the next piece writes the tiles
 }
 
-// fp32: both tiles of a wave's 32 keys go through its part of LDS.
-template <int D>
-__global__ __launch_bounds__(SHORT_NT, 1) void chunk_short_f32_kernel(Args a) {
-  using L = TileLayout<float, D>;
-  using M = Mma<float, D>;
-  constexpr int WP = 2, TP = SHORT_NW * WP;   // pages of a wave and of the workgroup per step
+// Pages go through a wave's own part of LDS, two of K and two of V a step, and are requested a step
+// ahead.  Two workgroups a CU for bf16.  Bound by HBM reads.
+template <typename T, int D>
+__global__ __launch_bounds__(SHORT_NT, sizeof(T) == 2 ? 2 : 1) void chunk_short_kernel(Args a) {
+  using L = TileLayout<T, D>;
+  using M = Mma<T, D>;
+  constexpr int WP = STEP_PAGES / SHORT_NW;
+  static_assert(WP == 2, "a wave's step is 32 keys");
   constexpr int WAVE = 32 * (L::K_ROW + L::V_ROW);
   static_assert(WAVE >= 32 * (D / 2 + 4) * 4, "the join's sums fit the tiles");
   __shared__ __align__(16) char s_buf[SHORT_NW * WAVE];
   __shared__ float s_m[SHORT_NW][32], s_l[SHORT_NW][32];
+  __shared__ int s_first[SHORT_NT + 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const ShortWork w = short_work(a);
-  if (w.p1 < 0) return;
-  const int r = min(lane & 31, w.rows - 1), tok = r / a.G, off = w.end - w.c.len + 1;
-  const int seen = off + tok, seen_all = off;
-  typename M::Query q[1];
-  M::load_q(q[0], reinterpret_cast<const float*>(a.q) + (int64_t)(w.c.first + tok) * a.q_row + (w.kv * a.G + (r - tok * a.G)) * D);
-  const float bias = bias_of(w.pages);
-  State<float, D, 1> st;
-  st.init();
+  const Runs u = short_runs(a, s_first);
   char* my_k = s_buf + wave * WAVE;
   char* my_v = my_k + 32 * L::K_ROW;
-  const int steps = w.p1 > w.p0 ? (w.p1 - w.p0 + TP - 1) / TP : 0;
-  PageRegs<float, D> rk[WP], rv[WP];
-  uint32_t mask[WP];
-  auto page_id = [&](int p) { return min(max(w.trow[min(p, w.p1 - 1)], 0), a.num_pages - 1); };
-  auto load = [&](int t) {
+  const int stop = min((int)(blockIdx.x + 1) * u.share, u.total);
+  for (int x = blockIdx.x * u.share; x < stop;) {
+    const Piece w = short_piece(a, s_first, x, stop);
+    x += w.to - w.from;
+    const int kv = w.h % a.Hkv, r = min(lane & 31, w.row.rows - 1), tok = r / a.G, off = w.row.end - w.row.c.len + 1;
+    const int seen = off + tok, seen_all = off;
+    const int32_t* trow = a.table + (size_t)w.h * a.max_pages;
+    const uint16_t* mrow = a.masks + (size_t)w.h * a.max_pages;
+    const int p0 = w.from * STEP_PAGES, p1 = min(w.to * STEP_PAGES, w.row.pages);
+    typename M::Query q[1];
+    M::load_q(q[0], reinterpret_cast<const T*>(a.q) + (int64_t)(w.row.c.first + tok) * a.q_row + (kv * a.G + (r - tok * a.G)) * D);
+    const float bias = bias_of(w.row.pages);
+    State<T, D, 1> st;
+    st.init();
+    PageRegs<T, D> rk[WP], rv[WP];
+    int id[WP];
+    uint32_t mask[WP], next_mask[WP];
+    auto page_id = [&](int p) { return min(max(trow[min(p, p1 - 1)], 0), a.num_pages - 1); };
+    auto load_id = [&](int t) {
 #pragma unroll
-    for (int i = 0; i < WP; ++i) {
-      const int p = w.p0 + t * TP + wave * WP + i, id = page_id(p);
-      mask[i] = p < w.p1 ? w.mrow[p] : 0u;
-      rk[i].load(a.k_pool, id);
-      rv[i].load(a.v_pool, id);
-    }
-  };
-  if (steps > 0) load(0);
-  for (int t = 0; t < steps; ++t) {
-    // the wave's own region of LDS: its reads of the last step are done before these writes, in
-    // the order of its instructions
-    const int p = w.p0 + t * TP + wave * WP, key = p * HK_PAGE;
-    uint32_t odd = 0;
-    const uint32_t valid = mask[0] | mask[1] << 16;
-#pragma unroll
-    for (int i = 0; i < WP; ++i) {
-      uint32_t keep = mask[i];
-      if ((p + i + 1) * HK_PAGE > seen_all) {
-        const uint32_t o = rv[i].odd_rows() & keep;
-        keep &= ~o;
-        odd |= o << (16 * i);
+      for (int i = 0; i < WP; ++i) {
+        const int p = p0 + t * STEP_PAGES + wave * WP + i;
+        next_mask[i] = p < p1 ? mrow[p] : 0u;
+        id[i] = page_id(p);
       }
-      if (keep != 0xffffu) rv[i].clear(keep);
-      rk[i].store(my_k + i * HK_PAGE * L::K_ROW, L::K_ROW);
-      rv[i].store(my_v + i * HK_PAGE * L::V_ROW, L::V_ROW);
+    };
+    auto load = [&] {
+#pragma unroll
+      for (int i = 0; i < WP; ++i) rk[i].load(a.k_pool, id[i]);
+#pragma unroll
+      for (int i = 0; i < WP; ++i) rv[i].load(a.v_pool, id[i]);
+    };
+    const int steps = p1 > p0 ? w.to - w.from : 0;
+    if (steps > 0) {
+      load_id(0);
+      load();
     }
-    if (t + 1 < steps) load(t + 1);
-    const bool all = valid == 0xffffffffu && key + 32 <= seen_all;
-    const int k = seen - key;
-    const uint32_t vis[1] = {valid & (k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u)};
-    __builtin_amdgcn_wave_barrier();
-    st.block(q, my_k, my_v, vis, all, a.c2, bias, __builtin_amdgcn_readfirstlane(odd), [&](int j) {
-      return reinterpret_cast<const float*>(a.v_pool) + ((size_t)page_id(p + j / HK_PAGE) * HK_PAGE + j % HK_PAGE) * D;
-    });
-    __builtin_amdgcn_wave_barrier();
-  }
-  join_waves<float, D>(a, w, st.acc[0], st.mb[0], st.l[0], reinterpret_cast<float*>(s_buf), s_m, s_l);
-}
-
-// bf16: K goes from memory to the registers that are the scores' operand, a key a lane, and only V
-// through LDS; both are requested a step ahead.  Two workgroups a CU.  Bound by HBM reads.
-template <int D>
-__global__ __launch_bounds__(SHORT_NT, 2) void chunk_short_bf16_kernel(Args a) {
-  using L = TileLayout<uint16_t, D>;
-  using M = Mma<uint16_t, D>;
-  constexpr int WP = 2, TP = SHORT_NW * WP, KS = D / 16;
-  constexpr int V_TILE = 32 * L::V_ROW, O_TILE = 32 * (D / 2 + 4) * 4, WAVE = V_TILE > O_TILE ? V_TILE : O_TILE;
-  __shared__ __align__(16) char s_buf[SHORT_NW * WAVE];
-  __shared__ float s_m[SHORT_NW][32], s_l[SHORT_NW][32];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hi = lane >> 5;
-  const ShortWork w = short_work(a);
-  if (w.p1 < 0) return;
-  const int r = min(lane & 31, w.rows - 1), tok = r / a.G, off = w.end - w.c.len + 1;
-  const int seen = off + tok, seen_all = off;
-  typename M::Query q[1];
-  M::load_q(q[0], reinterpret_cast<const uint16_t*>(a.q) + (int64_t)(w.c.first + tok) * a.q_row + (w.kv * a.G + (r - tok * a.G)) * D);
-  const float bias = bias_of(w.pages);
-  State<uint16_t, D, 1> st;
-  st.init();
-  char* my_v = s_buf + wave * WAVE;
-  const int steps = w.p1 > w.p0 ? (w.p1 - w.p0 + TP - 1) / TP : 0;
-  u32x4 kf[KS];
-  PageRegs<uint16_t, D> rv[WP];
-  int id[WP];
-  uint32_t mask[WP], next_mask[WP];
-  auto page_id = [&](int p) { return min(max(w.trow[min(p, w.p1 - 1)], 0), a.num_pages - 1); };
-  auto load_id = [&](int t) {
+    for (int t = 0; t < steps; ++t) {
+      // the wave's own region of LDS: its reads of the last step are done before these writes, in
+      // the order of its instructions
+      const int p = p0 + t * STEP_PAGES + wave * WP, key = p * HK_PAGE;
 #pragma unroll
-    for (int i = 0; i < WP; ++i) {
-      const int p = w.p0 + t * TP + wave * WP + i;
-      next_mask[i] = p < w.p1 ? w.mrow[p] : 0u;
-      id[i] = page_id(p);
-    }
-  };
-  auto load_k = [&] {
-    const int my = (lane & 16) ? id[1] : id[0];                   // the page of key lane % 32
-    const char* row = a.k_pool + (size_t)my * L::PAGE + (lane & 15) * L::ROW + hi * 16;
+      for (int i = 0; i < WP; ++i) mask[i] = next_mask[i];
+      load_id(t + 1);
+      uint32_t odd = 0;
+      const uint32_t valid = mask[0] | mask[1] << 16;
 #pragma unroll
-    for (int s = 0; s < KS; ++s) kf[s] = *reinterpret_cast<const u32x4*>(row + 32 * s);
-  };
-  if (steps > 0) {
-    load_id(0);
-    load_k();
+      for (int i = 0; i < WP; ++i) rk[i].store(my_k + i * HK_PAGE * L::K_ROW, L::K_ROW);
 #pragma unroll
-    for (int i = 0; i < WP; ++i) rv[i].load(a.v_pool, id[i]);
-  }
-  for (int t = 0; t < steps; ++t) {
-    const int p = w.p0 + t * TP + wave * WP, key = p * HK_PAGE;
-#pragma unroll
-    for (int i = 0; i < WP; ++i) mask[i] = next_mask[i];
-    load_id(t + 1);
-    f32x16 z[1];
-#pragma unroll
-    for (int s = 0; s < KS; ++s)
-      z[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[s]), q[0].f[s], s ? z[0] : f32x16{}, 0, 0, 0);
-    // V of this step into the wave's own region of LDS: its reads of the last step are done before
-    // these writes, in the order of its instructions
-    uint32_t odd = 0;
-    const uint32_t valid = mask[0] | mask[1] << 16;
-#pragma unroll
-    for (int i = 0; i < WP; ++i) {
-      uint32_t keep = mask[i];
-      if ((p + i + 1) * HK_PAGE > seen_all) {
-        const uint32_t o = rv[i].odd_rows() & keep;
-        keep &= ~o;
-        odd |= o << (16 * i);
+      for (int i = 0; i < WP; ++i) {
+        uint32_t keep = mask[i];
+        if ((p + i + 1) * HK_PAGE > seen_all) {
+          const uint32_t o = rv[i].odd_rows() & keep;
+          keep &= ~o;
+          odd |= o << (16 * i);
+        }
+        if (keep != 0xffffu) rv[i].clear(keep);
+        rv[i].store(my_v + i * HK_PAGE * L::V_ROW, L::V_ROW);
       }
-      if (keep != 0xffffu) rv[i].clear(keep);
-      rv[i].store(my_v + i * HK_PAGE * L::V_ROW, L::V_ROW);
+      load();                                 // (past the last step its pages once more, with no valid slot)
+      const bool all = valid == 0xffffffffu && key + 32 <= seen_all;
+      const int k = seen - key;
+      const uint32_t vis[1] = {valid & (k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u)};
+      __builtin_amdgcn_wave_barrier();
+      st.block(q, my_k, my_v, vis, all, a.c2, bias, __builtin_amdgcn_readfirstlane(odd), [&](int j) {
+        return reinterpret_cast<const T*>(a.v_pool) + ((size_t)page_id(p + j / HK_PAGE) * HK_PAGE + j % HK_PAGE) * D;
+      });
+      __builtin_amdgcn_wave_barrier();
     }
-    // (past the last step its pages once more, with no valid slot)
-    load_k();
-#pragma unroll
-    for (int i = 0; i < WP; ++i) rv[i].load(a.v_pool, id[i]);
-    const bool all = valid == 0xffffffffu && key + 32 <= seen_all;
-    const int k = seen - key;
-    const uint32_t vis[1] = {valid & (k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u)};
-    __builtin_amdgcn_wave_barrier();
-    st.weigh(z, my_v, vis, all, a.c2, bias, __builtin_amdgcn_readfirstlane(odd), [&](int j) {
-      return reinterpret_cast<const uint16_t*>(a.v_pool) + ((size_t)page_id(p + j / HK_PAGE) * HK_PAGE + j % HK_PAGE) * D;
-    });
-    __builtin_amdgcn_wave_barrier();
+    join_waves<T, D>(a, w, st.acc[0], st.mb[0], st.l[0], reinterpret_cast<float*>(s_buf), s_m, s_l);
   }
-  join_waves<uint16_t, D>(a, w, st.acc[0], st.mb[0], st.l[0], reinterpret_cast<float*>(s_buf), s_m, s_l);
 }
 
 // ------------------------------------------------------------------ merge
-// One wave per query of a split item: the states of the splits that held pages.  Lanes read the
-// references and sums of all splits at once (at most 64), the outputs four at a time.  The first
-// short_q waves take the short kernel's queries (none when it did not split), the others a tile
-// kernel's.
+// One wave per query: the states of its row's pieces, in their order.  Lanes read the references and
+// sums of all of them at once (at most 64), the outputs four at a time.
 constexpr int MERGE_NT = 256, MERGE_NW = MERGE_NT / 64;
 constexpr int MAX_SPLITS = 64;
 
-template <typename T, int D, int TM>
-__global__ __launch_bounds__(MERGE_NT) void chunk_merge_kernel(Args a, int64_t short_q, int64_t all_q) {
-  const int lane = threadIdx.x & 63;
-  int64_t q = (int64_t)blockIdx.x * MERGE_NW + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (q >= all_q) return;
-  const bool is_short = q < short_q;
-  const int splits = is_short ? a.short_splits : a.tile_splits;
-  int s = 0, kv, r;
-  if (!is_short) q -= short_q;
-  const float* ml = (is_short ? a.short_ml : a.tile_ml) + q * splits * 2;
-  const float* po = (is_short ? a.short_o : a.tile_o) + q * splits * D;
-  const f32x2 mine = lane < splits ? *reinterpret_cast<const f32x2*>(ml + 2 * lane) : f32x2{0.f, 0.f};
-  if (is_short) {
-    const int h = (int)(q / SHORT_ROWS);
-    s = h / a.Hkv;
-    kv = h % a.Hkv;
-    r = (int)(q % SHORT_ROWS);
-  } else {
-    const int item = (int)(q / TM), u = item / a.Hkv;
-    s = tile_sequence<TM>(a, u);
-    kv = item % a.Hkv;
-    r = (u - tiles_before<TM>(a, s)) * TM + (int)(q % TM);
-  }
-  const Chunk c = chunk_of(a.start, s, a.n_tokens, a.max_len);
-  const int rows = c.len * a.G;
-  if (r < 0 || r >= rows || (rows <= SHORT_ROWS) != is_short) return;
-  const int h = s * a.Hkv + kv, n = min(max(a.n_pages[h], 0), a.max_pages);
-  const int end = row_end(n, n > 0 ? a.masks[(size_t)h * a.max_pages + n - 1] : 0u);
-  const int last = is_short ? c.len - 1 : (min((r / TM + 1) * TM, rows) - 1) / a.G;
-  const int pages = tile_pages(n, end, c.len, last), share = split_share(pages, splits);
-  const int used = max((pages + share - 1) / share, 1);
+template <typename T, int D, typename F>
+__device__ __forceinline__ void merge_states(const Args& a, int64_t row, int used, const float* o_states,
+                                             const float* ml_states, F at) {
   constexpr int PER = D / 64, U = 4;
+  const int lane = threadIdx.x & 63;
+  const f32x2 mine = *reinterpret_cast<const f32x2*>(ml_states + at(min(lane, used - 1)) * 2);
   const float m = lane < used ? mine[0] : -INFINITY;
   const float M_ = wave_max(m);
   const float f = M_ == -INFINITY ? 1.f : fast_exp2(m - M_);     // (no valid key anywhere: sums of 0, or NaN)
@@ -1094,9 +1090,11 @@ __global__ __launch_bounds__(MERGE_NT) void chunk_merge_kernel(Args a, int64_t s
   for (int j0 = 0; j0 < used; j0 += U) {
     float x[U][PER];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u) {
+      const float* po = o_states + at(min(j0 + u, used - 1)) * D + lane * PER;
 #pragma unroll
-      for (int e = 0; e < PER; ++e) x[u][e] = po[(size_t)min(j0 + u, used - 1) * D + lane * PER + e];
+      for (int e = 0; e < PER; ++e) x[u][e] = po[e];
+    }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const float fu = __shfl(f, j0 + u, 64);
@@ -1106,8 +1104,6 @@ __global__ __launch_bounds__(MERGE_NT) void chunk_merge_kernel(Args a, int64_t s
     }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;   // (a NaN stays one)
-  const int tok = r / a.G;
-  const int64_t row = (int64_t)(c.first + tok) * a.Hq + kv * a.G + (r - tok * a.G);
   T* to = reinterpret_cast<T*>(a.o) + row * D + lane * PER;
   if constexpr (PER == 2) Mma<T, D>::put2(to, o[0] * inv, o[1] * inv);
   else if constexpr (std::is_same<T, float>::value) *to = o[0] * inv;
@@ -1115,11 +1111,49 @@ __global__ __launch_bounds__(MERGE_NT) void chunk_merge_kernel(Args a, int64_t s
   if (lane == 0 && a.lse) a.lse[row] = l == 0.f ? -INFINITY : (M_ + __log2f(l)) * kLn2;
 }
 
+// Short rows: workgroup (h, y) takes every MERGE_Y-th four queries of head h.
+constexpr int MERGE_Y = 4;
+template <typename T, int D>
+__global__ __launch_bounds__(MERGE_NT) void chunk_merge_short_kernel(Args a) {
+  const int h = blockIdx.x, heads = a.n_seq * a.Hkv;
+  const int first = a.short_first[h], steps = a.short_first[h + 1] - first, share = a.short_first[heads + 1];
+  const Chunk c = chunk_of(a.start, h / a.Hkv, a.n_tokens, a.max_len);
+  if (steps <= 0) return;
+  const int w0 = first / share, used = (first + steps - 1) / share - w0 + 1;
+  if (used <= 1) return;                      // written as it is
+  for (int r = blockIdx.y * MERGE_NW + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); r < c.len * a.G;
+       r += MERGE_Y * MERGE_NW) {
+    const int tok = r / a.G;
+    const int64_t row = (int64_t)(c.first + tok) * a.Hq + (h % a.Hkv) * a.G + (r - tok * a.G);
+    merge_states<T, D>(a, row, used, a.short_o, a.short_ml, [&](int j) {
+      return (int64_t)(2 * (w0 + j) + (j == 0 ? 1 : 0)) * SHORT_ROWS + r;
+    });
+  }
+}
+
+// A tile kernel's queries: tile and KV head, then the query.
+template <typename T, int D, int TM>
+__global__ __launch_bounds__(MERGE_NT) void chunk_merge_tile_kernel(Args a) {
+  const int64_t q = (int64_t)blockIdx.x * MERGE_NW + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int item = (int)(q / TM), u = item / a.Hkv, kv = item % a.Hkv, s = tile_sequence<TM>(a, u);
+  const int r = (u - tiles_before<TM>(a, s)) * TM + (int)(q % TM);
+  const Chunk c = chunk_of(a.start, s, a.n_tokens, a.max_len);
+  const int rows = c.len * a.G;
+  if (r < 0 || r >= rows || rows <= SHORT_ROWS) return;
+  const int h = s * a.Hkv + kv, n = min(max(a.n_pages[h], 0), a.max_pages);
+  const int end = row_end(n, n > 0 ? a.masks[(size_t)h * a.max_pages + n - 1] : 0u);
+  const int pages = tile_pages(n, end, c.len, (min((r / TM + 1) * TM, rows) - 1) / a.G);
+  const int share = split_share(pages, a.tile_splits), used = max((pages + share - 1) / share, 1);
+  const int tok = r / a.G;
+  const int64_t row = (int64_t)(c.first + tok) * a.Hq + kv * a.G + (r - tok * a.G);
+  merge_states<T, D>(a, row, used, a.tile_o, a.tile_ml, [&](int j) { return q * a.tile_splits + j; });
+}
+
 // Rows of a tile kernel's workgroup.
 static constexpr int tile_rows(bool bf, int D) { return bf || D == 64 ? 256 : 128; }
 
 template <typename T, int D>
-static void launch(const Args& a, hipStream_t st, int short_wg, int tile_wg) {
+static void launch(const Args& a, hipStream_t st, int heads, int tile_wg) {
   constexpr bool bf = sizeof(T) == 2;
   constexpr int TM = tile_rows(bf, D);
   {
@@ -1129,42 +1163,31 @@ static void launch(const Args& a, hipStream_t st, int short_wg, int tile_wg) {
       if constexpr (bf) hipLaunchKernelGGL((chunk_tile_bf16_kernel<D>), grid, block, 0, st, a);
       else hipLaunchKernelGGL((chunk_tile_f32_kernel<D, TM / 32>), grid, block, 0, st, a);
     }
-    if (short_wg > 0) {
-      const dim3 grid(short_wg, a.short_splits);
-      if constexpr (bf) hipLaunchKernelGGL((chunk_short_bf16_kernel<D>), grid, dim3(SHORT_NT), 0, st, a);
-      else hipLaunchKernelGGL((chunk_short_f32_kernel<D>), grid, dim3(SHORT_NT), 0, st, a);
-    }
+    if (heads > 0) hipLaunchKernelGGL((chunk_short_kernel<T, D>), dim3(SHORT_WG), dim3(SHORT_NT), 0, st, a);
   }
-  const int64_t short_q = a.short_splits > 1 ? (int64_t)short_wg * SHORT_ROWS : 0;
-  const int64_t all_q = short_q + (a.tile_splits > 1 ? (int64_t)tile_wg * TM : 0);
-  if (all_q > 0) {
-    TimedLaunch t(HK_TK_CHUNK_MERGE, st);
-    hipLaunchKernelGGL((chunk_merge_kernel<T, D, TM>), dim3((uint32_t)((all_q + MERGE_NW - 1) / MERGE_NW)), dim3(MERGE_NT),
-                       0, st, a, short_q, all_q);
-  }
+  TimedLaunch t(HK_TK_CHUNK_MERGE, st);
+  if (a.tile_splits > 1)
+    hipLaunchKernelGGL((chunk_merge_tile_kernel<T, D, TM>), dim3((uint32_t)tile_wg * (TM / MERGE_NW)), dim3(MERGE_NT), 0, st, a);
+  if (heads > 0) hipLaunchKernelGGL((chunk_merge_short_kernel<T, D>), dim3(heads, MERGE_Y), dim3(MERGE_NT), 0, st, a);
 }
 
-// Workgroups and splits of a call.  A launch is split until it offers `want` workgroups, no split
-// of a full-width row having less than MIN_PAGES pages: the short kernel 2048 (four for each that
-// runs at once, as the rows' lengths differ), the tile kernel 512.
+// Workgroups and splits of a call.  A tile launch is split until it offers 512 workgroups, no split
+// of a full-width row having less than MIN_PAGES pages.  heads: of the short kernel, 0 where no row
+// can be a short one.
 struct Plan {
-  int short_wg, tile_wg, short_splits, tile_splits;
+  int heads, tile_wg, tile_splits;
 };
-static int splits_for(long long wg, int want, int max_pages) {
-  const int most = std::min((max_pages + MIN_PAGES - 1) / MIN_PAGES, MAX_SPLITS);
-  int n = 1;
-  while (n < most && wg * n < want) n *= 2;
-  return std::min(n, most);
-}
 static Plan plan(int NS, int Hq, int Hkv, int TM, int n_tokens, int max_len, int max_pages) {
   const int G = Hq / Hkv;
   const long long rows = (long long)n_tokens * G;
   const bool tiles = (long long)max_len * G > SHORT_ROWS && rows > SHORT_ROWS;
   Plan p;
-  p.short_wg = G <= SHORT_ROWS ? NS * Hkv : 0;
+  p.heads = G <= SHORT_ROWS ? NS * Hkv : 0;
   p.tile_wg = tiles ? (int)((rows / TM + NS) * Hkv) : 0;
-  p.short_splits = p.short_wg ? splits_for(p.short_wg, 2048, max_pages) : 1;
-  p.tile_splits = tiles ? splits_for(p.tile_wg, 512, max_pages) : 1;
+  const int most = std::min((max_pages + MIN_PAGES - 1) / MIN_PAGES, MAX_SPLITS);
+  p.tile_splits = 1;
+  while (tiles && p.tile_splits < most && (long long)p.tile_wg * p.tile_splits < 512) p.tile_splits *= 2;
+  p.tile_splits = std::min(p.tile_splits, most);
   return p;
 }
 
@@ -1172,12 +1195,10 @@ static Plan plan(int NS, int Hq, int Hkv, int TM, int n_tokens, int max_len, int
 
 using namespace hk;
 
-// Split states of a call: rows of D + 2 floats.
-static size_t short_states(const Plan& p) {
-  return p.short_splits > 1 ? (size_t)p.short_wg * SHORT_ROWS * p.short_splits : 0;
-}
-// Grows with the tokens and does not depend on the type: a launch of tiles that splits has fewer
-// than twice 512 workgroups.
+// Split states (rows of D + 2 floats) of the short kernel's workgroups, two each, of the tiles', and
+// the short rows' first steps.  Grows with the tokens and does not depend on the type: a launch of
+// tiles that splits has fewer than twice 512 workgroups.
+static size_t short_states(const Plan& p) { return p.heads ? (size_t)2 * SHORT_WG * SHORT_ROWS : 0; }
 size_t hk_chunk_attn_ws(int NS, int Hq, int Hkv, int D, int n_tokens, int max_len, int max_pages) {
   size_t rows = 0;
   for (int TM : {128, 256}) {
@@ -1186,7 +1207,7 @@ size_t hk_chunk_attn_ws(int NS, int Hq, int Hkv, int D, int n_tokens, int max_le
     const size_t tiles = most > 1 ? std::min((size_t)p.tile_wg * most, (size_t)1024) * TM : 0;
     rows = std::max(rows, short_states(p) + tiles);
   }
-  return rows * (D + 2) * sizeof(float);
+  return rows * (D + 2) * sizeof(float) + ((size_t)NS * Hkv + 2) * sizeof(int32_t);
 }
 
 hipError_t hk_launch_chunk_attn(int NS, int Hq, int Hkv, int D, const hk_paged_kv* kv, const hk_chunks* ch,
@@ -1205,13 +1226,13 @@ hipError_t hk_launch_chunk_attn(int NS, int Hq, int Hkv, int D, const hk_paged_k
   a.q_row = q_row;
   a.o = static_cast<char*>(o);
   a.lse = lse;
-  a.short_splits = p.short_splits;
   a.tile_splits = p.tile_splits;
   const size_t ss = short_states(p), ts = p.tile_splits > 1 ? (size_t)p.tile_wg * p.tile_splits * tile_rows(bf, D) : 0;
   a.short_o = static_cast<float*>(ws);
   a.tile_o = a.short_o + ss * D;
   a.short_ml = a.tile_o + ts * D;
   a.tile_ml = a.short_ml + ss * 2;
+  a.short_first = reinterpret_cast<int32_t*>(a.tile_ml + ts * 2);
   a.Hq = Hq;
   a.Hkv = Hkv;
   a.G = Hq / Hkv;
@@ -1221,9 +1242,9 @@ hipError_t hk_launch_chunk_attn(int NS, int Hq, int Hkv, int D, const hk_paged_k
   a.n_tokens = ch->n_tokens;
   a.max_len = ch->max_len;
   a.c2 = sm_scale * kLog2e;
-  if (bf && D == 128) launch<uint16_t, 128>(a, st, p.short_wg, p.tile_wg);
-  else if (bf) launch<uint16_t, 64>(a, st, p.short_wg, p.tile_wg);
-  else if (D == 128) launch<float, 128>(a, st, p.short_wg, p.tile_wg);
-  else launch<float, 64>(a, st, p.short_wg, p.tile_wg);
+  if (bf && D == 128) launch<uint16_t, 128>(a, st, p.heads, p.tile_wg);
+  else if (bf) launch<uint16_t, 64>(a, st, p.heads, p.tile_wg);
+  else if (D == 128) launch<float, 128>(a, st, p.heads, p.tile_wg);
+  else launch<float, 64>(a, st, p.heads, p.tile_wg);
   return hipGetLastError();
 }
