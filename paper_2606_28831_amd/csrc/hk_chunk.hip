@@ -531,18 +531,56 @@ __global__ __launch_bounds__(64 * NW, 1) void chunk_tile_f32_kernel(Args a) {
   if (w0 + (lane & 31) < w.rows) put_state<float, D>(a, row, ((int64_t)w.item * 32 * NW + r - w.r0) * a.tile_splits, w.split, st.acc[0], st.mb[0], l);
 }
 
+// LDS tiles of the bf16 kernel: filled straight from memory, 1 KB an instruction, 16 bytes a lane in
+// lane order, so a tile is made of 1 KB groups of rows (8 of D 64, 4 of D 128), 16 or 32 bytes apart.
+// Within a group the row's 64-byte quarters come first, then the rows, then the 16-byte pieces (of D
+// 64 swapped in pairs in rows 4 to 7): four lanes fetch 64 bytes of a row, the eight or sixteen keys
+// of a K fragment's read lie in different banks, those of a V fragment's two to a bank at best, and
+// every fragment's offset is a constant.
+template <int D>
+struct DirectTile {
+  static constexpr int ROWS = 512 / D, GROUP = D == 128 ? 1040 : 1056, HALF = 32 / ROWS * GROUP, BYTES = 2 * HALF;
+  static constexpr int LOADS = HK_PAGE / ROWS, QUARTER = ROWS * 64;
+  // the row within a group and the byte within the row that a lane fetches
+  __device__ static __forceinline__ int row(int lane) { return (lane >> 2) & (ROWS - 1); }
+  __device__ static __forceinline__ int byte(int lane) {
+    return lane / (4 * ROWS) * 64 + ((lane & 3) ^ (D == 64 ? (lane >> 4) & 1 : 0)) * 16;
+  }
+  // fragment s of key lane % 32, dims 16 s + 8 (lane / 32) ..: at k_lane + k_step(s)
+  __device__ static __forceinline__ int k_lane(int lane) {
+    const int key = lane & 31, hi = lane >> 5, swap = D == 64 ? (key >> 2) & 1 : 0;
+    return key / ROWS * GROUP + key % ROWS * 64 + (hi ^ swap) * 16;
+  }
+  static constexpr int k_step(int s) { return (s >> 1) * QUARTER + (s & 1) * 32; }
+  // transposing read h of the keys 16 s + 8 h + 4 (lane / 32) .. of dims 32 dt ..: v_lane + v_step
+  __device__ static __forceinline__ int v_lane(int lane) {
+    const int i = lane & 15, g = (lane >> 4) & 1, hi = lane >> 5;
+    if (D == 128) return hi * GROUP + (i >> 2) * 64 + g * 32 + (i & 3) * 8;
+    return (4 * hi + (i >> 2)) * 64 + g * 32 + (((i & 3) >> 1) ^ hi) * 16 + (i & 1) * 8;
+  }
+  static constexpr int v_step(int s, int h, int dt) { return (16 * s + 8 * h) / ROWS * GROUP + dt * QUARTER; }
+};
+static __device__ const u32x4 zero_row[1] = {};
+
+// 1 KB from memory to LDS: lane l's 16 bytes at `from` to `to` + 16 l.  It is on its way afterwards; the
+// wave waits by direct_wait.
+__device__ __forceinline__ void direct_load(const char* from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "m0", "memory");
+}
+__device__ __forceinline__ void direct_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 // bf16.  Eight waves, two a SIMD, take 32 rows each against tiles of 64 keys.  A wave's steps of 32
 // keys are a pipeline: the scores of the next block run beside the exponentials of this one, its
 // P V beside the next one's maximum; MFMAs and the vector work between them are laid out by hand.
-// Three tiles in LDS: while one is computed the next is stored, and a wave that is a barrier ahead
-// stores over none that another still reads.
+// Three tiles in LDS: one is computed, the next has arrived, the one after is on its way.
 template <int D>
 __global__ __launch_bounds__(512, 2) void chunk_tile_bf16_kernel(Args a) {
-  using L = TileLayout<uint16_t, D>;
+  using L = DirectTile<D>;
   using M = Mma<uint16_t, D>;
   constexpr int TP = TILE_PAGES, KS = D / 16, DT = D / 32, VS = 2 * DT, AHEAD = 3;
-  __shared__ __align__(16) char s_k[3][TILE_KEYS * L::K_ROW], s_v[3][TILE_KEYS * L::V_ROW];
-  __shared__ __align__(8) uint16_t s_mask[3][TP], s_odd[3][TP];
+  constexpr int PAGE = HK_PAGE * D * 2, PAGE_LDS = HK_PAGE / L::ROWS * L::GROUP;
+  __shared__ __align__(16) char s_k[3][L::BYTES], s_v[3][L::BYTES];
+  __shared__ __align__(16) uint32_t s_flag[3][TP];               // mask | odd rows << 16 of a tile's pages
   const int lane = threadIdx.x & 63, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // (conditions on it are scalar)
   const TileWork w = tile_work<256>(a);
@@ -559,38 +597,59 @@ __global__ __launch_bounds__(512, 2) void chunk_tile_bf16_kernel(Args a) {
   const float bias = bias_of(w.pages), c2 = a.c2;
   const int tiles = w.p1 > w.p0 ? (w.p1 - w.p0 + TP - 1) / TP : 0;
 
-  // waves 0 to 3 bring a page of K each, waves 4 to 7 the same pages of V; a page's id and mask are
-  // loaded a tile before the page
+  // Waves 0 to 3 bring a page of K each, waves 4 to 7 the same pages of V.  A page's id and mask are
+  // loaded a tile before the page is requested.  V rows that are not valid are fetched as zeros.
   const int my = wave & 3;
   const bool is_v = wave >= 4;
-  const char* pool = is_v ? a.v_pool : a.k_pool;
-  PageRegs<uint16_t, D> rp;
+  const char* pool = (is_v ? a.v_pool : a.k_pool) + L::row(lane) * (D * 2) + L::byte(lane);
   int id = 0;
-  uint32_t mask = 0, next_mask = 0;
+  uint32_t mask = 0, next_mask = 0;                              // of the page on its way, and of the next
   auto load_id = [&](int t) {
     const int p = w.p0 + t * TP + my;
-    next_mask = p < w.p1 ? w.mrow[p] : 0u;
-    id = w.trow[min(p, w.p1 - 1)];
+    int at = min(p, w.p1 - 1);
+    asm volatile("" : "+v"(at));                                 // (a vector load: a scalar one's wait is for LDS too)
+    next_mask = p < w.p1 ? w.mrow[at] : 0u;
+    id = w.trow[at];
   };
-  auto load = [&] {
-    mask = next_mask;
-    rp.load(pool, min(max(id, 0), a.num_pages - 1));
-  };
-  auto store = [&](int t, int buf) {
-    if (is_v) {
-      uint32_t keep = mask, odd = 0;
-      if ((w.p0 + t * TP + my + 1) * HK_PAGE > tile_seen) {
-        odd = rp.odd_rows() & mask;
-        keep &= ~odd;
+  auto request = [&](int buf) {
+    mask = __builtin_amdgcn_readfirstlane(next_mask);
+    const char* from = pool + (size_t)min(max(__builtin_amdgcn_readfirstlane(id), 0), a.num_pages - 1) * PAGE;
+    uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(is_v ? s_v[buf] : s_k[buf]) + my * PAGE_LDS;
+    to = __builtin_amdgcn_readfirstlane(to);
+    if (is_v && mask != 0xffffu) {
+#pragma unroll
+      for (int j = 0; j < L::LOADS; ++j) {
+        const bool valid = (mask >> (j * L::ROWS + L::row(lane))) & 1u;
+        direct_load(valid ? from + j * 1024 : reinterpret_cast<const char*>(zero_row), to + j * L::GROUP);
       }
-      if (keep != 0xffffu) rp.clear(keep);
-      if (lane == 0) {
-        s_mask[buf][my] = (uint16_t)mask;
-        s_odd[buf][my] = (uint16_t)odd;
+    } else {
+#pragma unroll
+      for (int j = 0; j < L::LOADS; ++j) direct_load(from + j * 1024, to + j * L::GROUP);
+    }
+  };
+  // The page of tile t is in LDS: its flags; rows of V that hold infinite values and are not seen by
+  // every query of the tile become zeros.
+  auto settle = [&](int t, int buf) {
+    direct_wait();
+    if (!is_v) return;
+    uint32_t odd = 0;
+    if (mask != 0 && (w.p0 + t * TP + my + 1) * HK_PAGE > tile_seen) {
+      char* at = s_v[buf] + my * PAGE_LDS + lane * 16;
+#pragma unroll
+      for (int j = 0; j < L::LOADS; ++j) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(at + j * L::GROUP);
+        bool bad = false;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) bad |= (x[k] & 0x7f800000u) == 0x7f800000u || (x[k] & 0x7f80u) == 0x7f80u;
+        if (__any(bad))
+          for (int r = 0; r < L::ROWS; ++r)
+            if (__any(bad && L::row(lane) == r)) {
+              odd |= 1u << (j * L::ROWS + r);
+              if (L::row(lane) == r) *reinterpret_cast<u32x4*>(at + j * L::GROUP) = u32x4{0u, 0u, 0u, 0u};
+            }
       }
     }
-    if (is_v) rp.store(s_v[buf] + my * HK_PAGE * L::V_ROW, L::V_ROW);
-    else rp.store(s_k[buf] + my * HK_PAGE * L::K_ROW, L::K_ROW);
+    if (lane == 0) s_flag[buf][my] = mask | odd << 16;
   };
 
   f32x16 acc[DT];
@@ -600,19 +659,15 @@ __global__ __launch_bounds__(512, 2) void chunk_tile_bf16_kernel(Args a) {
     for (int e = 0; e < 16; ++e) acc[dt][e] = 0.f;
   float m = -INFINITY, mb = 0.f, l = 0.f;
 
-  // LDS addresses of the lane's fragments within 32 keys: K by 16-byte pieces of key l % 32, V by
-  // transposing reads of 4 keys x 16 dims (two a fragment)
-  const int i16 = lane & 15, k_at = (lane & 31) * L::K_ROW + hi * 16;
-  const int v_at = (4 * hi + (i16 >> 2)) * L::V_ROW + ((lane >> 4) & 1) * 32 + (i16 & 3) * 8;
+  const int k_at = L::k_lane(lane), v_at = L::v_lane(lane);      // the lane's fragments within 32 keys
   auto k_frag = [&](const char* k, int s) {
-    return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(k + k_at + 32 * s));
+    return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(k + k_at + L::k_step(s)));
   };
   auto v_frag = [&](const char* v, int i) {                      // i = s * DT + dt
-    const int s = i / DT, dt = i % DT;
     s16x4 x[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const char* at = v + v_at + (16 * s + 8 * h) * L::V_ROW + dt * 64;
+      const char* at = v + v_at + L::v_step(i / DT, h, i % DT);
       x[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
           (__attribute__((address_space(3))) s16x4*)(uintptr_t)(__attribute__((address_space(3))) const char*)at);
     }
@@ -716,44 +771,45 @@ __global__ __launch_bounds__(512, 2) void chunk_tile_bf16_kernel(Args a) {
         }
     }
   };
-  auto flags = [&](const uint16_t* x) {
-    const uint64_t y = *reinterpret_cast<const uint64_t*>(x);
-    return ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(y >> 32)) << 32) |
-           (uint32_t)__builtin_amdgcn_readfirstlane((int)y);
+  uint64_t valid = 0, odd = 0;                                   // of the tile's 64 keys
+  auto flags = [&](int buf) {
+    const u32x4 f = *reinterpret_cast<const u32x4*>(s_flag[buf]);
+    uint32_t x[TP];
+#pragma unroll
+    for (int i = 0; i < TP; ++i) x[i] = __builtin_amdgcn_readfirstlane(f[i]);
+    valid = (uint64_t)((x[3] << 16) | (x[2] & 0xffffu)) << 32 | ((x[1] << 16) | (x[0] & 0xffffu));
+    odd = (uint64_t)((x[3] & 0xffff0000u) | (x[2] >> 16)) << 32 | ((x[1] & 0xffff0000u) | (x[0] >> 16));
   };
 
+  auto after = [](int buf) { return buf == 2 ? 0 : buf + 1; };
+  // Tile t is computed between a barrier that finds tile t + 1 arrived and the tile before t read by
+  // all, whose place tile t + 2 then takes.  (Past the last tile its last page once more, with no
+  // valid slot.)
+  auto turn = [&](int t, int next) {
+    settle(t + 1, next);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    request(after(next));
+    load_id(t + 3);
+  };
   if (tiles > 0) {
     load_id(0);
-    load();
+    request(0);
     load_id(1);
-    store(0, 0);
-    load();
+    settle(0, 0);
+    request(1);
     load_id(2);
     __syncthreads();
   }
-  auto after = [](int buf) { return buf == 2 ? 0 : buf + 1; };
-  auto bring = [&](int t, int buf) {                             // tile t into LDS, tile t + 1 on its way
-    if (t < tiles) {
-      store(t, buf);
-      load();
-      load_id(t + 2);
-    }
-  };
   if (w0 >= w.rows) {                                            // a wave without rows brings its pages
-    for (int t = 0, buf = 1; t < tiles; ++t, buf = after(buf)) {
-      bring(t + 1, buf);
-      __syncthreads();
-    }
+    for (int t = 0, buf = 0; t < tiles; ++t, buf = after(buf)) turn(t, after(buf));
+    direct_wait();
     return;
   }
-  constexpr int K_HALF = 32 * L::K_ROW, V_HALF = 32 * L::V_ROW;
   // the queries are here before the loop, where a wait for them would be one for the next tile too
 #pragma unroll
   for (int i = 0; i < KS; ++i) asm volatile("" : "+v"(q.f[i]));
-  uint64_t valid = 0, odd = 0;
   if (tiles > 0) {
-    valid = flags(s_mask[0]);
-    odd = flags(s_odd[0]);
+    flags(0);
     first_k(s_k[0]);
 #pragma unroll
     for (int i = 0; i < KS; ++i) {
@@ -765,28 +821,26 @@ __global__ __launch_bounds__(512, 2) void chunk_tile_bf16_kernel(Args a) {
 #pragma unroll
     for (int e = 1; e < 16; ++e) zm = fmaxf(zm, z[0][e]);
     refer(zm);
-    first_k(s_k[0] + K_HALF);
+    first_k(s_k[0] + L::HALF);
   }
   for (int t = 0, buf = 0; t < tiles; ++t) {
     const int p = w.p0 + t * TP, next = after(buf);
-    // past the last tile the scores are of whatever LDS holds, and hidden
-    bring(t + 1, next);
-    scores(z[1], z[0], s_k[buf] + K_HALF, s_v[buf]);
-    __syncthreads();
+    scores(z[1], z[0], s_k[buf] + L::HALF, s_v[buf]);
+    turn(t, next);
     hide(z[1], p + 2, (uint32_t)(valid >> 32));
     float zm = values(z[1], s_v[buf], s_k[next]);
     if ((uint32_t)odd) add_odd((uint32_t)odd, p, (uint32_t)valid);
     refer(zm);
-    const uint64_t valid_next = t + 1 < tiles ? flags(s_mask[next]) : 0;
-    scores(z[0], z[1], s_k[next], s_v[buf] + V_HALF);
-    hide(z[0], p + 4, (uint32_t)valid_next);
-    zm = values(z[0], s_v[buf] + V_HALF, s_k[next] + K_HALF);
-    if (odd >> 32) add_odd((uint32_t)(odd >> 32), p + 2, (uint32_t)(valid >> 32));
+    const uint32_t odd1 = (uint32_t)(odd >> 32), valid1 = (uint32_t)(valid >> 32);
+    flags(next);
+    scores(z[0], z[1], s_k[next], s_v[buf] + L::HALF);
+    hide(z[0], p + 4, (uint32_t)valid);
+    zm = values(z[0], s_v[buf] + L::HALF, s_k[next] + L::HALF);
+    if (odd1) add_odd(odd1, p + 2, valid1);
     refer(zm);
-    valid = valid_next;
-    odd = t + 1 < tiles ? flags(s_odd[next]) : 0;
     buf = next;
   }
+  direct_wait();                                                 // (nothing on its way into LDS that is given back)
   l += __shfl_xor(l, 32, 64);
   if (w0 + (lane & 31) < w.rows) put_state<uint16_t, D>(a, row, ((int64_t)w.item * 256 + r - w.r0) * a.tile_splits, w.split, acc, mb, l);
 }
