@@ -3,13 +3,13 @@
 // The query rows of one KV head are folded: row r of a chunk is query head r % G of token r / G,
 // and all of them read the same K and V.  Two kernels share the work by the folded rows of a
 // sequence:
-//   tile   more than SHORT_ROWS rows: a workgroup takes TM rows, its four waves 64 (fp32: 32) rows
-//          each, all against the same K and V tiles in LDS;
+//   tile   more than SHORT_ROWS rows: a workgroup takes TILE_ROWS rows, its four waves 32 each, all
+//          against the same K and V tiles in LDS;
 //   short  up to SHORT_ROWS rows (drafts, single tokens): a workgroup takes the 32 rows, its four
 //          waves take the pages in turn, every page read once by one wave, and meet at the end.
-// Both may split a row's pages over workgroups; merge_kernel joins the splits' states with the
-// operator of App. F.  Work and split of a workgroup follow from the chunk starts and page counts
-// in device memory.
+// Both may cut a row's pages into pieces for several workgroups; chunk_merge_kernel joins the
+// pieces' states with the operator of App. F.  Work and pieces of a workgroup follow from the chunk
+// starts and page counts in device memory.
 //
 // Arithmetic of a wave, per block of 32 keys: C[key][query] = K Q^T on MFMA, so that a lane holds
 // 16 keys of one query and the softmax needs no cross-lane step but for a new reference; then
@@ -33,7 +33,6 @@ namespace hk {
 
 constexpr float CH_SLACK = 12.f;
 constexpr int SHORT_ROWS = 32;
-constexpr int MIN_PAGES = 8;                  // fewest pages of a split
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -318,24 +317,13 @@ struct State {
   }
 };
 
-// What a workgroup works on: rows of one sequence and KV head, and a range of its pages.
-struct Work {
-  int first, len, rows;                       // the chunk, and its folded rows len * G
-  int end;                                    // one past the row's newest valid slot
-  int pages;                                  // pages that the workgroup's last token sees
-  int share;                                  // of them per split
-};
+// Pages that the token last_token of a chunk sees.
 __device__ __forceinline__ int tile_pages(int n, int end, int len, int last_token) {
   const int seen = max(end - len + last_token + 1, 0);
   return min(n, (seen + HK_PAGE - 1) / HK_PAGE);
 }
-__device__ __forceinline__ int split_share(int pages, int n_split) {
-  return max((pages + n_split - 1) / n_split, MIN_PAGES);
-}
 __device__ __forceinline__ float bias_of(int pages) { return (float)(32 - __clz(pages * HK_PAGE)) + CH_SLACK; }
 
-// Split states lie by workgroup: of the short kernel two each, of a tile kernel query r of item i (tile
-// and KV head) has tile_splits of them from (i * TM + r) * tile_splits on.
 struct Args {
   const char *q, *k_pool, *v_pool;
   const int32_t *table, *n_pages, *start;
@@ -345,19 +333,19 @@ struct Args {
   float *lse;
   float *short_o, *short_ml, *tile_o, *tile_ml;
   int32_t* short_first;                       // the short rows' first steps, their total, a workgroup's share
+  int32_t* tile_split;                        // the tiles' pieces: see TileSplit
   int Hq, Hkv, G, max_pages, num_pages, n_seq, n_tokens, max_len;
-  int tile_splits;
+  int n_tiles;                                // of a KV head, for the tile kernels
   float c2;
 };
 
-// One query's result of a tile kernel (lane: half of the dims): normalised into o, or the split's
-// state.  at: the query's first state.
+// One query's result of a tile kernel (lane: half of the dims): normalised into o, or state `at` of
+// its pieces (at < 0: there is one piece).
 template <typename T, int D>
-__device__ __forceinline__ void put_state(const Args& a, int64_t row, int64_t at, int split, const f32x16 (&acc)[D / 32],
+__device__ __forceinline__ void put_state(const Args& a, int64_t row, int64_t at, const f32x16 (&acc)[D / 32],
                                           float mb, float l) {
   const int hi = (threadIdx.x & 63) >> 5;
-  if (a.tile_splits > 1) {
-    at += split;
+  if (at >= 0) {
     float* to = a.tile_o + at * D;
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
@@ -380,155 +368,325 @@ __device__ __forceinline__ void put_state(const Args& a, int64_t row, int64_t at
 }
 
 // ------------------------------------------------------------------ tile kernels
-constexpr int TILE_PAGES = 4, TILE_KEYS = TILE_PAGES * HK_PAGE;
+constexpr int TILE_ROWS = 128, TILE_PAGES = 4, TILE_KEYS = TILE_PAGES * HK_PAGE;
 
-// Tiles of TM folded rows are numbered over the batch: a sequence's begin at tiles_before, which
+// Tiles of TILE_ROWS folded rows are numbered over the batch: a sequence's begin at tiles_before, which
 // leaves at most one of a sequence without rows.
-template <int TM>
 __device__ __forceinline__ int tiles_before(const Args& a, int s) {
-  return min(max(a.start[s], 0), a.n_tokens) * a.G / TM + s;
-}
-template <int TM>
-__device__ __forceinline__ int tile_sequence(const Args& a, int u) {
-  int s = 0;
-  for (int hi = a.n_seq; hi - s > 1;) {
-    const int mid = (s + hi) / 2;
-    if (tiles_before<TM>(a, mid) <= u) s = mid;
-    else hi = mid;
-  }
-  return s;
+  return min(max(a.start[s], 0), a.n_tokens) * a.G / TILE_ROWS + s;
 }
 
-// What a workgroup of a tile kernel works on: TM folded rows of one sequence and KV head, and a
-// range of its pages.  None: nothing (p1 < 0).
-struct TileWork {
+// TILE_ROWS folded rows of one sequence and KV head, and the pages of them that a workgroup takes.  No
+// steps: there are no such rows.
+struct Tile {
   Chunk c;
-  int item, kv, split, rows, r0, end, pages, p0, p1;
+  int kv, rows, r0, end, pages, steps, p0, p1;
   const int32_t* trow;
   const uint16_t* mrow;
 };
-template <int TM>
-__device__ __forceinline__ TileWork tile_work(const Args& a) {
-  TileWork w;
-  // the largest tiles of a sequence first: tile u of the launch counts down
-  const int u = (int)(gridDim.x / a.Hkv) - 1 - (int)(blockIdx.x / a.Hkv);
-  w.kv = blockIdx.x % a.Hkv;
-  w.item = u * a.Hkv + w.kv;
-  w.split = blockIdx.y;
-  w.p1 = -1;
-  const int s = tile_sequence<TM>(a, u);
+__device__ __forceinline__ Tile tile_of(const Args& a, int u, int kv) {
+  Tile w;
+  int s = 0;
+  for (int hi = a.n_seq; hi - s > 1;) {
+    const int mid = (s + hi) / 2;
+    if (tiles_before(a, mid) <= u) s = mid;
+    else hi = mid;
+  }
+  w.kv = kv;
   w.c = chunk_of(a.start, s, a.n_tokens, a.max_len);
   w.rows = w.c.len * a.G;
-  w.r0 = (u - tiles_before<TM>(a, s)) * TM;
+  w.r0 = (u - tiles_before(a, s)) * TILE_ROWS;
+  w.steps = 0;
   if (w.rows <= SHORT_ROWS || w.r0 < 0 || w.r0 >= w.rows) return w;
-  const int h = s * a.Hkv + w.kv, n = min(max(a.n_pages[h], 0), a.max_pages);
+  const int h = s * a.Hkv + kv, n = min(max(a.n_pages[h], 0), a.max_pages);
   w.trow = a.table + (size_t)h * a.max_pages;
   w.mrow = a.masks + (size_t)h * a.max_pages;
   w.end = row_end(n, n > 0 ? w.mrow[n - 1] : 0u);
-  w.pages = tile_pages(n, w.end, w.c.len, (min(w.r0 + TM, w.rows) - 1) / a.G);
-  const int share = split_share(w.pages, a.tile_splits);
-  w.p0 = w.split * share;
-  w.p1 = w.split > 0 && w.p0 >= w.pages ? -1 : min(w.p0 + share, w.pages);
+  w.pages = tile_pages(n, w.end, w.c.len, (min(w.r0 + TILE_ROWS, w.rows) - 1) / a.G);
+  w.steps = max((w.pages + TILE_PAGES - 1) / TILE_PAGES, 1);     // (rows without pages have empty results to write)
+  w.p0 = 0;
+  w.p1 = w.pages;
   return w;
 }
 
+// A launch of many tiles has a workgroup for each, the largest of a sequence first.  One of few
+// (PLANNED) has at most TILE_WG workgroups, which see from the rows' lengths into how many pieces to
+// split the tiles: pieces of one length, that of the longest tile over one of SPLITS, so that the
+// pieces of a KV head's tiles that run beside one another read the same pages.
+constexpr int TILE_WG = 512, PLAN_TILES = 1024, PLAN_PIECES = 1536;
+constexpr int SPLITS[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}, N_SPLITS = sizeof(SPLITS) / sizeof(SPLITS[0]);
+constexpr int MAX_STATES = 64;                // pieces of a row at most
+// What a piece costs beside its steps, in steps of its type: its start, or that and its state's way to
+// the merge; and what a step costs where a CU has one workgroup, in tenths of one where it has two.
+template <typename T>
+struct Cost;
+template <>
+struct Cost<uint16_t> {
+  static constexpr int START = 7, STATE = 18, ALONE = 7;
+};
+template <>
+struct Cost<float> {
+  static constexpr int START = 2, STATE = 4, ALONE = 5;
+};
+
+struct TileSplit {                            // for the merge, by tile: its pieces and its rows
+  int32_t at, used, first, rows, r0, kv;
+};
+
+template <int NT>
+struct Planned {
+  int first[PLAN_TILES + 1];                  // piece that a tile begins at
+  int sum[NT / 64], most[NT / 64];
+  int pieces[N_SPLITS][NT / 64], whole[N_SPLITS][NT / 64];
+};
+// Counts the pieces of all tiles (into s.first); returns their length in steps.
+template <typename T, int NT>
+__device__ __forceinline__ int plan_tiles(const Args& a, Planned<NT>& s) {
+  const int n = a.n_tiles * a.Hkv, per = (n + NT - 1) / NT, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int MOST = (PLAN_TILES + NT - 1) / NT;
+  auto add = [](uint32_t p, uint32_t q) { return p + q; };
+  int k[MOST], sum = 0, most = 0;
+#pragma unroll
+  for (int j = 0; j < MOST; ++j) {
+    const int i = threadIdx.x * per + j;
+    k[j] = j < per && i < n ? tile_of(a, i % a.n_tiles, i / a.n_tiles).steps : 0;
+    sum += k[j];
+    most = max(most, k[j]);
+  }
+  sum = (int)wave_reduce_u32((uint32_t)sum, 0u, add);
+  most = (int)wave_reduce_u32((uint32_t)most, 0u, [](uint32_t p, uint32_t q) { return p > q ? p : q; });
+  if (lane == 63) {
+    s.sum[wave] = sum;
+    s.most[wave] = most;
+  }
+  __syncthreads();
+  sum = 0;
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) {
+    sum += s.sum[w];
+    most = max(most, s.most[w]);
+  }
+  most = max(most, 1);
+#pragma unroll
+  for (int c = 0; c < N_SPLITS; ++c) {
+    const uint32_t len = (uint32_t)(most + SPLITS[c] - 1) / SPLITS[c];
+    uint32_t pieces = 0, whole = 0;
+#pragma unroll
+    for (int j = 0; j < MOST; ++j)
+      if (j < per) {
+        const uint32_t x = (uint32_t)k[j] / len, rest = (uint32_t)k[j] - x * len;
+        whole += x + (rest > len - len / 8);
+        pieces += x + (rest > 0);
+      }
+    pieces = wave_reduce_u32(pieces, 0u, add);
+    whole = wave_reduce_u32(whole, 0u, add);
+    if (lane == 63) {
+      s.pieces[c][wave] = (int)pieces;
+      s.whole[c][wave] = (int)whole;
+    }
+  }
+  __syncthreads();
+  // the cheapest, in tenths of a step: rounds of (nearly) whole pieces, or an even share of all steps,
+  // and a quarter piece of unevenness where not all pieces run at once
+  int best = 0x7fffffff, length = most;
+#pragma unroll
+  for (int c = 0; c < N_SPLITS; ++c) {
+    const int len = (most + SPLITS[c] - 1) / SPLITS[c];
+    int pieces = 0, whole = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+      pieces += s.pieces[c][w];
+      whole += s.whole[c][w];
+    }
+    const int extra = c ? Cost<T>::STATE : Cost<T>::START, rest = whole % TILE_WG;
+    const int last = rest == 0 ? 0 : Cost<T>::ALONE + (10 - Cost<T>::ALONE) * max(rest - TILE_WG / 2, 0) / (TILE_WG / 2);
+    const int cost = max((whole / TILE_WG * 10 + last) * (len + extra), (sum + extra * pieces) / (TILE_WG / 10) + (pieces > TILE_WG ? len * 10 / 4 : 0));
+    if (cost < best && (c == 0 || pieces <= PLAN_PIECES)) {
+      best = cost;
+      length = len;
+    }
+  }
+  int x = 0;
+#pragma unroll
+  for (int j = 0; j < MOST; ++j) {
+    k[j] = (k[j] + length - 1) / length;
+    x += k[j];
+  }
+  int before = -x;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o, 64);
+    if (lane >= o) x += y;
+  }
+  if (lane == 63) s.sum[wave] = x;
+  __syncthreads();
+  before += x;
+  int total = 0;
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) {
+    if (w < wave) before += s.sum[w];
+    total += s.sum[w];
+  }
+#pragma unroll
+  for (int j = 0; j < MOST; ++j) {
+    const int i = threadIdx.x * per + j;
+    if (j < per && i < n) s.first[i] = before;
+    before += k[j];
+  }
+  if (threadIdx.x == 0) s.first[n] = total;
+  __syncthreads();
+  if (blockIdx.x == gridDim.x - 1)            // (often without a piece)
+    for (int i = threadIdx.x; i < n; i += NT) {
+      const Tile w = tile_of(a, i % a.n_tiles, i / a.n_tiles);
+      reinterpret_cast<TileSplit*>(a.tile_split)[i] = {s.first[i], s.first[i + 1] - s.first[i], w.c.first, w.rows, w.r0, w.kv};
+    }
+  return length;
+}
+
+// The pieces of a workgroup.  next(): the next one, or false.
+template <typename T, int NT, bool PLANNED>
+struct Pieces {
+  const Args& a;
+  Planned<NT>& s;
+  int x, stop, stride, length;
+  int64_t state;                              // of the piece's first row; -1: the piece is all of its tile
+  __device__ __forceinline__ Pieces(const Args& args, Planned<NT>& lds) : a(args), s(lds), state(-1) {
+    x = 0;
+    if (PLANNED) {
+      length = __builtin_amdgcn_readfirstlane(plan_tiles<T, NT>(a, s));
+      const int total = __builtin_amdgcn_readfirstlane(s.first[a.n_tiles * a.Hkv]);
+      // the workgroups of a die (every eighth) share an eighth of the pieces that lie behind one another
+      const int b = blockIdx.x, dies = gridDim.x % 8 ? 1 : 8;
+      x = total * (b % dies) / dies + b / dies;
+      stop = total * (b % dies + 1) / dies;
+      stride = gridDim.x / dies;
+    }
+  }
+  __device__ __forceinline__ bool next(Tile& w) {
+    if (!PLANNED) {
+      if (x++) return false;
+      w = tile_of(a, a.n_tiles - 1 - (int)(blockIdx.x / a.Hkv), blockIdx.x % a.Hkv);
+      return w.steps > 0;
+    }
+    if (x >= stop) return false;
+    int i = 0;                                // the last tile that begins at or before x
+    for (int hi = a.n_tiles * a.Hkv; hi - i > 1;) {
+      const int mid = (i + hi) / 2;
+      if (s.first[mid] <= x) i = mid;
+      else hi = mid;
+    }
+    i = __builtin_amdgcn_readfirstlane(i);
+    const int split = x - __builtin_amdgcn_readfirstlane(s.first[i]);
+    w = tile_of(a, i % a.n_tiles, i / a.n_tiles);
+    state = w.steps > length ? (int64_t)x * TILE_ROWS : -1;
+    w.p0 = __builtin_amdgcn_readfirstlane(split * length * TILE_PAGES);
+    w.p1 = __builtin_amdgcn_readfirstlane(min(w.p0 + length * TILE_PAGES, w.pages));
+    x += stride;
+    return true;
+  }
+};
+
 // fp32: a wave takes 32 rows; the next tile's pages load while a tile is computed.  Bound by the
 // fp32 matrix rate, which is a sixteenth of bf16's.
-template <int D, int NW>
-__global__ __launch_bounds__(64 * NW, 1) void chunk_tile_f32_kernel(Args a) {
+template <int D, bool PLANNED>
+__global__ __launch_bounds__(256, D == 64 ? 2 : 1) void chunk_tile_f32_kernel(Args a) {
   using L = TileLayout<float, D>;
   using M = Mma<float, D>;
-  constexpr int TP = TILE_PAGES, PPW = 2 * TP / NW;               // pages that a wave brings
+  constexpr int NW = 4, TP = TILE_PAGES, PPW = 2 * TP / NW;               // pages that a wave brings
   __shared__ __align__(16) char s_k[2][TILE_KEYS * L::K_ROW], s_v[2][TILE_KEYS * L::V_ROW];
   __shared__ __align__(8) uint16_t s_mask[2][TP], s_odd[2][TP];
+  __shared__ Planned<256> s_plan;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const TileWork w = tile_work<32 * NW>(a);
-  if (w.p1 < 0) return;
-  // rows past the chunk repeat its last one; they are not stored
-  const int w0 = w.r0 + wave * 32, off = w.end - w.c.len + 1;
-  const int r = min(w0 + (lane & 31), w.rows - 1), tok = r / a.G, g = r - tok * a.G;
-  const int64_t row = (int64_t)(w.c.first + tok) * a.Hq + w.kv * a.G + g;
-  const int seen = off + tok;                                    // keys before this one are seen by the lane's query,
-  const int seen_all = off + min(w0, w.rows - 1) / a.G;          // by every query of the wave,
-  const int tile_seen = off + w.r0 / a.G;                        // of the workgroup
-  typename M::Query q[1];
-  M::load_q(q[0], reinterpret_cast<const float*>(a.q) + (int64_t)(w.c.first + tok) * a.q_row + (w.kv * a.G + g) * D);
-  const float bias = bias_of(w.pages);
-  State<float, D, 1> st;
-  st.init();
-  const int tiles = w.p1 > w.p0 ? (w.p1 - w.p0 + TP - 1) / TP : 0;
-  PageRegs<float, D> rp[PPW];
-  int id[PPW];
-  uint32_t mask[PPW], next_mask[PPW];
-  auto load_id = [&](int t) {
+  Pieces<float, 256, PLANNED> pieces(a, s_plan);
+  for (Tile w; pieces.next(w);) {
+    if (PLANNED) __syncthreads();                                   // (the last piece's tiles are read)
+    // rows past the chunk repeat its last one; they are not stored
+    const int w0 = w.r0 + wave * 32, off = w.end - w.c.len + 1;
+    const int r = min(w0 + (lane & 31), w.rows - 1), tok = r / a.G, g = r - tok * a.G;
+    const int64_t row = (int64_t)(w.c.first + tok) * a.Hq + w.kv * a.G + g;
+    const int seen = off + tok;                                  // keys before this one are seen by the lane's query,
+    const int seen_all = off + min(w0, w.rows - 1) / a.G;        // by every query of the wave,
+    const int tile_seen = off + w.r0 / a.G;                      // of the workgroup
+    typename M::Query q[1];
+    M::load_q(q[0], reinterpret_cast<const float*>(a.q) + (int64_t)(w.c.first + tok) * a.q_row + (w.kv * a.G + g) * D);
+    const float bias = bias_of(w.pages);
+    State<float, D, 1> st;
+    st.init();
+    const int tiles = w.p1 > w.p0 ? (w.p1 - w.p0 + TP - 1) / TP : 0;
+    PageRegs<float, D> rp[PPW];
+    int id[PPW];
+    uint32_t mask[PPW], next_mask[PPW];
+    auto load_id = [&](int t) {
 #pragma unroll
-    for (int i = 0; i < PPW; ++i) {
-      const int p = w.p0 + t * TP + (wave * PPW + i) % TP;
-      next_mask[i] = p < w.p1 ? w.mrow[p] : 0u;
-      id[i] = w.trow[min(p, w.p1 - 1)];
-    }
-  };
-  auto load = [&] {
-#pragma unroll
-    for (int i = 0; i < PPW; ++i) {
-      mask[i] = next_mask[i];
-      rp[i].load((wave * PPW + i) / TP ? a.v_pool : a.k_pool, min(max(id[i], 0), a.num_pages - 1));
-    }
-  };
-  auto row_at = [&](int p) {                                     // V row of key k of the 32 from page p on
-    return [&, p](int k) {
-      const int at = min(max(w.trow[min(p + k / HK_PAGE, w.p1 - 1)], 0), a.num_pages - 1);
-      return reinterpret_cast<const float*>(a.v_pool) + ((size_t)at * HK_PAGE + k % HK_PAGE) * D;
+      for (int i = 0; i < PPW; ++i) {
+        const int p = w.p0 + t * TP + (wave * PPW + i) % TP;
+        next_mask[i] = p < w.p1 ? w.mrow[p] : 0u;
+        id[i] = w.trow[min(p, w.p1 - 1)];
+      }
     };
-  };
-  if (tiles > 0) {
-    load_id(0);
-    load();
-    load_id(1);
-  }
-  for (int t = 0; t < tiles; ++t) {
-    const int p = w.p0 + t * TP, buf = t & 1;
+    auto load = [&] {
 #pragma unroll
-    for (int i = 0; i < PPW; ++i) {
-      const int my = (wave * PPW + i) % TP, is_v = (wave * PPW + i) / TP;
-      if (is_v) {
-        uint32_t keep = mask[i], odd = 0;
-        if ((p + my + 1) * HK_PAGE > tile_seen) {
-          odd = rp[i].odd_rows() & keep;
-          keep &= ~odd;
-        }
-        if (keep != 0xffffu) rp[i].clear(keep);
-        if (lane == 0) {
-          s_mask[buf][my] = (uint16_t)mask[i];
-          s_odd[buf][my] = (uint16_t)odd;
-        }
+      for (int i = 0; i < PPW; ++i) {
+        mask[i] = next_mask[i];
+        rp[i].load((wave * PPW + i) / TP ? a.v_pool : a.k_pool, min(max(id[i], 0), a.num_pages - 1));
       }
-      if (is_v) rp[i].store(s_v[buf] + my * HK_PAGE * L::V_ROW, L::V_ROW);
-      else rp[i].store(s_k[buf] + my * HK_PAGE * L::K_ROW, L::K_ROW);
-    }
-    __syncthreads();
-    if (t + 1 < tiles) {
+    };
+    auto row_at = [&](int p) {                                   // V row of key k of the 32 from page p on
+      return [&, p](int k) {
+        const int at = min(max(w.trow[min(p + k / HK_PAGE, w.p1 - 1)], 0), a.num_pages - 1);
+        return reinterpret_cast<const float*>(a.v_pool) + ((size_t)at * HK_PAGE + k % HK_PAGE) * D;
+      };
+    };
+    if (tiles > 0) {
+      load_id(0);
       load();
-      load_id(t + 2);
+      load_id(1);
     }
-    if (w0 < w.rows) {
-      const uint64_t m64 = *reinterpret_cast<const uint64_t*>(s_mask[buf]);
-      const uint64_t o64 = *reinterpret_cast<const uint64_t*>(s_odd[buf]);
+    for (int t = 0; t < tiles; ++t) {
+      const int p = w.p0 + t * TP, buf = t & 1;
 #pragma unroll
-      for (int hb = 0; hb < TILE_KEYS / 32; ++hb) {
-        const int key = (p + 2 * hb) * HK_PAGE;
-        const uint32_t valid = __builtin_amdgcn_readfirstlane((uint32_t)(m64 >> (32 * hb)));
-        const uint32_t odd = __builtin_amdgcn_readfirstlane((uint32_t)(o64 >> (32 * hb)));
-        const bool all = valid == 0xffffffffu && key + 32 <= seen_all;
-        const int k = seen - key;
-        const uint32_t vis[1] = {valid & (k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u)};
-        st.block(q, s_k[buf] + hb * 32 * L::K_ROW, s_v[buf] + hb * 32 * L::V_ROW, vis, all, a.c2, bias, odd,
-                 row_at(p + 2 * hb));
+      for (int i = 0; i < PPW; ++i) {
+        const int my = (wave * PPW + i) % TP, is_v = (wave * PPW + i) / TP;
+        if (is_v) {
+          uint32_t keep = mask[i], odd = 0;
+          if ((p + my + 1) * HK_PAGE > tile_seen) {
+            odd = rp[i].odd_rows() & keep;
+            keep &= ~odd;
+          }
+          if (keep != 0xffffu) rp[i].clear(keep);
+          if (lane == 0) {
+            s_mask[buf][my] = (uint16_t)mask[i];
+            s_odd[buf][my] = (uint16_t)odd;
+          }
+        }
+        if (is_v) rp[i].store(s_v[buf] + my * HK_PAGE * L::V_ROW, L::V_ROW);
+        else rp[i].store(s_k[buf] + my * HK_PAGE * L::K_ROW, L::K_ROW);
+      }
+      __syncthreads();
+      if (t + 1 < tiles) {
+        load();
+        load_id(t + 2);
+      }
+      if (w0 < w.rows) {
+        const uint64_t m64 = *reinterpret_cast<const uint64_t*>(s_mask[buf]);
+        const uint64_t o64 = *reinterpret_cast<const uint64_t*>(s_odd[buf]);
+#pragma unroll
+        for (int hb = 0; hb < TILE_KEYS / 32; ++hb) {
+          const int key = (p + 2 * hb) * HK_PAGE;
+          const uint32_t valid = __builtin_amdgcn_readfirstlane((uint32_t)(m64 >> (32 * hb)));
+          const uint32_t odd = __builtin_amdgcn_readfirstlane((uint32_t)(o64 >> (32 * hb)));
+          const bool all = valid == 0xffffffffu && key + 32 <= seen_all;
+          const int k = seen - key;
+          const uint32_t vis[1] = {valid & (k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u)};
+          st.block(q, s_k[buf] + hb * 32 * L::K_ROW, s_v[buf] + hb * 32 * L::V_ROW, vis, all, a.c2, bias, odd,
+                   row_at(p + 2 * hb));
+        }
       }
     }
+    const float l = st.l[0] + __shfl_xor(st.l[0], 32, 64);
+    if (w0 + (lane & 31) < w.rows)
+      put_state<float, D>(a, row, pieces.state < 0 ? -1 : pieces.state + r - w.r0, st.acc[0], st.mb[0], l);
   }
-  const float l = st.l[0] + __shfl_xor(st.l[0], 32, 64);
-  if (w0 + (lane & 31) < w.rows) put_state<float, D>(a, row, ((int64_t)w.item * 32 * NW + r - w.r0) * a.tile_splits, w.split, st.acc[0], st.mb[0], l);
 }
 
 // LDS tiles of the bf16 kernel: filled straight from memory, 1 KB an instruction, 16 bytes a lane in
@@ -539,7 +697,7 @@ __global__ __launch_bounds__(64 * NW, 1) void chunk_tile_f32_kernel(Args a) {
 // every fragment's offset is a constant.
 template <int D>
 struct DirectTile {
-  static constexpr int ROWS = 512 / D, GROUP = D == 128 ? 1040 : 1056, HALF = 32 / ROWS * GROUP, BYTES = 2 * HALF;
+  static constexpr int ROWS = 512 / D, GROUP = D == 128 ? 1040 : 1056, BYTES = 32 / ROWS * GROUP;
   static constexpr int LOADS = HK_PAGE / ROWS, QUARTER = ROWS * 64;
   // the row within a group and the byte within the row that a lane fetches
   __device__ static __forceinline__ int row(int lane) { return (lane >> 2) & (ROWS - 1); }
@@ -562,287 +720,316 @@ struct DirectTile {
 };
 static __device__ const u32x4 zero_row[1] = {};
 
-// 1 KB from memory to LDS: lane l's 16 bytes at `from` to `to` + 16 l.  It is on its way afterwards; the
-// wave waits by direct_wait.
+// 1 KB from memory to LDS: lane l's 16 bytes at `from` (+ `at`) to `to` + 16 l.  It is on its way
+// afterwards; direct_wait waits until `later` such loads or fewer are.
 __device__ __forceinline__ void direct_load(const char* from, uint32_t to) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "m0", "memory");
 }
-__device__ __forceinline__ void direct_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void direct_load(const char* from, uint32_t at, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(at), "s"(from), "s"(to) : "m0", "memory");
+}
+template <int later>
+__device__ __forceinline__ void direct_wait() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(later) : "memory"); }
 
-// bf16.  Eight waves, two a SIMD, take 32 rows each against tiles of 64 keys.  A wave's steps of 32
-// keys are a pipeline: the scores of the next block run beside the exponentials of this one, its
-// P V beside the next one's maximum; MFMAs and the vector work between them are laid out by hand.
-// Three tiles in LDS: one is computed, the next has arrived, the one after is on its way.
-template <int D>
-__global__ __launch_bounds__(512, 2) void chunk_tile_bf16_kernel(Args a) {
+// bf16.  Four waves take 32 rows each against tiles of 32 keys.  A wave's tiles are a pipeline: the
+// scores of the next tile run beside the exponentials of this one, its P V beside the next one's
+// maximum; MFMAs and the vector work between them are laid out by hand.  Two workgroups a CU, for
+// one's start, end and waits to be beside the other's work (measured against one of eight waves and
+// tiles of 64 keys, 8 prompts of 4096 tokens, 32 / 8 heads: D 128 1152 us and 1172, D 64 697 and 786).
+// Waves 0 and 1 bring a page of K each, three tiles ahead of the wait for it, waves 2 and 3 the pages
+// of V.
+template <int D, bool PLANNED>
+__global__ __launch_bounds__(256, 2) void chunk_tile_bf16_kernel(Args a) {
   using L = DirectTile<D>;
   using M = Mma<uint16_t, D>;
-  constexpr int TP = TILE_PAGES, KS = D / 16, DT = D / 32, VS = 2 * DT, AHEAD = 3;
+  constexpr int KS = D / 16, DT = D / 32, VS = 2 * DT, AHEAD = 4;
   constexpr int PAGE = HK_PAGE * D * 2, PAGE_LDS = HK_PAGE / L::ROWS * L::GROUP;
-  __shared__ __align__(16) char s_k[3][L::BYTES], s_v[3][L::BYTES];
-  __shared__ __align__(16) uint32_t s_flag[3][TP];               // mask | odd rows << 16 of a tile's pages
+  constexpr int NK = 4, NV = 5;                                  // tiles in LDS
+  __shared__ __align__(16) char s_k[NK][L::BYTES], s_v[NV][L::BYTES];
+  __shared__ uint32_t s_odd[NV][2];                              // odd rows of a tile's pages
   const int lane = threadIdx.x & 63, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // (conditions on it are scalar)
-  const TileWork w = tile_work<256>(a);
-  if (w.p1 < 0) return;
-  // rows past the chunk repeat its last one; they are not stored
-  const int w0 = w.r0 + wave * 32, off = w.end - w.c.len + 1;
-  const int r = min(w0 + (lane & 31), w.rows - 1), tok = r / a.G, g = r - tok * a.G;
-  const int64_t row = (int64_t)(w.c.first + tok) * a.Hq + w.kv * a.G + g;
-  const int seen = off + tok;                                    // keys before this one are seen by the lane's query,
-  const int seen_all = off + min(w0, w.rows - 1) / a.G;          // by every query of the wave,
-  const int tile_seen = off + w.r0 / a.G;                        // of the workgroup
-  typename M::Query q;
-  M::load_q(q, reinterpret_cast<const uint16_t*>(a.q) + (int64_t)(w.c.first + tok) * a.q_row + (w.kv * a.G + g) * D);
-  const float bias = bias_of(w.pages), c2 = a.c2;
-  const int tiles = w.p1 > w.p0 ? (w.p1 - w.p0 + TP - 1) / TP : 0;
+  __shared__ Planned<256> s_plan;
+  Pieces<uint16_t, 256, PLANNED> pieces(a, s_plan);
+  for (Tile w; pieces.next(w);) {
+    if (PLANNED) __syncthreads();                                   // (the last piece's tiles are read)
+    // rows past the chunk repeat its last one; they are not stored
+    const int w0 = w.r0 + wave * 32, off = w.end - w.c.len + 1;
+    const int r = min(w0 + (lane & 31), w.rows - 1), tok = r / a.G, g = r - tok * a.G;
+    const int64_t row = (int64_t)(w.c.first + tok) * a.Hq + w.kv * a.G + g;
+    const int seen = off + tok;                                  // keys before this one are seen by the lane's query,
+    const int seen_all = off + min(w0, w.rows - 1) / a.G;        // by every query of the wave,
+    const int tile_seen = off + w.r0 / a.G;                      // of the workgroup
+    typename M::Query q;
+    M::load_q(q, reinterpret_cast<const uint16_t*>(a.q) + (int64_t)(w.c.first + tok) * a.q_row + (w.kv * a.G + g) * D);
+    const float bias = bias_of(w.pages), c2 = a.c2;
+    const int tiles = w.p1 > w.p0 ? (w.p1 - w.p0 + 1) / 2 : 0;
 
-  // Waves 0 to 3 bring a page of K each, waves 4 to 7 the same pages of V.  A page's id and mask are
-  // loaded a tile before the page is requested.  V rows that are not valid are fetched as zeros.
-  const int my = wave & 3;
-  const bool is_v = wave >= 4;
-  const char* pool = (is_v ? a.v_pool : a.k_pool) + L::row(lane) * (D * 2) + L::byte(lane);
-  int id = 0;
-  uint32_t mask = 0, next_mask = 0;                              // of the page on its way, and of the next
-  auto load_id = [&](int t) {
-    const int p = w.p0 + t * TP + my;
-    int at = min(p, w.p1 - 1);
-    asm volatile("" : "+v"(at));                                 // (a vector load: a scalar one's wait is for LDS too)
-    next_mask = p < w.p1 ? w.mrow[at] : 0u;
-    id = w.trow[at];
-  };
-  auto request = [&](int buf) {
-    mask = __builtin_amdgcn_readfirstlane(next_mask);
-    const char* from = pool + (size_t)min(max(__builtin_amdgcn_readfirstlane(id), 0), a.num_pages - 1) * PAGE;
-    uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(is_v ? s_v[buf] : s_k[buf]) + my * PAGE_LDS;
-    to = __builtin_amdgcn_readfirstlane(to);
-    if (is_v && mask != 0xffffu) {
+    // At the middle of tile t a wave has the pages up to K of t + 4 or V of t + 3 requested, and the
+    // slots of K of t + 1 and V of t - 1 are read by all: K of t + 5 and V of t + 4 take them.  Ids and
+    // masks come 64 tiles at a time: lane i holds tile i's masks, and the id of K's page of tile i or
+    // V's of tile i - 1.  V rows that are not valid are fetched as zeros.
+    constexpr int LEAD = 5;
+    const int my = wave & 1, is_v = wave >> 1;
+    const char* pool = is_v ? a.v_pool : a.k_pool;
+    const uint32_t lane_at = L::row(lane) * (D * 2) + L::byte(lane);
+    int ids, next_ids;
+    uint32_t masks, next_masks;
+    auto load_ids = [&](int t) {
+      const int p = w.p0 + 2 * (t + lane);
+      next_masks = (p < w.p1 ? w.mrow[p] : 0u) | (p + 1 < w.p1 ? (uint32_t)w.mrow[p + 1] << 16 : 0u);
+      next_ids = min(max(w.trow[min(max(p - 2 * is_v + my, w.p0), w.p1 - 1)], 0), a.num_pages - 1);
+    };
+    auto request = [&](int id, uint32_t mask, uint32_t to) {     // mask: of the page's rows
+      const char* from = pool + (size_t)(uint32_t)id * PAGE;
+      to += my * PAGE_LDS;
+      if (is_v && mask != 0xffffu) {
 #pragma unroll
-      for (int j = 0; j < L::LOADS; ++j) {
-        const bool valid = (mask >> (j * L::ROWS + L::row(lane))) & 1u;
-        direct_load(valid ? from + j * 1024 : reinterpret_cast<const char*>(zero_row), to + j * L::GROUP);
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < L::LOADS; ++j) direct_load(from + j * 1024, to + j * L::GROUP);
-    }
-  };
-  // The page of tile t is in LDS: its flags; rows of V that hold infinite values and are not seen by
-  // every query of the tile become zeros.
-  auto settle = [&](int t, int buf) {
-    direct_wait();
-    if (!is_v) return;
-    uint32_t odd = 0;
-    if (mask != 0 && (w.p0 + t * TP + my + 1) * HK_PAGE > tile_seen) {
-      char* at = s_v[buf] + my * PAGE_LDS + lane * 16;
-#pragma unroll
-      for (int j = 0; j < L::LOADS; ++j) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(at + j * L::GROUP);
-        bool bad = false;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) bad |= (x[k] & 0x7f800000u) == 0x7f800000u || (x[k] & 0x7f80u) == 0x7f80u;
-        if (__any(bad))
-          for (int r = 0; r < L::ROWS; ++r)
-            if (__any(bad && L::row(lane) == r)) {
-              odd |= 1u << (j * L::ROWS + r);
-              if (L::row(lane) == r) *reinterpret_cast<u32x4*>(at + j * L::GROUP) = u32x4{0u, 0u, 0u, 0u};
-            }
-      }
-    }
-    if (lane == 0) s_flag[buf][my] = mask | odd << 16;
-  };
-
-  f32x16 acc[DT];
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) acc[dt][e] = 0.f;
-  float m = -INFINITY, mb = 0.f, l = 0.f;
-
-  const int k_at = L::k_lane(lane), v_at = L::v_lane(lane);      // the lane's fragments within 32 keys
-  auto k_frag = [&](const char* k, int s) {
-    return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(k + k_at + L::k_step(s)));
-  };
-  auto v_frag = [&](const char* v, int i) {                      // i = s * DT + dt
-    s16x4 x[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const char* at = v + v_at + L::v_step(i / DT, h, i % DT);
-      x[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (__attribute__((address_space(3))) s16x4*)(uintptr_t)(__attribute__((address_space(3))) const char*)at);
-    }
-    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
-  };
-  bf16x8 kf[AHEAD], vf[AHEAD];
-  uint32_t bp[8];                                                // P of 32 keys, two a word
-  f32x16 z[2];
-  auto first_k = [&](const char* k) {
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i) kf[i] = k_frag(k, i);
-  };
-  // scores of the block at k into zn, beside the probabilities of zc (into bp; the block at v is zc's).
-  // The empty asm statements keep what is computed beside an MFMA in its place.
-  auto scores = [&](f32x16& zn, const f32x16& zc, const char* k, const char* v) {
-    float sum[2] = {0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < KS; ++i) {
-      zn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % AHEAD], q.f[i], i ? zn : f32x16{}, 0, 0, 0);
-      if (i + AHEAD < KS) kf[i % AHEAD] = k_frag(k, i + AHEAD);
-      else vf[i + AHEAD - KS] = v_frag(v, i + AHEAD - KS);
-#pragma unroll
-      for (int e = i * 16 / KS; e < (i + 1) * 16 / KS; e += 2) {
-        const float x = fast_exp2(fmaf(zc[e], c2, -mb)), y = fast_exp2(fmaf(zc[e + 1], c2, -mb));
-        sum[0] += x;
-        sum[1] += y;
-        bp[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x, y}), bf16x2));
-        asm volatile("" : "+v"(bp[e / 2]), "+v"(sum[0]), "+v"(sum[1]));
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    l += sum[0] + sum[1];
-  };
-  // acc += P V of the block at v, beside the maximum of zn, which it returns; the first fragments of
-  // the scores after these come from k
-  auto values = [&](const f32x16& zn, const char* v, const char* k) {
-    float zm = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < VS; ++i) {
-      const int s = 4 * (i / DT);
-      const bf16x8 b = __builtin_bit_cast(bf16x8, (u32x4{bp[s], bp[s + 1], bp[s + 2], bp[s + 3]}));
-      acc[i % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % AHEAD], b, acc[i % DT], 0, 0, 0);
-      if (i + AHEAD < VS) vf[i % AHEAD] = v_frag(v, i + AHEAD);
-      else kf[i + AHEAD - VS] = k_frag(k, i + AHEAD - VS);
-#pragma unroll
-      for (int e = i * 16 / VS; e < (i + 1) * 16 / VS; e += 2) {
-        zm = fmaxf(fmaxf(zm, zn[e]), zn[e + 1]);
-        asm volatile("" : "+v"(zm));
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    return zm;
-  };
-  // keys of the 32 from page p on that the lane's query does not see: -inf
-  auto hide = [&](f32x16& zn, int p, uint32_t valid) {
-    const int key = p * HK_PAGE;
-    if (valid == 0xffffffffu && key + 32 <= seen_all) return;
-    const int k = seen - key;
-    uint32_t x = (valid & (k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u)) >> (4 * hi);
-    asm volatile("" : "+v"(x));                                  // (a branch, not selects in every block)
-#pragma unroll
-    for (int e = 0; e < 16; ++e)
-      if (!((x >> ((e & 3) + 8 * (e >> 2))) & 1u)) zn[e] = -INFINITY;
-  };
-  // a new reference where a score has outgrown it
-  auto refer = [&](float zm) {
-    zm *= c2;
-    if (__any(zm > m + CH_SLACK)) {
-      zm = fmaxf(zm, __shfl_xor(zm, 32, 64));
-      const float mn = fmaxf(m, ceilf(zm));
-      const float alpha = m == -INFINITY ? 0.f : fast_exp2(m - mn);
-      m = mn;
-      mb = mn == -INFINITY ? 0.f : mn + bias;
-      l *= alpha;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) acc[dt][e] *= alpha;
-    }
-  };
-  // rows of V with infinite values that not every query of the tile sees (zeros in LDS)
-  auto add_odd = [&](uint32_t odd, int p, uint32_t valid) {
-    while (odd) {
-      const int key = __builtin_ctz(odd), reg = (key & 3) + 4 * (key >> 3);
-      odd &= odd - 1;
-      const int at = min(max(w.trow[min(p + key / HK_PAGE, w.p1 - 1)], 0), a.num_pages - 1);
-      const uint16_t* vr = reinterpret_cast<const uint16_t*>(a.v_pool) + ((size_t)at * HK_PAGE + key % HK_PAGE) * D;
-      uint32_t two = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) two = reg / 2 == e ? bp[e] : two;
-      asm volatile("" : "+v"(two));
-      float pr = __uint_as_float(reg & 1 ? two & 0xffff0000u : two << 16);
-      pr = __shfl(pr, (lane & 31) + 32 * ((key >> 2) & 1), 64);
-      const bool sees = ((valid >> key) & 1u) && p * HK_PAGE + key < seen;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float x = M::value(vr[32 * dt + (e & 3) + 8 * (e >> 2) + 4 * hi]);
-          acc[dt][e] = sees ? fmaf(pr, x, acc[dt][e]) : acc[dt][e];
+        for (int j = 0; j < L::LOADS; ++j) {
+          const bool valid = (mask >> (j * L::ROWS + L::row(lane))) & 1u;
+          direct_load(valid ? from + j * 1024 + lane_at : reinterpret_cast<const char*>(zero_row), to + j * L::GROUP);
         }
-    }
-  };
-  uint64_t valid = 0, odd = 0;                                   // of the tile's 64 keys
-  auto flags = [&](int buf) {
-    const u32x4 f = *reinterpret_cast<const u32x4*>(s_flag[buf]);
-    uint32_t x[TP];
+      } else {
 #pragma unroll
-    for (int i = 0; i < TP; ++i) x[i] = __builtin_amdgcn_readfirstlane(f[i]);
-    valid = (uint64_t)((x[3] << 16) | (x[2] & 0xffffu)) << 32 | ((x[1] << 16) | (x[0] & 0xffffu));
-    odd = (uint64_t)((x[3] & 0xffff0000u) | (x[2] >> 16)) << 32 | ((x[1] & 0xffff0000u) | (x[0] >> 16));
-  };
+        for (int j = 0; j < L::LOADS; ++j) direct_load(from + j * 1024, lane_at, to + j * L::GROUP);
+      }
+    };
+    // V's page of tile t is in LDS: rows that hold infinite values and are not seen by every query of
+    // the workgroup become zeros.
+    auto settle = [&](int t, uint32_t mask, int slot) {
+      uint32_t odd = 0;
+      if (mask != 0) {
+        char* at = s_v[slot] + my * PAGE_LDS + lane * 16;
+#pragma unroll
+        for (int j = 0; j < L::LOADS; ++j) {
+          const u32x4 x = *reinterpret_cast<const u32x4*>(at + j * L::GROUP);
+          bool bad = false;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) bad |= (x[k] & 0x7f800000u) == 0x7f800000u || (x[k] & 0x7f80u) == 0x7f80u;
+          if (__any(bad))
+            for (int r = 0; r < L::ROWS; ++r)
+              if (__any(bad && L::row(lane) == r)) {
+                odd |= 1u << (j * L::ROWS + r);
+                if (L::row(lane) == r) *reinterpret_cast<u32x4*>(at + j * L::GROUP) = u32x4{0u, 0u, 0u, 0u};
+              }
+        }
+      }
+      if (lane == 0) s_odd[slot][my] = odd;
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    };
+    auto unseen = [&](int t) { return (w.p0 + 2 * t + 2) * HK_PAGE > tile_seen; };  // some keys of tile t, by some query
+    const uint32_t lds_k = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)s_k[0];
+    const uint32_t lds_v = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)s_v[0];
 
-  auto after = [](int buf) { return buf == 2 ? 0 : buf + 1; };
-  // Tile t is computed between a barrier that finds tile t + 1 arrived and the tile before t read by
-  // all, whose place tile t + 2 then takes.  (Past the last tile its last page once more, with no
-  // valid slot.)
-  auto turn = [&](int t, int next) {
-    settle(t + 1, next);
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    request(after(next));
-    load_id(t + 3);
-  };
-  if (tiles > 0) {
-    load_id(0);
-    request(0);
-    load_id(1);
-    settle(0, 0);
-    request(1);
-    load_id(2);
-    __syncthreads();
-  }
-  if (w0 >= w.rows) {                                            // a wave without rows brings its pages
-    for (int t = 0, buf = 0; t < tiles; ++t, buf = after(buf)) turn(t, after(buf));
-    direct_wait();
-    return;
-  }
-  // the queries are here before the loop, where a wait for them would be one for the next tile too
+    f32x16 acc[DT];
 #pragma unroll
-  for (int i = 0; i < KS; ++i) asm volatile("" : "+v"(q.f[i]));
-  if (tiles > 0) {
-    flags(0);
-    first_k(s_k[0]);
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int i = 0; i < KS; ++i) {
-      z[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % AHEAD], q.f[i], i ? z[0] : f32x16{}, 0, 0, 0);
-      if (i + AHEAD < KS) kf[i % AHEAD] = k_frag(s_k[0], i + AHEAD);
+      for (int e = 0; e < 16; ++e) acc[dt][e] = 0.f;
+    float m = -INFINITY, mb = 0.f, l = 0.f;
+
+    const int k_at = L::k_lane(lane), v_at = L::v_lane(lane);    // the lane's fragments within 32 keys
+    auto k_frag = [&](const char* k, int s) {
+      return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(k + k_at + L::k_step(s)));
+    };
+    auto v_frag = [&](const char* v, int i) {                    // i = s * DT + dt
+      s16x4 x[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const char* at = v + v_at + L::v_step(i / DT, h, i % DT);
+        x[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) s16x4*)(uintptr_t)(__attribute__((address_space(3))) const char*)at);
+      }
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    bf16x8 kf[AHEAD], vf[AHEAD];
+    uint32_t bp[8];                                              // P of 32 keys, two a word
+    f32x16 z[2];
+    auto first_k = [&](const char* k) {
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) kf[i] = k_frag(k, i);
+    };
+    // scores of the block at k into zn, beside the probabilities of zc (into bp; the block at v is zc's).
+    // The empty asm statements keep what is computed beside an MFMA in its place.
+    auto scores = [&](f32x16& zn, const f32x16& zc, const char* k, const char* v) {
+      float sum[2] = {0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        zn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % AHEAD], q.f[i], i ? zn : f32x16{}, 0, 0, 0);
+        if (i + AHEAD < KS) kf[i % AHEAD] = k_frag(k, i + AHEAD);
+        else vf[i + AHEAD - KS] = v_frag(v, i + AHEAD - KS);
+#pragma unroll
+        for (int e = i * 16 / KS; e < (i + 1) * 16 / KS; e += 2) {
+          const float x = fast_exp2(fmaf(zc[e], c2, -mb)), y = fast_exp2(fmaf(zc[e + 1], c2, -mb));
+          sum[0] += x;
+          sum[1] += y;
+          bp[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x, y}), bf16x2));
+          asm volatile("" : "+v"(bp[e / 2]), "+v"(sum[0]), "+v"(sum[1]));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      l += sum[0] + sum[1];
+    };
+    // acc += P V of the block at v, beside the maximum of zn, which it returns; the first fragments of
+    // the scores after these come from k
+    auto values = [&](const f32x16& zn, const char* v, const char* k) {
+      float zm = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < VS; ++i) {
+        const int s = 4 * (i / DT);
+        const bf16x8 b = __builtin_bit_cast(bf16x8, (u32x4{bp[s], bp[s + 1], bp[s + 2], bp[s + 3]}));
+        acc[i % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % AHEAD], b, acc[i % DT], 0, 0, 0);
+        if (i + AHEAD < VS) vf[i % AHEAD] = v_frag(v, i + AHEAD);
+        else kf[i + AHEAD - VS] = k_frag(k, i + AHEAD - VS);
+#pragma unroll
+        for (int e = i * 16 / VS; e < (i + 1) * 16 / VS; e += 2) {
+          zm = fmaxf(fmaxf(zm, zn[e]), zn[e + 1]);
+          asm volatile("" : "+v"(zm));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      return zm;
+    };
+    // keys of the 32 from page p on that the lane's query does not see: -inf
+    auto hide = [&](f32x16& zn, int p, uint32_t valid) {
+      const int key = p * HK_PAGE;
+      if (valid == 0xffffffffu && key + 32 <= seen_all) return;
+      const int k = seen - key;
+      uint32_t x = (valid & (k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u)) >> (4 * hi);
+      asm volatile("" : "+v"(x));                                // (a branch, not selects in every block)
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (!((x >> ((e & 3) + 8 * (e >> 2))) & 1u)) zn[e] = -INFINITY;
+    };
+    // a new reference where a score has outgrown it
+    auto refer = [&](float zm) {
+      zm *= c2;
+      if (__any(zm > m + CH_SLACK)) {
+        zm = fmaxf(zm, __shfl_xor(zm, 32, 64));
+        const float mn = fmaxf(m, ceilf(zm));
+        const float alpha = m == -INFINITY ? 0.f : fast_exp2(m - mn);
+        m = mn;
+        mb = mn == -INFINITY ? 0.f : mn + bias;
+        l *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[dt][e] *= alpha;
+      }
+    };
+    // rows of V with infinite values that not every query of the tile sees (zeros in LDS)
+    auto add_odd = [&](uint32_t odd, int p, uint32_t valid) {
+      while (odd) {
+        const int key = __builtin_ctz(odd), reg = (key & 3) + 4 * (key >> 3);
+        odd &= odd - 1;
+        const int at = min(max(w.trow[min(p + key / HK_PAGE, w.p1 - 1)], 0), a.num_pages - 1);
+        const uint16_t* vr = reinterpret_cast<const uint16_t*>(a.v_pool) + ((size_t)at * HK_PAGE + key % HK_PAGE) * D;
+        uint32_t two = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) two = reg / 2 == e ? bp[e] : two;
+        asm volatile("" : "+v"(two));
+        float pr = __uint_as_float(reg & 1 ? two & 0xffff0000u : two << 16);
+        pr = __shfl(pr, (lane & 31) + 32 * ((key >> 2) & 1), 64);
+        const bool sees = ((valid >> key) & 1u) && p * HK_PAGE + key < seen;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float x = M::value(vr[32 * dt + (e & 3) + 8 * (e >> 2) + 4 * hi]);
+            acc[dt][e] = sees ? fmaf(pr, x, acc[dt][e]) : acc[dt][e];
+          }
+      }
+    };
+    uint32_t valid[LEAD + 1];                                    // of tiles t .. t + LEAD
+    int slot = 0;                                                // of V of tile t
+    auto behind = [&](int n) { return slot + n >= NV ? slot + n - NV : slot + n; };
+    auto turn = [&](int t) {
+      if (t + LEAD - 1 < tiles) direct_wait<2 * L::LOADS>();
+      else direct_wait<0>();
+      if (is_v && unseen(t + 1) && t + 1 < tiles) settle(t + 1, (valid[1] >> (16 * my)) & 0xffffu, behind(1));
+      asm volatile("s_barrier" ::: "memory");
+      const int i = (t + LEAD) & 63;
+      if (i == 0) {
+        ids = next_ids;
+        masks = next_masks;
+        load_ids(t + LEAD + 64);
+      }
+      valid[LEAD] = __builtin_amdgcn_readlane(masks, i);
+      if (t + LEAD - is_v < tiles)
+        request(__builtin_amdgcn_readlane(ids, i), (valid[LEAD - 1] >> (16 * my)) & 0xffffu,
+                is_v ? lds_v + behind(NV - 1) * L::BYTES : lds_k + ((t + 1) & (NK - 1)) * L::BYTES);
+    };
+    auto first_read = [&] {                                      // K of tile 0 is read: tile 4's takes its slot
+      asm volatile("s_barrier" ::: "memory");
+      if (NK < tiles && !is_v) request(__builtin_amdgcn_readlane(ids, NK), 0, lds_k);
+    };
+    auto advance = [&] {
+#pragma unroll
+      for (int i = 0; i < LEAD; ++i) valid[i] = valid[i + 1];
+      slot = behind(1);
+    };
+    if (tiles > 0) {
+      load_ids(0);
+      ids = next_ids;
+      masks = next_masks;
+#pragma unroll
+      for (int i = 0; i < LEAD; ++i) valid[i] = __builtin_amdgcn_readlane(masks, i);
+#pragma unroll
+      for (int i = 0; i < NK; ++i)
+        if (i < tiles)
+          request(__builtin_amdgcn_readlane(ids, i + is_v), (valid[i] >> (16 * my)) & 0xffffu,
+                  is_v ? lds_v + i * L::BYTES : lds_k + i * L::BYTES);
+      if (tiles >= NK) direct_wait<2 * L::LOADS>();
+      else direct_wait<0>();
+      load_ids(64);
+      if (is_v && unseen(0)) settle(0, (valid[0] >> (16 * my)) & 0xffffu, 0);
+      __syncthreads();
     }
-    hide(z[0], w.p0, (uint32_t)valid);
-    float zm = z[0][0];
+    if (w0 >= w.rows) {                                          // a wave without rows brings its pages
+      if (tiles > 0) first_read();
+      for (int t = 0; t < tiles; ++t, advance()) turn(t);
+      continue;
+    }
+    // the queries are here before the loop, where a wait for them would be one for the next tile too
 #pragma unroll
-    for (int e = 1; e < 16; ++e) zm = fmaxf(zm, z[0][e]);
-    refer(zm);
-    first_k(s_k[0] + L::HALF);
+    for (int i = 0; i < KS; ++i) asm volatile("" : "+v"(q.f[i]));
+    if (tiles > 0) {
+      first_k(s_k[0]);
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        z[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % AHEAD], q.f[i], i ? z[0] : f32x16{}, 0, 0, 0);
+        if (i + AHEAD < KS) kf[i % AHEAD] = k_frag(s_k[0], i + AHEAD);
+      }
+      hide(z[0], w.p0, valid[0]);
+      float zm = z[0][0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) zm = fmaxf(zm, z[0][e]);
+      refer(zm);
+      first_read();
+      first_k(s_k[1]);
+    }
+    auto step = [&](int t, f32x16& zc, f32x16& zn) {
+      __builtin_amdgcn_s_setprio(0);
+      scores(zn, zc, s_k[(t + 1) & (NK - 1)], s_v[slot]);
+      turn(t);
+      __builtin_amdgcn_s_setprio(1);
+      hide(zn, w.p0 + 2 * t + 2, valid[1]);
+      const float zm = values(zn, s_v[slot], s_k[(t + 2) & (NK - 1)]);
+      if (unseen(t)) {
+        const uint32_t odd = __builtin_amdgcn_readfirstlane(s_odd[slot][0] | s_odd[slot][1] << 16);
+        if (odd) add_odd(odd, w.p0 + 2 * t, valid[0]);
+      }
+      if (t + 1 < tiles) refer(zm);
+      advance();
+    };
+    for (int t = 0; t < tiles; t += 2) {
+      step(t, z[0], z[1]);
+      if (t + 1 < tiles) step(t + 1, z[1], z[0]);
+    }
+    l += __shfl_xor(l, 32, 64);
+    if (w0 + (lane & 31) < w.rows)
+      put_state<uint16_t, D>(a, row, pieces.state < 0 ? -1 : pieces.state + r - w.r0, acc, mb, l);
   }
-  for (int t = 0, buf = 0; t < tiles; ++t) {
-    const int p = w.p0 + t * TP, next = after(buf);
-    scores(z[1], z[0], s_k[buf] + L::HALF, s_v[buf]);
-    turn(t, next);
-    hide(z[1], p + 2, (uint32_t)(valid >> 32));
-    float zm = values(z[1], s_v[buf], s_k[next]);
-    if ((uint32_t)odd) add_odd((uint32_t)odd, p, (uint32_t)valid);
-    refer(zm);
-    const uint32_t odd1 = (uint32_t)(odd >> 32), valid1 = (uint32_t)(valid >> 32);
-    flags(next);
-    scores(z[0], z[1], s_k[next], s_v[buf] + L::HALF);
-    hide(z[0], p + 4, (uint32_t)valid);
-    zm = values(z[0], s_v[buf] + L::HALF, s_k[next] + L::HALF);
-    if (odd1) add_odd(odd1, p + 2, valid1);
-    refer(zm);
-    buf = next;
-  }
-  direct_wait();                                                 // (nothing on its way into LDS that is given back)
-  l += __shfl_xor(l, 32, 64);
-  if (w0 + (lane & 31) < w.rows) put_state<uint16_t, D>(a, row, ((int64_t)w.item * 256 + r - w.r0) * a.tile_splits, w.split, acc, mb, l);
 }
 
 // ------------------------------------------------------------------ short kernels
@@ -850,7 +1037,6 @@ constexpr int SHORT_NT = 256, SHORT_NW = SHORT_NT / 64;
 
 constexpr int SHORT_WG = 512;                 // workgroups of a launch: two a CU
 constexpr int STEP_PAGES = 8;                 // pages of a step, two a wave
-constexpr int MAX_STATES = 64;                // workgroups that share a row at most
 
 // A row of the short kernels: the chunk of head h's sequence, its folded rows (0: not a short one),
 // and the pages and steps that its last token sees.
@@ -873,10 +1059,10 @@ __device__ __forceinline__ ShortRow short_row(const Args& a, int h) {
 // The steps of all rows lie behind one another, and every workgroup takes an equal run of them:
 // rows of any mixture of lengths fill the chip evenly, and a launch has no idle workgroups.  Each
 // workgroup sums the rows' steps itself.
-struct Runs {
+struct ShortRuns {
   int total, share;
 };
-__device__ inline Runs short_runs(const Args& a, int (&s_first)[SHORT_NT + 1]) {
+__device__ inline ShortRuns short_runs(const Args& a, int (&s_first)[SHORT_NT + 1]) {
   __shared__ int s_sum[SHORT_NW], s_most[SHORT_NW];
   const int heads = a.n_seq * a.Hkv, per = (heads + SHORT_NT - 1) / SHORT_NT;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -898,7 +1084,7 @@ __device__ inline Runs short_runs(const Args& a, int (&s_first)[SHORT_NT + 1]) {
     s_most[wave] = most;
   }
   __syncthreads();
-  Runs u = {0, 0};
+  ShortRuns u = {0, 0};
   int before = x - sum;
 #pragma unroll
   for (int w = 0; w < SHORT_NW; ++w) {
@@ -1046,7 +1232,7 @@ __global__ __launch_bounds__(SHORT_NT, sizeof(T) == 2 ? 2 : 1) void chunk_short_
   __shared__ float s_m[SHORT_NW][32], s_l[SHORT_NW][32];
   __shared__ int s_first[SHORT_NT + 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Runs u = short_runs(a, s_first);
+  const ShortRuns u = short_runs(a, s_first);
   char* my_k = s_buf + wave * WAVE;
   char* my_v = my_k + 32 * L::K_ROW;
   const int stop = min((int)(blockIdx.x + 1) * u.share, u.total);
@@ -1123,60 +1309,81 @@ __global__ __launch_bounds__(SHORT_NT, sizeof(T) == 2 ? 2 : 1) void chunk_short_
 }
 
 // ------------------------------------------------------------------ merge
-// One wave per query: the states of its row's pieces, in their order.  Lanes read the references and
-// sums of all of them at once (at most 64), the outputs four at a time.
-constexpr int MERGE_NT = 256, MERGE_NW = MERGE_NT / 64;
-constexpr int MAX_SPLITS = 64;
+// D / 4 lanes per query: the states of its row's pieces, in their order.  Lanes read the references and
+// sums of the pieces (at most 64) side by side, and four dims of four pieces' outputs at a time.
+constexpr int MERGE_NT = 256;
+template <int D>
+constexpr int MERGE_ROWS = MERGE_NT / (D / 4);                   // of a workgroup at a time
 
 template <typename T, int D, typename F>
 __device__ __forceinline__ void merge_states(const Args& a, int64_t row, int used, const float* o_states,
                                              const float* ml_states, F at) {
-  constexpr int PER = D / 64, U = 4;
-  const int lane = threadIdx.x & 63;
-  const f32x2 mine = *reinterpret_cast<const f32x2*>(ml_states + at(min(lane, used - 1)) * 2);
-  const float m = lane < used ? mine[0] : -INFINITY;
-  const float M_ = wave_max(m);
-  const float f = M_ == -INFINITY ? 1.f : fast_exp2(m - M_);     // (no valid key anywhere: sums of 0, or NaN)
-  const float l = wave_sum(lane < used ? mine[1] * f : 0.f);
-  float o[PER];
+  constexpr int LANES = D / 4, PER = MAX_STATES / LANES, U = 8;
+  const int lane = threadIdx.x % LANES;
+  f32x2 ml[PER];
+  float M_ = -INFINITY;
 #pragma unroll
-  for (int e = 0; e < PER; ++e) o[e] = 0.f;
+  for (int i = 0; i < PER; ++i) {
+    const int j = i * LANES + lane;
+    ml[i] = f32x2{-INFINITY, 0.f};
+    if (j < used) ml[i] = *reinterpret_cast<const f32x2*>(ml_states + at(j) * 2);
+    M_ = fmaxf(M_, ml[i][0]);
+  }
+#pragma unroll
+  for (int x = 1; x < LANES; x <<= 1) M_ = fmaxf(M_, __shfl_xor(M_, x, 64));
+  // (no valid key anywhere: sums of 0, or NaN)
+  auto factor = [&](float m) { return M_ == -INFINITY ? 1.f : fast_exp2(m - M_); };
+  float l = 0.f;
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (i * LANES + lane < used) l += ml[i][1] * factor(ml[i][0]);
+#pragma unroll
+  for (int x = 1; x < LANES; x <<= 1) l += __shfl_xor(l, x, 64);
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
   for (int j0 = 0; j0 < used; j0 += U) {
-    float x[U][PER];
+    f32x4 x[U];
+    float m[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const float* po = o_states + at(min(j0 + u, used - 1)) * D + lane * PER;
-#pragma unroll
-      for (int e = 0; e < PER; ++e) x[u][e] = po[e];
+      const int64_t state = at(min(j0 + u, used - 1));
+      x[u] = *reinterpret_cast<const f32x4*>(o_states + state * D + lane * 4);
+      m[u] = ml_states[state * 2];
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const float fu = __shfl(f, j0 + u, 64);
-      if (j0 + u < used && fu != 0.f)
+      const float f = factor(m[u]);
+      if (j0 + u < used && f != 0.f)
 #pragma unroll
-        for (int e = 0; e < PER; ++e) o[e] = fmaf(x[u][e], fu, o[e]);
+        for (int e = 0; e < 4; ++e) o[e] = fmaf(x[u][e], f, o[e]);
     }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;   // (a NaN stays one)
-  T* to = reinterpret_cast<T*>(a.o) + row * D + lane * PER;
-  if constexpr (PER == 2) Mma<T, D>::put2(to, o[0] * inv, o[1] * inv);
-  else if constexpr (std::is_same<T, float>::value) *to = o[0] * inv;
-  else *reinterpret_cast<__bf16*>(to) = (__bf16)(o[0] * inv);
+  Mma<T, D>::put4(reinterpret_cast<T*>(a.o) + row * D + lane * 4, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
   if (lane == 0 && a.lse) a.lse[row] = l == 0.f ? -INFINITY : (M_ + __log2f(l)) * kLn2;
 }
 
-// Short rows: workgroup (h, y) takes every MERGE_Y-th four queries of head h.
+// Tiles in pieces: tile_y workgroups each; then the short rows of a head: MERGE_Y each.
 constexpr int MERGE_Y = 4;
 template <typename T, int D>
-__global__ __launch_bounds__(MERGE_NT) void chunk_merge_short_kernel(Args a) {
-  const int h = blockIdx.x, heads = a.n_seq * a.Hkv;
+__global__ __launch_bounds__(MERGE_NT) void chunk_merge_kernel(Args a, int tile_wg, int tile_y) {
+  int r = threadIdx.x / (D / 4);
+  if ((int)blockIdx.x < tile_wg) {
+    const TileSplit t = reinterpret_cast<const TileSplit*>(a.tile_split)[blockIdx.x / tile_y];
+    if (t.used <= 1) return;                  // written as it is
+    for (r += blockIdx.x % tile_y * MERGE_ROWS<D>; r < min(TILE_ROWS, t.rows - t.r0); r += tile_y * MERGE_ROWS<D>) {
+      const int tok = (t.r0 + r) / a.G;
+      const int64_t row = (int64_t)(t.first + tok) * a.Hq + t.kv * a.G + (t.r0 + r - tok * a.G);
+      merge_states<T, D>(a, row, t.used, a.tile_o, a.tile_ml, [&](int j) { return (int64_t)(t.at + j) * TILE_ROWS + r; });
+    }
+    return;
+  }
+  const int x = blockIdx.x - tile_wg, h = x / MERGE_Y, heads = a.n_seq * a.Hkv;
   const int first = a.short_first[h], steps = a.short_first[h + 1] - first, share = a.short_first[heads + 1];
   const Chunk c = chunk_of(a.start, h / a.Hkv, a.n_tokens, a.max_len);
   if (steps <= 0) return;
   const int w0 = first / share, used = (first + steps - 1) / share - w0 + 1;
   if (used <= 1) return;                      // written as it is
-  for (int r = blockIdx.y * MERGE_NW + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); r < c.len * a.G;
-       r += MERGE_Y * MERGE_NW) {
+  for (r += x % MERGE_Y * MERGE_ROWS<D>; r < c.len * a.G; r += MERGE_Y * MERGE_ROWS<D>) {
     const int tok = r / a.G;
     const int64_t row = (int64_t)(c.first + tok) * a.Hq + (h % a.Hkv) * a.G + (r - tok * a.G);
     merge_states<T, D>(a, row, used, a.short_o, a.short_ml, [&](int j) {
@@ -1185,90 +1392,72 @@ __global__ __launch_bounds__(MERGE_NT) void chunk_merge_short_kernel(Args a) {
   }
 }
 
-// A tile kernel's queries: tile and KV head, then the query.
-template <typename T, int D, int TM>
-__global__ __launch_bounds__(MERGE_NT) void chunk_merge_tile_kernel(Args a) {
-  const int64_t q = (int64_t)blockIdx.x * MERGE_NW + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int item = (int)(q / TM), u = item / a.Hkv, kv = item % a.Hkv, s = tile_sequence<TM>(a, u);
-  const int r = (u - tiles_before<TM>(a, s)) * TM + (int)(q % TM);
-  const Chunk c = chunk_of(a.start, s, a.n_tokens, a.max_len);
-  const int rows = c.len * a.G;
-  if (r < 0 || r >= rows || rows <= SHORT_ROWS) return;
-  const int h = s * a.Hkv + kv, n = min(max(a.n_pages[h], 0), a.max_pages);
-  const int end = row_end(n, n > 0 ? a.masks[(size_t)h * a.max_pages + n - 1] : 0u);
-  const int pages = tile_pages(n, end, c.len, (min((r / TM + 1) * TM, rows) - 1) / a.G);
-  const int share = split_share(pages, a.tile_splits), used = max((pages + share - 1) / share, 1);
-  const int tok = r / a.G;
-  const int64_t row = (int64_t)(c.first + tok) * a.Hq + kv * a.G + (r - tok * a.G);
-  merge_states<T, D>(a, row, used, a.tile_o, a.tile_ml, [&](int j) { return q * a.tile_splits + j; });
-}
-
-// Rows of a tile kernel's workgroup.
-static constexpr int tile_rows(bool bf, int D) { return bf || D == 64 ? 256 : 128; }
-
-template <typename T, int D>
-static void launch(const Args& a, hipStream_t st, int heads, int tile_wg) {
-  constexpr bool bf = sizeof(T) == 2;
-  constexpr int TM = tile_rows(bf, D);
-  {
-    TimedLaunch t(HK_TK_CHUNK_ATTN, st);
-    if (tile_wg > 0) {
-      const dim3 grid(tile_wg, a.tile_splits), block(2 * TM);
-      if constexpr (bf) hipLaunchKernelGGL((chunk_tile_bf16_kernel<D>), grid, block, 0, st, a);
-      else hipLaunchKernelGGL((chunk_tile_f32_kernel<D, TM / 32>), grid, block, 0, st, a);
-    }
-    if (heads > 0) hipLaunchKernelGGL((chunk_short_kernel<T, D>), dim3(SHORT_WG), dim3(SHORT_NT), 0, st, a);
-  }
-  TimedLaunch t(HK_TK_CHUNK_MERGE, st);
-  if (a.tile_splits > 1)
-    hipLaunchKernelGGL((chunk_merge_tile_kernel<T, D, TM>), dim3((uint32_t)tile_wg * (TM / MERGE_NW)), dim3(MERGE_NT), 0, st, a);
-  if (heads > 0) hipLaunchKernelGGL((chunk_merge_short_kernel<T, D>), dim3(heads, MERGE_Y), dim3(MERGE_NT), 0, st, a);
-}
-
-// Workgroups and splits of a call.  A tile launch is split until it offers 512 workgroups, no split
-// of a full-width row having less than MIN_PAGES pages.  heads: of the short kernel, 0 where no row
-// can be a short one.
+// Workgroups of a call.  heads: of the short kernel, 0 where no row can be a short one; tiles: numbers
+// of tiles of a KV head; pieces: most of them that a planned launch makes, 0 for one of many tiles.
 struct Plan {
-  int heads, tile_wg, tile_splits;
+  int heads, tiles, pieces;
 };
-static Plan plan(int NS, int Hq, int Hkv, int TM, int n_tokens, int max_len, int max_pages) {
+static int most_pieces(long long tiles, int max_pages) {
+  const int steps = std::max((max_pages + TILE_PAGES - 1) / TILE_PAGES, 1);
+  return (int)std::min<long long>(tiles * std::min(steps, MAX_STATES), PLAN_PIECES);
+}
+static Plan plan(int NS, int Hq, int Hkv, int cost, int n_tokens, int max_len, int max_pages) {
   const int G = Hq / Hkv;
   const long long rows = (long long)n_tokens * G;
   const bool tiles = (long long)max_len * G > SHORT_ROWS && rows > SHORT_ROWS;
   Plan p;
   p.heads = G <= SHORT_ROWS ? NS * Hkv : 0;
-  p.tile_wg = tiles ? (int)((rows / TM + NS) * Hkv) : 0;
-  const int most = std::min((max_pages + MIN_PAGES - 1) / MIN_PAGES, MAX_SPLITS);
-  p.tile_splits = 1;
-  while (tiles && p.tile_splits < most && (long long)p.tile_wg * p.tile_splits < 512) p.tile_splits *= 2;
-  p.tile_splits = std::min(p.tile_splits, most);
+  p.tiles = tiles ? (int)(rows / TILE_ROWS + NS) : 0;
+  const long long all = (long long)p.tiles * Hkv;
+  // (rows of fewer than two costs of a piece gain nothing by pieces)
+  p.pieces = all <= PLAN_TILES && max_pages >= 2 * cost * TILE_PAGES ? most_pieces(all, max_pages) : 0;
   return p;
+}
+
+template <typename T, int D>
+static void launch(const Args& a, hipStream_t st, const Plan& p) {
+  constexpr bool bf = sizeof(T) == 2;
+  {
+    TimedLaunch t(HK_TK_CHUNK_ATTN, st);
+    if (p.tiles > 0) {
+      const dim3 grid(p.pieces ? std::min(p.pieces, TILE_WG) : p.tiles * a.Hkv), block(2 * TILE_ROWS);
+      if constexpr (bf) {
+        if (p.pieces) hipLaunchKernelGGL((chunk_tile_bf16_kernel<D, true>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((chunk_tile_bf16_kernel<D, false>), grid, block, 0, st, a);
+      } else {
+        if (p.pieces) hipLaunchKernelGGL((chunk_tile_f32_kernel<D, true>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((chunk_tile_f32_kernel<D, false>), grid, block, 0, st, a);
+      }
+    }
+    if (p.heads > 0) hipLaunchKernelGGL((chunk_short_kernel<T, D>), dim3(SHORT_WG), dim3(SHORT_NT), 0, st, a);
+  }
+  const int tiles = p.pieces ? p.tiles * a.Hkv : 0;
+  const int tile_y = std::max(std::min(2048 / std::max(tiles, 1), TILE_ROWS / MERGE_ROWS<D>), 4);
+  if (tiles * tile_y + p.heads * MERGE_Y == 0) return;
+  TimedLaunch t(HK_TK_CHUNK_MERGE, st);
+  hipLaunchKernelGGL((chunk_merge_kernel<T, D>), dim3(tiles * tile_y + p.heads * MERGE_Y), dim3(MERGE_NT), 0, st, a,
+                     tiles * tile_y, tile_y);
 }
 
 }  // namespace hk
 
 using namespace hk;
 
-// Split states (rows of D + 2 floats) of the short kernel's workgroups, two each, of the tiles', and
-// the short rows' first steps.  Grows with the tokens and does not depend on the type: a launch of
-// tiles that splits has fewer than twice 512 workgroups.
+// States (rows of D + 2 floats) of the short kernel's workgroups, two each, and of the tiles' pieces,
+// what the pieces are, and the short rows' first steps.  Grows with the tokens and does not depend on the type.
 static size_t short_states(const Plan& p) { return p.heads ? (size_t)2 * SHORT_WG * SHORT_ROWS : 0; }
 size_t hk_chunk_attn_ws(int NS, int Hq, int Hkv, int D, int n_tokens, int max_len, int max_pages) {
-  size_t rows = 0;
-  for (int TM : {128, 256}) {
-    const Plan p = plan(NS, Hq, Hkv, TM, n_tokens, max_len, max_pages);
-    const size_t most = std::min((max_pages + MIN_PAGES - 1) / MIN_PAGES, MAX_SPLITS);
-    const size_t tiles = most > 1 ? std::min((size_t)p.tile_wg * most, (size_t)1024) * TM : 0;
-    rows = std::max(rows, short_states(p) + tiles);
-  }
-  return rows * (D + 2) * sizeof(float) + ((size_t)NS * Hkv + 2) * sizeof(int32_t);
+  const Plan p = plan(NS, Hq, Hkv, 0, n_tokens, max_len, max_pages);
+  const int pieces = most_pieces(std::min<long long>((long long)p.tiles * Hkv, PLAN_TILES), max_pages);
+  const size_t rows = short_states(p) + (size_t)pieces * TILE_ROWS;
+  return rows * (D + 2) * sizeof(float) + PLAN_TILES * sizeof(TileSplit) + ((size_t)NS * Hkv + 2) * sizeof(int32_t);
 }
 
 hipError_t hk_launch_chunk_attn(int NS, int Hq, int Hkv, int D, const hk_paged_kv* kv, const hk_chunks* ch,
                                 const void* q, int64_t q_row, float sm_scale, void* o, float* lse, void* ws,
                                 hipStream_t st) {
   const bool bf = kv->dtype == HK_BF16;
-  const Plan p = plan(NS, Hq, Hkv, tile_rows(bf, D), ch->n_tokens, ch->max_len, kv->max_pages);
+  const Plan p = plan(NS, Hq, Hkv, bf ? Cost<uint16_t>::STATE : Cost<float>::STATE, ch->n_tokens, ch->max_len, kv->max_pages);
   Args a;
   a.q = static_cast<const char*>(q);
   a.k_pool = static_cast<const char*>(kv->k_pool);
@@ -1280,13 +1469,14 @@ hipError_t hk_launch_chunk_attn(int NS, int Hq, int Hkv, int D, const hk_paged_k
   a.q_row = q_row;
   a.o = static_cast<char*>(o);
   a.lse = lse;
-  a.tile_splits = p.tile_splits;
-  const size_t ss = short_states(p), ts = p.tile_splits > 1 ? (size_t)p.tile_wg * p.tile_splits * tile_rows(bf, D) : 0;
+  a.n_tiles = p.tiles;
+  const size_t ss = short_states(p), ts = (size_t)p.pieces * TILE_ROWS;
   a.short_o = static_cast<float*>(ws);
   a.tile_o = a.short_o + ss * D;
   a.short_ml = a.tile_o + ts * D;
   a.tile_ml = a.short_ml + ss * 2;
-  a.short_first = reinterpret_cast<int32_t*>(a.tile_ml + ts * 2);
+  a.tile_split = reinterpret_cast<int32_t*>(a.tile_ml + ts * 2);
+  a.short_first = a.tile_split + PLAN_TILES * (sizeof(TileSplit) / sizeof(int32_t));
   a.Hq = Hq;
   a.Hkv = Hkv;
   a.G = Hq / Hkv;
@@ -1296,9 +1486,9 @@ hipError_t hk_launch_chunk_attn(int NS, int Hq, int Hkv, int D, const hk_paged_k
   a.n_tokens = ch->n_tokens;
   a.max_len = ch->max_len;
   a.c2 = sm_scale * kLog2e;
-  if (bf && D == 128) launch<uint16_t, 128>(a, st, p.heads, p.tile_wg);
-  else if (bf) launch<uint16_t, 64>(a, st, p.heads, p.tile_wg);
-  else if (D == 128) launch<float, 128>(a, st, p.heads, p.tile_wg);
-  else launch<float, 64>(a, st, p.heads, p.tile_wg);
+  if (bf && D == 128) launch<uint16_t, 128>(a, st, p);
+  else if (bf) launch<uint16_t, 64>(a, st, p);
+  else if (D == 128) launch<float, 128>(a, st, p);
+  else launch<float, 64>(a, st, p);
   return hipGetLastError();
 }

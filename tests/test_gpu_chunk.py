@@ -192,6 +192,18 @@ def test_chunk_attention_over_splits(dtype, D, G, lens, ctx, width):
     _attend(c, lens, 1, G, D, dtype, pad=1)
 
 
+@pytest.mark.parametrize("dtype,D,B,G", [("bf16", 128, 40, 8), ("bf16", 64, 70, 8), ("f32", 64, 40, 8), ("f32", 128, 70, 8)])
+def test_more_tiles_than_workgroups(dtype, D, B, G):
+    """Tables wide enough for tiles in pieces: workgroups with several pieces (B 40), a launch of too many
+    tiles for that (B 70); rows without pages and chunks that are short among them."""
+    lens = [20 - s % 3 - 17 * (s % 9 == 4) for s in range(B)]
+    ctx = [(97 * s) % 300 for s in range(B)]
+    rows = [lens[s] + max(ctx[s] - 5 * kv, 0) for s in range(B) for kv in range(8)]
+    rows[8 * 7 + 3] = 0
+    c = Cache(rows, D, dtype, width=200, seed=3, keep_last=20)
+    _attend(c, lens, 8, G, D, dtype, pad=2)
+
+
 def test_sharp_and_flat_scores():
     """Scores hundreds apart: the running reference moves in almost every block."""
     for dtype in ("bf16", "f32"):
