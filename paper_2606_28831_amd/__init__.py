@@ -468,24 +468,30 @@ def _kv_dtype(kv: PagedKV):
 
 def _run(name: str, t, stream, *args):
     """Call an entry point on the device that holds t."""
-    with torch.cuda.device(t.device):
-        s = torch.cuda.current_stream() if stream is None else stream
-        _check(getattr(lib(), name)(*args, C.c_void_p(s.cuda_stream)), name)
+    here = torch.cuda.current_device()
+    if t.get_device() != here:
+        with torch.cuda.device(t.device):
+            _check(getattr(lib(), name)(*args, _stream(stream)), name)
+        return
+    # (the raw handle: torch's stream object takes longer than a launch)
+    raw = torch._C._cuda_getCurrentRawStream(here) if stream is None else stream.cuda_stream
+    _check(getattr(lib(), name)(*args, C.c_void_p(raw)), name)
 
 
 def _vector(t, n: int, dtype, what: str):
-    _need(t.dtype == dtype and t.is_contiguous() and t.numel() >= n,
-          f"{what} must be a contiguous {dtype} tensor of at least {n} entries")
-    return _ptr(t)
+    if t.dtype != dtype or not t.is_contiguous() or t.numel() < n:
+        raise HardKVError(f"{what} must be a contiguous {dtype} tensor of at least {n} entries")
+    return C.c_void_p(t.data_ptr())
 
 
 def _token_rows(t, n_tokens: int, heads: int, D: int, dtype, what: str):
     """(pointer, row stride) of a [..., tokens, heads, D] tensor whose rows are contiguous."""
-    _need(t.dtype == dtype and t.dim() >= 3 and tuple(t.shape[-2:]) == (heads, D)
-          and t.shape[-3] >= n_tokens, f"{what} must be [tokens, {heads}, {D}] in {dtype}")
-    _need(t.stride(-1) == 1 and (heads == 1 or t.stride(-2) == D),
-          f"{what}: the heads of a token must be contiguous")
-    return C.c_void_p(t.data_ptr()), t.stride(-3) if n_tokens > 1 else max(t.stride(-3), heads * D)
+    shape, stride = t.shape, t.stride()
+    if t.dtype != dtype or len(shape) < 3 or shape[-1] != D or shape[-2] != heads or shape[-3] < n_tokens:
+        raise HardKVError(f"{what} must be [tokens, {heads}, {D}] in {dtype}")
+    if stride[-1] != 1 or (heads > 1 and stride[-2] != D):
+        raise HardKVError(f"{what}: the heads of a token must be contiguous")
+    return C.c_void_p(t.data_ptr()), stride[-3] if n_tokens > 1 else max(stride[-3], heads * D)
 
 
 def hk_reserve_slots(d: hk_dims, kv: PagedKV, chunks: Chunks, alloc: Allocator, ws, slot_map=None,
@@ -548,9 +554,9 @@ def hk_verify_draft(chunks: Chunks, V: int, tokens, p, u, n_accept, next_token, 
     dt = {torch.float32: HK_F32, torch.bfloat16: HK_BF16}.get(p.dtype)
     _need(dt is not None, "probabilities must be float32 or bfloat16")
     for t, what in ((p, "p"), (q, "q")):
-        _need(t is None or (t.dtype == p.dtype and t.dim() == 2 and t.shape[0] >= T
-                            and t.shape[1] >= V and (t.stride(1) == 1 or V == 1)),
-              f"{what} must be [tokens, V] with contiguous rows, both in one type")
+        if t is not None and (t.dtype != p.dtype or t.dim() != 2 or t.shape[0] < T or t.shape[1] < V
+                              or (t.stride(1) != 1 and V > 1)):
+            raise HardKVError(f"{what} must be [tokens, V] with contiguous rows, both in one type")
     row = lambda t: 0 if t is None else (t.stride(0) if T > 1 else max(t.stride(0), V))  # noqa: E731
     _run("hk_verify_draft", p, stream, C.byref(chunks.desc), int(V), dt,
          _vector(tokens, T, i32, "tokens"), C.c_void_p(p.data_ptr()), row(p),
