@@ -742,7 +742,7 @@ template <int D, bool PLANNED>
 __global__ __launch_bounds__(256, 2) void chunk_tile_bf16_kernel(Args a) {
   using L = DirectTile<D>;
   using M = Mma<uint16_t, D>;
-  constexpr int KS = D / 16, DT = D / 32, VS = 2 * DT, AHEAD = 4;
+  constexpr int KS = D / 16, DT = D / 32, VS = 2 * DT, AHEAD = 3;
   constexpr int PAGE = HK_PAGE * D * 2, PAGE_LDS = HK_PAGE / L::ROWS * L::GROUP;
   constexpr int NK = 4, NV = 5;                                  // tiles in LDS
   __shared__ __align__(16) char s_k[NK][L::BYTES], s_v[NV][L::BYTES];
@@ -849,23 +849,41 @@ __global__ __launch_bounds__(256, 2) void chunk_tile_bf16_kernel(Args a) {
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i) kf[i] = k_frag(k, i);
     };
-    // scores of the block at k into zn, beside the probabilities of zc (into bp; the block at v is zc's).
-    // The empty asm statements keep what is computed beside an MFMA in its place.
-    auto scores = [&](f32x16& zn, const f32x16& zc, const char* k, const char* v) {
-      float sum[2] = {0.f, 0.f};
+    // Probabilities of zc's pairs of elements, in place, in three stages a slot apart: an exponential's
+    // latency is behind an MFMA and another pair's work.  The empty asm statements keep what is computed
+    // beside an MFMA in its place.
+    float sum[2];
+    auto scale = [&](f32x16& zc, int k) {
+      zc[2 * k] = fmaf(zc[2 * k], c2, -mb);
+      zc[2 * k + 1] = fmaf(zc[2 * k + 1], c2, -mb);
+    };
+    auto raise = [&](f32x16& zc, int k) {
+      zc[2 * k] = fast_exp2(zc[2 * k]);
+      zc[2 * k + 1] = fast_exp2(zc[2 * k + 1]);
+    };
+    auto finish = [&](const f32x16& zc, int k) {
+      sum[0] = k ? sum[0] + zc[2 * k] : zc[0];
+      sum[1] = k ? sum[1] + zc[2 * k + 1] : zc[1];
+      bp[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{zc[2 * k], zc[2 * k + 1]}), bf16x2));
+      asm volatile("" : "+v"(bp[k]), "+v"(sum[0]), "+v"(sum[1]));
+    };
+    auto weigh = [&](f32x16& zc, int k) {
+      if (k + 1 < 8) raise(zc, k + 1);
+      if (k + 2 < 8) scale(zc, k + 2);
+      finish(zc, k);
+    };
+    // scores of the block at k into zn, beside the probabilities of zc (into bp; the block at v is zc's)
+    auto scores = [&](f32x16& zn, f32x16& zc, const char* k, const char* v) {
+      scale(zc, 0);
+      scale(zc, 1);
+      raise(zc, 0);
 #pragma unroll
       for (int i = 0; i < KS; ++i) {
         zn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % AHEAD], q.f[i], i ? zn : f32x16{}, 0, 0, 0);
         if (i + AHEAD < KS) kf[i % AHEAD] = k_frag(k, i + AHEAD);
         else vf[i + AHEAD - KS] = v_frag(v, i + AHEAD - KS);
 #pragma unroll
-        for (int e = i * 16 / KS; e < (i + 1) * 16 / KS; e += 2) {
-          const float x = fast_exp2(fmaf(zc[e], c2, -mb)), y = fast_exp2(fmaf(zc[e + 1], c2, -mb));
-          sum[0] += x;
-          sum[1] += y;
-          bp[e / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x, y}), bf16x2));
-          asm volatile("" : "+v"(bp[e / 2]), "+v"(sum[0]), "+v"(sum[1]));
-        }
+        for (int e = i * 8 / KS; e < (i + 1) * 8 / KS; ++e) weigh(zc, e);
         __builtin_amdgcn_sched_barrier(0);
       }
       l += sum[0] + sum[1];
