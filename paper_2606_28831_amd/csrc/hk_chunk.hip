@@ -1114,7 +1114,7 @@ __device__ inline ShortRuns short_runs(const Args& a, int (&s_first)[SHORT_NT + 
   u.share = max((u.total + SHORT_WG - 1) / SHORT_WG, (most + MAX_STATES - 2) / (MAX_STATES - 1));
   s_first[threadIdx.x] = before;
   if (threadIdx.x == 0) s_first[SHORT_NT] = u.total;
-  if (blockIdx.x == 0) {                      // for the merge
+  if (blockIdx.x == gridDim.x - 1) {          // for the merge
     int32_t* first = a.short_first;
     for (int h = threadIdx.x * per; h < min((int)(threadIdx.x + 1) * per, heads); ++h) {
       first[h] = before;
@@ -1147,7 +1147,10 @@ __device__ inline Piece short_piece(const Args& a, const int (&s_first)[SHORT_NT
   int first = s_first[t];
   Piece p;
   for (int h0 = t * per;; h0 += 64) {
-    const int h = h0 + lane, k = lane < per && h < heads && h < (t + 1) * per ? short_row(a, h).steps : 0;
+    const int h = h0 + lane;
+    const bool mine = h < heads && h < (t + 1) * per;
+    const ShortRow r = short_row(a, mine ? h : heads - 1);
+    const int k = mine ? r.steps : 0;
     int y = k;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -1156,14 +1159,15 @@ __device__ inline Piece short_piece(const Args& a, const int (&s_first)[SHORT_NT
     }
     const unsigned long long in = __ballot(first + y > x);
     if (in || h0 + 64 >= heads) {
-      const int l = in ? __builtin_ctzll(in) : 63;
-      p.h = __builtin_amdgcn_readfirstlane(min(h0 + l, heads - 1));
-      p.from = x - __builtin_amdgcn_readfirstlane(first + __shfl(y - k, l, 64));
+      const int l = __builtin_amdgcn_readfirstlane(in ? __builtin_ctzll(in) : 63);
+      auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+      p.h = min(h0 + l, heads - 1);
+      p.from = x - of(first + y - k);
+      p.row = {{of(r.c.first), of(r.c.len)}, of(r.rows), of(r.end), of(r.pages), of(r.steps)};
       break;
     }
     first += __shfl(y, 63, 64);
   }
-  p.row = short_row(a, p.h);
   p.to = min(p.row.steps, p.from + stop - x);
   return p;
 }
