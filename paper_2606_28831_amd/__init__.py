@@ -466,10 +466,14 @@ def _kv_dtype(kv: PagedKV):
     return kv.k_pool.dtype
 
 
-def _run(name: str, t, stream, *args):
-    """Call an entry point on the device that holds t."""
+def _run(name: str, t, tensors, stream, *args):
+    """Call an entry point on the device that holds t and the tensors it works on."""
+    dev = t.get_device()
+    for x in tensors:
+        if x is not None and x.get_device() != dev:
+            raise HardKVError(f"{name}: tensors on different devices")
     here = torch.cuda.current_device()
-    if t.get_device() != here:
+    if dev != here:
         with torch.cuda.device(t.device):
             _check(getattr(lib(), name)(*args, _stream(stream)), name)
         return
@@ -487,7 +491,8 @@ def _vector(t, n: int, dtype, what: str):
 def _token_rows(t, n_tokens: int, heads: int, D: int, dtype, what: str):
     """(pointer, row stride) of a [..., tokens, heads, D] tensor whose rows are contiguous."""
     shape, stride = t.shape, t.stride()
-    if t.dtype != dtype or len(shape) < 3 or shape[-1] != D or shape[-2] != heads or shape[-3] < n_tokens:
+    if (t.dtype != dtype or len(shape) < 3 or shape[-1] != D or shape[-2] != heads
+            or shape[-3] < n_tokens):
         raise HardKVError(f"{what} must be [tokens, {heads}, {D}] in {dtype}")
     if stride[-1] != 1 or (heads > 1 and stride[-2] != D):
         raise HardKVError(f"{what}: the heads of a token must be contiguous")
@@ -499,7 +504,8 @@ def hk_reserve_slots(d: hk_dims, kv: PagedKV, chunks: Chunks, alloc: Allocator, 
     heads = d.NS * d.Hkv
     _need(kv.page_table.shape[0] >= heads, "the cache has fewer rows than NS * Hkv")
     n = d.NS // max(chunks.n_seq, 1) * chunks.n_tokens * d.Hkv
-    _run("hk_reserve_slots", kv.page_table, stream, C.byref(d), C.byref(kv.desc),
+    _run("hk_reserve_slots", kv.page_table, (chunks.start, alloc.free_ids, slot_map, status, ws),
+         stream, C.byref(d), C.byref(kv.desc),
          C.byref(chunks.desc), C.byref(alloc.desc),
          None if slot_map is None else _vector(slot_map, n, torch.int64, "slot_map"), _ptr(status),
          _ptr(ws), ws.numel())
@@ -513,7 +519,8 @@ def hk_write_kv(d: hk_dims, kv: PagedKV, n_tokens: int, slot_map, k_new, v_new, 
     _need(v_new.dim() == 3 or v_new.shape[0] == layers, "k_new and v_new differ in layers")
     kp, kr = _token_rows(k_new, n_tokens, d.Hkv, d.D, _kv_dtype(kv), "k_new")
     vp, vr = _token_rows(v_new, n_tokens, d.Hkv, d.D, _kv_dtype(kv), "v_new")
-    _run("hk_write_kv", kv.k_pool, stream, C.byref(d), C.byref(kv.desc), layers, int(n_tokens),
+    _run("hk_write_kv", kv.k_pool, (slot_map, k_new, v_new), stream, C.byref(d), C.byref(kv.desc),
+         layers, int(n_tokens),
          _vector(slot_map, layers * n_tokens * d.Hkv, torch.int64, "slot_map"), kp,
          k_new.stride(0) if layers > 1 else 0, kr, vp, v_new.stride(0) if layers > 1 else 0, vr)
 
@@ -535,7 +542,8 @@ def hk_chunk_attn(d: hk_dims, kv: PagedKV, chunks: Chunks, q, sm_scale: float, o
     _need(q.dim() == 3, "q must be 3-d")
     op = _vector(o, T * d.Hq * d.D, _kv_dtype(kv), "o")
     lp = None if lse is None else _vector(lse, T * d.Hq, torch.float32, "lse")
-    _run("hk_chunk_attn", kv.k_pool, stream, C.byref(d), C.byref(kv.desc), C.byref(chunks.desc), qp,
+    _run("hk_chunk_attn", kv.k_pool, (kv.page_table, chunks.start, q, o, lse, ws), stream,
+         C.byref(d), C.byref(kv.desc), C.byref(chunks.desc), qp,
          qr, float(sm_scale), op, lp, _ptr(ws), 0 if ws is None else ws.numel())
 
 
@@ -558,7 +566,9 @@ def hk_verify_draft(chunks: Chunks, V: int, tokens, p, u, n_accept, next_token, 
                               or (t.stride(1) != 1 and V > 1)):
             raise HardKVError(f"{what} must be [tokens, V] with contiguous rows, both in one type")
     row = lambda t: 0 if t is None else (t.stride(0) if T > 1 else max(t.stride(0), V))  # noqa: E731
-    _run("hk_verify_draft", p, stream, C.byref(chunks.desc), int(V), dt,
+    _run("hk_verify_draft", p,
+         (chunks.start, tokens, q, u, n_accept, next_token, n_drop, status, ws), stream,
+         C.byref(chunks.desc), int(V), dt,
          _vector(tokens, T, i32, "tokens"), C.c_void_p(p.data_ptr()), row(p),
          None if q is None else C.c_void_p(q.data_ptr()), row(q),
          _vector(u, T, torch.float32, "u"), _vector(n_accept, B, i32, "n_accept"),
@@ -569,7 +579,8 @@ def hk_verify_draft(chunks: Chunks, V: int, tokens, p, u, n_accept, next_token, 
 def hk_trim_slots(d: hk_dims, kv: PagedKV, n_drop, alloc: Allocator, ws, stream=None):
     _need(kv.page_table.shape[0] >= d.NS * d.Hkv, "the cache has fewer rows than NS * Hkv")
     n = n_drop.numel()
-    _run("hk_trim_slots", kv.page_table, stream, C.byref(d), C.byref(kv.desc), n,
+    _run("hk_trim_slots", kv.page_table, (n_drop, alloc.free_ids, ws), stream, C.byref(d),
+         C.byref(kv.desc), n,
          _vector(n_drop, n, torch.int32, "n_drop"), C.byref(alloc.desc), _ptr(ws), ws.numel())
 
 

@@ -61,6 +61,7 @@ hk_status launched(hipError_t e) { return e == hipSuccess ? HK_OK : HK_ERR_HIP; 
 size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 constexpr int kMaxRows = 1 << 24;        // token rows of a call
+constexpr double kMaxQueries = 17179869184.0;   // token rows x query heads of the chunk attention
 constexpr int kMaxVocab = 1 << 20;
 constexpr int kMaxGroup = 64;            // query heads per KV head of the chunk attention
 
@@ -586,6 +587,7 @@ hk_status hk_chunk_attn(const hk_dims* dims, const hk_paged_kv* kv, const hk_chu
   if ((e = check_chunks(chunks))) return e;
   if (!o || !(sm_scale > 0.f) || !std::isfinite(sm_scale)) return HK_ERR_ARG;
   if (dims->NS != chunks->n_seq || dims->Hq / dims->Hkv > kMaxGroup) return HK_ERR_SHAPE;
+  if ((double)chunks->n_tokens * dims->Hq > kMaxQueries) return HK_ERR_SHAPE;
   const int es = kv->dtype == HK_BF16 ? 2 : 4;
   if ((e = check_rows_at(q, q_row_stride, (int64_t)dims->Hq * dims->D, es))) return e;
   if (!aligned16(o)) return HK_ERR_ALIGN;

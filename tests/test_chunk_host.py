@@ -169,6 +169,14 @@ def test_chunk_attn_refusals(hk):
     assert L.hk_chunk_attn_workspace_size(C.byref(d), None, 4) == 0
 
 
+def test_chunk_attn_refuses_more_queries_than_a_launch_takes(hk):
+    L = hk.lib()
+    d, kv = hk.dims(1, 64 * 1000, 1000, 128), _kv(hk)
+    for tokens, want in ((1 << 24, 3), (1 << 19, 3), (1 << 18, 5)):              # the last: no workspace
+        c = hk.hk_chunks(P, 1, tokens, 8)
+        assert L.hk_chunk_attn(C.byref(d), C.byref(kv), C.byref(c), P, 64 * 1000 * 128, 0.1, P, None, None, 0, None) == want
+
+
 def test_verify_refusals(hk):
     L = hk.lib()
     ch, need = hk.hk_chunks(P, 2, 16, 8), L.hk_verify_workspace_size(2, 1000)

@@ -290,6 +290,76 @@ def test_query_views_streams_and_no_lse():
     assert torch.equal(o, o2)
 
 
+def test_tensors_on_other_devices_are_refused():
+    """Any one of a call's tensors in host memory: an error before the launch."""
+    import paper_2606_28831_amd as hk
+    c = Cache([20, 30], 64, "bf16", seed=1)
+    d, ch = hk.dims(1, 4, 2, 64), _chunks([3])
+    q = torch.zeros(3, 4, 64, dtype=torch.bfloat16, device=DEV)
+    k, sm = torch.zeros(3, 2, 64, dtype=torch.bfloat16, device=DEV), torch.full((6,), -1, dtype=torch.int64, device=DEV)
+    ws, n = torch.empty(1 << 22, dtype=torch.uint8, device=DEV), torch.zeros(1, dtype=I32, device=DEV)
+    away = hk.Chunks(ch.start.cpu(), 3, 3)
+    p, u, tok = torch.ones(3, 8, device=DEV), torch.zeros(3, device=DEV), torch.zeros(3, dtype=I32, device=DEV)
+    for f, args in ((lambda q, o, ws: hk.hk_chunk_attn(d, c.kv, ch, q, 0.1, o, ws), (q, q.clone(), ws)),
+                    (lambda a, b, s: hk.hk_write_kv(d, c.kv, 3, s, a, b), (k, k, sm)),
+                    (lambda s, w: hk.hk_reserve_slots(d, c.kv, ch, c.alloc, w, slot_map=s), (sm, ws)),
+                    (lambda x, w: hk.hk_trim_slots(d, c.kv, x, c.alloc, w), (n, ws)),
+                    (lambda t, q, u, x, w: hk.hk_verify_draft(ch, 8, t, p, u, x, x.clone(), x.clone(), w, q=q), (tok, p, u, n, ws))):
+        for i in range(len(args)):
+            with pytest.raises(hk.HardKVError):
+                f(*(x.cpu() if i == j else x for j, x in enumerate(args)))
+    with pytest.raises(hk.HardKVError):
+        hk.hk_chunk_attn(d, c.kv, away, q, 0.1, q.clone(), ws)
+    c.check()
+
+
+def test_infinite_rows_in_pieces():
+    """The same over rows in several pieces: unseen infinite rows of the newest pages change nothing."""
+    for dtype, D, G, n in (("bf16", 128, 4, 70), ("bf16", 64, 3, 60), ("f32", 64, 4, 70)):
+        L = 6000
+        c = Cache([L], D, dtype, seed=36, keep_last=n, width=512)
+        q, o, lse = _attend(c, [n], 1, G, D, dtype)
+        for x in range(L - n // 2, L):
+            c.v_pool[int(c.t[0, x // 16]), x % 16] = float("inf") if x % 2 else float("nan")
+        q2, o2, lse2 = _attend(c, [n], 1, G, D, dtype, check=False)
+        m = n - n // 2
+        assert torch.equal(o[:m], o2[:m]) and torch.equal(lse, lse2)
+        assert not torch.isfinite(o2[m:]).any()
+
+
+def test_graphs_of_one_workspace():
+    """Two captured calls of different sizes on one workspace, replayed in turn over other lengths: tiles in
+    pieces, whole tiles and short rows, each replay equal to the eager call."""
+    import paper_2606_28831_amd as hk
+    Hkv, G, D, width = 2, 4, 128, 300
+    c = Cache([4000, 3000, 700, 690, 2500, 2600], D, "bf16", seed=31, width=width, keep_last=300, holes=0.1)
+    d, scale = hk.dims(3, Hkv * G, Hkv, D), 1 / math.sqrt(D)
+    calls, ws = [], None
+    for T, most in ((400, 300), (24, 8)):
+        start = torch.zeros(4, dtype=I32, device=DEV)
+        ch = hk.Chunks(start, T, most)
+        q = torch.zeros(T, Hkv * G, D, dtype=torch.bfloat16, device=DEV)
+        o = [torch.zeros_like(q) for _ in range(2)]
+        lse = [torch.zeros(T, Hkv * G, device=DEV) for _ in range(2)]
+        ws = hk.chunk_attn_workspace(d, ch, width, DEV) if ws is None else ws     # the larger call's
+        own = hk.chunk_attn_workspace(d, ch, width, DEV)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            hk.hk_chunk_attn(d, c.kv, ch, q, scale, o[1], ws, lse=lse[1])
+        calls.append((ch, start, q, o, lse, own, graph))
+    for lens in (([300, 1, 99], [8, 8, 8]), ([1, 2, 3], [1, 0, 8]), ([0, 0, 300], [0, 0, 0]), ([130, 140, 130], [5, 6, 7])):
+        for (ch, start, q, o, lse, own, graph), n in zip(calls, lens):
+            start.copy_(torch.tensor(np.concatenate([[0], np.cumsum(n)]), device=DEV).to(I32))
+            q.copy_(torch.randn(q.shape, device=DEV).bfloat16())
+            hk.hk_chunk_attn(d, c.kv, ch, q, scale, o[0], own, lse=lse[0])
+        for _ in range(2):
+            for call in calls:
+                call[6].replay()
+        torch.cuda.synchronize()
+        for ch, start, q, o, lse, own, graph in calls:
+            assert torch.equal(o[0], o[1]) and torch.equal(lse[0], lse[1]), lens
+
+
 def test_chunks_out_of_bounds_stay_in_bounds():
     """Starts outside the rows or descending, chunks over max_len: every access stays within the rows,
     and the sequences that are as promised have their results."""
