@@ -416,17 +416,21 @@ __device__ __forceinline__ Tile tile_of(const Args& a, int u, int kv) {
 constexpr int TILE_WG = 512, PLAN_TILES = 1024, PLAN_PIECES = 1536;
 constexpr int SPLITS[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}, N_SPLITS = sizeof(SPLITS) / sizeof(SPLITS[0]);
 constexpr int MAX_STATES = 64;                // pieces of a row at most
+__device__ __forceinline__ int piece_length(int most, int c) { return (most + SPLITS[c] - 1) / SPLITS[c]; }
 // What a piece costs beside its steps, in steps of its type: its start, or that and its state's way to
 // the merge; and what a step costs where a CU has one workgroup, in tenths of one where it has two.
+// From timings with every split forced (bf16, 32/8 heads over 20000: 1024 tokens in 1, 2, 3, 4 pieces
+// 457, 359, 395, 385 us, 2560 in 1, 2, 3 1122, 977, 940; 256 in 4, 8 135, 132; fp32, 2 sequences over
+// 2000: 1, 2, 4, 8 177, 100, 58, 40).  STATE 10, 14, 18: 256 tokens 108, 108, 115 us, 16 tokens 43, 39, 39.
 template <typename T>
 struct Cost;
 template <>
 struct Cost<uint16_t> {
-  static constexpr int START = 7, STATE = 18, ALONE = 7;
+  static constexpr int START = 7, STATE = 14, ALONE = 7;
 };
 template <>
 struct Cost<float> {
-  static constexpr int START = 2, STATE = 4, ALONE = 5;
+  static constexpr int START = 2, STATE = 3, ALONE = 5;
 };
 
 struct TileSplit {                            // for the merge, by tile: its pieces and its rows
@@ -437,7 +441,7 @@ template <int NT>
 struct Planned {
   int first[PLAN_TILES + 1];                  // piece that a tile begins at
   int sum[NT / 64], most[NT / 64];
-  int pieces[N_SPLITS][NT / 64], whole[N_SPLITS][NT / 64];
+  uint32_t pieces[N_SPLITS][NT / 64];         // and nearly whole ones, in the upper half
 };
 // Counts the pieces of all tiles (into s.first); returns their length in steps.
 template <typename T, int NT>
@@ -469,21 +473,16 @@ __device__ __forceinline__ int plan_tiles(const Args& a, Planned<NT>& s) {
   most = max(most, 1);
 #pragma unroll
   for (int c = 0; c < N_SPLITS; ++c) {
-    const uint32_t len = (uint32_t)(most + SPLITS[c] - 1) / SPLITS[c];
-    uint32_t pieces = 0, whole = 0;
+    const int len = piece_length(most, c);
+    uint32_t pieces = 0;                      // a wave's tiles have at most 256 x 64
 #pragma unroll
     for (int j = 0; j < MOST; ++j)
       if (j < per) {
-        const uint32_t x = (uint32_t)k[j] / len, rest = (uint32_t)k[j] - x * len;
-        whole += x + (rest > len - len / 8);
-        pieces += x + (rest > 0);
+        const int x = k[j] / len, rest = k[j] - x * len;
+        pieces += (uint32_t)(x + (rest > 0) + ((x + (rest > len - len / 8)) << 16));
       }
     pieces = wave_reduce_u32(pieces, 0u, add);
-    whole = wave_reduce_u32(whole, 0u, add);
-    if (lane == 63) {
-      s.pieces[c][wave] = (int)pieces;
-      s.whole[c][wave] = (int)whole;
-    }
+    if (lane == 63) s.pieces[c][wave] = pieces;
   }
   __syncthreads();
   // the cheapest, in tenths of a step: rounds of (nearly) whole pieces, or an even share of all steps,
@@ -491,12 +490,12 @@ __device__ __forceinline__ int plan_tiles(const Args& a, Planned<NT>& s) {
   int best = 0x7fffffff, length = most;
 #pragma unroll
   for (int c = 0; c < N_SPLITS; ++c) {
-    const int len = (most + SPLITS[c] - 1) / SPLITS[c];
+    const int len = piece_length(most, c);
     int pieces = 0, whole = 0;
 #pragma unroll
     for (int w = 0; w < NT / 64; ++w) {
-      pieces += s.pieces[c][w];
-      whole += s.whole[c][w];
+      pieces += (int)(s.pieces[c][w] & 0xffffu);
+      whole += (int)(s.pieces[c][w] >> 16);
     }
     const int extra = c ? Cost<T>::STATE : Cost<T>::START, rest = whole % TILE_WG;
     const int last = rest == 0 ? 0 : Cost<T>::ALONE + (10 - Cost<T>::ALONE) * max(rest - TILE_WG / 2, 0) / (TILE_WG / 2);
@@ -586,8 +585,9 @@ struct Pieces {
   }
 };
 
-// fp32: a wave takes 32 rows; the next tile's pages load while a tile is computed.  Bound by the
-// fp32 matrix rate, which is a sixteenth of bf16's.
+// fp32: four waves take 32 rows each; the next tile's pages load while a tile is computed.  Bound by
+// the fp32 matrix rate, a sixteenth of bf16's (154 TFLOP/s in a large product): 16 sequences of up to
+// 203 tokens over 2000, 32/8 heads of 64: 318 us, 96 TFLOP/s (tiles of 256 rows: 497).
 template <int D, bool PLANNED>
 __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void chunk_tile_f32_kernel(Args a) {
   using L = TileLayout<float, D>;
@@ -736,6 +736,9 @@ __device__ __forceinline__ void direct_wait() { asm volatile("s_waitcnt vmcnt(%0
 // maximum; MFMAs and the vector work between them are laid out by hand.  Two workgroups a CU, for
 // one's start, end and waits to be beside the other's work (measured against one of eight waves and
 // tiles of 64 keys, 8 prompts of 4096 tokens, 32 / 8 heads: D 128 1152 us and 1172, D 64 697 and 786).
+// Bound by the products (2048 cycles of each SIMD for 64 keys) beside as many cycles of exponentials,
+// sums and maxima, which overlap in part, and LDS reads at half their rate: 950 to 980 TFLOP/s, of
+// 1231 in a large library product; the products alone run at 1363.
 // Waves 0 and 1 bring a page of K each, three tiles ahead of the wait for it, waves 2 and 3 the pages
 // of V.
 template <int D, bool PLANNED>
@@ -1241,7 +1244,9 @@ __device__ __forceinline__ void join_waves(const Args& a, const Piece& w, const 
 }
 
 // Pages go through a wave's own part of LDS, two of K and two of V a step, and are requested a step
-// ahead.  Two workgroups a CU for bf16.  Bound by HBM reads.
+// ahead.  Two workgroups a CU for bf16.  Bound by HBM reads: 64 sequences of 1 to 8 tokens over 784 to
+// 5600, 32/8 heads of 128: 167 us, 5.0 TB/s of pages; 164 without the products and the softmax, and no
+// faster with twice the loads in flight or with more workgroups (1024: 178).
 template <typename T, int D>
 __global__ __launch_bounds__(SHORT_NT, sizeof(T) == 2 ? 2 : 1) void chunk_short_kernel(Args a) {
   using L = TileLayout<T, D>;
@@ -1332,7 +1337,8 @@ __global__ __launch_bounds__(SHORT_NT, sizeof(T) == 2 ? 2 : 1) void chunk_short_
 
 // ------------------------------------------------------------------ merge
 // D / 4 lanes per query: the states of its row's pieces, in their order.  Lanes read the references and
-// sums of the pieces (at most 64) side by side, and four dims of four pieces' outputs at a time.
+// sums of the pieces (at most 64) side by side, and four dims of eight pieces' outputs at a time.
+// Bound by reading the states: 17 us for 50 MB.
 constexpr int MERGE_NT = 256;
 template <int D>
 constexpr int MERGE_ROWS = MERGE_NT / (D / 4);                   // of a workgroup at a time
@@ -1454,7 +1460,8 @@ static void launch(const Args& a, hipStream_t st, const Plan& p) {
     if (p.heads > 0) hipLaunchKernelGGL((chunk_short_kernel<T, D>), dim3(SHORT_WG), dim3(SHORT_NT), 0, st, a);
   }
   const int tiles = p.pieces ? p.tiles * a.Hkv : 0;
-  const int tile_y = std::max(std::min(2048 / std::max(tiles, 1), TILE_ROWS / MERGE_ROWS<D>), 4);
+  // (one prompt of 500 among 31 single tokens, 392 tiles: 143 us, with 2048 here 149; others equal)
+  const int tile_y = std::max(std::min(8192 / std::max(tiles, 1), TILE_ROWS / MERGE_ROWS<D>), 4);
   if (tiles * tile_y + p.heads * MERGE_Y == 0) return;
   TimedLaunch t(HK_TK_CHUNK_MERGE, st);
   hipLaunchKernelGGL((chunk_merge_kernel<T, D>), dim3(tiles * tile_y + p.heads * MERGE_Y), dim3(MERGE_NT), 0, st, a,
