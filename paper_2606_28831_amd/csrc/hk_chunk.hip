@@ -411,12 +411,15 @@ __device__ __forceinline__ Tile tile_of(const Args& a, int u, int kv) {
 
 // A launch of many tiles has a workgroup for each, the largest of a sequence first.  One of few
 // (PLANNED) has at most TILE_WG workgroups, which see from the rows' lengths into how many pieces to
-// split the tiles: pieces of one length, that of the longest tile over one of SPLITS, so that the
-// pieces of a KV head's tiles that run beside one another read the same pages.
+// split the tiles: pieces of one length, that of the longest tile over one of twelve numbers, so that
+// the pieces of a KV head's tiles that run beside one another read the same pages.
 constexpr int TILE_WG = 512, PLAN_TILES = 1024, PLAN_PIECES = 1536;
-constexpr int SPLITS[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}, N_SPLITS = sizeof(SPLITS) / sizeof(SPLITS[0]);
-constexpr int MAX_STATES = 64;                // pieces of a row at most
-__device__ __forceinline__ int piece_length(int most, int c) { return (most + SPLITS[c] - 1) / SPLITS[c]; }
+constexpr int N_SPLITS = 12, MAX_STATES = 64; // choices, and pieces of a row at most
+// length of a piece, choice c: the longest tile over 1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48 or 64
+__device__ __forceinline__ int piece_length(int most, int c) {
+  const int n = c == 0 ? 1 : c & 1 ? 2 << (c >> 1) : 3 << ((c >> 1) - 1);
+  return (most + n - 1) / n;
+}
 // What a piece costs beside its steps, in steps of its type: its start, or that and its state's way to
 // the merge; and what a step costs where a CU has one workgroup, in tenths of one where it has two.
 // From timings with every split forced (bf16, 32/8 heads over 20000: 1024 tokens in 1, 2, 3, 4 pieces
@@ -441,7 +444,7 @@ template <int NT>
 struct Planned {
   int first[PLAN_TILES + 1];                  // piece that a tile begins at
   int sum[NT / 64], most[NT / 64];
-  uint32_t pieces[N_SPLITS][NT / 64];         // and nearly whole ones, in the upper half
+  int pieces[N_SPLITS], whole[N_SPLITS];      // by choice of their length; whole: nearly all of it
 };
 // Counts the pieces of all tiles (into s.first); returns their length in steps.
 template <typename T, int NT>
@@ -454,9 +457,11 @@ __device__ __forceinline__ int plan_tiles(const Args& a, Planned<NT>& s) {
   for (int j = 0; j < MOST; ++j) {
     const int i = threadIdx.x * per + j;
     k[j] = j < per && i < n ? tile_of(a, i % a.n_tiles, i / a.n_tiles).steps : 0;
+    if (j < per && i < n) s.first[i] = k[j];  // (until the pieces are counted)
     sum += k[j];
     most = max(most, k[j]);
   }
+  if (threadIdx.x < N_SPLITS) s.pieces[threadIdx.x] = s.whole[threadIdx.x] = 0;
   sum = (int)wave_reduce_u32((uint32_t)sum, 0u, add);
   most = (int)wave_reduce_u32((uint32_t)most, 0u, [](uint32_t p, uint32_t q) { return p > q ? p : q; });
   if (lane == 63) {
@@ -471,40 +476,35 @@ __device__ __forceinline__ int plan_tiles(const Args& a, Planned<NT>& s) {
     most = max(most, s.most[w]);
   }
   most = max(most, 1);
-#pragma unroll
-  for (int c = 0; c < N_SPLITS; ++c) {
-    const int len = piece_length(most, c);
-    uint32_t pieces = 0;                      // a wave's tiles have at most 256 x 64
-#pragma unroll
-    for (int j = 0; j < MOST; ++j)
-      if (j < per) {
-        const int x = k[j] / len, rest = k[j] - x * len;
-        pieces += (uint32_t)(x + (rest > 0) + ((x + (rest > len - len / 8)) << 16));
-      }
-    pieces = wave_reduce_u32(pieces, 0u, add);
-    if (lane == 63) s.pieces[c][wave] = pieces;
+  constexpr int GROUPS = NT / N_SPLITS;       // a thread takes one length and every GROUPS-th tile
+  if (threadIdx.x < GROUPS * N_SPLITS) {
+    const int c = threadIdx.x % N_SPLITS, len = piece_length(most, c);
+    const float inv = 1.f / (float)len;
+    int pieces = 0, whole = 0;
+    for (int i = threadIdx.x / N_SPLITS; i < n; i += GROUPS) {
+      const int steps = s.first[i];
+      int x = (int)((float)steps * inv), rest = steps - x * len;       // (x at most 64: off by one at most)
+      if (rest < 0) --x, rest += len;
+      if (rest >= len) ++x, rest -= len;
+      pieces += x + (rest > 0);
+      whole += x + (rest > len - len / 8);
+    }
+    atomicAdd(&s.pieces[c], pieces);
+    atomicAdd(&s.whole[c], whole);
   }
   __syncthreads();
   // the cheapest, in tenths of a step: rounds of (nearly) whole pieces, or an even share of all steps,
-  // and a quarter piece of unevenness where not all pieces run at once
-  int best = 0x7fffffff, length = most;
+  // and a quarter piece of unevenness where not all pieces run at once; lane c of 16 computes choice c
+  const int c = min(lane & 15, N_SPLITS - 1), len = piece_length(most, c), pieces = s.pieces[c], whole = s.whole[c];
+  const int extra = c ? Cost<T>::STATE : Cost<T>::START, rest = whole % TILE_WG;
+  const int last = rest == 0 ? 0 : Cost<T>::ALONE + (10 - Cost<T>::ALONE) * max(rest - TILE_WG / 2, 0) / (TILE_WG / 2);
+  const int rounds = (whole / TILE_WG * 10 + last) * (len + extra);
+  const int share = (sum + extra * pieces) / (TILE_WG / 10) + (pieces > TILE_WG ? len * 10 / 4 : 0);
+  const bool fits = c == 0 || pieces <= PLAN_PIECES;
+  int best = fits ? min(max(rounds, share), (1 << 27) - 1) << 4 | c : 0x7fffffff;
 #pragma unroll
-  for (int c = 0; c < N_SPLITS; ++c) {
-    const int len = piece_length(most, c);
-    int pieces = 0, whole = 0;
-#pragma unroll
-    for (int w = 0; w < NT / 64; ++w) {
-      pieces += (int)(s.pieces[c][w] & 0xffffu);
-      whole += (int)(s.pieces[c][w] >> 16);
-    }
-    const int extra = c ? Cost<T>::STATE : Cost<T>::START, rest = whole % TILE_WG;
-    const int last = rest == 0 ? 0 : Cost<T>::ALONE + (10 - Cost<T>::ALONE) * max(rest - TILE_WG / 2, 0) / (TILE_WG / 2);
-    const int cost = max((whole / TILE_WG * 10 + last) * (len + extra), (sum + extra * pieces) / (TILE_WG / 10) + (pieces > TILE_WG ? len * 10 / 4 : 0));
-    if (cost < best && (c == 0 || pieces <= PLAN_PIECES)) {
-      best = cost;
-      length = len;
-    }
-  }
+  for (int o = 1; o < 16; o <<= 1) best = min(best, __shfl_xor(best, o, 64));
+  const int length = piece_length(most, best & 15);
   int x = 0;
 #pragma unroll
   for (int j = 0; j < MOST; ++j) {
