@@ -446,7 +446,8 @@ struct Planned {
   int sum[NT / 64], most[NT / 64];
   int pieces[N_SPLITS], whole[N_SPLITS];      // by choice of their length; whole: nearly all of it
 };
-// Counts the pieces of all tiles (into s.first); returns their length in steps.
+// Counts the pieces of all tiles (into s.first); returns their length in steps.  The lengths are tried
+// side by side (one after the other, unrolled or not: 3 and 6 us more a launch).
 template <typename T, int NT>
 __device__ __forceinline__ int plan_tiles(const Args& a, Planned<NT>& s) {
   const int n = a.n_tiles * a.Hkv, per = (n + NT - 1) / NT, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -537,7 +538,8 @@ __device__ __forceinline__ int plan_tiles(const Args& a, Planned<NT>& s) {
   if (blockIdx.x == gridDim.x - 1)            // (often without a piece)
     for (int i = threadIdx.x; i < n; i += NT) {
       const Tile w = tile_of(a, i % a.n_tiles, i / a.n_tiles);
-      reinterpret_cast<TileSplit*>(a.tile_split)[i] = {s.first[i], s.first[i + 1] - s.first[i], w.c.first, w.rows, w.r0, w.kv};
+      reinterpret_cast<TileSplit*>(a.tile_split)[i] = {s.first[i], s.first[i + 1] - s.first[i], w.c.first, w.rows,
+                                                       w.r0, w.kv};
     }
   return length;
 }
@@ -820,7 +822,8 @@ __global__ __launch_bounds__(256, 2) void chunk_tile_bf16_kernel(Args a) {
       if (lane == 0) s_odd[slot][my] = odd;
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     };
-    auto unseen = [&](int t) { return (w.p0 + 2 * t + 2) * HK_PAGE > tile_seen; };  // some keys of tile t, by some query
+    // some keys of tile t, by some query
+    auto unseen = [&](int t) { return (w.p0 + 2 * t + 2) * HK_PAGE > tile_seen; };
     const uint32_t lds_k = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)s_k[0];
     const uint32_t lds_v = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)s_v[0];
 
@@ -1338,7 +1341,7 @@ __global__ __launch_bounds__(SHORT_NT, sizeof(T) == 2 ? 2 : 1) void chunk_short_
 // ------------------------------------------------------------------ merge
 // D / 4 lanes per query: the states of its row's pieces, in their order.  Lanes read the references and
 // sums of the pieces (at most 64) side by side, and four dims of eight pieces' outputs at a time.
-// Bound by reading the states: 17 us for 50 MB.
+// Bound by reading the states: 12 us for 30 MB.
 constexpr int MERGE_NT = 256;
 template <int D>
 constexpr int MERGE_ROWS = MERGE_NT / (D / 4);                   // of a workgroup at a time
@@ -1401,7 +1404,8 @@ __global__ __launch_bounds__(MERGE_NT) void chunk_merge_kernel(Args a, int tile_
     for (r += blockIdx.x % tile_y * MERGE_ROWS<D>; r < min(TILE_ROWS, t.rows - t.r0); r += tile_y * MERGE_ROWS<D>) {
       const int tok = (t.r0 + r) / a.G;
       const int64_t row = (int64_t)(t.first + tok) * a.Hq + t.kv * a.G + (t.r0 + r - tok * a.G);
-      merge_states<T, D>(a, row, t.used, a.tile_o, a.tile_ml, [&](int j) { return (int64_t)(t.at + j) * TILE_ROWS + r; });
+      merge_states<T, D>(a, row, t.used, a.tile_o, a.tile_ml,
+                         [&](int j) { return (int64_t)(t.at + j) * TILE_ROWS + r; });
     }
     return;
   }

@@ -238,8 +238,9 @@ __global__ __launch_bounds__(64) void trim_count_kernel(int n_heads, int Hkv, in
 }
 
 // LANES lanes per head: a wave where heads are few, for long cuts; eight where they are many and
-// cuts are a few pages (16384 heads, 8 tokens: 5.0 us, a wave each 9.4).  The stack holds every page of the pool (checked by the caller), so a push
-// only misses where the tables list more pages than there are: such a page is not pushed.
+// cuts are a few pages (16384 heads, 8 tokens: 5.0 us, a wave each 9.4).  The stack holds every page
+// of the pool (checked by the caller), so a push only misses where the tables list more pages than
+// there are: such a page is not pushed.
 template <int LANES>
 __global__ __launch_bounds__(SL_NT) void trim_write_kernel(int n_heads, int Hkv, int n_seq,
                                                            const int32_t* __restrict__ n_drop,
