@@ -420,6 +420,8 @@ typedef struct {
   int32_t n_seq;         /* sequences of the batch                                      */
   int32_t n_tokens;      /* rows of the token tensors                                   */
   int32_t max_len;       /* no chunk is longer                                          */
+  int32_t* granted;      /* device word or NULL: hk_reserve_slots sets it to 1, or to 0 where
+                            it refused; hk_verify_draft takes chunks at 0 as empty ones  */
 } hk_chunks;
 
 /* Slots for the chunks at the rows' ends.  Token i of a chunk of len goes to logical slot
@@ -434,8 +436,9 @@ typedef struct {
  *            padding; K row r of the pool as [16 * num_pages][D] is then slot_map's.
  * All or nothing: if the free list is too short or a row would pass max_pages (HK_FLAG_NOSPACE),
  * or the chunks are not as promised (HK_FLAG_CHUNK), the cache is left as it was and slot_map is
- * all -1, so that hk_write_kv writes nothing; hk_chunk_attn then reads the rows as they are, and
- * hk_trim_slots must not be called for the slots that were never given.
+ * all -1, so that hk_write_kv writes nothing; hk_chunk_attn then reads the rows as they are, so that
+ * what it returns means nothing, and hk_trim_slots must not be called for the slots that were never
+ * given: with chunks->granted hk_verify_draft sees to it (it drops none), also in a captured graph.
  * Until hk_write_kv has run the new slots hold what the pool held.
  * workspace: >= hk_workspace_size(HK_OP_RESERVE) bytes, 256-byte aligned.
  * HK_ERR_ARG for null pointers or sizes below 1, HK_ERR_SHAPE unless NS % n_seq == 0, n_tokens and
@@ -492,7 +495,8 @@ hk_status hk_chunk_attn(const hk_dims* dims, const hk_paged_kv* kv, const hk_chu
  *   weight[v] = max(0, F(p[a + r][v]) - F(q[a + r + 1][v])) where a draft was rejected (with q NULL:
  *   F(p) without the rejected token), F(p[a + r][v]) where none was or where the former sum is 0;
  * -1 if every weight is 0.  Whole numbers throughout: the same inputs give the same tokens whatever
- * the batch.  An empty chunk gives 0, -1, 0.
+ * the batch.  An empty chunk gives 0, -1, 0, and so does every chunk of a batch whose slots were refused
+ * (*chunks->granted is 0; NULL: none were).
  *   tokens [n_tokens] int32; u [n_tokens] fp32; p row t at p + t * p_row_stride, q likewise, in
  *   `dtype` (HK_F32 or HK_BF16), strides in elements, >= V, any alignment of the type
  *   n_accept, next_token, n_drop [n_seq] int32; n_drop is what hk_trim_slots takes

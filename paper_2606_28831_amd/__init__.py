@@ -74,7 +74,7 @@ class hk_allocator(C.Structure):
 
 class hk_chunks(C.Structure):
     _fields_ = [("start", C.c_void_p), ("n_seq", C.c_int32), ("n_tokens", C.c_int32),
-                ("max_len", C.c_int32)]
+                ("max_len", C.c_int32), ("granted", C.c_void_p)]
 
 
 _lib = None
@@ -447,14 +447,24 @@ def hk_compact_modes(d: hk_dims, kv: PagedKV, sel_bits, L_dense: int, head_mode,
 # its end) and run on the tensors' own device, on its current stream unless one is given.
 class Chunks:
     """The new tokens of a batch: sequence s has the token rows start[s] .. start[s + 1] of
-    n_tokens (start: int32 device tensor of n_seq + 1 entries), at most max_len of them."""
+    n_tokens (start: int32 device tensor of n_seq + 1 entries), at most max_len of them.
+    granted: None, or an int32 device word that hk_reserve_slots sets to 1 or, where it refused, to
+    0: hk_verify_draft then takes the chunks as empty, so that nothing is dropped that was not given."""
 
-    def __init__(self, start, n_tokens: int, max_len: int):
+    def __init__(self, start, n_tokens: int, max_len: int, granted=None):
         if start.dtype != torch.int32 or start.dim() != 1 or not start.is_contiguous():
             raise HardKVError("chunk starts must be a contiguous int32 vector")
         self.start, self.n_tokens, self.max_len = start, int(n_tokens), int(max_len)
         self.n_seq = start.numel() - 1
         self.desc = hk_chunks(start.data_ptr(), self.n_seq, self.n_tokens, self.max_len)
+        self.granted_by(granted)
+
+    def granted_by(self, word):
+        """The word that later calls set and read (None: none)."""
+        if word is not None and (word.dtype != torch.int32 or word.numel() < 1 or word.device != self.start.device):
+            raise HardKVError("granted must be an int32 word on the chunk starts' device")
+        self.granted = word
+        self.desc.granted = None if word is None else word.data_ptr()
 
 
 def _need(ok: bool, what: str):

@@ -117,7 +117,7 @@ __global__ __launch_bounds__(SL_NT) void reserve_write_kernel(
     int touched, uint32_t n_table, int32_t* __restrict__ table, uint16_t* __restrict__ masks,
     int32_t* __restrict__ n_pages, int max_pages, const int32_t* __restrict__ free_ids,
     int32_t* __restrict__ free_top, int capacity, int64_t* __restrict__ slot_map,
-    int32_t* __restrict__ status, const void* ws) {
+    int32_t* __restrict__ status, int32_t* __restrict__ granted, const void* ws) {
   __shared__ int32_t s_before[SL_BLOCKS];
   __shared__ int s_refuse;
   const SlotWs w = slot_ws(const_cast<void*>(ws), n_heads);
@@ -135,6 +135,7 @@ __global__ __launch_bounds__(SL_NT) void reserve_write_kernel(
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     if (ok) *free_top = first_pop;
     else if (status) atomicOr(status, refuse);
+    if (granted) *granted = ok;
   }
   if (blockIdx.x < n_table) {
     const size_t e = (size_t)blockIdx.x * SL_NT + threadIdx.x;
@@ -300,7 +301,7 @@ hipError_t hk_launch_reserve(int n_heads, int Hkv, const hk_paged_kv* kv, const 
   hipLaunchKernelGGL(reserve_write_kernel, dim3((uint32_t)(n_table + n_map)), dim3(SL_NT), 0, st, n_heads, Hkv,
                      ch->n_seq, ch->start, ch->n_tokens, ch->max_len, touched, (uint32_t)n_table, kv->page_table,
                      kv->page_mask, kv->n_pages, kv->max_pages, alloc->free_ids, alloc->free_top, alloc->capacity,
-                     slot_map, status, ws);
+                     slot_map, status, ch->granted, ws);
   return hipGetLastError();
 }
 

@@ -126,15 +126,24 @@ __device__ __forceinline__ void weigh(const float (&a)[N], const float (&b)[N], 
   odd = (__any(odd & HK_FLAG_NAN) ? HK_FLAG_NAN : 0) | (__any(odd & HK_FLAG_RANGE) ? HK_FLAG_RANGE : 0);
 }
 
+// The chunk of sequence s; an empty one where the batch's slots were refused.
+__device__ __forceinline__ Chunk granted_chunk(const int32_t* __restrict__ start, int s, int n_tokens, int max_len,
+                                               const int32_t* __restrict__ granted) {
+  const int given = granted ? *granted : 1;
+  Chunk c = chunk_of(start, s, n_tokens, max_len);
+  if (given == 0) c.len = 0;
+  return c;
+}
+
 template <typename T>
 __global__ __launch_bounds__(VF_NT) void verify_mass_kernel(
-    int n_seq, int V, const int32_t* __restrict__ start, int n_tokens, int max_len,
+    int n_seq, int V, const int32_t* __restrict__ start, int n_tokens, int max_len, const int32_t* __restrict__ granted,
     const int32_t* __restrict__ tokens, const T* __restrict__ p, int64_t p_row, const T* __restrict__ q,
     int64_t q_row, const float* __restrict__ u, int32_t* __restrict__ n_accept, int32_t* __restrict__ n_drop,
     int32_t* __restrict__ status, unsigned long long* __restrict__ mass) {
   __shared__ unsigned long long s_red[VF_NT / 64];
   const int s = blockIdx.y, piece = blockIdx.x;
-  const Chunk c = chunk_of(start, s, n_tokens, max_len);
+  const Chunk c = granted_chunk(start, s, n_tokens, max_len, granted);
   const int kept = c.len > 0 ? kept_drafts(c, V, tokens, p, p_row, q, q_row, u) : 0;
   if (piece == 0 && threadIdx.x == 0) {
     n_accept[s] = kept;
@@ -171,14 +180,14 @@ __device__ __forceinline__ unsigned long long wave_scan_u64(unsigned long long x
 
 template <typename T>
 __global__ __launch_bounds__(VF_NT) void verify_pick_kernel(
-    int V, const int32_t* __restrict__ start, int n_tokens, int max_len, const int32_t* __restrict__ tokens,
-    const T* __restrict__ p, int64_t p_row, const T* __restrict__ q, int64_t q_row, const float* __restrict__ u,
-    const int32_t* __restrict__ n_accept, const unsigned long long* __restrict__ mass, int pieces,
+    int V, const int32_t* __restrict__ start, int n_tokens, int max_len, const int32_t* __restrict__ granted,
+    const int32_t* __restrict__ tokens, const T* __restrict__ p, int64_t p_row, const T* __restrict__ q, int64_t q_row,
+    const float* __restrict__ u, const int32_t* __restrict__ n_accept, const unsigned long long* __restrict__ mass, int pieces,
     int32_t* __restrict__ next_token) {
   __shared__ unsigned long long s_red[VF_NT / 64], s_before;
   __shared__ int s_piece;
   const int s = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const Chunk c = chunk_of(start, s, n_tokens, max_len);
+  const Chunk c = granted_chunk(start, s, n_tokens, max_len, granted);
   if (c.len <= 0) {
     if (threadIdx.x == 0) next_token[s] = -1;
     return;
@@ -246,10 +255,10 @@ static void launch_verify(int n_seq, int V, const hk_chunks* ch, const int32_t* 
   const int pieces = (V + VF_PIECE - 1) / VF_PIECE;
   unsigned long long* mass = static_cast<unsigned long long*>(ws);
   hipLaunchKernelGGL(verify_mass_kernel<T>, dim3(pieces, n_seq), dim3(VF_NT), 0, st, n_seq, V, ch->start, ch->n_tokens,
-                     ch->max_len, tokens, static_cast<const T*>(p), p_row, static_cast<const T*>(q), q_row, u,
+                     ch->max_len, ch->granted, tokens, static_cast<const T*>(p), p_row, static_cast<const T*>(q), q_row, u,
                      n_accept, n_drop, status, mass);
   hipLaunchKernelGGL(verify_pick_kernel<T>, dim3(n_seq), dim3(VF_NT), 0, st, V, ch->start, ch->n_tokens, ch->max_len,
-                     tokens, static_cast<const T*>(p), p_row, static_cast<const T*>(q), q_row, u, n_accept, mass,
+                     ch->granted, tokens, static_cast<const T*>(p), p_row, static_cast<const T*>(q), q_row, u, n_accept, mass,
                      pieces, next_token);
 }
 

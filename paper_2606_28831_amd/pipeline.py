@@ -233,6 +233,8 @@ class ChunkDecoder:
     trim(): the newest n_drop[s] tokens of every sequence taken back, in every layer.
     The buffers serve any chunks of at most max_tokens rows and max_len tokens a sequence.
     status collects FLAG_NOSPACE / FLAG_CHUNK: such a reserve() gave no slots (see hardkv.h).
+    granted says on the device whether the last reserve() gave them; its chunks carry the word on to
+    the Verifier, which drops nothing of refused chunks.  trim() itself always takes n_drop back.
     """
 
     def __init__(self, B, Hq, Hkv, D, kv: PagedKV, alloc: Allocator, max_tokens: int, max_len: int,
@@ -248,6 +250,7 @@ class ChunkDecoder:
         most = Chunks(torch.empty(B + 1, dtype=torch.int32), max_tokens, max_len)
         self.ws = chunk_attn_workspace(self.d, most, kv.max_pages, dev)
         self.status = torch.zeros(1, dtype=torch.int32, device=dev)
+        self.granted = torch.ones(1, dtype=torch.int32, device=dev)
 
     def _fits(self, chunks: Chunks):
         if chunks.n_seq != self.B or chunks.n_tokens > self.max_tokens or chunks.max_len > self.max_len:
@@ -256,6 +259,7 @@ class ChunkDecoder:
     def reserve(self, chunks: Chunks, slot_map, stream=None):
         """slot_map: [layers, n_tokens, Hkv] int64, written in full."""
         self._fits(chunks)
+        chunks.granted_by(self.granted)
         hk_reserve_slots(self.d_all, self.kv, chunks, self.alloc, self.ws_slots, slot_map=slot_map,
                          status=self.status, stream=stream)
 
@@ -306,7 +310,8 @@ class DecodeLoop:
     extend():   prompts in chunks, or the last token and its drafts: slots and K/V for every
                 layer, then one chunk attention per layer;
     accept():   drafts against the target's probabilities, the rejected ones taken back in
-                every layer.
+                every layer.  After an extend() whose slots were refused (status) it takes
+                nothing back and draws no token (-1): the cache stays as it was.
     Heads are ordered (layer, sequence, KV head); sequence index = layer * B + b.
     """
 
@@ -347,6 +352,7 @@ class DecodeLoop:
                stream=None):
         if self.chunked is None:
             raise HardKVError("the loop was made without max_tokens")
+        chunks.granted_by(self.chunked.granted)
         verifier.verify(chunks, tokens, p, u, n_accept, next_token, n_drop, q=q, stream=stream)
         self.chunked.trim(n_drop, stream=stream)
 
