@@ -473,7 +473,8 @@ hk_status hk_write_kv(const hk_dims* dims, const hk_paged_kv* kv, int32_t n_laye
  *   o    [n_tokens][Hq][D] in kv->dtype, 16-byte aligned
  *   lse  [n_tokens][Hq] fp32 or NULL
  * dims->NS == chunks->n_seq; Hq / Hkv at most 64, n_tokens * Hq at most 2^34.  Scores, sums and outputs are accumulated in
- * fp32; a bf16 cache's probabilities enter the product with V in bf16.
+ * fp32.  A bf16 cache's probabilities enter the product with V in two bf16 parts (16 bits and more) in
+ * chunks of up to 32 queries of a KV head (len * Hq / Hkv), rounded to bf16 once in longer ones.
  * workspace: >= hk_chunk_attn_workspace_size(dims, chunks, kv->max_pages) bytes, 256-byte aligned
  * (0 for some sizes: it may then be NULL); calls that overlap on one workspace race.
  */

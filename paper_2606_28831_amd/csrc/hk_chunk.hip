@@ -21,9 +21,13 @@
 // score exceeds it by 2^CH_SLACK, so most blocks need no rescaling.  Probabilities are formed as
 // exp2(z - m - bias), where 2^bias is at least 2^CH_SLACK times the keys of the row: sums of P V
 // and their merge cannot leave the fp32 range where the result does not.
-// Precision: scores, sums and outputs in fp32.  P enters the bf16 product rounded to nearest bf16:
-// an error of 2^-9 of each term, of the size of the output's own rounding; the row sum is taken
-// from the unrounded values, for the LSE.
+// Precision: scores, sums and outputs in fp32; the row sum, and so the LSE, is of the unrounded P.
+// Into the bf16 product P enters in the short kernel in two bf16 parts, to 2^-16 of each term: the
+// output is then off by its own rounding and little else, and as the kernel is bound by memory the
+// second product takes no time (64 sequences of 1 to 8 tokens over 784 to 5600: 175 us and 173,
+// single tokens 163 and 162).  In the tile kernel P is rounded once, to 2^-8 of each term at most: o
+// is off by 2.3e-3 of its norm instead of the 1.7e-3 of its own rounding, and a second part costs 31%
+// (8 prompts of 4096 1173 -> 1542 us, one chunk of 2048 over 28671 902 -> 1201).
 #include <algorithm>
 #include <type_traits>
 
@@ -135,14 +139,20 @@ struct Mma<uint16_t, D> {
     const int lane = threadIdx.x & 63, hi = lane >> 5, g1 = (lane >> 4) & 1, i16 = lane & 15;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      bf16x8 bp[NB];
+      __builtin_amdgcn_sched_barrier(0);        // (here and below: the fragments of one product at a time, 247
+                                                // registers at D 128; without, 256 and spills)
+      bf16x8 bp[NB], low[NB];                   // P = bp + low, to 2^-16 of it
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int j = 0; j < 8; j += 2) {
-          const bf16x2 t = __builtin_convertvector((f32x2{p[b][8 * s + j], p[b][8 * s + j + 1]}), bf16x2);
+          const f32x2 x = {p[b][8 * s + j], p[b][8 * s + j + 1]};
+          const bf16x2 t = __builtin_convertvector(x, bf16x2);
+          const bf16x2 r = __builtin_convertvector((f32x2{x[0] - (float)t[0], x[1] - (float)t[1]}), bf16x2);
           bp[b][j] = t[0];
           bp[b][j + 1] = t[1];
+          low[b][j] = r[0];
+          low[b][j + 1] = r[1];
         }
 #pragma unroll
       for (int dt = 0; dt < D / 32; ++dt) {
@@ -156,8 +166,11 @@ struct Mma<uint16_t, D> {
         }
         const bf16x8 av = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a[0], a[1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int b = 0; b < NB; ++b) {
+          acc[b][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, low[b], acc[b][dt], 0, 0, 0);
           acc[b][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, bp[b], acc[b][dt], 0, 0, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
   }

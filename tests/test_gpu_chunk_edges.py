@@ -65,3 +65,30 @@ def test_a_refused_chunk_takes_nothing_back(graph):
             assert ok
             c.t, c.m, c.n, c.free, c.top = CO.trim(c.t, c.m, c.n, c.free, c.top, got[2], Hkv)
         c.check(starts)
+
+
+# ------------------------------------------------------------------ the bits of short chunks
+@pytest.mark.parametrize("D,G,lens,ctx", [
+    (128, 4, [1, 8, 3, 0], [0, 1, 500, 20]), (64, 8, [4, 1, 2], [3, 0, 900]),
+    (128, 1, [1, 32, 1], [0, 2, 1500]), (64, 3, [10, 1], [0, 40])])
+def test_short_chunks_keep_the_bits_of_their_probabilities(D, G, lens, ctx):
+    """Drafts and single tokens of a bf16 cache are off by the rounding of their output and little else,
+    as the framework's decode is: probabilities enter the product with V in two bf16 parts, off by half a
+    step of the second, 2^-8 of the 2^-8 that the first leaves.  A query that sees one key has its V."""
+    rows = [a + n for a, n in zip(ctx, lens) for _ in range(2)]
+    c = Cache(rows, D, "bf16", holes=0.2, seed=40 + G, keep_last=max(lens))
+    q, o, lse = _attend(c, lens, 2, G, D, "bf16")
+    first = [sum(lens[:s]) for s in range(len(lens))]
+    qn, on = np64(q), np64(o)
+    for h in range(len(rows)):
+        s, kv = divmod(h, 2)
+        n, a, g = lens[s], first[s], slice(kv * G, kv * G + G)
+        if n == 0:
+            continue
+        k, v, valid, end = c.head(h)
+        ro, rl, zabs, absv = CO.chunk_attn_head(qn[a:a + n, g], k, v, valid, end, 1 / math.sqrt(D))
+        dz, rest = (D + 8) * 2.0 ** -23 * zabs, (len(valid) / 32 + 64) * 2.0 ** -23
+        bo = 2.0 ** -8 * np.abs(ro) * 1.01 + (2.0 ** -16 + 2 * dz[..., None] + 2 * rest) * 1.05 * absv
+        assert (np.abs(on[a:a + n, g] - ro) <= bo).all(), h
+        if valid[:end - n + 1].sum() == 1:
+            assert (on[a, g] == v[np.nonzero(valid)[0][0]]).all()
