@@ -226,6 +226,24 @@ class PagedKV:
         self.desc = hk_paged_kv(k_pool.data_ptr(), v_pool.data_ptr() if v_pool is not None else None,
                                 page_table.data_ptr(), page_mask.data_ptr(), n_pages.data_ptr(),
                                 k_pool.shape[0], page_table.shape[1], dt)
+        self._sizes = None
+
+    def sizes(self):
+        """(heads, head size, device) that the tensors of desc hold, once they are found to agree."""
+        if self._sizes is None:
+            t, m, n, k, v = self.page_table, self.page_mask, self.n_pages, self.k_pool, self.v_pool
+            of = lambda x: x is None or (x.is_contiguous() and x.get_device() == k.get_device())  # noqa: E731
+            if not all(of(x) for x in (t, m, n, k, v)):
+                raise HardKVError("a cache's tensors must be contiguous and on one device")
+            if (t.dtype != torch.int32 or n.dtype != torch.int32 or m.dtype not in (torch.int16, torch.uint16)
+                    or t.dim() != 2 or m.dim() != 2 or m.shape[1] != t.shape[1]):
+                raise HardKVError("a cache's tables must be int32 [heads, pages], masks 16-bit [heads, pages], "
+                                  "counts int32 [heads]")
+            slots = k.shape[0] * 16
+            if slots == 0 or k.numel() % slots or (v is not None and (v.dtype != k.dtype or v.numel() != k.numel())):
+                raise HardKVError("a cache's pools must be [pages, 16, D], both in one type")
+            self._sizes = min(t.shape[0], m.shape[0], n.numel()), k.numel() // slots, k.get_device()
+        return self._sizes
 
     def rows(self, first_head: int, n_heads: int) -> "PagedKV":
         """A view of heads [first_head, first_head + n_heads) (e.g. one layer)."""
@@ -242,6 +260,17 @@ class Allocator:
     def __init__(self, free_ids, free_top):
         self.free_ids, self.free_top = free_ids, free_top
         self.desc = hk_allocator(free_ids.data_ptr(), free_top.data_ptr(), free_ids.shape[0])
+        self._device = None
+
+    def device(self):
+        """The device of desc's tensors, once they are found to be what it says."""
+        if self._device is None:
+            ids, top = self.free_ids, self.free_top
+            if (ids.dtype != torch.int32 or top.dtype != torch.int32 or ids.dim() != 1 or not ids.is_contiguous()
+                    or top.numel() < 1 or ids.get_device() != top.get_device()):
+                raise HardKVError("an allocator's stack and top must be contiguous int32, on one device")
+            self._device = ids.get_device()
+        return self._device
 
 
 def hk_workspace_size(op: int, d: hk_dims, max_pages: int) -> int:
@@ -444,7 +473,8 @@ def hk_compact_modes(d: hk_dims, kv: PagedKV, sel_bits, L_dense: int, head_mode,
 
 # ---------------------------------------------------------------- chunks of new tokens
 # The wrappers below compare the tensors with the sizes given (a row too few would be read past
-# its end) and run on the tensors' own device, on its current stream unless one is given.
+# its end, a pool of another head size past the pool's) and run on the tensors' own device, on its
+# current stream unless one is given.
 class Chunks:
     """The new tokens of a batch: sequence s has the token rows start[s] .. start[s + 1] of
     n_tokens (start: int32 device tensor of n_seq + 1 entries), at most max_len of them.
@@ -476,9 +506,26 @@ def _kv_dtype(kv: PagedKV):
     return kv.k_pool.dtype
 
 
+def _fits(d: hk_dims, kv: PagedKV, heads: int, alloc: Allocator = None):
+    """The cache has the heads and the head size of d, and the allocator is beside it."""
+    have, D, dev = kv.sizes()
+    if have < heads:
+        raise HardKVError("the cache has fewer rows than NS * Hkv")
+    if D != d.D:
+        raise HardKVError(f"the cache's head size is {D}, not {d.D}")
+    if alloc is not None and alloc.device() != dev:
+        raise HardKVError("the allocator is on another device than the cache")
+
+
+def _status(status):
+    return None if status is None else _vector(status, 1, torch.int32, "status")
+
+
 def _run(name: str, t, tensors, stream, *args):
     """Call an entry point on the device that holds t and the tensors it works on."""
     dev = t.get_device()
+    if dev < 0:
+        raise HardKVError(f"{name}: tensors outside the GPU")
     for x in tensors:
         if x is not None and x.get_device() != dev:
             raise HardKVError(f"{name}: tensors on different devices")
@@ -511,13 +558,12 @@ def _token_rows(t, n_tokens: int, heads: int, D: int, dtype, what: str):
 
 def hk_reserve_slots(d: hk_dims, kv: PagedKV, chunks: Chunks, alloc: Allocator, ws, slot_map=None,
                      status=None, stream=None):
-    heads = d.NS * d.Hkv
-    _need(kv.page_table.shape[0] >= heads, "the cache has fewer rows than NS * Hkv")
+    _fits(d, kv, d.NS * d.Hkv, alloc)
     n = d.NS // max(chunks.n_seq, 1) * chunks.n_tokens * d.Hkv
-    _run("hk_reserve_slots", kv.page_table, (chunks.start, alloc.free_ids, slot_map, status, ws),
+    _run("hk_reserve_slots", kv.page_table, (chunks.start, slot_map, status, ws),
          stream, C.byref(d), C.byref(kv.desc),
          C.byref(chunks.desc), C.byref(alloc.desc),
-         None if slot_map is None else _vector(slot_map, n, torch.int64, "slot_map"), _ptr(status),
+         None if slot_map is None else _vector(slot_map, n, torch.int64, "slot_map"), _status(status),
          _ptr(ws), ws.numel())
 
 
@@ -525,6 +571,7 @@ def hk_write_kv(d: hk_dims, kv: PagedKV, n_tokens: int, slot_map, k_new, v_new, 
     """k_new, v_new: [tokens, Hkv, D], or [layers, tokens, Hkv, D] with the slot map of as many
     layers; views into larger tensors are fine as long as a token's heads are contiguous."""
     _need(k_new.dim() == v_new.dim() and k_new.dim() in (3, 4), "k_new and v_new must be 3- or 4-d")
+    _fits(d, kv, 0)
     layers = k_new.shape[0] if k_new.dim() == 4 else 1
     _need(v_new.dim() == 3 or v_new.shape[0] == layers, "k_new and v_new differ in layers")
     kp, kr = _token_rows(k_new, n_tokens, d.Hkv, d.D, _kv_dtype(kv), "k_new")
@@ -547,12 +594,12 @@ def chunk_attn_workspace(d: hk_dims, chunks: Chunks, max_pages: int, device) -> 
 def hk_chunk_attn(d: hk_dims, kv: PagedKV, chunks: Chunks, q, sm_scale: float, o, ws, lse=None,
                   stream=None):
     T = chunks.n_tokens
-    _need(kv.page_table.shape[0] >= d.NS * d.Hkv, "the cache has fewer rows than NS * Hkv")
+    _fits(d, kv, d.NS * d.Hkv)
     qp, qr = _token_rows(q, T, d.Hq, d.D, _kv_dtype(kv), "q")
     _need(q.dim() == 3, "q must be 3-d")
     op = _vector(o, T * d.Hq * d.D, _kv_dtype(kv), "o")
     lp = None if lse is None else _vector(lse, T * d.Hq, torch.float32, "lse")
-    _run("hk_chunk_attn", kv.k_pool, (kv.page_table, chunks.start, q, o, lse, ws), stream,
+    _run("hk_chunk_attn", kv.k_pool, (chunks.start, q, o, lse, ws), stream,
          C.byref(d), C.byref(kv.desc), C.byref(chunks.desc), qp,
          qr, float(sm_scale), op, lp, _ptr(ws), 0 if ws is None else ws.numel())
 
@@ -582,14 +629,14 @@ def hk_verify_draft(chunks: Chunks, V: int, tokens, p, u, n_accept, next_token, 
          _vector(tokens, T, i32, "tokens"), C.c_void_p(p.data_ptr()), row(p),
          None if q is None else C.c_void_p(q.data_ptr()), row(q),
          _vector(u, T, torch.float32, "u"), _vector(n_accept, B, i32, "n_accept"),
-         _vector(next_token, B, i32, "next_token"), _vector(n_drop, B, i32, "n_drop"), _ptr(status),
+         _vector(next_token, B, i32, "next_token"), _vector(n_drop, B, i32, "n_drop"), _status(status),
          _ptr(ws), ws.numel())
 
 
 def hk_trim_slots(d: hk_dims, kv: PagedKV, n_drop, alloc: Allocator, ws, stream=None):
-    _need(kv.page_table.shape[0] >= d.NS * d.Hkv, "the cache has fewer rows than NS * Hkv")
+    _fits(d, kv, d.NS * d.Hkv, alloc)
     n = n_drop.numel()
-    _run("hk_trim_slots", kv.page_table, (n_drop, alloc.free_ids, ws), stream, C.byref(d),
+    _run("hk_trim_slots", kv.page_table, (n_drop, ws), stream, C.byref(d),
          C.byref(kv.desc), n,
          _vector(n_drop, n, torch.int32, "n_drop"), C.byref(alloc.desc), _ptr(ws), ws.numel())
 
