@@ -472,7 +472,9 @@ hk_status hk_write_kv(const hk_dims* dims, const hk_paged_kv* kv, int32_t n_laye
  *        bytes a multiple of 16; 16-byte aligned
  *   o    [n_tokens][Hq][D] in kv->dtype, 16-byte aligned
  *   lse  [n_tokens][Hq] fp32 or NULL
- * dims->NS == chunks->n_seq; Hq / Hkv at most 64, n_tokens * Hq at most 2^34.  Scores, sums and outputs are accumulated in
+ * dims->NS == chunks->n_seq; Hq / Hkv at most 64, n_tokens * Hq at most 2^34, and where chunks of
+ * more than 32 queries of a KV head can come (floor(n_tokens * Hq / Hkv / 128) + NS) * Hkv < 2^24, the
+ * workgroups that a launch takes (HK_ERR_SHAPE).  Scores, sums and outputs are accumulated in
  * fp32.  A bf16 cache's probabilities enter the product with V in two bf16 parts (16 bits and more) in
  * chunks of up to 32 queries of a KV head (len * Hq / Hkv), rounded to bf16 once in longer ones.
  * workspace: >= hk_chunk_attn_workspace_size(dims, chunks, kv->max_pages) bytes, 256-byte aligned

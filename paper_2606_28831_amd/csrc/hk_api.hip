@@ -62,6 +62,7 @@ size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 constexpr int kMaxRows = 1 << 24;        // token rows of a call
 constexpr double kMaxQueries = 17179869184.0;   // token rows x query heads of the chunk attention
+constexpr long long kMaxThreads = 1ll << 32;    // of a launch, in one dimension: fewer
 constexpr int kMaxVocab = 1 << 20;
 constexpr int kMaxGroup = 64;            // query heads per KV head of the chunk attention
 
@@ -597,6 +598,8 @@ hk_status hk_chunk_attn(const hk_dims* dims, const hk_paged_kv* kv, const hk_chu
     if (!workspace || ws_bytes < need) return HK_ERR_WORKSPACE;
     if (!aligned256(workspace)) return HK_ERR_ALIGN;
   }
+  if (hk_chunk_attn_threads(dims->NS, dims->Hq, dims->Hkv, chunks->n_tokens, chunks->max_len, kv->max_pages) >= kMaxThreads)
+    return HK_ERR_SHAPE;
   return launched(hk_launch_chunk_attn(dims->NS, dims->Hq, dims->Hkv, dims->D, kv, chunks, q, q_row_stride, sm_scale,
                                        o, lse, workspace, stream));
 }

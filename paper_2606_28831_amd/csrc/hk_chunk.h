@@ -36,6 +36,8 @@ hipError_t hk_launch_trim(int n_heads, int Hkv, const hk_paged_kv* kv, int n_seq
                           const hk_allocator* alloc, void* ws, hipStream_t st);
 
 size_t hk_chunk_attn_ws(int NS, int Hq, int Hkv, int D, int n_tokens, int max_len, int max_pages);
+// threads of its largest launch at most
+long long hk_chunk_attn_threads(int NS, int Hq, int Hkv, int n_tokens, int max_len, int max_pages);
 hipError_t hk_launch_chunk_attn(int NS, int Hq, int Hkv, int D, const hk_paged_kv* kv, const hk_chunks* ch,
                                 const void* q, int64_t q_row, float sm_scale, void* o, float* lse, void* ws,
                                 hipStream_t st);

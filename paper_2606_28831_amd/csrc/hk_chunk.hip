@@ -1499,6 +1499,11 @@ size_t hk_chunk_attn_ws(int NS, int Hq, int Hkv, int D, int n_tokens, int max_le
   return rows * (D + 2) * sizeof(float) + PLAN_TILES * sizeof(TileSplit) + ((size_t)NS * Hkv + 2) * sizeof(int32_t);
 }
 
+long long hk_chunk_attn_threads(int NS, int Hq, int Hkv, int n_tokens, int max_len, int max_pages) {
+  const Plan p = plan(NS, Hq, Hkv, 0, n_tokens, max_len, max_pages);
+  return (long long)p.tiles * Hkv * (2 * TILE_ROWS);
+}
+
 hipError_t hk_launch_chunk_attn(int NS, int Hq, int Hkv, int D, const hk_paged_kv* kv, const hk_chunks* ch,
                                 const void* q, int64_t q_row, float sm_scale, void* o, float* lse, void* ws,
                                 hipStream_t st) {

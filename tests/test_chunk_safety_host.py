@@ -105,3 +105,17 @@ def test_status_words_and_tensors_outside_the_gpu_are_refused(hk):
             call(kv, al)
     with pytest.raises(hk.HardKVError, match="outside the GPU"):
         hk.hk_verify_draft(ch, 10, tok, p, u, out, out, out, ws)
+
+
+def test_chunk_attn_refuses_launches_that_the_hardware_does_not_take(hk):
+    """Tiles of 128 queries x KV heads x 256 threads pass 2^32 from 33554 tokens of 64000 query heads on,
+    also with a workspace and with fewer than 2^34 queries."""
+    L = hk.lib()
+    P = 1 << 20
+    d, kv = hk.dims(1, 64 * 1000, 1000, 128), hk.hk_paged_kv(P, P, P, P, P, 64, 4, 1)
+    for tokens in (33554, 1 << 17, 1 << 18):
+        c = hk.hk_chunks(P, 1, tokens, 8)
+        need = L.hk_chunk_attn_workspace_size(C.byref(d), C.byref(c), 4)
+        args = (C.byref(d), C.byref(kv), C.byref(c), P, 64 * 1000 * 128, 0.1, P, None)
+        assert L.hk_chunk_attn(*args, P, need, None) == 3
+        assert L.hk_chunk_attn(*args, P, need - 1, None) == 5
