@@ -478,7 +478,7 @@ hk_status hk_write_kv(const hk_dims* dims, const hk_paged_kv* kv, int32_t n_laye
  * fp32.  A bf16 cache's probabilities enter the product with V in two bf16 parts (16 bits and more) in
  * chunks of up to 32 queries of a KV head (len * Hq / Hkv), rounded to bf16 once in longer ones.
  * workspace: >= hk_chunk_attn_workspace_size(dims, chunks, kv->max_pages) bytes, 256-byte aligned
- * (0 for some sizes: it may then be NULL); calls that overlap on one workspace race.
+ * (never 0 for sizes that are accepted); calls that overlap on one workspace race.
  */
 size_t hk_chunk_attn_workspace_size(const hk_dims* dims, const hk_chunks* chunks,
                                     int32_t max_pages);

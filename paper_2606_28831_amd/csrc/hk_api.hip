@@ -594,10 +594,8 @@ hk_status hk_chunk_attn(const hk_dims* dims, const hk_paged_kv* kv, const hk_chu
   if (!aligned16(o)) return HK_ERR_ALIGN;
   const size_t need = hk_chunk_attn_ws(dims->NS, dims->Hq, dims->Hkv, dims->D, chunks->n_tokens, chunks->max_len,
                                        kv->max_pages);
-  if (need) {
-    if (!workspace || ws_bytes < need) return HK_ERR_WORKSPACE;
-    if (!aligned256(workspace)) return HK_ERR_ALIGN;
-  }
+  if (!workspace || ws_bytes < need) return HK_ERR_WORKSPACE;
+  if (!aligned256(workspace)) return HK_ERR_ALIGN;
   if (hk_chunk_attn_threads(dims->NS, dims->Hq, dims->Hkv, chunks->n_tokens, chunks->max_len, kv->max_pages) >= kMaxThreads)
     return HK_ERR_SHAPE;
   return launched(hk_launch_chunk_attn(dims->NS, dims->Hq, dims->Hkv, dims->D, kv, chunks, q, q_row_stride, sm_scale,
