@@ -120,40 +120,32 @@ struct Mma<uint16_t, D> {
     for (int s = 0; s < D / 16; ++s)
       q.f[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(row + (2 * s + hi) * 8));
   }
-  template <int NB>
-  __device__ static __forceinline__ void scores(f32x16 (&z)[NB], const Query (&q)[NB], const char* k) {
+  __device__ static __forceinline__ void scores(f32x16& z, const Query& q, const char* k) {
     const int lane = threadIdx.x & 63, key = lane & 31, hi = lane >> 5;
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) z[b][r] = 0.f;
+    z = f32x16{};
 #pragma unroll
     for (int s = 0; s < D / 16; ++s) {
       const bf16x8 a = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(k + key * L::K_ROW + (2 * s + hi) * 16));
-#pragma unroll
-      for (int b = 0; b < NB; ++b) z[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[b].f[s], z[b], 0, 0, 0);
+      z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q.f[s], z, 0, 0, 0);
     }
   }
-  template <int NB>
-  __device__ static __forceinline__ void values(f32x16 (&acc)[NB][D / 32], const f32x16 (&p)[NB], const char* v) {
+  __device__ static __forceinline__ void values(f32x16 (&acc)[D / 32], const f32x16& p, const char* v) {
     const int lane = threadIdx.x & 63, hi = lane >> 5, g1 = (lane >> 4) & 1, i16 = lane & 15;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       __builtin_amdgcn_sched_barrier(0);        // (here and below: the fragments of one product at a time, 247
                                                 // registers at D 128; without, 256 and spills)
-      bf16x8 bp[NB], low[NB];                   // P = bp + low, to 2^-16 of it
+      bf16x8 bp, low;                           // P = bp + low, to 2^-16 of it
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int j = 0; j < 8; j += 2) {
-          const f32x2 x = {p[b][8 * s + j], p[b][8 * s + j + 1]};
-          const bf16x2 t = __builtin_convertvector(x, bf16x2);
-          const bf16x2 r = __builtin_convertvector((f32x2{x[0] - (float)t[0], x[1] - (float)t[1]}), bf16x2);
-          bp[b][j] = t[0];
-          bp[b][j + 1] = t[1];
-          low[b][j] = r[0];
-          low[b][j + 1] = r[1];
-        }
+      for (int j = 0; j < 8; j += 2) {
+        const f32x2 x = {p[8 * s + j], p[8 * s + j + 1]};
+        const bf16x2 t = __builtin_convertvector(x, bf16x2);
+        const bf16x2 r = __builtin_convertvector((f32x2{x[0] - (float)t[0], x[1] - (float)t[1]}), bf16x2);
+        bp[j] = t[0];
+        bp[j + 1] = t[1];
+        low[j] = r[0];
+        low[j + 1] = r[1];
+      }
 #pragma unroll
       for (int dt = 0; dt < D / 32; ++dt) {
         s16x4 a[2];
@@ -165,11 +157,8 @@ struct Mma<uint16_t, D> {
               (__attribute__((address_space(3))) s16x4*)(uintptr_t)(__attribute__((address_space(3))) const char*)at);
         }
         const bf16x8 av = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a[0], a[1], 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          acc[b][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, low[b], acc[b][dt], 0, 0, 0);
-          acc[b][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, bp[b], acc[b][dt], 0, 0, 0);
-        }
+        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, low, acc[dt], 0, 0, 0);
+        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, bp, acc[dt], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -180,9 +169,6 @@ struct Mma<uint16_t, D> {
     const uint32_t a = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x, y}), bf16x2));
     const uint32_t b = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{z, w}), bf16x2));
     *reinterpret_cast<u32x2*>(to) = u32x2{a, b};
-  }
-  __device__ static __forceinline__ void put2(uint16_t* to, float x, float y) {
-    *reinterpret_cast<uint32_t*>(to) = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x, y}), bf16x2));
   }
 };
 
@@ -197,24 +183,17 @@ struct Mma<float, D> {
 #pragma unroll
     for (int s = 0; s < D / 8; ++s) q.f[s] = *reinterpret_cast<const f32x4*>(row + (2 * s + hi) * 4);
   }
-  template <int NB>
-  __device__ static __forceinline__ void scores(f32x16 (&z)[NB], const Query (&q)[NB], const char* k) {
+  __device__ static __forceinline__ void scores(f32x16& z, const Query& q, const char* k) {
     const int lane = threadIdx.x & 63, key = lane & 31, hi = lane >> 5;
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) z[b][r] = 0.f;
+    z = f32x16{};
 #pragma unroll
     for (int s = 0; s < D / 8; ++s) {
       const f32x4 a = *reinterpret_cast<const f32x4*>(k + key * L::K_ROW + (2 * s + hi) * 16);
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int b = 0; b < NB; ++b) z[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], q[b].f[s][j], z[b], 0, 0, 0);
+      for (int j = 0; j < 4; ++j) z = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], q.f[s][j], z, 0, 0, 0);
     }
   }
-  template <int NB>
-  __device__ static __forceinline__ void values(f32x16 (&acc)[NB][D / 32], const f32x16 (&p)[NB], const char* v) {
+  __device__ static __forceinline__ void values(f32x16 (&acc)[D / 32], const f32x16& p, const char* v) {
     const int lane = threadIdx.x & 63, hi = lane >> 5, dim = lane & 31;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
@@ -222,9 +201,7 @@ struct Mma<float, D> {
 #pragma unroll
       for (int dt = 0; dt < D / 32; ++dt) {
         const float a = *reinterpret_cast<const float*>(v + key * L::V_ROW + (32 * dt + dim) * 4);
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-          acc[b][dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p[b][r], acc[b][dt], 0, 0, 0);
+        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p[r], acc[dt], 0, 0, 0);
       }
     }
   }
@@ -232,100 +209,81 @@ struct Mma<float, D> {
   __device__ static __forceinline__ void put4(float* to, float x, float y, float z, float w) {
     *reinterpret_cast<f32x4*>(to) = f32x4{x, y, z, w};
   }
-  __device__ static __forceinline__ void put2(float* to, float x, float y) {
-    *reinterpret_cast<f32x2*>(to) = f32x2{x, y};
-  }
 };
 
 // ------------------------------------------------------------------ the softmax state of a wave
-// NB blocks of 32 queries; lane l holds query l % 32 of each, and half of its keys.
-template <typename T, int D, int NB>
+// 32 queries; lane l holds query l % 32, and half of its keys.
+template <typename T, int D>
 struct State {
   using M = Mma<T, D>;
-  f32x16 acc[NB][D / 32];                     // O^T: register r is dim 32 dt + (r & 3) + 8 (r >> 2) + 4 hi
-  float m[NB], mb[NB], l[NB];                 // reference, reference + bias (0 while there is none), sum
+  f32x16 acc[D / 32];                         // O^T: register r is dim 32 dt + (r & 3) + 8 (r >> 2) + 4 hi
+  float m, mb, l;                             // reference, reference + bias (0 while there is none), sum
   __device__ __forceinline__ void init() {
+    m = -INFINITY;
+    mb = 0.f;
+    l = 0.f;
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      m[b] = -INFINITY;
-      mb[b] = 0.f;
-      l[b] = 0.f;
+    for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[b][dt][r] = 0.f;
-    }
+      for (int r = 0; r < 16; ++r) acc[dt][r] = 0.f;
   }
-  // 32 keys from LDS; vis[b]: bit k, key k of them is seen by the lane's query (all: every bit of
+  // 32 keys from LDS; vis: bit k, key k of them is seen by the lane's query (all: every bit of
   // every lane is 1).  odd: keys whose V row holds infinite values and is not seen by every query;
   // it is zeros in LDS and added here, at row(key), to the queries that see it: for the others
   // its product with a probability of 0 would be NaN.
   template <typename F>
-  __device__ __forceinline__ void block(const typename M::Query (&q)[NB], const char* k, const char* v,
-                                        const uint32_t (&vis)[NB], bool all, float c2, float bias, uint32_t odd,
-                                        F row) {
-    f32x16 z[NB];
-    M::template scores<NB>(z, q, k);
-    weigh(z, v, vis, all, c2, bias, odd, row);
-  }
-  // the same from their scores z
-  template <typename F>
-  __device__ __forceinline__ void weigh(f32x16 (&z)[NB], const char* v, const uint32_t (&vis)[NB], bool all, float c2,
-                                        float bias, uint32_t odd, F row) {
+  __device__ __forceinline__ void block(const typename M::Query& q, const char* k, const char* v, uint32_t vis, bool all,
+                                        float c2, float bias, uint32_t odd, F row) {
     const int hi = (threadIdx.x & 63) >> 5;
+    f32x16 z;
+    M::scores(z, q, k);
+    if (!all) {
+      uint32_t w = vis >> (4 * hi);
+      asm volatile("" : "+v"(w));             // (a branch, not selects in every block)
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      if (!all) {
-        uint32_t w = vis[b] >> (4 * hi);
-        asm volatile("" : "+v"(w));           // (a branch, not selects in every block)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (!((w >> ((r & 3) + 8 * (r >> 2))) & 1u)) z[b][r] = -INFINITY;
-      }
-      float zm = z[b][0];
-#pragma unroll
-      for (int r = 1; r < 16; ++r) zm = fmaxf(zm, z[b][r]);
-      zm *= c2;
-      if (__any(zm > m[b] + CH_SLACK)) {
-        zm = fmaxf(zm, __shfl_xor(zm, 32, 64));
-        const float mn = fmaxf(m[b], ceilf(zm));
-        const float alpha = m[b] == -INFINITY ? 0.f : fast_exp2(m[b] - mn);
-        m[b] = mn;
-        mb[b] = mn == -INFINITY ? 0.f : mn + bias;
-        l[b] *= alpha;
-#pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) acc[b][dt][r] *= alpha;
-      }
-      float s[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        z[b][r] = fast_exp2(fmaf(z[b][r], c2, -mb[b]));
-        s[r & 3] += z[b][r];
-      }
-      l[b] += (s[0] + s[1]) + (s[2] + s[3]);
+      for (int r = 0; r < 16; ++r)
+        if (!((w >> ((r & 3) + 8 * (r >> 2))) & 1u)) z[r] = -INFINITY;
     }
-    M::template values<NB>(acc, z, v);
+    float zm = z[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) zm = fmaxf(zm, z[r]);
+    zm *= c2;
+    if (__any(zm > m + CH_SLACK)) {
+      zm = fmaxf(zm, __shfl_xor(zm, 32, 64));
+      const float mn = fmaxf(m, ceilf(zm));
+      const float alpha = m == -INFINITY ? 0.f : fast_exp2(m - mn);
+      m = mn;
+      mb = mn == -INFINITY ? 0.f : mn + bias;
+      l *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[dt][r] *= alpha;
+    }
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      z[r] = fast_exp2(fmaf(z[r], c2, -mb));
+      s[r & 3] += z[r];
+    }
+    l += (s[0] + s[1]) + (s[2] + s[3]);
+    M::values(acc, z, v);
     while (odd) {
       const int key = __builtin_ctz(odd), reg = (key & 3) + 4 * (key >> 3), lane = threadIdx.x & 63;
       odd &= odd - 1;
       const T* vr = row(key);
+      float p = z[0];
 #pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        float p = z[b][0];
+      for (int r = 1; r < 16; ++r) p = reg == r ? z[r] : p;
+      p = __shfl(p, (lane & 31) + 32 * ((key >> 2) & 1), 64);
+      const bool sees = (vis >> key) & 1u;
 #pragma unroll
-        for (int r = 1; r < 16; ++r) p = reg == r ? z[b][r] : p;
-        p = __shfl(p, (lane & 31) + 32 * ((key >> 2) & 1), 64);
-        const bool sees = (vis[b] >> key) & 1u;
+      for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const float x = M::value(vr[32 * dt + (r & 3) + 8 * (r >> 2) + 4 * hi]);
-            acc[b][dt][r] = sees ? fmaf(p, x, acc[b][dt][r]) : acc[b][dt][r];
-          }
-      }
+        for (int r = 0; r < 16; ++r) {
+          const float x = M::value(vr[32 * dt + (r & 3) + 8 * (r >> 2) + 4 * hi]);
+          acc[dt][r] = sees ? fmaf(p, x, acc[dt][r]) : acc[dt][r];
+        }
     }
   }
 };
@@ -622,10 +580,10 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void chunk_tile_f32_kernel(Ar
     const int seen = off + tok;                                  // keys before this one are seen by the lane's query,
     const int seen_all = off + min(w0, w.rows - 1) / a.G;        // by every query of the wave,
     const int tile_seen = off + w.r0 / a.G;                      // of the workgroup
-    typename M::Query q[1];
-    M::load_q(q[0], reinterpret_cast<const float*>(a.q) + (int64_t)(w.c.first + tok) * a.q_row + (w.kv * a.G + g) * D);
+    typename M::Query q;
+    M::load_q(q, reinterpret_cast<const float*>(a.q) + (int64_t)(w.c.first + tok) * a.q_row + (w.kv * a.G + g) * D);
     const float bias = bias_of(w.pages);
-    State<float, D, 1> st;
+    State<float, D> st;
     st.init();
     const int tiles = w.p1 > w.p0 ? (w.p1 - w.p0 + TP - 1) / TP : 0;
     PageRegs<float, D> rp[PPW];
@@ -692,15 +650,15 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void chunk_tile_f32_kernel(Ar
           const uint32_t odd = __builtin_amdgcn_readfirstlane((uint32_t)(o64 >> (32 * hb)));
           const bool all = valid == 0xffffffffu && key + 32 <= seen_all;
           const int k = seen - key;
-          const uint32_t vis[1] = {valid & (k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u)};
+          const uint32_t vis = valid & (k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u);
           st.block(q, s_k[buf] + hb * 32 * L::K_ROW, s_v[buf] + hb * 32 * L::V_ROW, vis, all, a.c2, bias, odd,
                    row_at(p + 2 * hb));
         }
       }
     }
-    const float l = st.l[0] + __shfl_xor(st.l[0], 32, 64);
+    const float l = st.l + __shfl_xor(st.l, 32, 64);
     if (w0 + (lane & 31) < w.rows)
-      put_state<float, D>(a, row, pieces.state < 0 ? -1 : pieces.state + r - w.r0, st.acc[0], st.mb[0], l);
+      put_state<float, D>(a, row, pieces.state < 0 ? -1 : pieces.state + r - w.r0, st.acc, st.mb, l);
   }
 }
 
@@ -1287,10 +1245,10 @@ __global__ __launch_bounds__(SHORT_NT, sizeof(T) == 2 ? 2 : 1) void chunk_short_
     const int32_t* trow = a.table + (size_t)w.h * a.max_pages;
     const uint16_t* mrow = a.masks + (size_t)w.h * a.max_pages;
     const int p0 = w.from * STEP_PAGES, p1 = min(w.to * STEP_PAGES, w.row.pages);
-    typename M::Query q[1];
-    M::load_q(q[0], reinterpret_cast<const T*>(a.q) + (int64_t)(w.row.c.first + tok) * a.q_row + (kv * a.G + (r - tok * a.G)) * D);
+    typename M::Query q;
+    M::load_q(q, reinterpret_cast<const T*>(a.q) + (int64_t)(w.row.c.first + tok) * a.q_row + (kv * a.G + (r - tok * a.G)) * D);
     const float bias = bias_of(w.row.pages);
-    State<T, D, 1> st;
+    State<T, D> st;
     st.init();
     PageRegs<T, D> rk[WP], rv[WP];
     int id[WP];
@@ -1340,14 +1298,14 @@ __global__ __launch_bounds__(SHORT_NT, sizeof(T) == 2 ? 2 : 1) void chunk_short_
       load();                                 // (past the last step its pages once more, with no valid slot)
       const bool all = valid == 0xffffffffu && key + 32 <= seen_all;
       const int k = seen - key;
-      const uint32_t vis[1] = {valid & (k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u)};
+      const uint32_t vis = valid & (k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u);
       __builtin_amdgcn_wave_barrier();
       st.block(q, my_k, my_v, vis, all, a.c2, bias, __builtin_amdgcn_readfirstlane(odd), [&](int j) {
         return reinterpret_cast<const T*>(a.v_pool) + ((size_t)page_id(p + j / HK_PAGE) * HK_PAGE + j % HK_PAGE) * D;
       });
       __builtin_amdgcn_wave_barrier();
     }
-    join_waves<T, D>(a, w, st.acc[0], st.mb[0], st.l[0], reinterpret_cast<float*>(s_buf), s_m, s_l);
+    join_waves<T, D>(a, w, st.acc, st.mb, st.l, reinterpret_cast<float*>(s_buf), s_m, s_l);
   }
 }
 
