@@ -92,3 +92,90 @@ def test_short_chunks_keep_the_bits_of_their_probabilities(D, G, lens, ctx):
         assert (np.abs(on[a:a + n, g] - ro) <= bo).all(), h
         if valid[:end - n + 1].sum() == 1:
             assert (on[a, g] == v[np.nonzero(valid)[0][0]]).all()
+
+
+# ------------------------------------------------------------------ more blocks, heads and values
+@pytest.mark.parametrize("D,n,G", [(128, 40, 4), (64, 40, 4), (128, 131, 1), (64, 70, 2)])
+def test_one_long_row_in_a_launch_of_many_sequences(D, n, G):
+    """Whole tiles over more than 64 and more than 128 blocks of 32 keys: odd and even numbers of them,
+    rows that end just past, at and just before a multiple of 2048 keys, among sequences without rows."""
+    B, Hkv, at = 130, 8, 77
+    rows = [9000, 4097, 6145, 2049, 8192, 4064, 6177, 2111]
+    c = Cache([0] * (at * Hkv) + rows + [0] * ((B - at - 1) * Hkv), D, "bf16", holes=0.1, seed=n, keep_last=n)
+    lens = [0] * B
+    lens[at] = n
+    _attend(c, lens, Hkv, G, D, "bf16", pad=1, heads=range(at * Hkv, at * Hkv + Hkv))
+
+
+@pytest.mark.parametrize("layers,B,Hkv,lens,most", [
+    (3, 86, 8, [200, 1, 150, 0, 33], 60),           # 2064 heads: cuts of more than eight pages
+    (17, 121, 8, [17, 0, 1], 20)])                  # 16456 heads: sums of more than 256 blocks of 64
+def test_slots_of_many_heads(layers, B, Hkv, lens, most):
+    import paper_2606_28831_amd as hk
+    H = layers * B * Hkv
+    lens = [lens[s % len(lens)] for s in range(B)]
+    ctx = [(7 * h) % most for h in range(H)]
+    c = Cache(ctx, 64, "bf16", seed=5, width=(max(lens) + most) // 16 + 3, spare=H * (1 + max(lens) // 16) // 2 + 2 * H)
+    ok, t, m, n, top, slots = CO.reserve(c.t, c.m, c.n, c.free, c.top, lens, Hkv)
+    assert ok
+    ch, sm, status = _reserve(c, lens, Hkv, layers, pad=1)
+    c.t, c.m, c.n, c.top = t, m, n, top
+    assert status == 0
+    c.check("reserve")
+    got, first = np_i(sm), np.concatenate([[0], np.cumsum(lens)])
+    for h in range(0, H, 13):
+        l, s, kv = h // (B * Hkv), h // Hkv % B, h % Hkv
+        assert got[l, first[s]:first[s + 1], kv].tolist() == slots[h]
+    assert (got[:, -1] == -1).all() and (got[:, :-1] >= 0).all()
+    d = hk.dims(layers * B, Hkv, Hkv, 64)
+    ws = hk.workspace(hk.OP_TRIM, d, c.width, DEV)
+    for drops in ([x // 3 for x in lens], [x - x // 3 for x in lens], [most] * B):
+        c.t, c.m, c.n, c.free, c.top = CO.trim(c.t, c.m, c.n, np_i(c.free_ids), c.top, drops, Hkv)
+        hk.hk_trim_slots(d, c.kv, torch.tensor(drops, dtype=I32, device=DEV), c.alloc, ws)
+        torch.cuda.synchronize()
+        c.check(drops[:5])
+    assert (c.n == 0).all()
+
+
+@pytest.mark.parametrize("V", [262145, 1 << 20])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_verify_large_vocabularies(V, dtype):
+    """More than 64 pieces of 4096 values: tokens drawn from the first, a middle and the last piece."""
+    rng = np.random.default_rng(V)
+    lens = [2, 1, 1]
+    p, q = (rng.random((4, V)) ** 8 for _ in "pq")
+    p, q = p / p.sum(1, keepdims=True), q / q.sum(1, keepdims=True)
+    put = lambda x: torch.tensor(x, device=DEV).to({"f32": torch.float32, "bf16": torch.bfloat16}[dtype])  # noqa: E731
+    p, q = put(p), put(q)
+    tok = torch.tensor([3, int(q[1].float().argmax()), 9, 9], dtype=I32, device=DEV)
+    pn, qn, tn = np64(p), np64(q), np_i(tok)
+    for us, own in (([0.9999999, 0.99, 0.0, 0.5], q), ([0.3, 0.0, 0.9999999, 0.97], None)):
+        u = torch.tensor(us, dtype=torch.float32, device=DEV)
+        got, status = _verify(p, own, tok, u, lens, V)
+        for s, n in enumerate(lens):
+            a = sum(lens[:s])
+            want = CO.verify(tn[a:a + n], pn[a:a + n], None if own is None else qn[a:a + n], np_i(u)[a:a + n])
+            assert (got[0][s], got[1][s], got[2][s]) == want, (us, s)
+        assert status == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_written_layer_by_layer(dtype):
+    """K and V of one layer at a time: both pools hold what one call for all layers leaves."""
+    import paper_2606_28831_amd as hk
+    layers, Hkv, D, lens = 3, 2, 64, [4, 0, 21]
+    c = Cache([(5 * i) % 40 for i in range(layers * 3 * Hkv)], D, dtype, seed=3, width=8)
+    ch, sm, status = _reserve(c, lens, Hkv, layers, pad=2, lead=1)
+    T = ch.n_tokens
+    k, v = (torch.randn(layers, T, Hkv, D, device=DEV).to(c.k_pool.dtype) for _ in "kv")
+    d, at = hk.dims(3, Hkv, Hkv, D), sm.view(-1)
+    want = []
+    for pool, x in ((c.k_pool, k), (c.v_pool, v)):
+        want.append(pool.view(-1, D).clone())
+        want[-1][at[at >= 0]] = x.reshape(-1, D)[at >= 0]
+    for l in range(layers):
+        hk.hk_write_kv(d, c.kv, T, sm[l], k[l], v[l])
+    torch.cuda.synchronize()
+    bits = torch.int16 if dtype == "bf16" else I32
+    for pool, w in zip((c.k_pool, c.v_pool), want):
+        assert torch.equal(pool.view(-1, D).view(bits), w.view(bits))
