@@ -212,15 +212,51 @@ struct Mma<float, D> {
 };
 
 // ------------------------------------------------------------------ the softmax state of a wave
+// The reference of a query.  A probability is exp2(z c2 - off), off being m + bias (0 while there is no
+// m), one fma an element: exact where m is below FAR, 2^24.  From there on the product's rounding, which
+// the fma leaves out and m has, is a whole number and more, and would make a largest score's
+// probability infinite or 0: such a query's scores are brought to (z c2 - m) / c2, each step rounded as
+// m was, and have off = bias.
+constexpr float FAR = 16777216.f;
+struct Reference {
+  float m, off;
+  float limit;                                // a score above it: move (far: any score, for bring)
+  __device__ __forceinline__ void init() {
+    m = limit = -INFINITY;
+    off = 0.f;
+  }
+  __device__ static __forceinline__ bool is_far(float m) { return fabsf(m) >= FAR && fabsf(m) < INFINITY; }
+  // moved to mn; returns the factor of the sums so far
+  __device__ __forceinline__ float move(float mn, float bias) {
+    const float alpha = m == -INFINITY ? 0.f : fast_exp2(m - mn);
+    m = mn;
+    off = mn == -INFINITY ? 0.f : is_far(mn) ? bias : mn + bias;
+    limit = is_far(mn) ? -INFINITY : mn + CH_SLACK;
+    return alpha;
+  }
+  __device__ __forceinline__ void bring(f32x16& z, float c2) const {
+#pragma clang fp contract(off)
+    if (!__any(is_far(m))) return;
+    const float back = fminf(1.f / c2, 0x1.fffffep127f);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float x = z[r] * c2, y = x - m;
+      z[r] = is_far(m) ? y * back : z[r];
+    }
+  }
+  // what the state's sums are relative to
+  __device__ __forceinline__ float whole(float bias) const { return m == -INFINITY ? 0.f : m + bias; }
+};
+
 // 32 queries; lane l holds query l % 32, and half of its keys.
 template <typename T, int D>
 struct State {
   using M = Mma<T, D>;
   f32x16 acc[D / 32];                         // O^T: register r is dim 32 dt + (r & 3) + 8 (r >> 2) + 4 hi
-  float m, mb, l;                             // reference, reference + bias (0 while there is none), sum
+  Reference ref;
+  float l;                                    // sum
   __device__ __forceinline__ void init() {
-    m = -INFINITY;
-    mb = 0.f;
+    ref.init();
     l = 0.f;
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
@@ -248,22 +284,20 @@ struct State {
 #pragma unroll
     for (int r = 1; r < 16; ++r) zm = fmaxf(zm, z[r]);
     zm *= c2;
-    if (__any(zm > m + CH_SLACK)) {
+    if (__builtin_expect(__any(zm > ref.limit), 0)) {
       zm = fmaxf(zm, __shfl_xor(zm, 32, 64));
-      const float mn = fmaxf(m, ceilf(zm));
-      const float alpha = m == -INFINITY ? 0.f : fast_exp2(m - mn);
-      m = mn;
-      mb = mn == -INFINITY ? 0.f : mn + bias;
+      const float alpha = ref.move(fmaxf(ref.m, ceilf(zm)), bias);
       l *= alpha;
 #pragma unroll
       for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[dt][r] *= alpha;
+      ref.bring(z, c2);
     }
     float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      z[r] = fast_exp2(fmaf(z[r], c2, -mb));
+      z[r] = fast_exp2(fmaf(z[r], c2, -ref.off));
       s[r & 3] += z[r];
     }
     l += (s[0] + s[1]) + (s[2] + s[3]);
@@ -658,7 +692,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void chunk_tile_f32_kernel(Ar
     }
     const float l = st.l + __shfl_xor(st.l, 32, 64);
     if (w0 + (lane & 31) < w.rows)
-      put_state<float, D>(a, row, pieces.state < 0 ? -1 : pieces.state + r - w.r0, st.acc, st.mb, l);
+      put_state<float, D>(a, row, pieces.state < 0 ? -1 : pieces.state + r - w.r0, st.acc, st.ref.whole(bias), l);
   }
 }
 
@@ -803,7 +837,9 @@ __global__ __launch_bounds__(256, 2) void chunk_tile_bf16_kernel(Args a) {
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[dt][e] = 0.f;
-    float m = -INFINITY, mb = 0.f, l = 0.f;
+    Reference ref;
+    ref.init();
+    float l = 0.f;
 
     const int k_at = L::k_lane(lane), v_at = L::v_lane(lane);    // the lane's fragments within 32 keys
     auto k_frag = [&](const char* k, int s) {
@@ -831,8 +867,8 @@ __global__ __launch_bounds__(256, 2) void chunk_tile_bf16_kernel(Args a) {
     // beside an MFMA in its place.
     float sum[2];
     auto scale = [&](f32x16& zc, int k) {
-      zc[2 * k] = fmaf(zc[2 * k], c2, -mb);
-      zc[2 * k + 1] = fmaf(zc[2 * k + 1], c2, -mb);
+      zc[2 * k] = fmaf(zc[2 * k], c2, -ref.off);
+      zc[2 * k + 1] = fmaf(zc[2 * k + 1], c2, -ref.off);
     };
     auto raise = [&](f32x16& zc, int k) {
       zc[2 * k] = fast_exp2(zc[2 * k]);
@@ -896,20 +932,18 @@ __global__ __launch_bounds__(256, 2) void chunk_tile_bf16_kernel(Args a) {
       for (int e = 0; e < 16; ++e)
         if (!((x >> ((e & 3) + 8 * (e >> 2))) & 1u)) zn[e] = -INFINITY;
     };
-    // a new reference where a score has outgrown it
-    auto refer = [&](float zm) {
+    // a new reference where a score of zn has outgrown it (zm: the lane's largest)
+    auto refer = [&](f32x16& zn, float zm) {
       zm *= c2;
-      if (__any(zm > m + CH_SLACK)) {
+      if (__builtin_expect(__any(zm > ref.limit), 0)) {
         zm = fmaxf(zm, __shfl_xor(zm, 32, 64));
-        const float mn = fmaxf(m, ceilf(zm));
-        const float alpha = m == -INFINITY ? 0.f : fast_exp2(m - mn);
-        m = mn;
-        mb = mn == -INFINITY ? 0.f : mn + bias;
+        const float alpha = ref.move(fmaxf(ref.m, ceilf(zm)), bias);
         l *= alpha;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
           for (int e = 0; e < 16; ++e) acc[dt][e] *= alpha;
+        ref.bring(zn, c2);
       }
     };
     // rows of V with infinite values that not every query of the tile sees (zeros in LDS)
@@ -999,7 +1033,7 @@ __global__ __launch_bounds__(256, 2) void chunk_tile_bf16_kernel(Args a) {
       float zm = z[0][0];
 #pragma unroll
       for (int e = 1; e < 16; ++e) zm = fmaxf(zm, z[0][e]);
-      refer(zm);
+      refer(z[0], zm);
       first_read();
       first_k(s_k[1]);
     }
@@ -1014,7 +1048,7 @@ __global__ __launch_bounds__(256, 2) void chunk_tile_bf16_kernel(Args a) {
         const uint32_t odd = __builtin_amdgcn_readfirstlane(s_odd[slot][0] | s_odd[slot][1] << 16);
         if (odd) add_odd(odd, w.p0 + 2 * t, valid[0]);
       }
-      if (t + 1 < tiles) refer(zm);
+      if (t + 1 < tiles) refer(zn, zm);
       advance();
     };
     for (int t = 0; t < tiles; t += 2) {
@@ -1023,7 +1057,7 @@ __global__ __launch_bounds__(256, 2) void chunk_tile_bf16_kernel(Args a) {
     }
     l += __shfl_xor(l, 32, 64);
     if (w0 + (lane & 31) < w.rows)
-      put_state<uint16_t, D>(a, row, pieces.state < 0 ? -1 : pieces.state + r - w.r0, acc, mb, l);
+      put_state<uint16_t, D>(a, row, pieces.state < 0 ? -1 : pieces.state + r - w.r0, acc, ref.whole(bias), l);
   }
 }
 
@@ -1218,11 +1252,11 @@ __device__ __forceinline__ void join_waves(const Args& a, const Piece& w, const 
 }
 
 // Pages go through a wave's own part of LDS, two of K and two of V a step, and are requested a step
-// ahead.  Two workgroups a CU for bf16.  Bound by HBM reads: 64 sequences of 1 to 8 tokens over 784 to
+// ahead.  Two workgroups a CU, but for fp32 of 128.  Bound by HBM reads: 64 sequences of 1 to 8 tokens over 784 to
 // 5600, 32/8 heads of 128: 167 us, 5.0 TB/s of pages; 164 without the products and the softmax, and no
 // faster with twice the loads in flight or with more workgroups (1024: 178).
 template <typename T, int D>
-__global__ __launch_bounds__(SHORT_NT, sizeof(T) == 2 ? 2 : 1) void chunk_short_kernel(Args a) {
+__global__ __launch_bounds__(SHORT_NT, sizeof(T) * D <= 256 ? 2 : 1) void chunk_short_kernel(Args a) {
   using L = TileLayout<T, D>;
   using M = Mma<T, D>;
   constexpr int WP = STEP_PAGES / SHORT_NW;
@@ -1305,7 +1339,7 @@ __global__ __launch_bounds__(SHORT_NT, sizeof(T) == 2 ? 2 : 1) void chunk_short_
       });
       __builtin_amdgcn_wave_barrier();
     }
-    join_waves<T, D>(a, w, st.acc, st.mb, st.l, reinterpret_cast<float*>(s_buf), s_m, s_l);
+    join_waves<T, D>(a, w, st.acc, st.ref.whole(bias), st.l, reinterpret_cast<float*>(s_buf), s_m, s_l);
   }
 }
 

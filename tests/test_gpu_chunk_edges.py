@@ -179,3 +179,53 @@ def test_rows_written_layer_by_layer(dtype):
     bits = torch.int16 if dtype == "bf16" else I32
     for pool, w in zip((c.k_pool, c.v_pool), want):
         assert torch.equal(pool.view(-1, D).view(bits), w.view(bits))
+
+
+# ------------------------------------------------------------------ scores past 2^24
+@pytest.mark.parametrize("L,n,width", [(310, 70, None), (300, 5, None), (6000, 70, 512), (6000, 3, 512)])
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+def test_scores_past_the_last_bit(dtype, D, L, n, width):
+    """Scores up to 1e18, of either sign and beside ordinary ones: results are finite, the largest score's V
+    where no other score is within the products' error of it, and the LSE is off by that error."""
+    import paper_2606_28831_amd as hk
+    G, scale = 2, 1 / math.sqrt(D)
+    c = Cache([L, L - 9], D, dtype, seed=n, width=width, keep_last=n, holes=0.1)
+    T, d = n, hk.dims(1, 2 * G, 2, D)
+    ch = _chunks([n])
+    g = torch.Generator(device=DEV).manual_seed(7)
+    base = torch.randn(T, 2 * G, D, generator=g, device=DEV)
+    ws = hk.chunk_attn_workspace(d, ch, c.width, DEV)
+    for k_scale, q_scale, sign in ((1e3, 1e3, 0), (1e5, 1e5, 0), (1e9, 1e9, 0), (3e4, 1e6, -1), (1e5, 1e5, 1)):
+        k = c.k_pool.float()
+        k = k / k[~k.isnan()].abs().max() * 4.0 * k_scale
+        q = base * q_scale
+        if sign:
+            k, q = k.abs(), q.abs() * sign
+        q[1::3] = base[1::3] / (4.0 * k_scale)               # every third token's scores are ordinary
+        c.k_pool.copy_(k)
+        q = q.to(c.k_pool.dtype)
+        o, lse = torch.zeros(T, 2 * G, D, dtype=q.dtype, device=DEV), torch.zeros(T, 2 * G, device=DEV)
+        hk.hk_chunk_attn(d, c.kv, ch, q, scale, o, ws, lse=lse)
+        torch.cuda.synchronize()
+        assert torch.isfinite(o).all() and torch.isfinite(lse).all(), (k_scale, q_scale, sign)
+        qn, on, ln = np64(q), np64(o), np64(lse)
+        for h in range(2):
+            keys, vals, valid, end = c.head(h)
+            hs = slice(h * G, h * G + G)
+            ro, rl, zabs, absv = CO.chunk_attn_head(qn[:, hs], keys, vals, valid, end, scale)
+            bo, bl = _bound(dtype, len(valid), rl, zabs, absv, ro, D)
+            assert (np.abs(ln[:, hs] - rl) <= bl).all(), (k_scale, q_scale, sign, h)
+            dz = (D + 8) * 2.0 ** -23 * zabs
+            sure = 0
+            for i in range(n):
+                see = np.nonzero(valid[:end - n + i + 1])[0]
+                for x in range(G):
+                    z = scale * (keys[see] @ qn[i, h * G + x])
+                    first, second = np.argsort(z)[::-1][:2]
+                    if dz[i, x] < 0.01:                      # the ordinary ones
+                        assert (np.abs(on[i, h * G + x] - ro[i, x]) <= bo[i, x]).all()
+                    elif z[first] - z[second] > 2 * dz[i, x] + 30:
+                        v = vals[see[first]]
+                        assert (np.abs(on[i, h * G + x] - v) <= 2.0 ** -7 * np.abs(v) + 2.0 ** -30).all(), (i, x, k_scale)
+                        sure += 1
+            assert sure >= n // 3
