@@ -410,8 +410,9 @@ hk_status hk_append_kv(const hk_dims* dims, const hk_paged_kv* kv, const void* k
  * every layer of the cache at once.
  *
  * The new tokens of the batch lie behind one another in token rows; sequence s has the rows
- * [start[s], start[s + 1]), possibly none.  Rows outside every chunk are padding: no call reads
- * or writes them, but for their slot map entries (-1).  max_len bounds the launches: it need not
+ * [start[s], start[s + 1]), possibly none.  Rows outside every chunk are padding: no result depends
+ * on what they hold and no call writes them, but for their slot map entries (-1); hk_write_kv may load
+ * them, so they lie in allocated memory as the others do.  max_len bounds the launches: it need not
  * be met.  Only the fields' sizes are seen by the host, so one captured graph serves every
  * mixture of lengths within them.
  */
@@ -466,7 +467,10 @@ hk_status hk_write_kv(const hk_dims* dims, const hk_paged_kv* kv, int32_t n_laye
  * the row's newest slots: with end as above and len the chunk's length, query i of the chunk sees
  * the valid slots j <= end - len + i of each KV head h:
  *   o = sum_j Softmax_j(sm_scale q.k_j) v_j,   lse = log sum_j exp(sm_scale q.k_j).
- * A query that sees no valid slot gives o = 0, lse = -inf.  K and V of masked slots and of slots
+ * A query that sees no valid slot gives o = 0, lse = -inf.  How rows are split over workgroups follows
+ * from all chunks and rows of the call, so the last bits of o and lse can change with the batch; the
+ * same call gives the same bits.  Sums hold to the top of the fp32 range; V below 2^-100 (1e-30) loses
+ * bits.  K and V of masked slots and of slots
  * past the row's end are not read into the result, whatever they hold.
  *   q    row t, head g at q[t * q_row_stride + g * D], in kv->dtype; q_row_stride >= Hq * D, its
  *        bytes a multiple of 16; 16-byte aligned
@@ -516,8 +520,9 @@ hk_status hk_verify_draft(const hk_chunks* chunks, int32_t V, hk_dtype dtype, co
  * other, as for hk_reserve_slots) the last drop = max(0, n_drop[s % n_seq]) logical slots,
  *   end' = max(0, end - drop): mask bits from end' on are cleared, pages from ceil(end' / 16) on are
  *   pushed, in head order and ascending page order, their table entries set to -1.
- * Undoes hk_reserve_slots of the same lengths, free list included.  A head with drop = 0 is left as
- * it is.  alloc->capacity >= kv->num_pages (HK_ERR_ARG otherwise).
+ * Undoes hk_reserve_slots of the same lengths, free list included, but for a row whose newest page had
+ * no valid slot before: that page, which the new slots began in, is pushed too.  A head with drop = 0
+ * is left as it is.  alloc->capacity >= kv->num_pages (HK_ERR_ARG otherwise).
  * workspace: >= hk_workspace_size(HK_OP_TRIM) bytes, 256-byte aligned.
  */
 hk_status hk_trim_slots(const hk_dims* dims, const hk_paged_kv* kv, int32_t n_seq,

@@ -20,7 +20,8 @@
 // Softmax: one pass with a running reference m per query, a whole number that moves only when a
 // score exceeds it by 2^CH_SLACK, so most blocks need no rescaling.  Probabilities are formed as
 // exp2(z - m - bias), where 2^bias is at least 2^CH_SLACK times the keys of the row: sums of P V
-// and their merge cannot leave the fp32 range where the result does not.
+// and their merge cannot pass the top of the fp32 range where the result does not.  At its other end
+// that costs bits: V of 1e-32 is off by 4e-7 of its norm, 1e-34 by 2e-5, 1e-36 by 2e-3 (fp32).
 // Precision: scores, sums and outputs in fp32; the row sum, and so the LSE, is of the unrounded P.
 // Into the bf16 product P enters in the short kernel in two bf16 parts, to 2^-16 of each term: the
 // output is then off by its own rounding and little else, and as the kernel is bound by memory the
@@ -594,7 +595,8 @@ struct Pieces {
 
 // fp32: four waves take 32 rows each; the next tile's pages load while a tile is computed.  Bound by
 // the fp32 matrix rate, a sixteenth of bf16's (154 TFLOP/s in a large product): 16 sequences of up to
-// 203 tokens over 2000, 32/8 heads of 64: 318 us, 96 TFLOP/s (tiles of 256 rows: 497).
+// 203 tokens over 2000, 32/8 heads of 64: 312 us, 98 TFLOP/s (tiles of 256 rows: 497); 4 prompts of 2000:
+// 106 TFLOP/s, of 128 101, at one workgroup a CU.
 template <int D, bool PLANNED>
 __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void chunk_tile_f32_kernel(Args a) {
   using L = TileLayout<float, D>;
@@ -744,8 +746,9 @@ __device__ __forceinline__ void direct_wait() { asm volatile("s_waitcnt vmcnt(%0
 // one's start, end and waits to be beside the other's work (measured against one of eight waves and
 // tiles of 64 keys, 8 prompts of 4096 tokens, 32 / 8 heads: D 128 1152 us and 1172, D 64 697 and 786).
 // Bound by the products (2048 cycles of each SIMD for 64 keys) beside as many cycles of exponentials,
-// sums and maxima, which overlap in part, and LDS reads at half their rate: 950 to 980 TFLOP/s, of
-// 1231 in a large library product; the products alone run at 1363.
+// sums and maxima, which overlap in part, and LDS reads at half their rate: 890 to 990 TFLOP/s by the
+// card, of 1231 in a large library product; the products alone run at 1363.  By counters, 8 prompts of
+// 4096: MFMA busy for 45% of the SIMDs' cycles at 1.93 GHz, vector instructions for 42%, no LDS conflicts.
 // Waves 0 and 1 bring a page of K each, three tiles ahead of the wait for it, waves 2 and 3 the pages
 // of V.
 template <int D, bool PLANNED>
@@ -1253,8 +1256,9 @@ __device__ __forceinline__ void join_waves(const Args& a, const Piece& w, const 
 
 // Pages go through a wave's own part of LDS, two of K and two of V a step, and are requested a step
 // ahead.  Two workgroups a CU, but for fp32 of 128.  Bound by HBM reads: 64 sequences of 1 to 8 tokens over 784 to
-// 5600, 32/8 heads of 128: 167 us, 5.0 TB/s of pages; 164 without the products and the softmax, and no
-// faster with twice the loads in flight or with more workgroups (1024: 178).
+// 5600, 32/8 heads of 128: 165 to 171 us, 850 MB by the counter at 5.0 TB/s; 164 without the products and
+// the softmax, and no faster with twice the loads in flight or with more workgroups (1024: 178).  fp32,
+// 16 sequences of 1 to 6 tokens over 2000: heads of 64 39 us, of 128, where a CU has one workgroup, 78.
 template <typename T, int D>
 __global__ __launch_bounds__(SHORT_NT, sizeof(T) * D <= 256 ? 2 : 1) void chunk_short_kernel(Args a) {
   using L = TileLayout<T, D>;
@@ -1431,6 +1435,9 @@ __global__ __launch_bounds__(MERGE_NT) void chunk_merge_kernel(Args a, int tile_
 
 // Workgroups of a call.  heads: of the short kernel, 0 where no row can be a short one; tiles: numbers
 // of tiles of a KV head; pieces: most of them that a planned launch makes, 0 for one of many tiles.
+// The host knows no lengths, so it numbers a tile more for every sequence: with 8 KV heads, batches of
+// about 125 sequences have no pieces, whatever they hold (500 tokens over 20000 among 127 single tokens
+// 2209 us, the single tokens alone 1795; among 31 638, and about 440 by that rate).
 struct Plan {
   int heads, tiles, pieces;
 };

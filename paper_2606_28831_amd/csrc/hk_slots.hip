@@ -182,8 +182,8 @@ __global__ __launch_bounds__(SL_NT) void reserve_write_kernel(
 }
 
 // ------------------------------------------------------------------ write
-// One 16-byte piece of a K row and the same of its V row per thread.  A row without a slot (-1,
-// or one outside the pool) is skipped.  Bound by the copy.
+// One 16-byte piece of a K row and the same of its V row per thread, loaded beside the slot.  A row
+// without one (-1, or one outside the pool) is not written.  Bound by the copy.
 __global__ __launch_bounds__(SL_NT) void write_kv_kernel(
     int Hkv, int pieces, int n_layers, int n_tokens, int64_t n_slots, const int64_t* __restrict__ slot_map,
     const char* __restrict__ k_new, int64_t k_layer, int64_t k_row, const char* __restrict__ v_new,
