@@ -19,7 +19,8 @@
 //
 // Softmax: one pass with a running reference m per query, a whole number that moves only when a
 // score exceeds it by 2^CH_SLACK, so most blocks need no rescaling.  Probabilities are formed as
-// exp2(z - m - bias), where 2^bias is at least 2^CH_SLACK times the keys of the row: sums of P V
+// exp2(z - m) 2^-bias (in the bf16 tile kernel, whose P keeps 8 bits and whose LSE is off by some 2^-20,
+// as exp2(z - m - bias)), where 2^bias is at least 2^CH_SLACK times the keys of the row: sums of P V
 // and their merge cannot pass the top of the fp32 range where the result does not.  At its other end
 // that costs bits: V of 1e-32 is off by 4e-7 of its norm, 1e-34 by 2e-5, 1e-36 by 2e-3 (fp32).
 // Precision: scores, sums and outputs in fp32; the row sum, and so the LSE, is of the unrounded P.
@@ -213,11 +214,11 @@ struct Mma<float, D> {
 };
 
 // ------------------------------------------------------------------ the softmax state of a wave
-// The reference of a query.  A probability is exp2(z c2 - off), off being m + bias (0 while there is no
-// m), one fma an element: exact where m is below FAR, 2^24.  From there on the product's rounding, which
+// The reference of a query.  A probability's exponent is z c2 - off, off being m and the kernel's shift (0
+// while there is no m), one fma an element: exact where m is below FAR, 2^24.  From there on the product's rounding, which
 // the fma leaves out and m has, is a whole number and more, and would make a largest score's
 // probability infinite or 0: such a query's scores are brought to (z c2 - m) / c2, each step rounded as
-// m was, and have off = bias.
+// m was, and have off = shift.
 constexpr float FAR = 16777216.f;
 struct Reference {
   float m, off;
@@ -227,11 +228,11 @@ struct Reference {
     off = 0.f;
   }
   __device__ static __forceinline__ bool is_far(float m) { return fabsf(m) >= FAR && fabsf(m) < INFINITY; }
-  // moved to mn; returns the factor of the sums so far
-  __device__ __forceinline__ float move(float mn, float bias) {
+  // moved to mn; returns the factor of the sums so far.  shift: of the exponent, beside mn
+  __device__ __forceinline__ float move(float mn, float shift) {
     const float alpha = m == -INFINITY ? 0.f : fast_exp2(m - mn);
     m = mn;
-    off = mn == -INFINITY ? 0.f : is_far(mn) ? bias : mn + bias;
+    off = mn == -INFINITY ? 0.f : is_far(mn) ? shift : mn + shift;
     limit = is_far(mn) ? -INFINITY : mn + CH_SLACK;
     return alpha;
   }
@@ -268,9 +269,12 @@ struct State {
   // every lane is 1).  odd: keys whose V row holds infinite values and is not seen by every query;
   // it is zeros in LDS and added here, at row(key), to the queries that see it: for the others
   // its product with a probability of 0 would be NaN.
+  // down: 2^-bias.  It is a factor of the probabilities here, and no part of the exponent, which it would
+  // bring to 17 and more, where its rounding is 2^-20: o of an fp32 cache was off by 3.7e-7 of its norm
+  // over short rows and is by 1.9e-7.
   template <typename F>
   __device__ __forceinline__ void block(const typename M::Query& q, const char* k, const char* v, uint32_t vis, bool all,
-                                        float c2, float bias, uint32_t odd, F row) {
+                                        float c2, float down, uint32_t odd, F row) {
     const int hi = (threadIdx.x & 63) >> 5;
     f32x16 z;
     M::scores(z, q, k);
@@ -287,7 +291,7 @@ struct State {
     zm *= c2;
     if (__builtin_expect(__any(zm > ref.limit), 0)) {
       zm = fmaxf(zm, __shfl_xor(zm, 32, 64));
-      const float alpha = ref.move(fmaxf(ref.m, ceilf(zm)), bias);
+      const float alpha = ref.move(fmaxf(ref.m, ceilf(zm)), 0.f);
       l *= alpha;
 #pragma unroll
       for (int dt = 0; dt < D / 32; ++dt)
@@ -298,7 +302,7 @@ struct State {
     float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      z[r] = fast_exp2(fmaf(z[r], c2, -ref.off));
+      z[r] = fast_exp2(fmaf(z[r], c2, -ref.off)) * down;
       s[r & 3] += z[r];
     }
     l += (s[0] + s[1]) + (s[2] + s[3]);
@@ -329,6 +333,7 @@ __device__ __forceinline__ int tile_pages(int n, int end, int len, int last_toke
   return min(n, (seen + HK_PAGE - 1) / HK_PAGE);
 }
 __device__ __forceinline__ float bias_of(int pages) { return (float)(32 - __clz(pages * HK_PAGE)) + CH_SLACK; }
+__device__ __forceinline__ float down_of(float bias) { return __uint_as_float((uint32_t)(127 - (int)bias) << 23); }
 
 struct Args {
   const char *q, *k_pool, *v_pool;
@@ -595,7 +600,7 @@ struct Pieces {
 
 // fp32: four waves take 32 rows each; the next tile's pages load while a tile is computed.  Bound by
 // the fp32 matrix rate, a sixteenth of bf16's (154 TFLOP/s in a large product): 16 sequences of up to
-// 203 tokens over 2000, 32/8 heads of 64: 312 us, 98 TFLOP/s (tiles of 256 rows: 497); 4 prompts of 2000:
+// 203 tokens over 2000, 32/8 heads of 64: 316 us, 97 TFLOP/s (tiles of 256 rows: 497); 4 prompts of 2000:
 // 106 TFLOP/s, of 128 101, at one workgroup a CU.
 template <int D, bool PLANNED>
 __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void chunk_tile_f32_kernel(Args a) {
@@ -687,7 +692,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void chunk_tile_f32_kernel(Ar
           const bool all = valid == 0xffffffffu && key + 32 <= seen_all;
           const int k = seen - key;
           const uint32_t vis = valid & (k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u);
-          st.block(q, s_k[buf] + hb * 32 * L::K_ROW, s_v[buf] + hb * 32 * L::V_ROW, vis, all, a.c2, bias, odd,
+          st.block(q, s_k[buf] + hb * 32 * L::K_ROW, s_v[buf] + hb * 32 * L::V_ROW, vis, all, a.c2, down_of(bias), odd,
                    row_at(p + 2 * hb));
         }
       }
@@ -1338,7 +1343,7 @@ __global__ __launch_bounds__(SHORT_NT, sizeof(T) * D <= 256 ? 2 : 1) void chunk_
       const int k = seen - key;
       const uint32_t vis = valid & (k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u);
       __builtin_amdgcn_wave_barrier();
-      st.block(q, my_k, my_v, vis, all, a.c2, bias, __builtin_amdgcn_readfirstlane(odd), [&](int j) {
+      st.block(q, my_k, my_v, vis, all, a.c2, down_of(bias), __builtin_amdgcn_readfirstlane(odd), [&](int j) {
         return reinterpret_cast<const T*>(a.v_pool) + ((size_t)page_id(p + j / HK_PAGE) * HK_PAGE + j % HK_PAGE) * D;
       });
       __builtin_amdgcn_wave_barrier();

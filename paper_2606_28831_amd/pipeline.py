@@ -234,7 +234,8 @@ class ChunkDecoder:
     The buffers serve any chunks of at most max_tokens rows and max_len tokens a sequence.
     status collects FLAG_NOSPACE / FLAG_CHUNK: such a reserve() gave no slots (see hardkv.h).
     granted says on the device whether the last reserve() gave them; its chunks carry the word on to
-    the Verifier, which drops nothing of refused chunks.  trim() itself always takes n_drop back.
+    the Verifier, which drops nothing of refused chunks (one Chunks reserved by several decoders carries
+    the last one's word: give each its own).  trim() itself always takes n_drop back.
     """
 
     def __init__(self, B, Hq, Hkv, D, kv: PagedKV, alloc: Allocator, max_tokens: int, max_len: int,

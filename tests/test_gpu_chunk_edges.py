@@ -229,3 +229,47 @@ def test_scores_past_the_last_bit(dtype, D, L, n, width):
                         assert (np.abs(on[i, h * G + x] - v) <= 2.0 ** -7 * np.abs(v) + 2.0 ** -30).all(), (i, x, k_scale)
                         sure += 1
             assert sure >= n // 3
+
+
+# ------------------------------------------------------------------ the bits of fp32 caches
+def _two_keys(dtype, D, n, heads, width=None, ctx=2, seed=3):
+    """A cache whose queries weigh two keys alone: z = q0 k0 within [-0.5, 0.5], products of one term; every
+    other key's probability is below 2^-500.  V is 1 and -1 in the two, 0 elsewhere.  Returns (cache, q,
+    z [heads, n, 2])."""
+    c = Cache([ctx + n] * heads, D, dtype, seed=seed, width=width, keep_last=ctx + n)
+    k, v = torch.zeros_like(c.k_pool), torch.zeros_like(c.v_pool)
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    pair = (torch.rand(heads, 2, generator=g, device=DEV) - 0.5).to(k.dtype)
+    k[..., 0] = -1000.0
+    for h in range(heads):
+        at = int(c.t[h, 0])
+        k[at, :2, 0] = pair[h]
+        v[at, 0], v[at, 1] = 1.0, -1.0
+    c.k_pool.copy_(k)
+    c.v_pool.copy_(v)
+    q = torch.zeros(n, heads, D, device=DEV)
+    q[..., 0] = 0.5 + 0.5 * torch.rand(n, heads, generator=g, device=DEV)
+    q = q.to(k.dtype)
+    return c, q, np64(q[..., 0]).T[:, :, None] * np64(pair)[:, None, :]
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n,ctx,width", [(20, 2, None), (64, 2, None), (20, 3000, 400), (64, 3000, 400)])
+def test_fp32_probabilities_keep_their_bits(D, n, ctx, width):
+    """o = tanh((z0 - z1) / 2) of two keys.  In base 2 an exponent lies within [-1.73, 0] below the reference:
+    its rounding is 2^-24, c2's share 2^-25, the score's product 2^-25, so 0.7 (2^-24 + 2^-24) of a probability,
+    and 2^-23 of the exponential itself; o takes p0 p1 |v0 - v1| = 2 p0 p1 <= 0.5 of both keys' errors.  Sums
+    and products with V of a few steps, cut by the matrix cores: 2^-23 of a probability each (2 of V, 2 of the
+    sum), the joins' factors are powers of two, 1 / l and its product 2^-23 of o."""
+    import paper_2606_28831_amd as hk
+    heads = 16
+    c, q, z = _two_keys("f32", D, n, heads, width, ctx)
+    d, ch = hk.dims(1, heads, heads, D), _chunks([n])
+    o, lse = torch.zeros(n, heads, D, device=DEV), torch.zeros(n, heads, device=DEV)
+    hk.hk_chunk_attn(d, c.kv, ch, q, 1.0, o, hk.chunk_attn_workspace(d, ch, c.width, DEV), lse=lse)
+    torch.cuda.synchronize()
+    want = np.tanh((z[..., 0] - z[..., 1]) / 2).T[:, :, None]
+    p = 0.5 * (1 + np.abs(want))
+    each = 0.7 * (2.0 ** -24 + 2.0 ** -24) + 2.0 ** -23
+    bound = 2 * p * (1 - p) * 2 * each + 4 * 2.0 ** -23 * p + 2.0 ** -23 * np.abs(want)
+    assert (np.abs(np64(o) - want) <= bound).all()
