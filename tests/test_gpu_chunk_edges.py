@@ -273,3 +273,24 @@ def test_fp32_probabilities_keep_their_bits(D, n, ctx, width):
     each = 0.7 * (2.0 ** -24 + 2.0 ** -24) + 2.0 ** -23
     bound = 2 * p * (1 - p) * 2 * each + 4 * 2.0 ** -23 * p + 2.0 ** -23 * np.abs(want)
     assert (np.abs(np64(o) - want) <= bound).all()
+
+
+@pytest.mark.parametrize("dtype,D,n,ctx,width", [
+    ("f32", 64, 20, 2, None), ("f32", 128, 64, 2, None), ("f32", 128, 20, 3000, 400), ("f32", 64, 64, 3000, 400),
+    ("bf16", 128, 20, 2, None), ("bf16", 64, 20, 3000, 400), ("bf16", 128, 64, 2, None), ("bf16", 64, 64, 3000, 400)])
+def test_small_lses(dtype, D, n, ctx, width):
+    """LSEs of two keys, 0.2 to 1.2: off by what the probabilities are (above; in bf16 tiles an exponent of up to
+    32, rounded to 2^-20), by two additions of the sum, cut, by the logarithm of a value in [0.5, 1), by the sum
+    of it and a whole number up to 4 (2^-22), and by the product."""
+    import paper_2606_28831_amd as hk
+    heads = 16
+    c, q, z = _two_keys(dtype, D, n, heads, width, ctx)
+    d, ch = hk.dims(1, heads, heads, D), _chunks([n])
+    o, lse = torch.zeros(n, heads, D, dtype=q.dtype, device=DEV), torch.zeros(n, heads, device=DEV)
+    hk.hk_chunk_attn(d, c.kv, ch, q, 1.0, o, hk.chunk_attn_workspace(d, ch, c.width, DEV), lse=lse)
+    torch.cuda.synchronize()
+    want = np.logaddexp(z[..., 0], z[..., 1]).T
+    tile = dtype == "bf16" and n > 32
+    each = 0.7 * (2.0 ** -24 + (2.0 ** -20 if tile else 2.0 ** -24)) + 2.0 ** -23
+    bound = each + 2 * 2.0 ** -23 + 0.7 * (2.0 ** -23 + 2.0 ** -23) + 2.0 ** -23 * np.abs(want)
+    assert (np.abs(np64(lse) - want) <= bound).all()
