@@ -480,7 +480,8 @@ hk_status hk_write_kv(const hk_dims* dims, const hk_paged_kv* kv, int32_t n_laye
  * more than 32 queries of a KV head can come (floor(n_tokens * Hq / Hkv / 128) + NS) * Hkv < 2^24, the
  * workgroups that a launch takes (HK_ERR_SHAPE).  Scores, sums and outputs are accumulated in
  * fp32.  A bf16 cache's probabilities enter the product with V in two bf16 parts (16 bits and more) in
- * chunks of up to 32 queries of a KV head (len * Hq / Hkv), rounded to bf16 once in longer ones.
+ * chunks of up to 32 queries of a KV head (len * Hq / Hkv), rounded to bf16 once in longer ones, where o is
+ * normalised by the sum of the rounded.
  * workspace: >= hk_chunk_attn_workspace_size(dims, chunks, kv->max_pages) bytes, 256-byte aligned
  * (never 0 for sizes that are accepted); calls that overlap on one workspace race.
  */

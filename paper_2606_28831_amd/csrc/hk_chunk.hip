@@ -23,13 +23,15 @@
 // as exp2(z - m - bias)), where 2^bias is at least 2^CH_SLACK times the keys of the row: sums of P V
 // and their merge cannot pass the top of the fp32 range where the result does not.  At its other end
 // that costs bits: V of 1e-32 is off by 4e-7 of its norm, 1e-34 by 2e-5, 1e-36 by 2e-3 (fp32).
-// Precision: scores, sums and outputs in fp32; the row sum, and so the LSE, is of the unrounded P.
+// Precision: scores, sums and outputs in fp32; the LSE is of the unrounded P.
 // Into the bf16 product P enters in the short kernel in two bf16 parts, to 2^-16 of each term: the
 // output is then off by its own rounding and little else, and as the kernel is bound by memory the
 // second product takes no time (64 sequences of 1 to 8 tokens over 784 to 5600: 175 us and 173,
-// single tokens 163 and 162).  In the tile kernel P is rounded once, to 2^-8 of each term at most: o
-// is off by 2.3e-3 of its norm instead of the 1.7e-3 of its own rounding, and a second part costs 31%
-// (8 prompts of 4096 1173 -> 1542 us, one chunk of 2048 over 28671 902 -> 1201).
+// single tokens 163 and 162).  In the tile kernel P is rounded once, to 2^-8 of each term at most, and o is
+// normalised by the sum of the rounded: over many keys it is off by 2.3e-3 of its norm instead of the
+// 1.7e-3 of its own rounding, and by no more than that where one key or few have the weight.  That sum takes
+// 1% to 2% at D 128 and 5% at 64 (8 prompts of 4096 1190 -> 1201 us, 656 -> 699; one chunk of 2048 over 28671
+// 869 -> 890); a second part of P would take 31% (1173 -> 1542, 902 -> 1201).
 #include <algorithm>
 #include <type_traits>
 
@@ -358,23 +360,25 @@ struct Args {
 };
 
 // One query's result of a tile kernel (lane: half of the dims): normalised into o, or state `at` of
-// its pieces (at < 0: there is one piece).
+// its pieces (at < 0: there is one piece).  l: sum of the probabilities, for the LSE and a piece's weight;
+// of_o: of those in acc, as they were rounded (acc / of_o is a mean of V, with one key that key's V).
 template <typename T, int D>
 __device__ __forceinline__ void put_state(const Args& a, int64_t row, int64_t at, const f32x16 (&acc)[D / 32],
-                                          float mb, float l) {
+                                          float mb, float l, float of_o) {
   const int hi = (threadIdx.x & 63) >> 5;
   if (at >= 0) {
+    const float up = sizeof(T) == 4 || l == 0.f ? 1.f : l / of_o;
     float* to = a.tile_o + at * D;
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         *reinterpret_cast<f32x4*>(to + 32 * dt + 8 * j + 4 * hi) =
-            f32x4{acc[dt][4 * j], acc[dt][4 * j + 1], acc[dt][4 * j + 2], acc[dt][4 * j + 3]};
+            f32x4{acc[dt][4 * j] * up, acc[dt][4 * j + 1] * up, acc[dt][4 * j + 2] * up, acc[dt][4 * j + 3] * up};
     if (hi == 0) *reinterpret_cast<f32x2*>(a.tile_ml + at * 2) = f32x2{l == 0.f ? -INFINITY : mb, l};
     return;
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;   // (a NaN stays one)
+  const float inv = l == 0.f ? 0.f : 1.f / of_o;   // (a NaN stays one)
   T* to = reinterpret_cast<T*>(a.o) + row * D;
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
@@ -706,7 +710,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void chunk_tile_f32_kernel(Ar
     }
     const float l = st.l + __shfl_xor(st.l, 32, 64);
     if (w0 + (lane & 31) < w.rows)
-      put_state<float, D>(a, row, pieces.state < 0 ? -1 : pieces.state + r - w.r0, st.acc, st.ref.whole(bias), l);
+      put_state<float, D>(a, row, pieces.state < 0 ? -1 : pieces.state + r - w.r0, st.acc, st.ref.whole(bias), l, l);
   }
 }
 
@@ -854,7 +858,7 @@ __global__ __launch_bounds__(256, 2) void chunk_tile_bf16_kernel(Args a) {
       for (int e = 0; e < 16; ++e) acc[dt][e] = 0.f;
     Reference ref;
     ref.init();
-    float l = 0.f;
+    float l = 0.f, rounded[2] = {0.f, 0.f};                      // sums of P, and of P as it enters the product
 
     const int k_at = L::k_lane(lane), v_at = L::v_lane(lane);    // the lane's fragments within 32 keys
     auto k_frag = [&](const char* k, int s) {
@@ -881,6 +885,8 @@ __global__ __launch_bounds__(256, 2) void chunk_tile_bf16_kernel(Args a) {
     // latency is behind an MFMA and another pair's work.  The empty asm statements keep what is computed
     // beside an MFMA in its place.
     float sum[2];
+    uint32_t ones = 0x3f803f80;                                  // two bf16 of 1
+    asm volatile("" : "+s"(ones));
     auto scale = [&](f32x16& zc, int k) {
       zc[2 * k] = fmaf(zc[2 * k], c2, -ref.off);
       zc[2 * k + 1] = fmaf(zc[2 * k + 1], c2, -ref.off);
@@ -893,7 +899,12 @@ __global__ __launch_bounds__(256, 2) void chunk_tile_bf16_kernel(Args a) {
       sum[0] = k ? sum[0] + zc[2 * k] : zc[0];
       sum[1] = k ? sum[1] + zc[2 * k + 1] : zc[1];
       bp[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{zc[2 * k], zc[2 * k + 1]}), bf16x2));
-      asm volatile("" : "+v"(bp[k]), "+v"(sum[0]), "+v"(sum[1]));
+      if (k & 1)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          rounded[i] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, bp[k - 1 + i]),
+                                                       __builtin_bit_cast(bf16x2, ones), rounded[i], false);
+      asm volatile("" : "+v"(bp[k]), "+v"(sum[0]), "+v"(sum[1]), "+v"(rounded[0]), "+v"(rounded[1]));
     };
     auto weigh = [&](f32x16& zc, int k) {
       if (k + 1 < 8) raise(zc, k + 1);
@@ -954,6 +965,8 @@ __global__ __launch_bounds__(256, 2) void chunk_tile_bf16_kernel(Args a) {
         zm = fmaxf(zm, __shfl_xor(zm, 32, 64));
         const float alpha = ref.move(fmaxf(ref.m, ceilf(zm)), bias);
         l *= alpha;
+        rounded[0] *= alpha;
+        rounded[1] *= alpha;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -1071,8 +1084,10 @@ __global__ __launch_bounds__(256, 2) void chunk_tile_bf16_kernel(Args a) {
       if (t + 1 < tiles) step(t + 1, z[1], z[0]);
     }
     l += __shfl_xor(l, 32, 64);
+    float of_o = rounded[0] + rounded[1];
+    of_o += __shfl_xor(of_o, 32, 64);
     if (w0 + (lane & 31) < w.rows)
-      put_state<uint16_t, D>(a, row, pieces.state < 0 ? -1 : pieces.state + r - w.r0, acc, ref.whole(bias), l);
+      put_state<uint16_t, D>(a, row, pieces.state < 0 ? -1 : pieces.state + r - w.r0, acc, ref.whole(bias), l, of_o);
   }
 }
 

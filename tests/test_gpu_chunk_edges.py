@@ -294,3 +294,29 @@ def test_small_lses(dtype, D, n, ctx, width):
     each = 0.7 * (2.0 ** -24 + (2.0 ** -20 if tile else 2.0 ** -24)) + 2.0 ** -23
     bound = each + 2 * 2.0 ** -23 + 0.7 * (2.0 ** -23 + 2.0 ** -23) + 2.0 ** -23 * np.abs(want)
     assert (np.abs(np64(lse) - want) <= bound).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n,ctx,width", [(64, 2, None), (64, 3000, 400)])
+def test_one_key_of_weight_has_its_v(D, n, ctx, width):
+    """Longer chunks of a bf16 cache round P, but o stays a mean of V: of two keys V0 and V1 = -V0 it is off by
+    p0 p1 |V0 - V1| of the two roundings' difference, 2 x 2^-8 at most, and by its own rounding; sums and
+    products of a few steps beside.  A prompt's first token has the first V."""
+    import paper_2606_28831_amd as hk
+    heads = 16
+    c, q, z = _two_keys("bf16", D, n, heads, width, ctx)
+    for h in range(heads):
+        c.k_pool[int(c.t[h, 0]), :2, 0] *= 16.0
+    z = z * 16.0
+    d, ch = hk.dims(1, heads, heads, D), _chunks([n])
+    o = torch.zeros(n, heads, D, dtype=q.dtype, device=DEV)
+    hk.hk_chunk_attn(d, c.kv, ch, q, 1.0, o, hk.chunk_attn_workspace(d, ch, c.width, DEV))
+    torch.cuda.synchronize()
+    want = np.tanh((z[..., 0] - z[..., 1]) / 2).T[:, :, None]
+    p = 0.5 * (1 + np.abs(want))
+    off = 2 * p * (1 - p) * (2 * 2.0 ** -8) * 1.02 + 2.0 ** -19
+    assert (np.abs(np64(o) - want) <= off + 2.0 ** -8 * (np.abs(want) + off)).all()
+    c = Cache([n] * 4, D, "bf16", seed=9)
+    q, o, lse = _attend(c, [n], 4, 1, D, "bf16")
+    for h in range(4):
+        assert torch.equal(o[0, h], c.v_pool[int(c.t[h, 0]), 0])
