@@ -612,7 +612,7 @@ struct Pieces {
 // fp32: four waves take 32 rows each; the next tile's pages load while a tile is computed.  Bound by
 // the fp32 matrix rate, a sixteenth of bf16's (154 TFLOP/s in a large product): 16 sequences of up to
 // 203 tokens over 2000, 32/8 heads of 64: 316 us, 97 TFLOP/s (tiles of 256 rows: 497); 4 prompts of 2000:
-// 106 TFLOP/s, of 128 101, at one workgroup a CU.
+// 105 TFLOP/s, of 128 101, at one workgroup a CU.
 template <int D, bool PLANNED>
 __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void chunk_tile_f32_kernel(Args a) {
   using L = TileLayout<float, D>;
@@ -762,9 +762,9 @@ __device__ __forceinline__ void direct_wait() { asm volatile("s_waitcnt vmcnt(%0
 // one's start, end and waits to be beside the other's work (measured against one of eight waves and
 // tiles of 64 keys, 8 prompts of 4096 tokens, 32 / 8 heads: D 128 1152 us and 1172, D 64 697 and 786).
 // Bound by the products (2048 cycles of each SIMD for 64 keys) beside as many cycles of exponentials,
-// sums and maxima, which overlap in part, and LDS reads at half their rate: 890 to 990 TFLOP/s by the
+// sums and maxima, which overlap in part, and LDS reads at half their rate: 880 to 980 TFLOP/s by the
 // card, of 1231 in a large library product; the products alone run at 1363.  By counters, 8 prompts of
-// 4096: MFMA busy for 45% of the SIMDs' cycles at 1.93 GHz, vector instructions for 42%, no LDS conflicts.
+// 4096: MFMA busy for 44% of the SIMDs' cycles at 1.88 GHz, vector instructions for 43%, no LDS conflicts.
 // Waves 0 and 1 bring a page of K each, three tiles ahead of the wait for it, waves 2 and 3 the pages
 // of V.
 template <int D, bool PLANNED>
