@@ -26,6 +26,12 @@
  *   hk_chunk_attn     causal attention of the chunks over the paged cache
  *   hk_verify_draft   drafted tokens against the target's probabilities
  *   hk_trim_slots     the newest slots of every head back to the pool
+ * A cache held in 8 bits (a scale per row, half the bytes of bf16):
+ *   hk_write_kv8      K and V rows quantised into the pool through a slot map
+ *   hk_read_kv8       rows read back through a slot map
+ *   hk_decode_attn8   decode attention over the 8-bit pages
+ *   hk_chunk_attn8    causal attention of chunks of new tokens over them
+ *   hk_compact8       the Cascade-Cache rewrite of codes and scales
  * Step 4 (Sec. 3.1, hard budget; Sec. 3.3.1 budget thresholds L_lower / L_upper):
  *   hk_score_rows     each window row's own attention probabilities over the candidates
  *   hk_vote_topp      Cautious Update: every row's own Top-p set, counted as votes
@@ -76,7 +82,7 @@ typedef int32_t hk_status;
 enum {
   HK_OK = 0,
   HK_ERR_ARG = 1,        /* null pointer, non-positive size, scalar out of range      */
-  HK_ERR_DTYPE = 2,      /* dtype is not HK_F32 or HK_BF16                             */
+  HK_ERR_DTYPE = 2,      /* dtype is not one that the call takes                       */
   HK_ERR_SHAPE = 3,      /* unsupported shape: D not 64/128, Hq % Hkv != 0,
                             G*W > 256, S_max > 32768, ...                              */
   HK_ERR_ALIGN = 4,      /* a pointer is not 16-byte aligned (256 for workspace)       */
@@ -94,7 +100,9 @@ enum {
                             token rows, or a chunk over max_len; cache left unchanged  */
 };
 
-typedef enum { HK_F32 = 0, HK_BF16 = 1 } hk_dtype;
+/* HK_I8 and HK_E4M3 are the codes of 8-bit caches (hk_paged_kv8): hk_reserve_slots, hk_trim_slots
+ * and hk_budget_plan, which read no rows, and the hk_*8 entry points take them, no other. */
+typedef enum { HK_F32 = 0, HK_BF16 = 1, HK_I8 = 2, HK_E4M3 = 3 } hk_dtype;
 
 /* One paged Cascade Cache (any number of heads; layers may share one pool). */
 typedef struct {
@@ -124,7 +132,7 @@ typedef struct {
 } hk_dims;
 
 enum { HK_OP_SCORE = 0, HK_OP_COMPACT = 1, HK_OP_DECODE = 2, HK_OP_APPEND = 3, HK_OP_COMPRESS = 4,
-       HK_OP_SELECT = 5, HK_OP_RESERVE = 6, HK_OP_TRIM = 7 };
+       HK_OP_SELECT = 5, HK_OP_RESERVE = 6, HK_OP_TRIM = 7, HK_OP_DECODE8 = 8 };
 
 /* Bytes of workspace entry point `op` needs for these dims and table width (HK_OP_SELECT:
  * hk_select_workspace_size(dims->NS * dims->Hkv, 16 * max_pages)). */
@@ -609,6 +617,82 @@ hk_status hk_compact_modes(const hk_dims* dims, const hk_paged_kv* kv, const uin
                            int32_t L_dense, const int32_t* head_mode, const hk_allocator* alloc,
                            int32_t* status, void* workspace, size_t ws_bytes, hipStream_t stream);
 
+/* ------------------------------------------------------------------ a8: a cache held in 8 bits
+ * Every K and V row of D values as D codes and one fp32 scale: 132 bytes of D 128 instead of bf16's
+ * 256.  A code stands for its value as int8 (HK_I8) or as an 8-bit float of 4 exponent and 3 mantissa
+ * bits (HK_E4M3, largest value 448, no infinities), and a row for code * scale.  With M = 127 or 448,
+ * a row x is written as
+ *   a = max(max_d |x_d|, 2^-100),  scale = a / M,  code_d = round(x_d * (M / a)),
+ * every step rounded to fp32, codes to the nearest, ties to even: off by half a step of int8,
+ * a / 254, or by 2^-4 of the value with e4m3 (half of its smallest step, a / 448 / 1024, below
+ * a / 448 / 64).  A row that holds an infinite value or NaN has codes 0 and the scale NaN: it reads
+ * back as NaN, and so do the results of the queries that see it.
+ * Tables, masks, allocator and slot maps are those of hk_paged_kv: hk_reserve_slots, hk_trim_slots and
+ * hk_budget_plan take &kv8->kv as it is.  hk_score and hk_score_rows take K read back (hk_read_kv8);
+ * the selection then goes to hk_compact8.
+ */
+typedef struct {
+  hk_paged_kv kv;        /* pools of codes, [num_pages][16][D] bytes; kv.dtype HK_I8 or HK_E4M3 */
+  float* k_scale;        /* [num_pages][16]                                             */
+  float* v_scale;        /* [num_pages][16]                                             */
+} hk_paged_kv8;
+
+/* K and V rows of `dtype` (HK_F32 or HK_BF16) into the pool, quantised as above: row (layer l, token
+ * t, KV head h) goes to pool row slot_map[l][t][h]; rows whose entry lies outside [0, 16 * num_pages)
+ * are neither read nor written.  Strides, alignment and limits as for hk_write_kv, the scales 16-byte
+ * aligned.  Two rows with one slot race.  Of kv8->kv only the pools, num_pages and dtype are used.
+ */
+hk_status hk_write_kv8(const hk_dims* dims, const hk_paged_kv8* kv8, int32_t n_layers,
+                       int32_t n_tokens, const int64_t* slot_map, hk_dtype dtype, const void* k_new,
+                       int64_t k_layer_stride, int64_t k_row_stride, const void* v_new,
+                       int64_t v_layer_stride, int64_t v_row_stride, hipStream_t stream);
+
+/* Its inverse: pool rows read back, code * scale rounded to fp32 and then to `dtype`, into rows of
+ * k_out and v_out laid out as hk_write_kv8's are (v_out NULL: K alone).  Rows whose entry lies outside
+ * [0, 16 * num_pages) are left as they are; several rows may have one slot.
+ */
+hk_status hk_read_kv8(const hk_dims* dims, const hk_paged_kv8* kv8, int32_t n_layers,
+                      int32_t n_tokens, const int64_t* slot_map, hk_dtype dtype, void* k_out,
+                      int64_t k_layer_stride, int64_t k_row_stride, void* v_out,
+                      int64_t v_layer_stride, int64_t v_row_stride, hipStream_t stream);
+
+/* hk_decode_attn over an 8-bit cache: q [NS][Hq][D] in `dtype` (HK_F32 or HK_BF16), o [NS][Hq][D]
+ * fp32, lse [NS][Hq] fp32 or NULL.  Codes enter the products exactly; q, scores, probabilities, sums
+ * and outputs keep fp32.  A head with no valid slot gives o = 0, lse = -inf.  What masked slots and
+ * slots past the row's end hold is not read into the result.  Sums stay finite to the top of the fp32
+ * range; values below 2^-80 (1e-24) lose bits.  A valid slot must not hold an e4m3 code of NaN (0x7f,
+ * 0xff): hk_write_kv8 writes none, and what the sequence's results then are is not said.
+ * The ranges that a row is split into follow from the sizes of the call alone; the same row's last bits
+ * can change with them.
+ * Hq / Hkv at most 64 (HK_ERR_SHAPE); all pointers 16-byte aligned but the tables' and lse, of their
+ * types' alignment; workspace: >= hk_workspace_size(HK_OP_DECODE8) bytes, 256-byte aligned; calls that
+ * overlap on one workspace race.
+ */
+hk_status hk_decode_attn8(const hk_dims* dims, hk_dtype dtype, const void* q,
+                          const hk_paged_kv8* kv8, float sm_scale, float* o, float* lse,
+                          void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* hk_chunk_attn over an 8-bit cache: q and o in `dtype` (HK_F32 or HK_BF16), the meaning, layouts,
+ * strides and limits of hk_chunk_attn otherwise; range and codes as for hk_decode_attn8.
+ * workspace: >= hk_chunk_attn8_workspace_size(dims, chunks, kv8->kv.max_pages) bytes, 256-byte aligned
+ * (never 0 for sizes that are accepted); calls that overlap on one workspace race.
+ */
+size_t hk_chunk_attn8_workspace_size(const hk_dims* dims, const hk_chunks* chunks,
+                                     int32_t max_pages);
+hk_status hk_chunk_attn8(const hk_dims* dims, const hk_paged_kv8* kv8, const hk_chunks* chunks,
+                         hk_dtype dtype, const void* q, int64_t q_row_stride, float sm_scale,
+                         void* o, float* lse, void* workspace, size_t ws_bytes,
+                         hipStream_t stream);
+
+/* hk_compact (head_mode NULL) or hk_compact_modes (head_mode [n_heads] HK_BUDGET_*, L_sparse not used)
+ * of an 8-bit cache: every moved row takes its codes and its scales along, bit for bit.  Workspace
+ * (HK_OP_COMPACT), allocator, order and HK_FLAG_NOSPACE as there.
+ */
+hk_status hk_compact8(const hk_dims* dims, const hk_paged_kv8* kv8, const uint32_t* sel_bits,
+                      int32_t L_dense, int32_t L_sparse, const int32_t* head_mode,
+                      const hk_allocator* alloc, int32_t* status, void* workspace,
+                      size_t ws_bytes, hipStream_t stream);
+
 /* ------------------------------------------------------------------ kernel timing
  * Optional HIP-event timing of individual kernels, for measurement harnesses (not part of
  * the method).  hk_timing_enable(mask) selects the kernels to time: bit k of mask stands
@@ -626,8 +710,8 @@ enum {
   HK_TK_CALIBRATE = 3,     /* hk_calibrate                                               */
   HK_TK_TOPP = 4,          /* hk_topp_select                                             */
   HK_TK_SOLVE_T = 5,       /* hk_calibrate_solve_T and hk_calibrate_solve_T_gd           */
-  HK_TK_COMPACT_GATHER = 6,/* hk_compact: condensed-row gather into fresh pages          */
-  HK_TK_COMPACT_META = 7,  /* hk_compact: plan, alloc, table, push (four launches)       */
+  HK_TK_COMPACT_GATHER = 6,/* hk_compact(8): condensed-row gather into fresh pages       */
+  HK_TK_COMPACT_META = 7,  /* hk_compact(8): plan, alloc, table, push (four launches)    */
   HK_TK_DECODE_SPLIT = 8,  /* hk_decode_attn: split-K partial states                     */
   HK_TK_DECODE_MERGE = 9,  /* hk_decode_attn: merge of the partial states                */
   HK_TK_APPEND = 10,       /* hk_append_kv: count + write, timed together                */
@@ -643,7 +727,11 @@ enum {
   HK_TK_CHUNK_MERGE = 20,  /* hk_chunk_attn: merge of the splits' states                 */
   HK_TK_VERIFY = 21,       /* hk_verify_draft: sums + pick, timed together               */
   HK_TK_TRIM = 22,         /* hk_trim_slots: count + write, timed together               */
-  HK_TK_COUNT = 23
+  HK_TK_WRITE_KV8 = 23,    /* hk_write_kv8                                               */
+  HK_TK_READ_KV8 = 24,     /* hk_read_kv8                                                */
+  HK_TK_ATTN8 = 25,        /* hk_decode_attn8, hk_chunk_attn8: attention of rows and ranges */
+  HK_TK_ATTN8_MERGE = 26,  /* hk_decode_attn8, hk_chunk_attn8: merge of the ranges' states */
+  HK_TK_COUNT = 27
 };
 hk_status hk_timing_enable(uint32_t kernel_mask);
 hk_status hk_timing_read(int32_t kernel, double* total_ms, int64_t* launches);

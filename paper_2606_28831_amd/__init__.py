@@ -26,13 +26,15 @@ __all__ = ["HardKVError", "lib", "PagedKV", "Allocator", "hk_score", "hk_calibra
            "OP_SELECT", "hk_select_workspace_size", "select_workspace", "hk_topp_select_ws",
            "hk_calibrate_topp_ws", "Chunks", "OP_RESERVE", "OP_TRIM", "FLAG_CHUNK", "hk_reserve_slots",
            "hk_write_kv", "hk_chunk_attn_workspace_size", "chunk_attn_workspace", "hk_chunk_attn",
-           "hk_verify_workspace_size", "verify_workspace", "hk_verify_draft", "hk_trim_slots"]
+           "hk_verify_workspace_size", "verify_workspace", "hk_verify_draft", "hk_trim_slots",
+           "PagedKV8", "OP_DECODE8", "hk_write_kv8", "hk_read_kv8", "hk_decode_attn8",
+           "hk_chunk_attn8_workspace_size", "chunk_attn8_workspace", "hk_chunk_attn8", "hk_compact8"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libhardkv.so")
 
-HK_F32, HK_BF16 = 0, 1
+HK_F32, HK_BF16, HK_I8, HK_E4M3 = 0, 1, 2, 3
 OP_SCORE, OP_COMPACT, OP_DECODE, OP_APPEND, OP_COMPRESS, OP_SELECT = 0, 1, 2, 3, 4, 5
-OP_RESERVE, OP_TRIM = 6, 7
+OP_RESERVE, OP_TRIM, OP_DECODE8 = 6, 7, 8
 FLAG_NOSPACE, FLAG_NAN, FLAG_RANGE, FLAG_CHUNK = 1, 2, 4, 8
 ERR_SCRATCH = 7
 BUDGET_KEEP, BUDGET_SPARSE, BUDGET_REWRITE = 0, 1, 2
@@ -45,12 +47,15 @@ EXPORTED = ["hk_score", "hk_calibrate", "hk_calibrate_solve_T", "hk_topp_select"
             "hk_probe", "hk_decode_plan", "hk_decode_attn_noalloc", "hk_decode_noalloc_scratch_bytes",
             "hk_select_workspace_size", "hk_topp_select_ws", "hk_calibrate_topp_ws",
             "hk_reserve_slots", "hk_write_kv", "hk_chunk_attn_workspace_size", "hk_chunk_attn",
-            "hk_verify_workspace_size", "hk_verify_draft", "hk_trim_slots"]
+            "hk_verify_workspace_size", "hk_verify_draft", "hk_trim_slots",
+            "hk_write_kv8", "hk_read_kv8", "hk_decode_attn8", "hk_chunk_attn8_workspace_size",
+            "hk_chunk_attn8", "hk_compact8"]
 # kernel ids of hk_timing_read, in header order
 TIMED_KERNELS = ["score_pass1", "score_merge", "score_pass2", "calibrate", "topp", "solve_T",
                  "compact_gather", "compact_meta", "decode_split", "decode_merge", "append",
                  "calib_topp", "score_rows", "vote", "vote_count", "budget_plan", "budget_select",
-                 "reserve", "write_kv", "chunk_attn", "chunk_merge", "verify", "trim"]
+                 "reserve", "write_kv", "chunk_attn", "chunk_merge", "verify", "trim",
+                 "write_kv8", "read_kv8", "attn8", "attn8_merge"]
 
 
 class HardKVError(RuntimeError):
@@ -66,6 +71,10 @@ class hk_paged_kv(C.Structure):
     _fields_ = [("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("page_table", C.c_void_p),
                 ("page_mask", C.c_void_p), ("n_pages", C.c_void_p), ("num_pages", C.c_int32),
                 ("max_pages", C.c_int32), ("dtype", C.c_int32)]
+
+
+class hk_paged_kv8(C.Structure):
+    _fields_ = [("kv", hk_paged_kv), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
 
 
 class hk_allocator(C.Structure):
@@ -171,6 +180,19 @@ def lib():
         L.hk_trim_slots.restype = I32
         L.hk_trim_slots.argtypes = [C.POINTER(hk_dims), C.POINTER(hk_paged_kv), I32, P,
                                     C.POINTER(hk_allocator), P, SZ, P]
+        KV8 = C.POINTER(hk_paged_kv8)
+        L.hk_write_kv8.restype = I32
+        L.hk_write_kv8.argtypes = [C.POINTER(hk_dims), KV8, I32, I32, P, I32, P, I64, I64, P, I64, I64, P]
+        L.hk_read_kv8.restype = I32
+        L.hk_read_kv8.argtypes = [C.POINTER(hk_dims), KV8, I32, I32, P, I32, P, I64, I64, P, I64, I64, P]
+        L.hk_decode_attn8.restype = I32
+        L.hk_decode_attn8.argtypes = [C.POINTER(hk_dims), I32, P, KV8, F, P, P, P, SZ, P]
+        L.hk_chunk_attn8_workspace_size.restype = SZ
+        L.hk_chunk_attn8_workspace_size.argtypes = [C.POINTER(hk_dims), C.POINTER(hk_chunks), I32]
+        L.hk_chunk_attn8.restype = I32
+        L.hk_chunk_attn8.argtypes = [C.POINTER(hk_dims), KV8, C.POINTER(hk_chunks), I32, P, I64, F, P, P, P, SZ, P]
+        L.hk_compact8.restype = I32
+        L.hk_compact8.argtypes = [C.POINTER(hk_dims), KV8, P, I32, I32, P, C.POINTER(hk_allocator), P, P, SZ, P]
         L.hk_probe.restype = I32
         L.hk_probe.argtypes = [I32, I32, I32, P, P]
         L.hk_timing_enable.restype = I32
@@ -254,6 +276,44 @@ class PagedKV:
     @property
     def max_pages(self):
         return self.page_table.shape[1]
+
+
+CODE_DTYPES = {torch.int8: HK_I8, torch.float8_e4m3fn: HK_E4M3}
+ROW_DTYPES = {torch.float32: HK_F32, torch.bfloat16: HK_BF16}
+
+
+class PagedKV8(PagedKV):
+    """A paged Cascade Cache held in 8 bits: pools [pages, 16, D] of int8 or float8_e4m3fn codes and
+    fp32 scales [pages, 16] of their rows.  Slots are reserved and trimmed as of a PagedKV; rows are
+    written, read back, attended to and rewritten by the hk_*8 calls."""
+
+    def __init__(self, k_pool, v_pool, k_scale, v_scale, page_table, page_mask, n_pages):
+        self.k_pool, self.v_pool, self.k_scale, self.v_scale = k_pool, v_pool, k_scale, v_scale
+        self.page_table, self.page_mask, self.n_pages = page_table, page_mask, n_pages
+        if k_pool.dtype not in CODE_DTYPES:
+            raise HardKVError("codes must be int8 or float8_e4m3fn")
+        self.desc8 = hk_paged_kv8(
+            hk_paged_kv(k_pool.data_ptr(), v_pool.data_ptr(), page_table.data_ptr(), page_mask.data_ptr(),
+                        n_pages.data_ptr(), k_pool.shape[0], page_table.shape[1], CODE_DTYPES[k_pool.dtype]),
+            k_scale.data_ptr(), v_scale.data_ptr())
+        self.desc = self.desc8.kv
+        self._sizes = None
+
+    def sizes(self):
+        if self._sizes is None:
+            sizes = super().sizes()
+            self._sizes = None
+            for s in (self.k_scale, self.v_scale):
+                if (s.dtype != torch.float32 or not s.is_contiguous() or s.numel() != self.k_pool.shape[0] * 16
+                        or s.get_device() != sizes[2]):
+                    raise HardKVError("scales must be contiguous float32 [pages, 16], beside the pools")
+            self._sizes = sizes
+        return self._sizes
+
+    def rows(self, first_head: int, n_heads: int) -> "PagedKV8":
+        sl = slice(first_head, first_head + n_heads)
+        return PagedKV8(self.k_pool, self.v_pool, self.k_scale, self.v_scale, self.page_table[sl],
+                        self.page_mask[sl], self.n_pages[sl])
 
 
 class Allocator:
@@ -639,6 +699,85 @@ def hk_trim_slots(d: hk_dims, kv: PagedKV, n_drop, alloc: Allocator, ws, stream=
     _run("hk_trim_slots", kv.page_table, (n_drop, ws), stream, C.byref(d),
          C.byref(kv.desc), n,
          _vector(n_drop, n, torch.int32, "n_drop"), C.byref(alloc.desc), _ptr(ws), ws.numel())
+
+
+# ---------------------------------------------------------------- a cache held in 8 bits
+def _kv8(kv) -> PagedKV8:
+    if not isinstance(kv, PagedKV8):
+        raise HardKVError("an 8-bit cache (PagedKV8) is needed")
+    return kv
+
+
+def _row_dtype(t, what: str) -> int:
+    if t.dtype not in ROW_DTYPES:
+        raise HardKVError(f"{what} must be float32 or bfloat16")
+    return ROW_DTYPES[t.dtype]
+
+
+def _rows8(name, d, kv, n_tokens, slot_map, k, v, stream):
+    _need(k.dim() in (3, 4) and (v is None or v.dim() == k.dim()), "rows must be 3- or 4-d")
+    _fits(d, _kv8(kv), 0)
+    layers = k.shape[0] if k.dim() == 4 else 1
+    _need(v is None or v.dim() == 3 or v.shape[0] == layers, "K and V differ in layers")
+    dt = _row_dtype(k, "rows")
+    kp, kr = _token_rows(k, n_tokens, d.Hkv, d.D, k.dtype, "K rows")
+    vp, vr = (None, 0) if v is None else _token_rows(v, n_tokens, d.Hkv, d.D, k.dtype, "V rows")
+    _run(name, kv.k_pool, (slot_map, k, v), stream, C.byref(d), C.byref(kv.desc8), layers, int(n_tokens),
+         _vector(slot_map, layers * n_tokens * d.Hkv, torch.int64, "slot_map"), dt, kp,
+         k.stride(0) if layers > 1 else 0, kr, vp, v.stride(0) if v is not None and layers > 1 else 0, vr)
+
+
+def hk_write_kv8(d: hk_dims, kv: PagedKV8, n_tokens: int, slot_map, k_new, v_new, stream=None):
+    """hk_write_kv into an 8-bit cache, k_new and v_new in float32 or bfloat16."""
+    _need(v_new is not None, "v_new is needed")
+    _rows8("hk_write_kv8", d, kv, n_tokens, slot_map, k_new, v_new, stream)
+
+
+def hk_read_kv8(d: hk_dims, kv: PagedKV8, n_tokens: int, slot_map, k_out, v_out=None, stream=None):
+    """Rows read back through a slot map into k_out and v_out, laid out as hk_write_kv8's rows are."""
+    _rows8("hk_read_kv8", d, kv, n_tokens, slot_map, k_out, v_out, stream)
+
+
+def hk_decode_attn8(d: hk_dims, q, kv: PagedKV8, sm_scale: float, o, lse, ws, stream=None):
+    """q [NS, Hq, D] in float32 or bfloat16, o [NS, Hq, D] and lse [NS, Hq] (or None) in float32."""
+    _fits(d, _kv8(kv), d.NS * d.Hkv)
+    n = d.NS * d.Hq
+    _run("hk_decode_attn8", kv.k_pool, (q, o, lse, ws), stream, C.byref(d), _row_dtype(q, "q"),
+         _vector(q, n * d.D, q.dtype, "q"), C.byref(kv.desc8), float(sm_scale),
+         _vector(o, n * d.D, torch.float32, "o"), None if lse is None else _vector(lse, n, torch.float32, "lse"),
+         _ptr(ws), ws.numel())
+
+
+def hk_chunk_attn8_workspace_size(d: hk_dims, chunks: Chunks, max_pages: int) -> int:
+    return int(lib().hk_chunk_attn8_workspace_size(C.byref(d), C.byref(chunks.desc), int(max_pages)))
+
+
+def chunk_attn8_workspace(d: hk_dims, chunks: Chunks, max_pages: int, device) -> torch.Tensor:
+    n = max(256, hk_chunk_attn8_workspace_size(d, chunks, max_pages))
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def hk_chunk_attn8(d: hk_dims, kv: PagedKV8, chunks: Chunks, q, sm_scale: float, o, ws, lse=None, stream=None):
+    """q [tokens, Hq, D] and o in float32 or bfloat16, lse [tokens, Hq] float32 or None."""
+    T = chunks.n_tokens
+    _fits(d, _kv8(kv), d.NS * d.Hkv)
+    dt = _row_dtype(q, "q")
+    qp, qr = _token_rows(q, T, d.Hq, d.D, q.dtype, "q")
+    _need(q.dim() == 3, "q must be 3-d")
+    _run("hk_chunk_attn8", kv.k_pool, (chunks.start, q, o, lse, ws), stream, C.byref(d), C.byref(kv.desc8),
+         C.byref(chunks.desc), dt, qp, qr, float(sm_scale), _vector(o, T * d.Hq * d.D, q.dtype, "o"),
+         None if lse is None else _vector(lse, T * d.Hq, torch.float32, "lse"), _ptr(ws), ws.numel())
+
+
+def hk_compact8(d: hk_dims, kv: PagedKV8, sel_bits, L_dense: int, L_sparse: int, alloc: Allocator, status, ws,
+                head_mode=None, stream=None):
+    """hk_compact of an 8-bit cache, or with head_mode hk_compact_modes."""
+    H = d.NS * d.Hkv
+    _fits(d, _kv8(kv), H, alloc)
+    _run("hk_compact8", kv.k_pool, (sel_bits, head_mode, status, ws), stream, C.byref(d), C.byref(kv.desc8),
+         _vector(sel_bits, H * (kv.max_pages // 2), torch.int32, "sel_bits"), int(L_dense), int(L_sparse),
+         None if head_mode is None else _vector(head_mode, H, torch.int32, "head_mode"), C.byref(alloc.desc),
+         _status(status), _ptr(ws), ws.numel())
 
 
 def hk_timing_enable(kernels=None):

@@ -6,6 +6,7 @@
 
 #include "hk_chunk.h"
 #include "hk_internal.h"
+#include "hk_kv8.h"
 
 bool hk_decode_supports_group(int G);
 
@@ -28,12 +29,15 @@ hk_status check_dims(const hk_dims* d, bool need_w) {
   return HK_OK;
 }
 
+bool is_code(hk_dtype t) { return t == HK_I8 || t == HK_E4M3; }
+
 // The tables' pointers are read 16 bytes at a time where `wide`, an entry at a time otherwise (any
 // run of rows of a cache, such as one layer's, then begins at a legal address).
-hk_status check_kv(const hk_paged_kv* kv, bool need_v, bool wide = true) {
+// bits8: codes of an 8-bit cache are taken too.
+hk_status check_kv(const hk_paged_kv* kv, bool need_v, bool wide = true, bool bits8 = false) {
   if (!kv || !kv->k_pool || !kv->page_table || !kv->page_mask || !kv->n_pages) return HK_ERR_ARG;
   if (need_v && !kv->v_pool) return HK_ERR_ARG;
-  if (kv->dtype != HK_F32 && kv->dtype != HK_BF16) return HK_ERR_DTYPE;
+  if (kv->dtype != HK_F32 && kv->dtype != HK_BF16 && !(bits8 && is_code(kv->dtype))) return HK_ERR_DTYPE;
   if (kv->num_pages <= 0 || kv->max_pages <= 0) return HK_ERR_ARG;
   if (kv->max_pages % 2 != 0) return HK_ERR_SHAPE;                 // S_max multiple of 32
   if (!aligned16(kv->k_pool) || (need_v && !aligned16(kv->v_pool))) return HK_ERR_ALIGN;
@@ -42,6 +46,16 @@ hk_status check_kv(const hk_paged_kv* kv, bool need_v, bool wide = true) {
   if ((reinterpret_cast<uintptr_t>(kv->page_table) | reinterpret_cast<uintptr_t>(kv->n_pages)) % 4 ||
       reinterpret_cast<uintptr_t>(kv->page_mask) % 2)
     return HK_ERR_ALIGN;
+  return HK_OK;
+}
+
+hk_status check_kv8(const hk_paged_kv8* kv8, bool wide) {
+  if (!kv8) return HK_ERR_ARG;
+  const hk_status e = check_kv(&kv8->kv, true, wide, true);
+  if (e) return e;
+  if (!is_code(kv8->kv.dtype)) return HK_ERR_DTYPE;
+  if (!kv8->k_scale || !kv8->v_scale) return HK_ERR_ARG;
+  if (!aligned16(kv8->k_scale) || !aligned16(kv8->v_scale)) return HK_ERR_ALIGN;
   return HK_OK;
 }
 
@@ -63,6 +77,7 @@ size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
 constexpr int kMaxRows = 1 << 24;        // token rows of a call
 constexpr double kMaxQueries = 17179869184.0;   // token rows x query heads of the chunk attention
 constexpr long long kMaxThreads = 1ll << 32;    // of a launch, in one dimension: fewer
+constexpr double kMaxGroups = 16777216.0;       // workgroups of 256 threads of a launch: fewer
 constexpr int kMaxVocab = 1 << 20;
 constexpr int kMaxGroup = 64;            // query heads per KV head of the chunk attention
 
@@ -115,6 +130,9 @@ size_t hk_workspace_size(int32_t op, const hk_dims* d, int32_t max_pages) {
     case HK_OP_COMPRESS: return compress_ws(d, max_pages).total;
     case HK_OP_SELECT: return hk_select_wide_ws(d->NS * d->Hkv, max_pages * HK_PAGE);
     case HK_OP_RESERVE: return hk_reserve_ws(d->NS * d->Hkv);
+    case HK_OP_DECODE8:
+      return check_dims(d, false) || d->Hq / d->Hkv > kMaxGroup
+                 ? 0 : hk_attn8_ws(d->NS, d->Hq, d->Hkv, d->D, nullptr, max_pages);
     case HK_OP_TRIM: return hk_trim_ws(d->NS * d->Hkv);
     default: return 0;
   }
@@ -133,7 +151,7 @@ const char* hk_status_string(int32_t code, int32_t flags) {
   switch (code) {
     case HK_OK: return "HK_OK";
     case HK_ERR_ARG: return "HK_ERR_ARG: null pointer or size/scalar out of range";
-    case HK_ERR_DTYPE: return "HK_ERR_DTYPE: dtype must be HK_F32 or HK_BF16";
+    case HK_ERR_DTYPE: return "HK_ERR_DTYPE: dtype must be HK_F32 or HK_BF16 (8-bit caches: HK_I8 or HK_E4M3)";
     case HK_ERR_SHAPE: return "HK_ERR_SHAPE: unsupported shape";
     case HK_ERR_ALIGN: return "HK_ERR_ALIGN: pointer not 16-byte (workspace: 256-byte) aligned";
     case HK_ERR_WORKSPACE: return "HK_ERR_WORKSPACE: workspace smaller than hk_workspace_size()";
@@ -439,7 +457,7 @@ hk_status hk_budget_plan(const hk_dims* dims, const hk_paged_kv* kv, int32_t L_d
                          hipStream_t stream) {
   hk_status e = check_dims(dims, false);
   if (e) return e;
-  if ((e = check_kv(kv, false))) return e;
+  if ((e = check_kv(kv, false, true, true))) return e;
   if (!head_mode || !k_cap) return HK_ERR_ARG;
   if (L_dense < 0 || L_lower < 0 || L_upper < L_lower) return HK_ERR_ARG;
   return launched(hk_launch_budget_plan(dims->NS * dims->Hkv, kv->max_pages, kv->n_pages,
@@ -539,7 +557,7 @@ hk_status hk_reserve_slots(const hk_dims* dims, const hk_paged_kv* kv, const hk_
                            void* workspace, size_t ws_bytes, hipStream_t stream) {
   hk_status e = check_dims(dims, false);
   if (e) return e;
-  if ((e = check_kv(kv, false, false))) return e;
+  if ((e = check_kv(kv, false, false, true))) return e;
   if ((e = check_chunks(chunks))) return e;
   if (!alloc || !alloc->free_ids || !alloc->free_top || alloc->capacity <= 0) return HK_ERR_ARG;
   if (dims->NS % chunks->n_seq != 0) return HK_ERR_SHAPE;
@@ -629,7 +647,7 @@ hk_status hk_trim_slots(const hk_dims* dims, const hk_paged_kv* kv, int32_t n_se
                         const hk_allocator* alloc, void* workspace, size_t ws_bytes, hipStream_t stream) {
   hk_status e = check_dims(dims, false);
   if (e) return e;
-  if ((e = check_kv(kv, false, false))) return e;
+  if ((e = check_kv(kv, false, false, true))) return e;
   if (n_seq <= 0 || !n_drop || !alloc || !alloc->free_ids || !alloc->free_top) return HK_ERR_ARG;
   if (alloc->capacity < kv->num_pages) return HK_ERR_ARG;        // every page can be pushed
   if (dims->NS % n_seq != 0) return HK_ERR_SHAPE;
@@ -637,6 +655,116 @@ hk_status hk_trim_slots(const hk_dims* dims, const hk_paged_kv* kv, int32_t n_se
   if (!workspace || ws_bytes < hk_trim_ws(n_heads)) return HK_ERR_WORKSPACE;
   if (!aligned256(workspace)) return HK_ERR_ALIGN;
   return launched(hk_launch_trim(n_heads, dims->Hkv, kv, n_seq, n_drop, alloc, workspace, stream));
+}
+
+// rows of hk_write_kv8 and hk_read_kv8
+static hk_status check_rows8(const hk_dims* dims, const hk_paged_kv8* kv8, int32_t n_layers, int32_t n_tokens,
+                             const int64_t* slot_map, hk_dtype dtype, const void* k, int64_t k_layer, int64_t k_row,
+                             const void* v, int64_t v_layer, int64_t v_row) {
+  hk_status e = check_dims(dims, false);
+  if (e) return e;
+  if ((e = check_kv8(kv8, false))) return e;
+  if (n_layers <= 0 || n_tokens <= 0 || !slot_map) return HK_ERR_ARG;
+  if (dtype != HK_F32 && dtype != HK_BF16) return HK_ERR_DTYPE;
+  if (reinterpret_cast<uintptr_t>(slot_map) % 8) return HK_ERR_ALIGN;
+  const int es = dtype == HK_BF16 ? 2 : 4;
+  const int64_t row = (int64_t)dims->Hkv * dims->D;
+  if ((e = check_rows_at(k, k_row, row, es))) return e;
+  if (v && (e = check_rows_at(v, v_row, row, es))) return e;
+  if (n_layers > 1 && (k_layer % (16 / es) || (v && v_layer % (16 / es)))) return HK_ERR_ALIGN;
+  if (n_layers > kMaxRows || n_tokens > kMaxRows) return HK_ERR_SHAPE;
+  if ((double)n_layers * n_tokens * row * es / 16 >= 2147483648.0) return HK_ERR_SHAPE;
+  return HK_OK;
+}
+
+hk_status hk_write_kv8(const hk_dims* dims, const hk_paged_kv8* kv8, int32_t n_layers, int32_t n_tokens,
+                       const int64_t* slot_map, hk_dtype dtype, const void* k_new, int64_t k_layer_stride,
+                       int64_t k_row_stride, const void* v_new, int64_t v_layer_stride, int64_t v_row_stride,
+                       hipStream_t stream) {
+  if (!v_new) return HK_ERR_ARG;
+  const hk_status e = check_rows8(dims, kv8, n_layers, n_tokens, slot_map, dtype, k_new, k_layer_stride, k_row_stride,
+                                  v_new, v_layer_stride, v_row_stride);
+  if (e) return e;
+  return launched(hk_launch_write_kv8(dims->Hkv, dims->D, kv8, n_layers, n_tokens, slot_map, dtype, k_new,
+                                      n_layers > 1 ? k_layer_stride : 0, k_row_stride, v_new,
+                                      n_layers > 1 ? v_layer_stride : 0, v_row_stride, stream));
+}
+
+hk_status hk_read_kv8(const hk_dims* dims, const hk_paged_kv8* kv8, int32_t n_layers, int32_t n_tokens,
+                      const int64_t* slot_map, hk_dtype dtype, void* k_out, int64_t k_layer_stride,
+                      int64_t k_row_stride, void* v_out, int64_t v_layer_stride, int64_t v_row_stride,
+                      hipStream_t stream) {
+  const hk_status e = check_rows8(dims, kv8, n_layers, n_tokens, slot_map, dtype, k_out, k_layer_stride, k_row_stride,
+                                  v_out, v_layer_stride, v_row_stride);
+  if (e) return e;
+  return launched(hk_launch_read_kv8(dims->Hkv, dims->D, kv8, n_layers, n_tokens, slot_map, dtype, k_out,
+                                     n_layers > 1 ? k_layer_stride : 0, k_row_stride, v_out,
+                                     n_layers > 1 ? v_layer_stride : 0, v_row_stride, stream));
+}
+
+hk_status hk_decode_attn8(const hk_dims* dims, hk_dtype dtype, const void* q, const hk_paged_kv8* kv8,
+                          float sm_scale, float* o, float* lse, void* workspace, size_t ws_bytes,
+                          hipStream_t stream) {
+  hk_status e = check_dims(dims, false);
+  if (e) return e;
+  if ((e = check_kv8(kv8, false))) return e;
+  if (!q || !o || !(sm_scale > 0.f) || !std::isfinite(sm_scale)) return HK_ERR_ARG;
+  if (dtype != HK_F32 && dtype != HK_BF16) return HK_ERR_DTYPE;
+  if (dims->Hq / dims->Hkv > kMaxGroup) return HK_ERR_SHAPE;
+  if (!aligned16(q) || !aligned16(o) || reinterpret_cast<uintptr_t>(lse) % 4) return HK_ERR_ALIGN;
+  if (!workspace || ws_bytes < hk_attn8_ws(dims->NS, dims->Hq, dims->Hkv, dims->D, nullptr, kv8->kv.max_pages))
+    return HK_ERR_WORKSPACE;
+  if (!aligned256(workspace)) return HK_ERR_ALIGN;
+  if (hk_attn8_groups(dims->NS, dims->Hq, dims->Hkv, nullptr, kv8->kv.max_pages) >= kMaxGroups) return HK_ERR_SHAPE;
+  return launched(hk_launch_attn8(dims->NS, dims->Hq, dims->Hkv, dims->D, kv8, nullptr, dtype, q,
+                                  (int64_t)dims->Hq * dims->D, sm_scale, o, lse, workspace, stream));
+}
+
+size_t hk_chunk_attn8_workspace_size(const hk_dims* dims, const hk_chunks* chunks, int32_t max_pages) {
+  if (check_dims(dims, false) || !chunks || chunks->n_tokens <= 0 || chunks->max_len <= 0 || max_pages <= 0) return 0;
+  if (chunks->n_tokens > kMaxRows || chunks->max_len > kMaxRows || dims->Hq / dims->Hkv > kMaxGroup) return 0;
+  return hk_attn8_ws(dims->NS, dims->Hq, dims->Hkv, dims->D, chunks, max_pages);
+}
+
+hk_status hk_chunk_attn8(const hk_dims* dims, const hk_paged_kv8* kv8, const hk_chunks* chunks, hk_dtype dtype,
+                         const void* q, int64_t q_row_stride, float sm_scale, void* o, float* lse, void* workspace,
+                         size_t ws_bytes, hipStream_t stream) {
+  hk_status e = check_dims(dims, false);
+  if (e) return e;
+  if ((e = check_kv8(kv8, false))) return e;
+  if ((e = check_chunks(chunks))) return e;
+  if (!o || !(sm_scale > 0.f) || !std::isfinite(sm_scale)) return HK_ERR_ARG;
+  if (dtype != HK_F32 && dtype != HK_BF16) return HK_ERR_DTYPE;
+  if (dims->NS != chunks->n_seq || dims->Hq / dims->Hkv > kMaxGroup) return HK_ERR_SHAPE;
+  if ((double)chunks->n_tokens * dims->Hq > kMaxQueries) return HK_ERR_SHAPE;
+  if ((e = check_rows_at(q, q_row_stride, (int64_t)dims->Hq * dims->D, dtype == HK_BF16 ? 2 : 4))) return e;
+  if (!aligned16(o) || reinterpret_cast<uintptr_t>(lse) % 4 || reinterpret_cast<uintptr_t>(chunks->start) % 4)
+    return HK_ERR_ALIGN;
+  if (!workspace ||
+      ws_bytes < hk_attn8_ws(dims->NS, dims->Hq, dims->Hkv, dims->D, chunks, kv8->kv.max_pages))
+    return HK_ERR_WORKSPACE;
+  if (!aligned256(workspace)) return HK_ERR_ALIGN;
+  if (hk_attn8_groups(dims->NS, dims->Hq, dims->Hkv, chunks, kv8->kv.max_pages) >= kMaxGroups) return HK_ERR_SHAPE;
+  return launched(hk_launch_attn8(dims->NS, dims->Hq, dims->Hkv, dims->D, kv8, chunks, dtype, q, q_row_stride,
+                                  sm_scale, o, lse, workspace, stream));
+}
+
+hk_status hk_compact8(const hk_dims* dims, const hk_paged_kv8* kv8, const uint32_t* sel_bits, int32_t L_dense,
+                      int32_t L_sparse, const int32_t* head_mode, const hk_allocator* alloc, int32_t* status,
+                      void* workspace, size_t ws_bytes, hipStream_t stream) {
+  hk_status e = check_dims(dims, false);
+  if (e) return e;
+  if ((e = check_kv8(kv8, true))) return e;
+  const hk_paged_kv* kv = &kv8->kv;
+  if (!sel_bits || !alloc || !alloc->free_ids || !alloc->free_top) return HK_ERR_ARG;
+  if (alloc->capacity < kv->num_pages) return HK_ERR_ARG;        // as for hk_compact
+  if (L_dense < 0 || L_sparse < 0) return HK_ERR_ARG;
+  if ((long long)kv->max_pages * 6 > 160 * 1024) return HK_ERR_SHAPE;
+  const int n_heads = dims->NS * dims->Hkv;
+  if (!workspace || ws_bytes < hk_compact_ws(n_heads, kv->max_pages)) return HK_ERR_WORKSPACE;
+  if (!aligned256(workspace)) return HK_ERR_ALIGN;
+  return launched(hk_launch_compact8(n_heads, dims->D, kv8, sel_bits, L_dense, L_sparse, head_mode, alloc, status,
+                                     workspace, stream));
 }
 
 hk_status hk_probe(int32_t kind, int32_t blocks, int32_t iters, float* out, hipStream_t stream) {

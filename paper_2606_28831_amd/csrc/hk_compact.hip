@@ -16,6 +16,7 @@
 // budget (Sec. 3.1 Step 4), set per head by its state: all older pages condensed
 // (rewrite), all sparse (sparse loading), or none (the row is kept).
 #include "hk_internal.h"
+#include "hk_kv8.h"
 
 namespace hk {
 
@@ -211,11 +212,13 @@ __device__ __forceinline__ void store16(char* p, uint4 v) {
 // packed densely onto lane groups (row k of the selection goes to group k % RPI), all
 // loads issued before any store.  A selected slot of rank r (within the head's condensed
 // band) lands in slot r % 16 of new page r / 16, so consecutive ranks fill pages in order.
-template <int ROW_BYTES>
+// SCALES: a row's scales (an 8-bit cache's) go with it, by its first lane.
+template <int ROW_BYTES, bool SCALES>
 __global__ __launch_bounds__(256) void compact_gather_kernel(
     char* __restrict__ k_pool, char* __restrict__ v_pool, const int32_t* __restrict__ table,
     const uint16_t* __restrict__ masks, const uint32_t* __restrict__ sel_bits,
-    const int32_t* __restrict__ free_ids, int max_pages, CompactWs w) {
+    const int32_t* __restrict__ free_ids, int max_pages, CompactWs w, float* __restrict__ k_scale,
+    float* __restrict__ v_scale) {
   if (!w.g->ok) return;
   const int h = blockIdx.y;
   const int pp = blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -234,6 +237,7 @@ __global__ __launch_bounds__(256) void compact_gather_kernel(
   const int* popped = free_ids + w.g->base + w.alloc_off[h];
   const int nsel = __popc(m);
   uint4 kv[NI], vv[NI];
+  float ks[NI], vs[NI];
   int dst_slot[NI];
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
@@ -246,6 +250,10 @@ __global__ __launch_bounds__(256) void compact_gather_kernel(
       const size_t src = (src_page * HK_PAGE + t) * ROW_BYTES + chunk * 16;
       kv[i] = load16(k_pool + src);
       vv[i] = load16(v_pool + src);
+      if (SCALES && chunk == 0) {
+        ks[i] = k_scale[src_page * HK_PAGE + t];
+        vs[i] = v_scale[src_page * HK_PAGE + t];
+      }
       dst_slot[i] = rank0 + k;
     }
   }
@@ -256,6 +264,10 @@ __global__ __launch_bounds__(256) void compact_gather_kernel(
       const size_t dst = ((size_t)popped[rank >> 4] * HK_PAGE + (rank & 15)) * ROW_BYTES + chunk * 16;
       store16(k_pool + dst, kv[i]);
       store16(v_pool + dst, vv[i]);
+      if (SCALES && chunk == 0) {
+        k_scale[dst / ROW_BYTES] = ks[i];
+        v_scale[dst / ROW_BYTES] = vs[i];
+      }
     }
   }
 }
@@ -372,9 +384,10 @@ size_t hk_compact_ws(int n_heads, int max_pages) {
          2 * align256(sizeof(int) * (size_t)n_heads * max_pages) + align256(sizeof(CompactGlobals));
 }
 
-hipError_t hk_launch_compact(int n_heads, int D, const hk_paged_kv* kv, const uint32_t* sel_bits,
-                             int L_dense, int L_sparse, const int32_t* head_mode,
-                             const hk_allocator* alloc, int32_t* status, void* ws, hipStream_t st) {
+// k_scale, v_scale: an 8-bit cache's, or NULL
+static hipError_t launch_compact(int n_heads, int D, const hk_paged_kv* kv, float* k_scale, float* v_scale,
+                                 const uint32_t* sel_bits, int L_dense, int L_sparse, const int32_t* head_mode,
+                                 const hk_allocator* alloc, int32_t* status, void* ws, hipStream_t st) {
   const CompactWs w = carve(ws, n_heads, kv->max_pages);
   const int mp = kv->max_pages;
   {
@@ -387,18 +400,27 @@ hipError_t hk_launch_compact(int n_heads, int D, const hk_paged_kv* kv, const ui
     hipLaunchKernelGGL(compact_alloc_kernel, dim3(1), dim3(AL_NT), 0, st, n_heads, alloc->free_top,
                        status, w);
   }
-  const int row_bytes = D * (kv->dtype == HK_BF16 ? 2 : 4);
+  const int row_bytes = D * (k_scale ? 1 : kv->dtype == HK_BF16 ? 2 : 4);
   dim3 gg((mp + 3) / 4, n_heads);
   char* kp = static_cast<char*>(kv->k_pool);
   char* vp = static_cast<char*>(kv->v_pool);
+#define HK_GATHER(RB_, SC_)                                                                          \
+  hipLaunchKernelGGL((compact_gather_kernel<RB_, SC_>), gg, dim3(256), 0, st, kp, vp, kv->page_table, \
+                     kv->page_mask, sel_bits, alloc->free_ids, mp, w, k_scale, v_scale)
   {
-  TimedLaunch t(HK_TK_COMPACT_GATHER, st);
-  switch (row_bytes) {
-    case 128: hipLaunchKernelGGL((compact_gather_kernel<128>), gg, dim3(256), 0, st, kp, vp, kv->page_table, kv->page_mask, sel_bits, alloc->free_ids, mp, w); break;
-    case 256: hipLaunchKernelGGL((compact_gather_kernel<256>), gg, dim3(256), 0, st, kp, vp, kv->page_table, kv->page_mask, sel_bits, alloc->free_ids, mp, w); break;
-    default: hipLaunchKernelGGL((compact_gather_kernel<512>), gg, dim3(256), 0, st, kp, vp, kv->page_table, kv->page_mask, sel_bits, alloc->free_ids, mp, w); break;
+    TimedLaunch t(HK_TK_COMPACT_GATHER, st);
+    if (k_scale) {
+      if (row_bytes == 64) HK_GATHER(64, true);
+      else HK_GATHER(128, true);
+    } else if (row_bytes == 128) {
+      HK_GATHER(128, false);
+    } else if (row_bytes == 256) {
+      HK_GATHER(256, false);
+    } else {
+      HK_GATHER(512, false);
+    }
   }
-  }
+#undef HK_GATHER
   const size_t lds = (size_t)mp * (sizeof(int32_t) + sizeof(uint16_t));
   allow_dynamic_lds<compact_table_kernel>(lds);
   {
@@ -412,4 +434,17 @@ hipError_t hk_launch_compact(int n_heads, int D, const hk_paged_kv* kv, const ui
                        alloc->free_top, w);
   }
   return hipGetLastError();
+}
+
+hipError_t hk_launch_compact(int n_heads, int D, const hk_paged_kv* kv, const uint32_t* sel_bits,
+                             int L_dense, int L_sparse, const int32_t* head_mode,
+                             const hk_allocator* alloc, int32_t* status, void* ws, hipStream_t st) {
+  return launch_compact(n_heads, D, kv, nullptr, nullptr, sel_bits, L_dense, L_sparse, head_mode, alloc, status, ws, st);
+}
+
+hipError_t hk_launch_compact8(int n_heads, int D, const hk_paged_kv8* kv8, const uint32_t* sel_bits,
+                              int L_dense, int L_sparse, const int32_t* head_mode, const hk_allocator* alloc,
+                              int32_t* status, void* ws, hipStream_t st) {
+  return launch_compact(n_heads, D, &kv8->kv, kv8->k_scale, kv8->v_scale, sel_bits, L_dense, L_sparse, head_mode, alloc,
+                        status, ws, st);
 }

@@ -12,8 +12,9 @@ from dataclasses import dataclass
 
 import torch
 
-from . import (Allocator, Chunks, PagedKV, OP_APPEND, OP_COMPACT, OP_DECODE, OP_RESERVE, OP_SCORE, OP_TRIM,
-               HardKVError, chunk_attn_workspace, dims, hk_append_kv, hk_chunk_attn, hk_reserve_slots,
+from . import (Allocator, Chunks, PagedKV, PagedKV8, OP_APPEND, OP_DECODE8, OP_COMPACT, OP_DECODE, OP_RESERVE, OP_SCORE, OP_TRIM,
+               HardKVError, chunk_attn8_workspace, chunk_attn_workspace, dims, hk_chunk_attn8, hk_compact8,
+               hk_decode_attn8, hk_read_kv8, hk_write_kv8, hk_append_kv, hk_chunk_attn, hk_reserve_slots,
                hk_trim_slots, hk_verify_draft, hk_write_kv, verify_workspace,
                hk_budget_plan, hk_budget_select, hk_calibrate, hk_calibrate_solve_T,
                hk_calibrate_solve_T_gd, hk_calibrate_topp_ws, hk_compact, hk_compact_modes, hk_decode_attn, hk_pool_max,
@@ -41,8 +42,60 @@ class CompressBuffers:
     ws_select: torch.Tensor
 
 
+class ScoringCopy:
+    """K of an 8-bit cache read back in bf16 or fp32, a few sequences at a time, as the score passes
+    take it: a paged cache of its own whose rows lie one after the other, at most max_bytes of it."""
+
+    def __init__(self, NS, Hq, Hkv, D, W, kv: PagedKV8, dtype=torch.bfloat16, max_bytes: int = 1 << 30):
+        dev, P = kv.k_pool.device, kv.max_pages
+        row = P * 16 * D * dtype.itemsize * Hkv
+        self.n = n = max(1, min(NS, max_bytes // row))
+        self.kv, self.NS, self.Hq, self.Hkv, self.D, self.W, self.P = kv, NS, Hq, Hkv, D, W, P
+        H, i32 = n * Hkv, torch.int32
+        self.k = torch.zeros(H * P, 16, D, dtype=dtype, device=dev)
+        self.table = torch.arange(H * P, dtype=i32, device=dev).view(H, P)
+        self.mask = torch.zeros(H, P, dtype=kv.page_mask.dtype, device=dev)
+        self.n_pages = torch.zeros(H, dtype=i32, device=dev)
+        self.slot = torch.arange(16, dtype=torch.int64, device=dev)
+        self.slot_map = torch.empty(H, P, 16, dtype=torch.int64, device=dev)
+        self.q = torch.empty(W * n * Hq * D, dtype=dtype, device=dev)
+        self.lse = torch.empty(W * n * Hq, dtype=torch.float32, device=dev)
+        self.ws = workspace(OP_SCORE, dims(n, Hq, Hkv, D, W), P, dev)
+
+    def groups(self, q_obs, stream=None):
+        """For every few sequences: (their dims, first head, heads, sequences as a slice, queries, K)."""
+        for s0 in range(0, self.NS, self.n):
+            ns = min(self.n, self.NS - s0)
+            h0, H, sl = s0 * self.Hkv, ns * self.Hkv, slice(s0, s0 + ns)
+            with torch.cuda.stream(stream):
+                self.mask[:H].copy_(self.kv.page_mask[h0:h0 + H])
+                self.n_pages[:H].copy_(self.kv.n_pages[h0:h0 + H])
+                # 16 page + slot; below 0 past the rows' ends, where the table holds -1
+                at = self.slot_map[:H]
+                at.copy_(self.kv.page_table[h0:h0 + H, :, None].expand(H, self.P, 16))
+                at.mul_(16).add_(self.slot)
+                q = self.q[:self.W * ns * self.Hq * self.D].view(self.W, ns, self.Hq, self.D)
+                q.copy_(q_obs[:, sl])
+            n = H * self.P * 16
+            hk_read_kv8(dims(1, 1, 1, self.D), self.kv, n, at, self.k.view(-1, 1, self.D), stream=stream)
+            yield (dims(ns, self.Hq, self.Hkv, self.D, self.W), h0, H, sl, q,
+                   PagedKV(self.k, None, self.table[:H], self.mask[:H], self.n_pages[:H]))
+
+    def group_lse(self, sl):
+        n = sl.stop - sl.start
+        return self.lse[:self.W * n * self.Hq].view(self.W, n, self.Hq)
+
+
+def _compact(d, kv, sel_bits, L_dense, L_sparse, alloc, status, ws, stream):
+    run = hk_compact8 if isinstance(kv, PagedKV8) else hk_compact
+    run(d, kv, sel_bits, L_dense, L_sparse, alloc, status, ws, stream=stream)
+
+
 class Compressor:
     """One compression step over every head of a paged cache.
+
+    An 8-bit cache (PagedKV8) is scored on copies of its K, read back in score_dtype, the type of its
+    window queries, and rewritten as it lies.
 
     metric "attn": attention mass over the window, calibrated with T = 1.
     metric "attn+red": attention mass and key redundancy, each calibrated (the
@@ -58,7 +111,7 @@ class Compressor:
     def __init__(self, NS, Hq, Hkv, D, W, kv: PagedKV, alloc: Allocator, p: float,
                  L_dense: int = 0, L_sparse: int = 0, metric: str = "attn", n_ref: int = 0,
                  k_max: int = 0, keep_c: bool = True, pool_radius: int | None = None,
-                 t_solver: str = "bisect"):
+                 t_solver: str = "bisect", score_dtype=torch.bfloat16):
         if t_solver not in ("bisect", "gd"):
             raise ValueError("t_solver must be 'bisect' or 'gd'")
         self.t_solver = t_solver
@@ -74,6 +127,7 @@ class Compressor:
         self.n_heads, self.S_max = H, S
         f32, i32 = torch.float32, torch.int32
         red = metric == "attn+red"
+        self.copy = ScoringCopy(NS, Hq, Hkv, D, W, kv, score_dtype) if isinstance(kv, PagedKV8) else None
         self.buf = CompressBuffers(
             s_attn=torch.empty(H, S, dtype=f32, device=dev),
             s_pool=torch.empty(H, S, dtype=f32, device=dev) if pool_radius is not None else None,
@@ -89,13 +143,29 @@ class Compressor:
             mass_attn=torch.empty(H, dtype=f32, device=dev) if red else None,
             T_red=None,
             status=torch.zeros(1, dtype=i32, device=dev),
-            ws_score=workspace(OP_SCORE, self.d, kv.max_pages, dev),
+            ws_score=workspace(OP_SCORE, self.d, kv.max_pages, dev) if self.copy is None else self.copy.ws,
             ws_compact=workspace(OP_COMPACT, self.d, kv.max_pages, dev),
             ws_select=select_workspace(H, S, dev),
         )
 
     def score(self, q_obs, ref_slots=None, row_lse_in=None, stream=None):
         b = self.buf
+        if self.copy is not None:
+            for d, h0, H, sl, q, kv in self.copy.groups(q_obs, stream):
+                heads, lse = slice(h0, h0 + H), self.copy.group_lse(sl)
+                if row_lse_in is not None:
+                    with torch.cuda.stream(stream):
+                        lse.copy_(row_lse_in[:, sl])
+                hk_score(d, q, kv, self.L_dense, self.sm_scale, b.s_attn[heads], b.cand_len[heads],
+                         row_lse_in=lse if row_lse_in is not None else None,
+                         row_lse_out=lse if row_lse_in is None else None,
+                         ref_slots=ref_slots[heads] if ref_slots is not None else None,
+                         n_ref=self.n_ref if ref_slots is not None else 0,
+                         x_red=b.x_red[heads] if ref_slots is not None else None, ws=b.ws_score, stream=stream)
+                if row_lse_in is None:
+                    with torch.cuda.stream(stream):
+                        b.row_lse[:, sl].copy_(lse)
+            return
         hk_score(self.d, q_obs, self.kv, self.L_dense, self.sm_scale, b.s_attn, b.cand_len,
                  row_lse_in=row_lse_in, row_lse_out=b.row_lse if row_lse_in is None else None,
                  ref_slots=ref_slots, n_ref=self.n_ref if ref_slots is not None else 0,
@@ -126,8 +196,8 @@ class Compressor:
 
     def compact(self, stream=None):
         b = self.buf
-        hk_compact(self.d, self.kv, b.sel_bits, self.L_dense, self.L_sparse, self.alloc, b.status,
-                   b.ws_compact, stream=stream)
+        _compact(self.d, self.kv, b.sel_bits, self.L_dense, self.L_sparse, self.alloc, b.status,
+                 b.ws_compact, stream)
 
     def step(self, q_obs, ref_slots=None, row_lse_in=None, stream=None):
         self.score(q_obs, ref_slots=ref_slots, row_lse_in=row_lse_in, stream=stream)
@@ -150,7 +220,8 @@ class BudgetCompressor:
 
     def __init__(self, NS, Hq, Hkv, D, W, kv: PagedKV, alloc: Allocator, p: float,
                  L_lower: int, L_upper: int, L_dense: int = 0, n_sink: int = 0,
-                 rank_by_c: bool = False):
+                 rank_by_c: bool = False, score_dtype=torch.bfloat16):
+        self.copy = ScoringCopy(NS, Hq, Hkv, D, W, kv, score_dtype) if isinstance(kv, PagedKV8) else None
         self.d = dims(NS, Hq, Hkv, D, W)
         self.kv, self.alloc, self.p = kv, alloc, p
         self.L_lower, self.L_upper, self.L_dense, self.n_sink = L_lower, L_upper, L_dense, n_sink
@@ -173,18 +244,32 @@ class BudgetCompressor:
             sel_bits=torch.empty(H, S // 32, dtype=i32, device=dev),
             k=torch.empty(H, dtype=i32, device=dev),
             status=torch.zeros(1, dtype=i32, device=dev),
-            ws_score=workspace(OP_SCORE, self.d, kv.max_pages, dev),
+            ws_score=workspace(OP_SCORE, self.d, kv.max_pages, dev) if self.copy is None else self.copy.ws,
             ws_compact=workspace(OP_COMPACT, self.d, kv.max_pages, dev),
         )
+
+    def _rows(self, q_obs, stream):
+        """Row LSEs, scores where they are needed, and every row's probabilities."""
+        b = self.buf
+        if self.copy is None:
+            hk_score(self.d, q_obs, self.kv, self.L_dense, self.sm_scale, b["s_attn"], b["cand_len"],
+                     row_lse_out=b["row_lse"], ws=b["ws_score"], stream=stream)
+            hk_score_rows(self.d, q_obs, self.kv, self.L_dense, self.sm_scale, b["row_lse"],
+                          b["a_rows"], stream=stream)
+            return
+        for d, h0, H, sl, q, kv in self.copy.groups(q_obs, stream):
+            heads, lse = slice(h0, h0 + H), self.copy.group_lse(sl)
+            hk_score(d, q, kv, self.L_dense, self.sm_scale, b["s_attn"][heads] if self.rank_by_c else None,
+                     b["cand_len"][heads], row_lse_out=lse, ws=b["ws_score"], stream=stream)
+            hk_score_rows(d, q, kv, self.L_dense, self.sm_scale, lse, b["a_rows"][heads], stream=stream)
+            with torch.cuda.stream(stream):
+                b["row_lse"][:, sl].copy_(lse)
 
     def select(self, q_obs, stream=None):
         b, H, S, pm = self.buf, self.n_heads, self.S_max, self.kv.page_mask
         hk_budget_plan(self.d, self.kv, self.L_dense, self.L_lower, self.L_upper, b["head_mode"],
                        b["k_cap"], stream=stream)
-        hk_score(self.d, q_obs, self.kv, self.L_dense, self.sm_scale, b["s_attn"], b["cand_len"],
-                 row_lse_out=b["row_lse"], ws=b["ws_score"], stream=stream)
-        hk_score_rows(self.d, q_obs, self.kv, self.L_dense, self.sm_scale, b["row_lse"],
-                      b["a_rows"], stream=stream)
+        self._rows(q_obs, stream)
         hk_vote_topp(H, self.R, S, b["cand_len"], pm, b["a_rows"], self.p, b["votes"],
                      b["row_sel"], status=b["status"], stream=stream)
         if self.rank_by_c:
@@ -195,6 +280,10 @@ class BudgetCompressor:
 
     def compact(self, stream=None):
         b = self.buf
+        if self.copy is not None:
+            hk_compact8(self.d, self.kv, b["sel_bits"], self.L_dense, 0, self.alloc, b["status"],
+                        b["ws_compact"], head_mode=b["head_mode"], stream=stream)
+            return
         hk_compact_modes(self.d, self.kv, b["sel_bits"], self.L_dense, b["head_mode"], self.alloc,
                          b["status"], b["ws_compact"], stream=stream)
 
@@ -203,24 +292,49 @@ class BudgetCompressor:
         self.compact(stream=stream)
 
 
+class OneToken:
+    """hk_append_kv's place for 8-bit caches: a chunk of one token per sequence, reserved and written."""
+
+    def __init__(self, NS, kv: PagedKV8, d, alloc: Allocator, status):
+        dev = kv.k_pool.device
+        self.kv, self.d, self.alloc, self.status, self.NS = kv, d, alloc, status, NS
+        self.chunks = Chunks(torch.arange(NS + 1, dtype=torch.int32, device=dev), NS, 1)
+        self.slot_map = torch.empty(NS * d.Hkv, dtype=torch.int64, device=dev)
+        self.ws = workspace(OP_RESERVE, d, kv.max_pages, dev)
+
+    def append(self, k_new, v_new, stream=None):
+        hk_reserve_slots(self.d, self.kv, self.chunks, self.alloc, self.ws, slot_map=self.slot_map,
+                         status=self.status, stream=stream)
+        hk_write_kv8(self.d, self.kv, self.NS, self.slot_map, k_new, v_new, stream=stream)
+
+
 class Decoder:
-    """One decode step of one layer: append the step's K/V, then attend."""
+    """One decode step of one layer: append the step's K/V, then attend.  An 8-bit cache (PagedKV8)
+    takes K, V and q in bf16 or fp32."""
 
     def __init__(self, NS, Hq, Hkv, D, kv: PagedKV, alloc: Allocator):
         self.d = dims(NS, Hq, Hkv, D, 0)
         self.kv, self.alloc = kv, alloc
         self.sm_scale = 1.0 / math.sqrt(D)
         dev = kv.k_pool.device
-        self.ws = workspace(OP_DECODE, self.d, kv.max_pages, dev)
-        self.ws_app = workspace(OP_APPEND, self.d, kv.max_pages, dev)
+        self.bits8 = isinstance(kv, PagedKV8)
+        self.ws = workspace(OP_DECODE8 if self.bits8 else OP_DECODE, self.d, kv.max_pages, dev)
         self.status = torch.zeros(1, dtype=torch.int32, device=dev)
+        if self.bits8:
+            self.one = OneToken(NS, kv, self.d, alloc, self.status)
+        else:
+            self.ws_app = workspace(OP_APPEND, self.d, kv.max_pages, dev)
 
     def append(self, k_new, v_new, stream=None):
+        if self.bits8:
+            self.one.append(k_new, v_new, stream=stream)
+            return
         hk_append_kv(self.d, self.kv, k_new, v_new, self.alloc, self.status, self.ws_app,
                      stream=stream)
 
     def attend(self, q, o, lse, stream=None):
-        hk_decode_attn(self.d, q, self.kv, self.sm_scale, o, lse, self.ws, stream=stream)
+        run = hk_decode_attn8 if self.bits8 else hk_decode_attn
+        run(self.d, q, self.kv, self.sm_scale, o, lse, self.ws, stream=stream)
 
 
 class ChunkDecoder:
@@ -236,6 +350,7 @@ class ChunkDecoder:
     granted says on the device whether the last reserve() gave them; its chunks carry the word on to
     the Verifier, which drops nothing of refused chunks (one Chunks reserved by several decoders carries
     the last one's word: give each its own).  trim() itself always takes n_drop back.
+    An 8-bit cache (PagedKV8) takes K, V, q and o in bf16 or fp32; write() quantises.
     """
 
     def __init__(self, B, Hq, Hkv, D, kv: PagedKV, alloc: Allocator, max_tokens: int, max_len: int,
@@ -249,7 +364,9 @@ class ChunkDecoder:
         self.ws_slots = workspace(OP_RESERVE, self.d_all, kv.max_pages, dev)
         self.ws_trim = workspace(OP_TRIM, self.d_all, kv.max_pages, dev)
         most = Chunks(torch.empty(B + 1, dtype=torch.int32), max_tokens, max_len)
-        self.ws = chunk_attn_workspace(self.d, most, kv.max_pages, dev)
+        self.bits8 = isinstance(kv, PagedKV8)
+        ws = chunk_attn8_workspace if self.bits8 else chunk_attn_workspace
+        self.ws = ws(self.d, most, kv.max_pages, dev)
         self.status = torch.zeros(1, dtype=torch.int32, device=dev)
         self.granted = torch.ones(1, dtype=torch.int32, device=dev)
 
@@ -267,7 +384,8 @@ class ChunkDecoder:
     def write(self, chunks: Chunks, slot_map, k_new, v_new, stream=None):
         """One layer ([tokens, Hkv, D], that layer's part of the slot map) or all of them
         ([layers, tokens, Hkv, D])."""
-        hk_write_kv(self.d, self.kv, chunks.n_tokens, slot_map, k_new, v_new, stream=stream)
+        run = hk_write_kv8 if self.bits8 else hk_write_kv
+        run(self.d, self.kv, chunks.n_tokens, slot_map, k_new, v_new, stream=stream)
 
     def append(self, chunks: Chunks, k_new, v_new, slot_map, stream=None):
         self.reserve(chunks, slot_map, stream=stream)
@@ -275,8 +393,8 @@ class ChunkDecoder:
 
     def attend(self, chunks: Chunks, q, o, lse=None, layer: int = 0, stream=None):
         self._fits(chunks)
-        hk_chunk_attn(self.d, self.kv_layer[layer], chunks, q, self.sm_scale, o, self.ws, lse=lse,
-                      stream=stream)
+        run = hk_chunk_attn8 if self.bits8 else hk_chunk_attn
+        run(self.d, self.kv_layer[layer], chunks, q, self.sm_scale, o, self.ws, lse=lse, stream=stream)
 
     def trim(self, n_drop, stream=None):
         if n_drop.numel() != self.B:
@@ -314,11 +432,12 @@ class DecodeLoop:
                 every layer.  After an extend() whose slots were refused (status) it takes
                 nothing back and draws no token (-1): the cache stays as it was.
     Heads are ordered (layer, sequence, KV head); sequence index = layer * B + b.
+    An 8-bit cache (PagedKV8) takes queries, K and V in bf16 (score_dtype), and so o of extend().
     """
 
     def __init__(self, L, B, Hq, Hkv, D, W, kv: PagedKV, alloc: Allocator, p: float,
                  L_dense: int, L_sparse: int = 0, keep_c: bool = True, max_tokens: int = 0,
-                 max_len: int = 0):
+                 max_len: int = 0, score_dtype=torch.bfloat16):
         self.L, self.B, self.Hq, self.Hkv, self.D, self.W = L, B, Hq, Hkv, D, W
         self.kv, self.alloc = kv, alloc
         self.NS = L * B
@@ -327,12 +446,16 @@ class DecodeLoop:
         self.d_layer = dims(B, Hq, Hkv, D, W)
         self.layers = [kv.rows(l * B * Hkv, B * Hkv) for l in range(L)]
         self.sm_scale = 1.0 / math.sqrt(D)
-        self.ws_dec = workspace(OP_DECODE, self.d_layer, kv.max_pages, dev)
-        self.ws_app = workspace(OP_APPEND, self.d_all, kv.max_pages, dev)
+        self.bits8 = isinstance(kv, PagedKV8)
+        self.ws_dec = workspace(OP_DECODE8 if self.bits8 else OP_DECODE, self.d_layer, kv.max_pages, dev)
         self.status = torch.zeros(1, dtype=torch.int32, device=dev)
+        if self.bits8:
+            self.one = OneToken(self.NS, kv, self.d_all, alloc, self.status)
+        else:
+            self.ws_app = workspace(OP_APPEND, self.d_all, kv.max_pages, dev)
         self.o = torch.empty(self.NS, Hq, D, dtype=torch.float32, device=dev)
         self.comp = Compressor(self.NS, Hq, Hkv, D, W, kv, alloc, p, L_dense=L_dense,
-                               L_sparse=L_sparse, metric="attn", keep_c=keep_c)
+                               L_sparse=L_sparse, metric="attn", keep_c=keep_c, score_dtype=score_dtype)
         self.chunked = None
         if max_tokens > 0:
             self.chunked = ChunkDecoder(B, Hq, Hkv, D, kv, alloc, max_tokens, max_len or max_tokens, layers=L)
@@ -358,13 +481,16 @@ class DecodeLoop:
         self.chunked.trim(n_drop, stream=stream)
 
     def step(self, q_t, k_t, v_t, lse_t, stream=None):
-        hk_append_kv(self.d_all, self.kv, k_t, v_t, self.alloc, self.status, self.ws_app,
-                     stream=stream)
-        B = self.B
+        if self.bits8:
+            self.one.append(k_t, v_t, stream=stream)
+        else:
+            hk_append_kv(self.d_all, self.kv, k_t, v_t, self.alloc, self.status, self.ws_app,
+                         stream=stream)
+        B, attend = self.B, hk_decode_attn8 if self.bits8 else hk_decode_attn
         for l, kv_l in enumerate(self.layers):
-            hk_decode_attn(self.d_layer, q_t[l * B:(l + 1) * B], kv_l, self.sm_scale,
-                           self.o[l * B:(l + 1) * B], lse_t[l * B:(l + 1) * B], self.ws_dec,
-                           stream=stream)
+            attend(self.d_layer, q_t[l * B:(l + 1) * B], kv_l, self.sm_scale,
+                   self.o[l * B:(l + 1) * B], lse_t[l * B:(l + 1) * B], self.ws_dec,
+                   stream=stream)
 
     def compress(self, q_win, lse_win, stream=None):
         self.comp.step(q_win, row_lse_in=lse_win, stream=stream)
