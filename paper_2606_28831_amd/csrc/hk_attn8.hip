@@ -21,6 +21,9 @@
 // Softmax: one pass with a running reference m per row, a whole number that moves when a score exceeds
 // it by 2^SLACK.  The sums of P V are kept smaller by 2^bias, at least their number of terms times
 // 2^SLACK, so that they stay finite where the result does.
+#include <algorithm>
+#include <type_traits>
+
 #include "hk_chunk.h"
 #include "hk_kv8.h"
 
@@ -29,7 +32,7 @@ namespace hk {
 constexpr int A8_NT = 256, A8_NW = 4;
 constexpr float A8_SLACK = 4.f;
 constexpr int A8_PPS = 128, A8_PPS_MIN = 8;   // pages of a range at most and at least
-constexpr int A8_TARGET = 2048;               // workgroups that a launch should have
+constexpr int A8_TARGET = 2048, A8_MOST = 4096;   // workgroups that a launch should have, and with ranges at most
 constexpr int A8_ROWS = 32;                   // rows of a workgroup at most
 
 struct Args8 {
@@ -214,6 +217,30 @@ __global__ __launch_bounds__(A8_NT, QP == 3 && NQ == 2 ? 1 : 2) void attn8_kerne
     for (int j = 0; j < DT; ++j) acc[nq][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
+  // P V of dims 4 j + 2 H and 4 j + 2 H + 1: the codes' pairs turned into pairs of keys
+  auto values = [&](auto half, const Block8<D>& b, const u32x4 (&pf)[NQ][PP], int j) {
+    constexpr int H = decltype(half)::value;
+    u32x4 vf[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t x = b.v[2 * i][j], y = b.v[2 * i + 1][j];
+      if constexpr (F == HK_I8) {
+        vf[0][i] = high_halves(Code<F>::template value<2 * H>(x), Code<F>::template value<2 * H>(y));
+        vf[1][i] = high_halves(Code<F>::template value<2 * H + 1>(x), Code<F>::template value<2 * H + 1>(y));
+      } else {
+        const uint32_t px = Code<F>::template pair<H>(x), py = Code<F>::template pair<H>(y);
+        vf[0][i] = __builtin_amdgcn_perm(py, px, 0x05040100u);
+        vf[1][i] = __builtin_amdgcn_perm(py, px, 0x07060302u);
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+        for (int i = PP - 1; i >= 0; --i)
+          acc[nq][4 * j + 2 * H + h] = mma8(vf[h], pf[nq][i], acc[nq][4 * j + 2 * H + h]);
+  };
   // 32 keys from page p on
   auto compute = [&](Block8<D>& b, int p) {
     const bool full = b.mask == 0xffffffffu && (!CHUNK || (p + 2) * HK_PAGE <= seen_all);
@@ -233,6 +260,9 @@ __global__ __launch_bounds__(A8_NT, QP == 3 && NQ == 2 ? 1 : 2) void attn8_kerne
       for (int nq = 0; nq < NQ; ++nq) z[nq][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
+        // (here and below: one product's codes converted at a time; without, D 128 spills)
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("" : "+v"(b.k[t][2 * s]), "+v"(b.k[t][2 * s + 1]));
         const u32x4 kf = {Code<F>::template pair<0>(b.k[t][2 * s]), Code<F>::template pair<1>(b.k[t][2 * s]),
                           Code<F>::template pair<0>(b.k[t][2 * s + 1]), Code<F>::template pair<1>(b.k[t][2 * s + 1])};
 #pragma unroll
@@ -289,30 +319,14 @@ __global__ __launch_bounds__(A8_NT, QP == 3 && NQ == 2 ? 1 : 2) void attn8_kerne
       }
     }
 #pragma unroll
-    for (int j = 0; j < DT / 2; ++j) {
-      // dims 2 j and 2 j + 1 of the lane's D / 16: the codes' pairs turned into pairs of keys
-      u32x4 vf[2];
+    for (int j = 0; j < DT / 4; ++j) {
+      // dims 4 j .. 4 j + 3 of the lane's D / 16
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t x = b.v[2 * i][j / 2], y = b.v[2 * i + 1][j / 2];
-        if constexpr (F == HK_I8) {
-          vf[0][i] = j & 1 ? high_halves(Code<F>::template value<2>(x), Code<F>::template value<2>(y))
-                           : high_halves(Code<F>::template value<0>(x), Code<F>::template value<0>(y));
-          vf[1][i] = j & 1 ? high_halves(Code<F>::template value<3>(x), Code<F>::template value<3>(y))
-                           : high_halves(Code<F>::template value<1>(x), Code<F>::template value<1>(y));
-        } else {
-          const uint32_t px = j & 1 ? Code<F>::template pair<1>(x) : Code<F>::template pair<0>(x);
-          const uint32_t py = j & 1 ? Code<F>::template pair<1>(y) : Code<F>::template pair<0>(y);
-          vf[0][i] = __builtin_amdgcn_perm(py, px, 0x05040100u);
-          vf[1][i] = __builtin_amdgcn_perm(py, px, 0x07060302u);
-        }
-      }
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int nq = 0; nq < NQ; ++nq)
-#pragma unroll
-          for (int i = PP - 1; i >= 0; --i) acc[nq][2 * j + h] = mma8(vf[h], pf[nq][i], acc[nq][2 * j + h]);
+      for (int i = 0; i < 8; ++i) asm volatile("" : "+v"(b.v[i][j]));
+      values(std::integral_constant<int, 0>{}, b, pf, j);
+      __builtin_amdgcn_sched_barrier(0);
+      values(std::integral_constant<int, 1>{}, b, pf, j);
     }
   };
 
@@ -479,7 +493,8 @@ inline Plan8 plan8(int NS, int Hkv, int G, const hk_chunks* ch, int max_pages) {
   p.units = tiles * Hkv;
   int pps = A8_PPS;
   while (pps > A8_PPS_MIN && p.units * ((max_pages + pps - 1) / pps) < A8_TARGET) pps >>= 1;
-  p.n_split = p.one_tile || p.units < A8_TARGET ? (max_pages + pps - 1) / pps : 1;
+  const int64_t most_split = (A8_MOST + p.units - 1) / p.units;
+  p.n_split = (int)std::min<int64_t>((max_pages + pps - 1) / pps, most_split);
   return p;
 }
 
@@ -491,9 +506,16 @@ static size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
 
 size_t hk_attn8_ws(int NS, int Hq, int Hkv, int D, const hk_chunks* ch, int max_pages) {
   const Plan8 p = plan8(NS, Hkv, Hq / Hkv, ch, max_pages);
-  if (p.n_split <= 1) return 256;
-  const size_t states = (size_t)p.units * p.n_split * p.cap;
-  return align_up(states * D * 4) + align_up(states * 8);
+  size_t states = p.n_split > 1 ? (size_t)p.units * p.n_split * p.cap : 0;
+  if (ch && max_pages > A8_PPS_MIN) {
+    // what any chunks of no more tokens, and none longer, can take: ranges are for fewer than MOST units,
+    // and leave fewer than 2 MOST workgroups
+    const int64_t units = ((int64_t)ch->n_tokens * (Hq / Hkv) / 16 + NS) * Hkv;
+    const int64_t groups = std::min<int64_t>(2 * A8_MOST, units * ((max_pages + A8_PPS_MIN - 1) / A8_PPS_MIN));
+    const int64_t rows = (int64_t)ch->max_len * (Hq / Hkv);
+    states = (size_t)(groups * std::min<int64_t>(rows, A8_ROWS));
+  }
+  return 256 + align_up(states * D * 4) + align_up(states * 8);
 }
 
 double hk_attn8_groups(int NS, int Hq, int Hkv, const hk_chunks* ch, int max_pages) {
