@@ -130,31 +130,29 @@ __device__ __forceinline__ void split_pair(float x, float y, uint32_t (&out)[N])
   }
 }
 
-// Codes of two pages on their way: see above for what a lane holds.
+// A block of 32 keys in LDS: K codes of two pages, V codes, and 64 scales (K's, V's).  It is filled
+// straight from memory, 1 KB of codes an instruction, 16 bytes a lane in lane order, so that every line
+// is asked for once (a fragment's loads into registers ask for it twice; the second waits on the first,
+// 42% of the time).  A lane may fetch any 16 bytes: rows lie in an order, and their 16-byte pieces in one
+// of a row's own, in which the fragments' reads meet no bank twice.
 template <int D>
-struct Block8 {
-  static constexpr int KW = D / 16, VW = D / 64;          // words of a K row's quarter, of a V row's piece
-  uint32_t k[2][KW], v[8][VW];
-  f32x4 ks[2], vs[2];
-  uint32_t mask;
-  __device__ __forceinline__ void load(const Args8& a, int id0, int id1, uint32_t m) {
-    const int lane = threadIdx.x & 63, i16 = lane & 15, qd = lane >> 4;
-    mask = m;
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const size_t page = (size_t)(t ? id1 : id0);
-      const char* kp = a.k_pool + page * (HK_PAGE * D) + (i16 * D + qd * (D / 4));
-#pragma unroll
-      for (int i = 0; i < KW / 4; ++i) *reinterpret_cast<u32x4*>(&k[t][4 * i]) = reinterpret_cast<const u32x4*>(kp)[i];
-      const char* vp = a.v_pool + page * (HK_PAGE * D) + (4 * qd * D + i16 * (D / 16));
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        if constexpr (VW == 2) *reinterpret_cast<u32x2*>(&v[4 * t + r][0]) = *reinterpret_cast<const u32x2*>(vp + r * D);
-        else v[4 * t + r][0] = *reinterpret_cast<const uint32_t*>(vp + r * D);
-      }
-      ks[t] = *reinterpret_cast<const f32x4*>(a.k_scale + page * HK_PAGE + 4 * qd);
-      vs[t] = *reinterpret_cast<const f32x4*>(a.v_scale + page * HK_PAGE + 4 * qd);
-    }
+struct Tile8 {
+  static constexpr int ROWS = 1024 / D, PIECES = D / 16, PAGE = HK_PAGE * D;
+  static constexpr int SCALES = 4 * PAGE, BYTES = SCALES + 256;
+  static constexpr int LOADS = 4 * PAGE / 1024 + 1;
+  // place of a key among the rows of its instruction, and what its pieces' places are changed by
+  __device__ static __forceinline__ int place(int key) {
+    return D == 128 ? (key & 3) * 2 + ((key >> 2) & 1) : (key & 3) * 4 + (key >> 2);
+  }
+  __device__ static __forceinline__ int turn(int key) { return D == 128 ? (key & 3) | (key >> 3) << 2 : key & 3; }
+  __device__ static __forceinline__ int at(int key, int piece) {
+    return (D == 128 ? (key >> 3) * 1024 : 0) + place(key) * D + (piece ^ turn(key)) * 16;
+  }
+  // the bytes of a page that a lane fetches with instruction g of it
+  __device__ static __forceinline__ int source(int lane, int g) {
+    const int pos = lane / PIECES;
+    const int key = D == 128 ? 8 * g + (pos >> 1) + 4 * (pos & 1) : (pos >> 2) + 4 * (pos & 3);
+    return key * D + (((lane % PIECES) ^ turn(key)) * 16);
   }
 };
 
@@ -162,12 +160,18 @@ __device__ __forceinline__ f32x4 mma8(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
+template <int D>
+constexpr int A8_DEPTH = D == 128 ? 2 : 3;   // blocks of a wave in LDS
 // QP: bf16 parts of q (1: q is bf16), PP: of P (2: o is bf16, 3: fp32)
 template <int F, int D, int NQ, int QP, int PP, bool CHUNK>
-__global__ __launch_bounds__(A8_NT, QP == 3 && NQ == 2 ? 1 : 2) void attn8_kernel(Args8 a) {
+__global__ __launch_bounds__(A8_NT, 2) void attn8_kernel(Args8 a) {
 #pragma clang fp contract(off)
   constexpr int ROWS = 16 * NQ, KS = D / 32, DT = D / 16;
-  __shared__ f32x4 s_acc[2][NQ * DT][64];
+  using L = Tile8<D>;
+  constexpr int DEPTH = A8_DEPTH<D>;
+  __shared__ __align__(16) char s_tiles[A8_NW * DEPTH * L::BYTES];
+  f32x4 (*s_acc)[NQ * DT][64] = reinterpret_cast<f32x4 (*)[NQ * DT][64]>(s_tiles);   // at the end
+  static_assert(sizeof(s_tiles) >= 2 * sizeof(*s_acc));
   __shared__ float s_m[A8_NW][NQ][16], s_l[A8_NW][NQ][16];
   const int lane = threadIdx.x & 63, i16 = lane & 15, qd = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -207,6 +211,10 @@ __global__ __launch_bounds__(A8_NT, QP == 3 && NQ == 2 ? 1 : 2) void attn8_kerne
   const int bias = (int)A8_SLACK + 33 - __clz(max(p1 - p0, 1) * HK_PAGE);
   const float down = __uint_as_float((uint32_t)(127 - bias) << 23), back = __uint_as_float((uint32_t)(127 + bias) << 23);
 
+  uint32_t source[L::PAGE / 1024];
+#pragma unroll
+  for (int g = 0; g < L::PAGE / 1024; ++g) source[g] = L::source(lane, g);
+
   float m[NQ], l[NQ];
   f32x4 acc[NQ][DT];
 #pragma unroll
@@ -217,13 +225,14 @@ __global__ __launch_bounds__(A8_NT, QP == 3 && NQ == 2 ? 1 : 2) void attn8_kerne
     for (int j = 0; j < DT; ++j) acc[nq][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  // P V of dims 4 j + 2 H and 4 j + 2 H + 1: the codes' pairs turned into pairs of keys
-  auto values = [&](auto half, const Block8<D>& b, const u32x4 (&pf)[NQ][PP], int j) {
+  // P V of dims 4 j + 2 H and 4 j + 2 H + 1 from the eight keys' words j: the codes' pairs turned into
+  // pairs of keys
+  auto values = [&](auto half, const uint32_t (&v)[8], const u32x4 (&pf)[NQ][PP], int j) {
     constexpr int H = decltype(half)::value;
     u32x4 vf[2];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint32_t x = b.v[2 * i][j], y = b.v[2 * i + 1][j];
+      const uint32_t x = v[2 * i], y = v[2 * i + 1];
       if constexpr (F == HK_I8) {
         vf[0][i] = high_halves(Code<F>::template value<2 * H>(x), Code<F>::template value<2 * H>(y));
         vf[1][i] = high_halves(Code<F>::template value<2 * H + 1>(x), Code<F>::template value<2 * H + 1>(y));
@@ -241,36 +250,38 @@ __global__ __launch_bounds__(A8_NT, QP == 3 && NQ == 2 ? 1 : 2) void attn8_kerne
         for (int i = PP - 1; i >= 0; --i)
           acc[nq][4 * j + 2 * H + h] = mma8(vf[h], pf[nq][i], acc[nq][4 * j + 2 * H + h]);
   };
-  // 32 keys from page p on
-  auto compute = [&](Block8<D>& b, int p) {
-    const bool full = b.mask == 0xffffffffu && (!CHUNK || (p + 2) * HK_PAGE <= seen_all);
+  int k_at[KS / 2], v_at[4];                  // the lane's fragments within a page
+#pragma unroll
+  for (int i = 0; i < KS / 2; ++i) k_at[i] = L::at(i16, KS / 2 * qd + i);
+#pragma unroll
+  for (int r = 0; r < 4; ++r) v_at[r] = L::at(4 * qd + r, i16 * (D / 16) / 16) + i16 * (D / 16) % 16;
+  // the block at `b`, from page p on, keys valid where the bits of mask are 1
+  auto compute = [&](const char* b, int p, uint32_t mask) {
+    const bool full = mask == 0xffffffffu && (!CHUNK || (p + 2) * HK_PAGE <= seen_all);
     // the lane's keys 4 t + r: slot 4 qd + r of page t
-    const uint32_t valid = ((b.mask >> (4 * qd)) & 15u) | ((b.mask >> (16 + 4 * qd)) & 15u) << 4;
-    if (F == HK_E4M3 && b.mask != 0xffffffffu) {
-      // a slot that is not valid may hold codes that stand for NaN
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int j = 0; j < Block8<D>::VW; ++j) b.v[i][j] = (valid >> i) & 1u ? b.v[i][j] : 0u;
-    }
+    const uint32_t valid = ((mask >> (4 * qd)) & 15u) | ((mask >> (16 + 4 * qd)) & 15u) << 4;
     f32x4 z[NQ][2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
 #pragma unroll
       for (int nq = 0; nq < NQ; ++nq) z[nq][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        // (here and below: one product's codes converted at a time; without, D 128 spills)
-        __builtin_amdgcn_sched_barrier(0);
-        asm volatile("" : "+v"(b.k[t][2 * s]), "+v"(b.k[t][2 * s + 1]));
-        const u32x4 kf = {Code<F>::template pair<0>(b.k[t][2 * s]), Code<F>::template pair<1>(b.k[t][2 * s]),
-                          Code<F>::template pair<0>(b.k[t][2 * s + 1]), Code<F>::template pair<1>(b.k[t][2 * s + 1])};
+      for (int s2 = 0; s2 < KS / 2; ++s2) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(b + t * L::PAGE + k_at[s2]);
 #pragma unroll
-        for (int nq = 0; nq < NQ; ++nq)
+        for (int h = 0; h < 2; ++h) {
+          const u32x4 kf = {Code<F>::template pair<0>(w[2 * h]), Code<F>::template pair<1>(w[2 * h]),
+                            Code<F>::template pair<0>(w[2 * h + 1]), Code<F>::template pair<1>(w[2 * h + 1])};
 #pragma unroll
-          for (int i = QP - 1; i >= 0; --i) z[nq][t] = mma8(kf, qf[nq][i][s], z[nq][t]);
+          for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+            for (int i = QP - 1; i >= 0; --i) z[nq][t] = mma8(kf, qf[nq][i][2 * s2 + h], z[nq][t]);
+        }
       }
     }
+    const float* scales = reinterpret_cast<const float*>(b + L::SCALES) + 4 * qd;
+    const f32x4 ks[2] = {*reinterpret_cast<const f32x4*>(scales), *reinterpret_cast<const f32x4*>(scales + 16)};
+    const f32x4 vs[2] = {*reinterpret_cast<const f32x4*>(scales + 32), *reinterpret_cast<const f32x4*>(scales + 48)};
     u32x4 pf[NQ][PP];
 #pragma unroll
     for (int nq = 0; nq < NQ; ++nq) {
@@ -286,7 +297,7 @@ __global__ __launch_bounds__(A8_NT, QP == 3 && NQ == 2 ? 1 : 2) void attn8_kerne
       float x[8], zm = -INFINITY;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        x[i] = z[nq][i >> 2][i & 3] * (b.ks[i >> 2][i & 3] * a.c2);
+        x[i] = z[nq][i >> 2][i & 3] * (ks[i >> 2][i & 3] * a.c2);
         if (!full) x[i] = (vis >> i) & 1u ? x[i] : -INFINITY;
         zm = fmaxf(zm, x[i]);
       }
@@ -306,7 +317,7 @@ __global__ __launch_bounds__(A8_NT, QP == 3 && NQ == 2 ? 1 : 2) void attn8_kerne
       for (int i = 0; i < 8; ++i) {
         x[i] = fast_exp2(x[i] - off);
         sum[i & 1] += x[i];
-        x[i] *= b.vs[i >> 2][i & 3] * down;
+        x[i] *= vs[i >> 2][i & 3] * down;
         if (!full) x[i] = (vis >> i) & 1u ? x[i] : 0.f;         // (whatever the slot's scale is)
       }
       l[nq] += sum[0] + sum[1];
@@ -318,41 +329,83 @@ __global__ __launch_bounds__(A8_NT, QP == 3 && NQ == 2 ? 1 : 2) void attn8_kerne
         for (int j = 0; j < PP; ++j) pf[nq][j][i] = part[j];
       }
     }
+    uint32_t v[DT / 4][8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const char* from = b + (2 + (i >> 2)) * L::PAGE + v_at[i & 3];
+      if constexpr (D == 128) {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(from);
+        v[0][i] = x[0];
+        v[1][i] = x[1];
+      } else {
+        v[0][i] = *reinterpret_cast<const uint32_t*>(from);
+      }
+    }
+    if (F == HK_E4M3 && mask != 0xffffffffu) {
+      // a slot that is not valid may hold codes that stand for NaN
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < DT / 4; ++j) v[j][i] = (valid >> i) & 1u ? v[j][i] : 0u;
+    }
 #pragma unroll
     for (int j = 0; j < DT / 4; ++j) {
-      // dims 4 j .. 4 j + 3 of the lane's D / 16
+      // dims 4 j .. 4 j + 3 of the lane's D / 16; one product's codes converted at a time (without, spills)
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) asm volatile("" : "+v"(b.v[i][j]));
-      values(std::integral_constant<int, 0>{}, b, pf, j);
+      for (int i = 0; i < 8; ++i) asm volatile("" : "+v"(v[j][i]));
+      values(std::integral_constant<int, 0>{}, v[j], pf, j);
       __builtin_amdgcn_sched_barrier(0);
-      values(std::integral_constant<int, 1>{}, b, pf, j);
+      values(std::integral_constant<int, 1>{}, v[j], pf, j);
     }
   };
 
-  // A wave's blocks are wave, wave + 4, ..; lane i holds id and mask of page i % 2 of its block i / 2.
-  for (int from = p0; from < p1; from += 64 * A8_NW) {
-    const int first = from + 2 * wave;
-    const int n = min((p1 - first + 2 * A8_NW - 1) / (2 * A8_NW), 32);
-    const int mine = first + 2 * A8_NW * (lane >> 1) + (lane & 1);
-    const int id = min(max(trow[min(mine, p1 - 1)], 0), a.num_pages - 1);
-    const int mk = mine < p1 ? mrow[mine] : 0;
-    auto load = [&](Block8<D>& b, int i) {
-      if (i >= n) return;
-      b.load(a, __builtin_amdgcn_readlane(id, 2 * i), __builtin_amdgcn_readlane(id, 2 * i + 1),
-             (uint32_t)__builtin_amdgcn_readlane(mk, 2 * i) | (uint32_t)__builtin_amdgcn_readlane(mk, 2 * i + 1) << 16);
-    };
-    if (n <= 0) continue;
-    Block8<D> x, y;
-    load(x, 0);
-    for (int i = 0; i < n; i += 2) {
-      load(y, i + 1);
-      compute(x, first + 2 * A8_NW * i);
-      if (i + 1 >= n) break;
-      load(x, i + 2);
-      compute(y, first + 2 * A8_NW * (i + 1));
+  // A wave's blocks are wave, wave + 4, .. of the range's; DEPTH of them are in LDS or on their way.
+  // Ids and masks come 32 blocks at a time: lane i holds those of page i % 2 of block i / 2.
+  char* mine = s_tiles + wave * (DEPTH * L::BYTES);
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mine;
+  const int first = p0 + 2 * wave, n = p1 > first ? (p1 - first + 2 * A8_NW - 1) / (2 * A8_NW) : 0;
+  int ids = 0, masks = 0;
+  uint32_t queue[DEPTH];                      // masks of the blocks on their way
+  auto request = [&](int i, int slot) {       // returns the block's mask
+    if ((i & 31) == 0) {
+      const int page = first + 2 * A8_NW * (i + (lane >> 1)) + (lane & 1);
+      ids = min(max(trow[min(page, p1 - 1)], 0), a.num_pages - 1);
+      masks = page < p1 ? mrow[page] : 0;
     }
-  }
+    const uint32_t to = lds + slot * L::BYTES;
+    const int e = 2 * (i & 31);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // (what lay there has been read)
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const size_t at = (size_t)(uint32_t)__builtin_amdgcn_readlane(ids, e + t) * L::PAGE;
+#pragma unroll
+      for (int g = 0; g < L::PAGE / 1024; ++g) {
+        direct_load(a.k_pool + at, source[g], to + t * L::PAGE + g * 1024);
+        direct_load(a.v_pool + at, source[g], to + (2 + t) * L::PAGE + g * 1024);
+      }
+    }
+    const int id = (qd & 1) ? __builtin_amdgcn_readlane(ids, e + 1) : __builtin_amdgcn_readlane(ids, e);
+    direct_load4(reinterpret_cast<const char*>((qd >> 1 ? a.v_scale : a.k_scale) + (size_t)(uint32_t)id * HK_PAGE + i16),
+                 to + L::SCALES);
+    return (uint32_t)__builtin_amdgcn_readlane(masks, e) | (uint32_t)__builtin_amdgcn_readlane(masks, e + 1) << 16;
+  };
+#pragma unroll
+  for (int d = 0; d < DEPTH - 1; ++d)
+    if (d < n) queue[d] = request(d, d);
+  for (int i0 = 0; i0 < n; i0 += DEPTH)
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) {
+      const int i = i0 + d;
+      if (i >= n) break;
+      if (i + DEPTH - 1 < n) {
+        queue[(d + DEPTH - 1) % DEPTH] = request(i + DEPTH - 1, (d + DEPTH - 1) % DEPTH);
+        direct_wait<(DEPTH - 1) * L::LOADS>();
+      } else {
+        direct_wait<0>();
+      }
+      compute(mine + d * L::BYTES, first + 2 * A8_NW * i, queue[d]);
+    }
 
   // the waves' states: to one reference, then 2 and 3 into 0 and 1, 1 into 0
 #pragma unroll
@@ -430,50 +483,82 @@ __global__ __launch_bounds__(A8_NT, QP == 3 && NQ == 2 ? 1 : 2) void attn8_kerne
   }
 }
 
-// The ranges' states (means of V, references, sums) to the row's: a workgroup takes a unit, a wave
-// every fourth of its rows.
-template <int D, int ROWS, int PP, bool CHUNK>
+// The ranges' states (means of V, references, sums) to the row's: a wave takes a row, or WAVES of them
+// share a row's ranges.  D / 4 lanes load a state; a wave has 256 / D of them on their way at once.
+template <int D, int ROWS, int PP, bool CHUNK, int WAVES>
 __global__ __launch_bounds__(A8_NT) void attn8_merge_kernel(Args8 a) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, u = blockIdx.x;
+  constexpr int LPR = D / 4, SIDE = 64 / LPR, PER = A8_NW / WAVES;
+  __shared__ float s_m[A8_NW], s_l[A8_NW];
+  __shared__ f32x4 s_o[A8_NW][LPR];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int per_unit = (a.cap + PER - 1) / PER, u = blockIdx.x / per_unit;
+  const int row = (blockIdx.x - u * per_unit) * PER + wave / WAVES;
   const Unit w = unit_of<ROWS, CHUNK>(a, u);
-  if (w.rows == 0) return;
+  // (the waves of a row leave together)
+  if (w.rows == 0 || row >= a.cap || w.r0 + row >= w.rows) return;
   const int share = share8(a, w.pages), used = max((w.pages + share - 1) / share, 1);
-  constexpr int PER = D / 64;
-  for (int row = wave; row < ROWS && w.r0 + row < w.rows; row += A8_NW) {
-    const int64_t first = (int64_t)u * a.n_split * a.cap + row;
-    const f32x2* ml = reinterpret_cast<const f32x2*>(a.part_ml) + first;
-    float mt = -INFINITY, lt = 0.f;
-    for (int i = lane; i < used; i += 64) mt = fmaxf(mt, ml[(int64_t)i * a.cap][0]);
-    mt = wave_max(mt);
-    for (int i = lane; i < used; i += 64) {
-      const f32x2 x = ml[(int64_t)i * a.cap];
-      lt += x[0] == -INFINITY ? 0.f : x[1] * fast_exp2(x[0] - mt);
+  const int per = (used + WAVES - 1) / WAVES, i0 = wave % WAVES * per, i1 = min(i0 + per, used);
+  const int64_t first = (int64_t)u * a.n_split * a.cap + row;
+  const f32x2* ml = reinterpret_cast<const f32x2*>(a.part_ml) + first;
+  float m = -INFINITY, l = 0.f;
+  for (int i = i0 + lane; i < i1; i += 64) m = fmaxf(m, ml[(int64_t)i * a.cap][0]);
+  m = wave_max(m);
+  const auto weight = [&](int i) {
+    const f32x2 x = ml[(int64_t)i * a.cap];
+    return x[0] == -INFINITY ? 0.f : x[1] * fast_exp2(x[0] - m);
+  };
+  for (int i = i0 + lane; i < i1; i += 64) l += weight(i);
+  l = wave_sum(l);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const int side = lane / LPR, at = lane % LPR;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int from = i0; from < i1; from += 64) {
+    const float f = from + lane < i1 ? weight(from + lane) * inv : 0.f;
+    const int n = min(i1 - from, 64);
+#pragma unroll 4
+    for (int j = 0; j < n; j += SIDE) {
+      const int i = min(j + side, n - 1);
+      const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_o + (first + (int64_t)(from + i) * a.cap) * D + 4 * at);
+      const float g = __shfl(f, j + side, 64);
+      if (j + side < n) o += g * x;
     }
-    lt = wave_sum(lt);
-    const float inv = lt == 0.f ? 0.f : 1.f / lt;
-    float o[PER];
-#pragma unroll
-    for (int j = 0; j < PER; ++j) o[j] = 0.f;
-#pragma unroll 8
-    for (int i = 0; i < used; ++i) {
-      const f32x2 x = ml[(int64_t)i * a.cap];
-      const float f = x[0] == -INFINITY ? 0.f : x[1] * fast_exp2(x[0] - mt) * inv;
-      const float* from = a.part_o + (first + (int64_t)i * a.cap) * D + lane * PER;
-#pragma unroll
-      for (int j = 0; j < PER; ++j) o[j] = fmaf(f, from[j], o[j]);
-    }
-    const int r = w.r0 + row, tok = r / a.G, g = r - tok * a.G;
-    const int64_t at = (int64_t)(w.c.first + tok) * a.Hq + w.kv * a.G + g;
-    if constexpr (PP == 3) {
-#pragma unroll
-      for (int j = 0; j < PER; ++j) static_cast<float*>(a.o)[at * D + lane * PER + j] = o[j];
-    } else {
-#pragma unroll
-      for (int j = 0; j < PER; ++j)
-        static_cast<__bf16*>(a.o)[at * D + lane * PER + j] = (__bf16)o[j];
-    }
-    if (lane == 0 && a.lse) a.lse[at] = lse8(mt, lt);
   }
+#pragma unroll
+  for (int d = LPR; d < 64; d <<= 1)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) o[k] += __shfl_xor(o[k], d, 64);
+  if constexpr (WAVES > 1) {
+    if (lane == 0) {
+      s_m[wave] = m;
+      s_l[wave] = l;
+    }
+    if (lane < LPR) s_o[wave][lane] = o;
+    __syncthreads();
+    if (wave != 0) return;
+    float mt = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) mt = fmaxf(mt, s_m[i]);
+    l = 0.f;
+    float part[WAVES];
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) {
+      part[i] = s_m[i] == -INFINITY ? 0.f : s_l[i] * fast_exp2(s_m[i] - mt);
+      l += part[i];
+    }
+    m = mt;
+    const float back = l == 0.f ? 0.f : 1.f / l;
+    o = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (lane < LPR)
+#pragma unroll
+      for (int i = 0; i < WAVES; ++i) o += part[i] * back * s_o[i][lane];
+  }
+  const int r = w.r0 + row, tok = r / a.G, g = r - tok * a.G;
+  const int64_t to = (int64_t)(w.c.first + tok) * a.Hq + w.kv * a.G + g;
+  if (lane < LPR) {
+    if constexpr (PP == 3) *reinterpret_cast<f32x4*>(static_cast<float*>(a.o) + to * D + 4 * lane) = o;
+    else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.o) + to * D + 4 * lane) = u32x2{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
+  }
+  if (lane == 0 && a.lse) a.lse[to] = lse8(m, l);
 }
 
 // ------------------------------------------------------------------ host
@@ -531,7 +616,10 @@ static void launch8(const Args8& a, hipStream_t st) {
   }
   if (a.n_split > 1) {
     TimedLaunch t(HK_TK_ATTN8_MERGE, st);
-    hipLaunchKernelGGL((attn8_merge_kernel<D, 16 * NQ, PP, CHUNK>), dim3((uint32_t)a.n_units), dim3(A8_NT), 0, st, a);
+    const bool few = a.n_split > 16 && a.n_units * a.cap <= 1024;
+    const uint32_t groups = (uint32_t)a.n_units * (few ? a.cap : (a.cap + A8_NW - 1) / A8_NW);
+    const auto merge = few ? attn8_merge_kernel<D, 16 * NQ, PP, CHUNK, A8_NW> : attn8_merge_kernel<D, 16 * NQ, PP, CHUNK, 1>;
+    hipLaunchKernelGGL(merge, dim3(groups), dim3(A8_NT), 0, st, a);
   }
 }
 template <int F, int D, int NQ>

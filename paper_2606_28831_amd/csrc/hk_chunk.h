@@ -22,6 +22,21 @@ __device__ __forceinline__ Chunk chunk_of(const int32_t* __restrict__ start, int
   return {a, min(b - a, max_len)};
 }
 
+// 1 KB from memory to LDS: lane l's 16 bytes at `from` (+ `at`) to `to` + 16 l.  It is on its way
+// afterwards; direct_wait waits until `later` such loads or fewer are.
+__device__ __forceinline__ void direct_load(const char* from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "m0", "memory");
+}
+__device__ __forceinline__ void direct_load(const char* from, uint32_t at, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(at), "s"(from), "s"(to) : "m0", "memory");
+}
+template <int later>
+__device__ __forceinline__ void direct_wait() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(later) : "memory"); }
+// the same with 4 bytes a lane
+__device__ __forceinline__ void direct_load4(const char* from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(to) : "m0", "memory");
+}
+
 }  // namespace hk
 
 size_t hk_reserve_ws(int n_heads);

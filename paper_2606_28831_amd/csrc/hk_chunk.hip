@@ -745,17 +745,6 @@ struct DirectTile {
 };
 static __device__ const u32x4 zero_row[1] = {};
 
-// 1 KB from memory to LDS: lane l's 16 bytes at `from` (+ `at`) to `to` + 16 l.  It is on its way
-// afterwards; direct_wait waits until `later` such loads or fewer are.
-__device__ __forceinline__ void direct_load(const char* from, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "m0", "memory");
-}
-__device__ __forceinline__ void direct_load(const char* from, uint32_t at, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(at), "s"(from), "s"(to) : "m0", "memory");
-}
-template <int later>
-__device__ __forceinline__ void direct_wait() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(later) : "memory"); }
-
 // bf16.  Four waves take 32 rows each against tiles of 32 keys.  A wave's tiles are a pipeline: the
 // scores of the next tile run beside the exponentials of this one, its P V beside the next one's
 // maximum; MFMAs and the vector work between them are laid out by hand.  Two workgroups a CU, for
