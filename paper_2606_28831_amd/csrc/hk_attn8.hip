@@ -1,9 +1,12 @@
 // 8-bit cache: attention of single tokens and of chunks of new tokens over its pages (gfx950).
 //
-// The query rows of a KV head are folded: row r of a chunk is query head r % G of token r / G.  A
-// workgroup takes ROWS of them and a range of the row's pages; its four waves take the range's pages
-// two at a time in turn, every page read once, straight into registers, and meet at the end in LDS.
-// attn8_merge_kernel joins the ranges of a row.
+// The query rows of a KV head are folded: row r of a chunk is query head r % G of token r / G.  Up to
+// 32 of them are a unit.  The units' pages, in steps of eight, are one long list that the workgroups of
+// a launch share evenly (two a CU, or three of D 64): a workgroup takes a run of steps, the end of one
+// unit, whole units and the beginning of another.  Its four waves take a step's pages two at a time, every
+// page read once, straight into LDS, and meet at a unit's end.  attn8_merge_kernel joins the units that
+// were cut.  (A grid of units x equal parts of each, 512 heads of 784 to 5600 tokens: 6 parts 104 us, 2
+// 102, 1 95, whose shortest units leave early.)
 //
 // With codes c and scales s of a key's row, a query's score is z = (q . ck) sk and its output
 // sum p (sv cv) / sum p: the codes are exact in bf16 and go into the matrix products as they are, the
@@ -31,8 +34,10 @@ namespace hk {
 
 constexpr int A8_NT = 256, A8_NW = 4;
 constexpr float A8_SLACK = 4.f;
-constexpr int A8_PPS = 128, A8_PPS_MIN = 8;   // pages of a range at most and at least
-constexpr int A8_TARGET = 2048, A8_MOST = 4096;   // workgroups that a launch should have, and with ranges at most
+constexpr int A8_STEP = 2 * A8_NW;            // pages of a step
+constexpr int A8_UNITS = 4096;                // units that a launch plans; one of more has a workgroup for each
+template <int D>
+constexpr int A8_GROUPS = D == 128 ? 512 : 768;   // workgroups that share the steps
 constexpr int A8_ROWS = 32;                   // rows of a workgroup at most
 
 struct Args8 {
@@ -43,9 +48,10 @@ struct Args8 {
   const int32_t *table, *n_pages, *start;     // start NULL: one token per sequence
   const uint16_t* masks;
   void* o;
-  float *lse, *part_o, *part_ml;
+  float *lse, *part_o, *part_ml;              // states: of workgroup b's first unit at 2 b, of its last at 2 b + 1
+  int32_t* first;                             // step that a unit begins at, and the number of steps; NULL: not planned
   int Hq, Hkv, G, max_pages, num_pages, n_seq, n_tokens, max_len;
-  int n_units, n_split, cap;                  // cap: rows of a unit in the workspace
+  int n_units, cap;                           // cap: rows of a unit in the workspace
   int one_tile;                               // no sequence has more rows than a workgroup
   float c2;
 };
@@ -100,10 +106,46 @@ __device__ __forceinline__ Unit unit_of(const Args8& a, int u) {
   }
   return w;
 }
-// pages of a range, an even number: the row's pages spread over the launch's ranges
-__device__ __forceinline__ int share8(const Args8& a, int pages) {
-  const int even = ((pages + a.n_split - 1) / a.n_split + 1) & ~1;
-  return max(even, A8_PPS_MIN);
+__device__ __forceinline__ int steps_of(const Unit& w) {
+  return w.rows == 0 ? 0 : max((w.pages + A8_STEP - 1) / A8_STEP, 1);
+}
+// Workgroup b of n, at most one a step, has the steps [run_of(b), run_of(b + 1)) of total; group_of: that
+// of step x.
+__device__ __forceinline__ int run_of(int b, int n, int total) { return (int)((int64_t)total * b / n); }
+__device__ __forceinline__ int group_of(int x, int n, int total) { return (int)(((int64_t)(x + 1) * n - 1) / total); }
+
+// Steps before every unit into first (LDS), the total at first[n_units]; the last workgroup leaves them
+// for the merge.
+template <int ROWS, bool CHUNK>
+__device__ __forceinline__ void plan_units(const Args8& a, int* first, int* sums) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int per = (a.n_units + A8_NT - 1) / A8_NT, u0 = threadIdx.x * per;
+  int mine = 0;
+  for (int u = u0; u < min(u0 + per, a.n_units); ++u) {
+    const int n = steps_of(unit_of<ROWS, CHUNK>(a, u));
+    first[u] = n;
+    mine += n;
+  }
+  int x = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o, 64);
+    if (lane >= o) x += y;
+  }
+  if (lane == 63) sums[wave] = x;
+  __syncthreads();
+  int before = x - mine;
+#pragma unroll
+  for (int i = 0; i < A8_NW; ++i) before += i < wave ? sums[i] : 0;
+  for (int u = u0; u < min(u0 + per, a.n_units); ++u) {
+    const int n = first[u];
+    first[u] = before;
+    before += n;
+  }
+  if (threadIdx.x == A8_NT - 1) first[a.n_units] = before;
+  __syncthreads();
+  if (blockIdx.x == gridDim.x - 1)
+    for (int u = threadIdx.x; u <= a.n_units; u += A8_NT) a.first[u] = first[u];
 }
 
 // log of l 2^m; the powers of two of both cancel as whole numbers
@@ -175,11 +217,45 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_kernel(Args8 a) {
   __shared__ float s_m[A8_NW][NQ][16], s_l[A8_NW][NQ][16];
   const int lane = threadIdx.x & 63, i16 = lane & 15, qd = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int u = blockIdx.x / a.n_split, split = blockIdx.x - u * a.n_split;
+  uint32_t source[L::PAGE / 1024];
+#pragma unroll
+  for (int g = 0; g < L::PAGE / 1024; ++g) source[g] = L::source(lane, g);
+  int k_at[KS / 2], v_at[4];                  // the lane's fragments within a page
+#pragma unroll
+  for (int i = 0; i < KS / 2; ++i) k_at[i] = L::at(i16, KS / 2 * qd + i);
+#pragma unroll
+  for (int r = 0; r < 4; ++r) v_at[r] = L::at(4 * qd + r, i16 * (D / 16) / 16) + i16 * (D / 16) % 16;
+
+  int u = blockIdx.x, skip = 0, left = 1 << 30;   // unit, its steps that are another's, steps of the run
+  if (a.first) {
+    int* first = reinterpret_cast<int*>(s_tiles);
+    static_assert(sizeof(s_tiles) >= (A8_UNITS + 1) * sizeof(int));
+    plan_units<ROWS, CHUNK>(a, first, reinterpret_cast<int*>(s_m));
+    const int total = __builtin_amdgcn_readfirstlane(first[a.n_units]), n = min((int)gridDim.x, total);
+    if ((int)blockIdx.x >= n) return;
+    const int x = run_of(blockIdx.x, n, total);
+    left = run_of(blockIdx.x + 1, n, total) - x;
+    u = 0;                                    // the last unit that begins at or before x
+    for (int hi = a.n_units; hi - u > 1;) {
+      const int mid = (u + hi) / 2;
+      if (first[mid] <= x) u = mid;
+      else hi = mid;
+    }
+    u = __builtin_amdgcn_readfirstlane(u);
+    skip = __builtin_amdgcn_readfirstlane(x - first[u]);
+    __syncthreads();                          // (the tiles take first's place)
+  }
+  for (; left > 0 && u < a.n_units; ++u) {
   const Unit w = unit_of<ROWS, CHUNK>(a, u);
-  if (w.rows == 0) return;
-  const int share = share8(a, w.pages), p0 = split * share, p1 = min(p0 + share, w.pages);
-  if (p0 >= w.pages && split > 0) return;
+  if (w.rows == 0) {
+    if (!a.first) return;
+    continue;                                 // (no steps)
+  }
+  const int steps = steps_of(w), take = min(steps - skip, left);
+  const int p0 = skip * A8_STEP, p1 = min(p0 + take * A8_STEP, w.pages);
+  const int64_t state = take == steps ? -1 : (int64_t)(2 * blockIdx.x + (skip == 0)) * a.cap;
+  left = a.first ? left - take : 0;
+  skip = 0;
   const int32_t* trow = a.table + (size_t)w.h * a.max_pages;
   const uint16_t* mrow = a.masks + (size_t)w.h * a.max_pages;
 
@@ -210,10 +286,6 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_kernel(Args8 a) {
   const int seen_all = w.off + w.r0 / a.G;    // by every row of the workgroup
   const int bias = (int)A8_SLACK + 33 - __clz(max(p1 - p0, 1) * HK_PAGE);
   const float down = __uint_as_float((uint32_t)(127 - bias) << 23), back = __uint_as_float((uint32_t)(127 + bias) << 23);
-
-  uint32_t source[L::PAGE / 1024];
-#pragma unroll
-  for (int g = 0; g < L::PAGE / 1024; ++g) source[g] = L::source(lane, g);
 
   float m[NQ], l[NQ];
   f32x4 acc[NQ][DT];
@@ -250,11 +322,6 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_kernel(Args8 a) {
         for (int i = PP - 1; i >= 0; --i)
           acc[nq][4 * j + 2 * H + h] = mma8(vf[h], pf[nq][i], acc[nq][4 * j + 2 * H + h]);
   };
-  int k_at[KS / 2], v_at[4];                  // the lane's fragments within a page
-#pragma unroll
-  for (int i = 0; i < KS / 2; ++i) k_at[i] = L::at(i16, KS / 2 * qd + i);
-#pragma unroll
-  for (int r = 0; r < 4; ++r) v_at[r] = L::at(4 * qd + r, i16 * (D / 16) / 16) + i16 * (D / 16) % 16;
   // the block at `b`, from page p on, keys valid where the bits of mask are 1
   auto compute = [&](const char* b, int p, uint32_t mask) {
     const bool full = mask == 0xffffffffu && (!CHUNK || (p + 2) * HK_PAGE <= seen_all);
@@ -449,7 +516,7 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_kernel(Args8 a) {
 #pragma unroll
         for (int j = 0; j < DT; ++j) acc[nq][j] += s_acc[wave][nq * DT + j][lane];
   }
-  if (wave != 0) return;
+  if (wave == 0)
 #pragma unroll
   for (int nq = 0; nq < NQ; ++nq) {
     const int row = 16 * nq + i16, r = w.r0 + row;
@@ -457,11 +524,10 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_kernel(Args8 a) {
     const float inv = lt[nq] == 0.f ? 0.f : 1.f / lt[nq];       // (a NaN stays one)
     const int tok = r / a.G, g = r - tok * a.G;
     const int64_t at = (int64_t)(w.c.first + tok) * a.Hq + w.kv * a.G + g;
-    const int64_t pt = ((int64_t)blockIdx.x * a.cap + row);
     // the lane's dims: D / 4 from qd D / 4 on, (D / 16) r + j of them in acc[j][r]
     const auto put = [&](int i, float x0, float x1, float x2, float x3) {
-      if (a.n_split > 1) {
-        *reinterpret_cast<f32x4*>(a.part_o + pt * D + qd * (D / 4) + i) = f32x4{x0, x1, x2, x3};
+      if (state >= 0) {
+        *reinterpret_cast<f32x4*>(a.part_o + (state + row) * D + qd * (D / 4) + i) = f32x4{x0, x1, x2, x3};
       } else if constexpr (PP == 3) {
         *reinterpret_cast<f32x4*>(static_cast<float*>(a.o) + at * D + qd * (D / 4) + i) = f32x4{x0, x1, x2, x3};
       } else {
@@ -477,16 +543,18 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_kernel(Args8 a) {
         put(DT * k + j, value(0), value(1), value(2), value(3));
       }
     if (qd == 0) {
-      if (a.n_split > 1) *reinterpret_cast<f32x2*>(a.part_ml + pt * 2) = f32x2{lt[nq] == 0.f ? -INFINITY : mt[nq], lt[nq]};
+      if (state >= 0) *reinterpret_cast<f32x2*>(a.part_ml + (state + row) * 2) = f32x2{lt[nq] == 0.f ? -INFINITY : mt[nq], lt[nq]};
       else if (a.lse) a.lse[at] = lse8(mt[nq], lt[nq]);
     }
   }
+  __syncthreads();                            // (the states in LDS are read)
+  }
 }
 
-// The ranges' states (means of V, references, sums) to the row's: a wave takes a row, or WAVES of them
-// share a row's ranges.  D / 4 lanes load a state; a wave has 256 / D of them on their way at once.
+// The states of a cut unit's parts (means of V, references, sums) to the row's: a wave takes a row, or
+// WAVES of them share a row's parts.  D / 4 lanes load a state; a wave has 256 / D of them on their way at once.
 template <int D, int ROWS, int PP, bool CHUNK, int WAVES>
-__global__ __launch_bounds__(A8_NT) void attn8_merge_kernel(Args8 a) {
+__global__ __launch_bounds__(A8_NT) void attn8_merge_kernel(Args8 a, int n_groups) {
   constexpr int LPR = D / 4, SIDE = 64 / LPR, PER = A8_NW / WAVES;
   __shared__ float s_m[A8_NW], s_l[A8_NW];
   __shared__ f32x4 s_o[A8_NW][LPR];
@@ -496,15 +564,17 @@ __global__ __launch_bounds__(A8_NT) void attn8_merge_kernel(Args8 a) {
   const Unit w = unit_of<ROWS, CHUNK>(a, u);
   // (the waves of a row leave together)
   if (w.rows == 0 || row >= a.cap || w.r0 + row >= w.rows) return;
-  const int share = share8(a, w.pages), used = max((w.pages + share - 1) / share, 1);
+  const int total = a.first[a.n_units], x0 = a.first[u], x1 = a.first[u + 1];
+  const int n = min(n_groups, total), b0 = group_of(x0, n, total), used = group_of(x1 - 1, n, total) - b0 + 1;
+  if (used < 2) return;                       // not cut
   const int per = (used + WAVES - 1) / WAVES, i0 = wave % WAVES * per, i1 = min(i0 + per, used);
-  const int64_t first = (int64_t)u * a.n_split * a.cap + row;
-  const f32x2* ml = reinterpret_cast<const f32x2*>(a.part_ml) + first;
+  const auto state = [&](int i) { return (int64_t)(2 * (b0 + i) + (i == 0)) * a.cap + row; };
+  const f32x2* ml = reinterpret_cast<const f32x2*>(a.part_ml);
   float m = -INFINITY, l = 0.f;
-  for (int i = i0 + lane; i < i1; i += 64) m = fmaxf(m, ml[(int64_t)i * a.cap][0]);
+  for (int i = i0 + lane; i < i1; i += 64) m = fmaxf(m, ml[state(i)][0]);
   m = wave_max(m);
   const auto weight = [&](int i) {
-    const f32x2 x = ml[(int64_t)i * a.cap];
+    const f32x2 x = ml[state(i)];
     return x[0] == -INFINITY ? 0.f : x[1] * fast_exp2(x[0] - m);
   };
   for (int i = i0 + lane; i < i1; i += 64) l += weight(i);
@@ -514,13 +584,13 @@ __global__ __launch_bounds__(A8_NT) void attn8_merge_kernel(Args8 a) {
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   for (int from = i0; from < i1; from += 64) {
     const float f = from + lane < i1 ? weight(from + lane) * inv : 0.f;
-    const int n = min(i1 - from, 64);
+    const int most = min(i1 - from, 64);
 #pragma unroll 4
-    for (int j = 0; j < n; j += SIDE) {
-      const int i = min(j + side, n - 1);
-      const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_o + (first + (int64_t)(from + i) * a.cap) * D + 4 * at);
+    for (int j = 0; j < most; j += SIDE) {
+      const int i = min(j + side, most - 1);
+      const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_o + state(from + i) * D + 4 * at);
       const float g = __shfl(f, j + side, 64);
-      if (j + side < n) o += g * x;
+      if (j + side < most) o += g * x;
     }
   }
 #pragma unroll
@@ -563,8 +633,9 @@ __global__ __launch_bounds__(A8_NT) void attn8_merge_kernel(Args8 a) {
 
 // ------------------------------------------------------------------ host
 struct Plan8 {
-  int nq, one_tile, cap, n_split;
+  int nq, one_tile, cap;
   int64_t units;
+  bool planned, cut;                          // whether units can be cut
 };
 inline Plan8 plan8(int NS, int Hkv, int G, const hk_chunks* ch, int max_pages) {
   Plan8 p;
@@ -576,61 +647,54 @@ inline Plan8 plan8(int NS, int Hkv, int G, const hk_chunks* ch, int max_pages) {
   const int64_t tiles = !ch ? (int64_t)NS * ((G + rows - 1) / rows)
                             : p.one_tile ? NS : (int64_t)ch->n_tokens * G / rows + NS;
   p.units = tiles * Hkv;
-  int pps = A8_PPS;
-  while (pps > A8_PPS_MIN && p.units * ((max_pages + pps - 1) / pps) < A8_TARGET) pps >>= 1;
-  const int64_t most_split = (A8_MOST + p.units - 1) / p.units;
-  p.n_split = (int)std::min<int64_t>((max_pages + pps - 1) / pps, most_split);
+  p.planned = p.units <= A8_UNITS && p.units * (((int64_t)max_pages + A8_STEP - 1) / A8_STEP) < (1ll << 31);
+  p.cut = p.planned && max_pages > A8_STEP;
   return p;
 }
+inline size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
+constexpr size_t kFirst8 = (A8_UNITS + 1) * sizeof(int32_t);
+inline size_t states8(int D, int cap) { return (size_t)2 * (D == 128 ? A8_GROUPS<128> : A8_GROUPS<64>) * cap; }
 
 }  // namespace hk
 
 using namespace hk;
 
-static size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
-
+// (any chunks of no more tokens, and none longer, take no more)
 size_t hk_attn8_ws(int NS, int Hq, int Hkv, int D, const hk_chunks* ch, int max_pages) {
   const Plan8 p = plan8(NS, Hkv, Hq / Hkv, ch, max_pages);
-  size_t states = p.n_split > 1 ? (size_t)p.units * p.n_split * p.cap : 0;
-  if (ch && max_pages > A8_PPS_MIN) {
-    // what any chunks of no more tokens, and none longer, can take: ranges are for fewer than MOST units,
-    // and leave fewer than 2 MOST workgroups
-    const int64_t units = ((int64_t)ch->n_tokens * (Hq / Hkv) / 16 + NS) * Hkv;
-    const int64_t groups = std::min<int64_t>(2 * A8_MOST, units * ((max_pages + A8_PPS_MIN - 1) / A8_PPS_MIN));
-    const int64_t rows = (int64_t)ch->max_len * (Hq / Hkv);
-    states = (size_t)(groups * std::min<int64_t>(rows, A8_ROWS));
-  }
-  return 256 + align_up(states * D * 4) + align_up(states * 8);
+  const size_t states = ch || p.cut ? states8(D, p.cap) : 0;
+  return align_up(kFirst8) + align_up(states * D * 4) + align_up(states * 8);
 }
 
 double hk_attn8_groups(int NS, int Hq, int Hkv, const hk_chunks* ch, int max_pages) {
-  const Plan8 p = plan8(NS, Hkv, Hq / Hkv, ch, max_pages);
-  return (double)p.units * p.n_split;
+  return (double)plan8(NS, Hkv, Hq / Hkv, ch, max_pages).units;
 }
 
 template <int F, int D, int NQ, int QP, int PP, bool CHUNK>
-static void launch8(const Args8& a, hipStream_t st) {
+static void launch8(const Args8& a, bool cut, hipStream_t st) {
+  const uint32_t groups = a.first ? A8_GROUPS<D> : (uint32_t)a.n_units;
   {
     TimedLaunch t(HK_TK_ATTN8, st);
-    hipLaunchKernelGGL((attn8_kernel<F, D, NQ, QP, PP, CHUNK>), dim3((uint32_t)a.n_units * a.n_split), dim3(A8_NT), 0, st, a);
+    hipLaunchKernelGGL((attn8_kernel<F, D, NQ, QP, PP, CHUNK>), dim3(groups), dim3(A8_NT), 0, st, a);
   }
-  if (a.n_split > 1) {
+  if (cut) {
     TimedLaunch t(HK_TK_ATTN8_MERGE, st);
-    const bool few = a.n_split > 16 && a.n_units * a.cap <= 1024;
-    const uint32_t groups = (uint32_t)a.n_units * (few ? a.cap : (a.cap + A8_NW - 1) / A8_NW);
+    // rows of many parts, where there are few
+    const bool few = a.n_units * 32 <= A8_GROUPS<D>;
+    const uint32_t rows = (uint32_t)a.n_units * (few ? a.cap : (a.cap + A8_NW - 1) / A8_NW);
     const auto merge = few ? attn8_merge_kernel<D, 16 * NQ, PP, CHUNK, A8_NW> : attn8_merge_kernel<D, 16 * NQ, PP, CHUNK, 1>;
-    hipLaunchKernelGGL(merge, dim3(groups), dim3(A8_NT), 0, st, a);
+    hipLaunchKernelGGL(merge, dim3(rows), dim3(A8_NT), 0, st, a, (int)groups);
   }
 }
 template <int F, int D, int NQ>
-static void launch8_t(const Args8& a, bool chunk, bool bf, hipStream_t st) {
-  if (chunk) bf ? launch8<F, D, NQ, 1, 2, true>(a, st) : launch8<F, D, NQ, 3, 3, true>(a, st);
-  else bf ? launch8<F, D, NQ, 1, 3, false>(a, st) : launch8<F, D, NQ, 3, 3, false>(a, st);
+static void launch8_t(const Args8& a, bool chunk, bool bf, bool cut, hipStream_t st) {
+  if (chunk) bf ? launch8<F, D, NQ, 1, 2, true>(a, cut, st) : launch8<F, D, NQ, 3, 3, true>(a, cut, st);
+  else bf ? launch8<F, D, NQ, 1, 3, false>(a, cut, st) : launch8<F, D, NQ, 3, 3, false>(a, cut, st);
 }
 template <int F>
-static void launch8_f(const Args8& a, int D, int nq, bool chunk, bool bf, hipStream_t st) {
-  if (D == 128) nq == 1 ? launch8_t<F, 128, 1>(a, chunk, bf, st) : launch8_t<F, 128, 2>(a, chunk, bf, st);
-  else nq == 1 ? launch8_t<F, 64, 1>(a, chunk, bf, st) : launch8_t<F, 64, 2>(a, chunk, bf, st);
+static void launch8_f(const Args8& a, int D, int nq, bool chunk, bool bf, bool cut, hipStream_t st) {
+  if (D == 128) nq == 1 ? launch8_t<F, 128, 1>(a, chunk, bf, cut, st) : launch8_t<F, 128, 2>(a, chunk, bf, cut, st);
+  else nq == 1 ? launch8_t<F, 64, 1>(a, chunk, bf, cut, st) : launch8_t<F, 64, 2>(a, chunk, bf, cut, st);
 }
 
 hipError_t hk_launch_attn8(int NS, int Hq, int Hkv, int D, const hk_paged_kv8* kv8, const hk_chunks* ch,
@@ -651,8 +715,11 @@ hipError_t hk_launch_attn8(int NS, int Hq, int Hkv, int D, const hk_paged_kv8* k
   a.start = ch ? ch->start : nullptr;
   a.o = o;
   a.lse = lse;
-  a.part_o = static_cast<float*>(ws);
-  a.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + align_up((size_t)p.units * p.n_split * p.cap * D * 4));
+  char* at = static_cast<char*>(ws);
+  a.first = p.planned ? reinterpret_cast<int32_t*>(at) : nullptr;
+  at += align_up(kFirst8);
+  a.part_o = reinterpret_cast<float*>(at);
+  a.part_ml = reinterpret_cast<float*>(at + align_up(states8(D, p.cap) * D * 4));
   a.Hq = Hq;
   a.Hkv = Hkv;
   a.G = Hq / Hkv;
@@ -662,11 +729,11 @@ hipError_t hk_launch_attn8(int NS, int Hq, int Hkv, int D, const hk_paged_kv8* k
   a.n_tokens = ch ? ch->n_tokens : NS;
   a.max_len = ch ? ch->max_len : 1;
   a.n_units = (int)p.units;
-  a.n_split = p.n_split;
   a.cap = p.cap;
   a.one_tile = p.one_tile;
   a.c2 = sm_scale * kLog2e;
-  if (kv.dtype == HK_I8) launch8_f<HK_I8>(a, D, p.nq, ch != nullptr, dtype == HK_BF16, st);
-  else launch8_f<HK_E4M3>(a, D, p.nq, ch != nullptr, dtype == HK_BF16, st);
+  const bool bf = dtype == HK_BF16;
+  if (kv.dtype == HK_I8) launch8_f<HK_I8>(a, D, p.nq, ch != nullptr, bf, p.cut, st);
+  else launch8_f<HK_E4M3>(a, D, p.nq, ch != nullptr, bf, p.cut, st);
   return hipGetLastError();
 }
