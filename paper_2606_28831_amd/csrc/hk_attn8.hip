@@ -27,150 +27,9 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "hk_chunk.h"
-#include "hk_kv8.h"
+#include "hk_attn8.h"
 
 namespace hk {
-
-constexpr int A8_NT = 256, A8_NW = 4;
-constexpr float A8_SLACK = 4.f;
-constexpr int A8_STEP = 2 * A8_NW;            // pages of a step
-constexpr int A8_UNITS = 4096;                // units that a launch plans; one of more has a workgroup for each
-template <int D>
-constexpr int A8_GROUPS = D == 128 ? 512 : 768;   // workgroups that share the steps
-constexpr int A8_ROWS = 32;                   // rows of a workgroup at most
-
-struct Args8 {
-  const void* q;
-  int64_t q_row;                              // elements
-  const char *k_pool, *v_pool;
-  const float *k_scale, *v_scale;
-  const int32_t *table, *n_pages, *start;     // start NULL: one token per sequence
-  const uint16_t* masks;
-  void* o;
-  float *lse, *part_o, *part_ml;              // states: of workgroup b's first unit at 2 b, of its last at 2 b + 1
-  int32_t* first;                             // step that a unit begins at, and the number of steps; NULL: not planned
-  int Hq, Hkv, G, max_pages, num_pages, n_seq, n_tokens, max_len;
-  int n_units, cap;                           // cap: rows of a unit in the workspace
-  int one_tile;                               // no sequence has more rows than a workgroup
-  float c2;
-};
-
-// ROWS folded rows of one sequence and KV head.
-struct Unit {
-  Chunk c;
-  int h, kv, rows, r0, off, pages;            // off: keys before off + token are seen by that token
-};
-__device__ __forceinline__ int tiles8_before(const Args8& a, int rows, int s) {
-  return min(max(a.start[s], 0), a.n_tokens) * a.G / rows + s;
-}
-// rows 0: there are none
-template <int ROWS, bool CHUNK>
-__device__ __forceinline__ Unit unit_of(const Args8& a, int u) {
-  Unit w;
-  w.kv = u % a.Hkv;
-  const int tile = u / a.Hkv;
-  int s = tile;
-  w.r0 = 0;
-  if (!CHUNK) {
-    const int per = (a.G + ROWS - 1) / ROWS;
-    s = tile / per;
-    w.r0 = (tile - s * per) * ROWS;
-    w.c = {s, 1};
-  } else {
-    if (!a.one_tile) {
-      s = 0;
-      for (int hi = a.n_seq; hi - s > 1;) {
-        const int mid = (s + hi) / 2;
-        if (tiles8_before(a, ROWS, mid) <= tile) s = mid;
-        else hi = mid;
-      }
-      w.r0 = (tile - tiles8_before(a, ROWS, s)) * ROWS;
-    }
-    w.c = chunk_of(a.start, s, a.n_tokens, a.max_len);
-  }
-  w.rows = w.c.len * a.G;
-  if (w.r0 < 0 || w.r0 >= w.rows) {
-    w.rows = 0;
-    return w;
-  }
-  w.h = s * a.Hkv + w.kv;
-  const int n = min(max(a.n_pages[w.h], 0), a.max_pages);
-  w.pages = n;
-  w.off = 0;
-  if (CHUNK) {
-    const int end = row_end(n, n > 0 ? a.masks[(size_t)w.h * a.max_pages + n - 1] : 0u);
-    w.off = end - w.c.len + 1;
-    const int last = (min(w.r0 + ROWS, w.rows) - 1) / a.G;
-    w.pages = min(n, (max(w.off + last, 0) + HK_PAGE - 1) / HK_PAGE);
-  }
-  return w;
-}
-__device__ __forceinline__ int steps_of(const Unit& w) {
-  return w.rows == 0 ? 0 : max((w.pages + A8_STEP - 1) / A8_STEP, 1);
-}
-// Workgroup b of n, at most one a step, has the steps [run_of(b), run_of(b + 1)) of total; group_of: that
-// of step x.
-__device__ __forceinline__ int run_of(int b, int n, int total) { return (int)((int64_t)total * b / n); }
-__device__ __forceinline__ int group_of(int x, int n, int total) { return (int)(((int64_t)(x + 1) * n - 1) / total); }
-
-// Steps before every unit into first (LDS), the total at first[n_units]; the last workgroup leaves them
-// for the merge.
-template <int ROWS, bool CHUNK>
-__device__ __forceinline__ void plan_units(const Args8& a, int* first, int* sums) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int per = (a.n_units + A8_NT - 1) / A8_NT, u0 = threadIdx.x * per;
-  int mine = 0;
-  for (int u = u0; u < min(u0 + per, a.n_units); ++u) {
-    const int n = steps_of(unit_of<ROWS, CHUNK>(a, u));
-    first[u] = n;
-    mine += n;
-  }
-  int x = mine;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(x, o, 64);
-    if (lane >= o) x += y;
-  }
-  if (lane == 63) sums[wave] = x;
-  __syncthreads();
-  int before = x - mine;
-#pragma unroll
-  for (int i = 0; i < A8_NW; ++i) before += i < wave ? sums[i] : 0;
-  for (int u = u0; u < min(u0 + per, a.n_units); ++u) {
-    const int n = first[u];
-    first[u] = before;
-    before += n;
-  }
-  if (threadIdx.x == A8_NT - 1) first[a.n_units] = before;
-  __syncthreads();
-  if (blockIdx.x == gridDim.x - 1)
-    for (int u = threadIdx.x; u <= a.n_units; u += A8_NT) a.first[u] = first[u];
-}
-
-// log of l 2^m; the powers of two of both cancel as whole numbers
-__device__ __forceinline__ float lse8(float m, float l) {
-  if (l == 0.f) return -INFINITY;
-  return (m + (float)__builtin_amdgcn_frexp_expf(l) + __log2f(__builtin_amdgcn_frexp_mantf(l))) * kLn2;
-}
-
-// fp32 in N bf16 parts, of two values a word: N 1: exact ones, 2: to 2^-16, 3: all of its bits
-template <int N>
-__device__ __forceinline__ void split_pair(float x, float y, uint32_t (&out)[N]) {
-  if constexpr (N == 1) {
-    out[0] = pack_bf16(x, y);
-  } else if constexpr (N == 2) {
-    out[0] = pack_bf16(x, y);
-    out[1] = pack_bf16(x - bf16_lo(out[0]), y - bf16_hi(out[0]));
-  } else {
-#pragma unroll
-    for (int i = 0; i < 3; ++i) {
-      out[i] = high_halves(x, y);
-      x -= bf16_lo(out[i]);
-      y -= bf16_hi(out[i]);
-    }
-  }
-}
 
 // A block of 32 keys in LDS: K codes of two pages, V codes, and 64 scales (K's, V's).  It is filled
 // straight from memory, 1 KB of codes an instruction, 16 bytes a lane in lane order, so that every line
@@ -551,109 +410,28 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_kernel(Args8 a) {
   }
 }
 
-// The states of a cut unit's parts (means of V, references, sums) to the row's: a wave takes a row, or
-// WAVES of them share a row's parts.  D / 4 lanes load a state; a wave has 256 / D of them on their way at once.
-template <int D, int ROWS, int PP, bool CHUNK, int WAVES>
-__global__ __launch_bounds__(A8_NT) void attn8_merge_kernel(Args8 a, int n_groups) {
-  constexpr int LPR = D / 4, SIDE = 64 / LPR, PER = A8_NW / WAVES;
-  __shared__ float s_m[A8_NW], s_l[A8_NW];
-  __shared__ f32x4 s_o[A8_NW][LPR];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int per_unit = (a.cap + PER - 1) / PER, u = blockIdx.x / per_unit;
-  const int row = (blockIdx.x - u * per_unit) * PER + wave / WAVES;
-  const Unit w = unit_of<ROWS, CHUNK>(a, u);
-  // (the waves of a row leave together)
-  if (w.rows == 0 || row >= a.cap || w.r0 + row >= w.rows) return;
-  const int total = a.first[a.n_units], x0 = a.first[u], x1 = a.first[u + 1];
-  const int n = min(n_groups, total), b0 = group_of(x0, n, total), used = group_of(x1 - 1, n, total) - b0 + 1;
-  if (used < 2) return;                       // not cut
-  const int per = (used + WAVES - 1) / WAVES, i0 = wave % WAVES * per, i1 = min(i0 + per, used);
-  const auto state = [&](int i) { return (int64_t)(2 * (b0 + i) + (i == 0)) * a.cap + row; };
-  const f32x2* ml = reinterpret_cast<const f32x2*>(a.part_ml);
-  float m = -INFINITY, l = 0.f;
-  for (int i = i0 + lane; i < i1; i += 64) m = fmaxf(m, ml[state(i)][0]);
-  m = wave_max(m);
-  const auto weight = [&](int i) {
-    const f32x2 x = ml[state(i)];
-    return x[0] == -INFINITY ? 0.f : x[1] * fast_exp2(x[0] - m);
-  };
-  for (int i = i0 + lane; i < i1; i += 64) l += weight(i);
-  l = wave_sum(l);
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  const int side = lane / LPR, at = lane % LPR;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int from = i0; from < i1; from += 64) {
-    const float f = from + lane < i1 ? weight(from + lane) * inv : 0.f;
-    const int most = min(i1 - from, 64);
-#pragma unroll 4
-    for (int j = 0; j < most; j += SIDE) {
-      const int i = min(j + side, most - 1);
-      const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_o + state(from + i) * D + 4 * at);
-      const float g = __shfl(f, j + side, 64);
-      if (j + side < most) o += g * x;
-    }
-  }
-#pragma unroll
-  for (int d = LPR; d < 64; d <<= 1)
-#pragma unroll
-    for (int k = 0; k < 4; ++k) o[k] += __shfl_xor(o[k], d, 64);
-  if constexpr (WAVES > 1) {
-    if (lane == 0) {
-      s_m[wave] = m;
-      s_l[wave] = l;
-    }
-    if (lane < LPR) s_o[wave][lane] = o;
-    __syncthreads();
-    if (wave != 0) return;
-    float mt = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < WAVES; ++i) mt = fmaxf(mt, s_m[i]);
-    l = 0.f;
-    float part[WAVES];
-#pragma unroll
-    for (int i = 0; i < WAVES; ++i) {
-      part[i] = s_m[i] == -INFINITY ? 0.f : s_l[i] * fast_exp2(s_m[i] - mt);
-      l += part[i];
-    }
-    m = mt;
-    const float back = l == 0.f ? 0.f : 1.f / l;
-    o = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (lane < LPR)
-#pragma unroll
-      for (int i = 0; i < WAVES; ++i) o += part[i] * back * s_o[i][lane];
-  }
-  const int r = w.r0 + row, tok = r / a.G, g = r - tok * a.G;
-  const int64_t to = (int64_t)(w.c.first + tok) * a.Hq + w.kv * a.G + g;
-  if (lane < LPR) {
-    if constexpr (PP == 3) *reinterpret_cast<f32x4*>(static_cast<float*>(a.o) + to * D + 4 * lane) = o;
-    else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.o) + to * D + 4 * lane) = u32x2{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
-  }
-  if (lane == 0 && a.lse) a.lse[to] = lse8(m, l);
-}
-
 // ------------------------------------------------------------------ host
 struct Plan8 {
   int nq, one_tile, cap;
   int64_t units;
+  bool tiles;                                 // chunks of more than A8_ROWS rows go to the tile kernel
   bool planned, cut;                          // whether units can be cut
 };
-inline Plan8 plan8(int NS, int Hkv, int G, const hk_chunks* ch, int max_pages) {
+inline Plan8 plan8(int NS, int Hkv, int G, const hk_chunks* ch, bool bf, int max_pages) {
   Plan8 p;
   const int64_t most = ch ? (int64_t)ch->max_len * G : G;       // rows of a sequence at most
   p.nq = most <= 16 ? 1 : 2;
   const int rows = 16 * p.nq;
-  p.one_tile = most <= rows;
+  p.tiles = ch && bf && most > rows;
+  p.one_tile = most <= rows || p.tiles;
   p.cap = (int)(most < rows ? most : rows);
   const int64_t tiles = !ch ? (int64_t)NS * ((G + rows - 1) / rows)
                             : p.one_tile ? NS : (int64_t)ch->n_tokens * G / rows + NS;
   p.units = tiles * Hkv;
-  p.planned = p.units <= A8_UNITS && p.units * (((int64_t)max_pages + A8_STEP - 1) / A8_STEP) < (1ll << 31);
+  p.planned = planned8(p.units, max_pages);
   p.cut = p.planned && max_pages > A8_STEP;
   return p;
 }
-inline size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
-constexpr size_t kFirst8 = (A8_UNITS + 1) * sizeof(int32_t);
-inline size_t states8(int D, int cap) { return (size_t)2 * (D == 128 ? A8_GROUPS<128> : A8_GROUPS<64>) * cap; }
 
 }  // namespace hk
 
@@ -661,13 +439,15 @@ using namespace hk;
 
 // (any chunks of no more tokens, and none longer, take no more)
 size_t hk_attn8_ws(int NS, int Hq, int Hkv, int D, const hk_chunks* ch, int max_pages) {
-  const Plan8 p = plan8(NS, Hkv, Hq / Hkv, ch, max_pages);
-  const size_t states = ch || p.cut ? states8(D, p.cap) : 0;
-  return align_up(kFirst8) + align_up(states * D * 4) + align_up(states * 8);
+  const int G = Hq / Hkv;
+  const bool long_ones = ch && (int64_t)ch->max_len * G > A8_ROWS;
+  const size_t most = states8_bytes(D, plan8(NS, Hkv, G, ch, false, max_pages).cap);
+  return long_ones ? std::max(most, hk_attn8_tile_ws(D)) : most;
 }
 
 double hk_attn8_groups(int NS, int Hq, int Hkv, const hk_chunks* ch, int max_pages) {
-  return (double)plan8(NS, Hkv, Hq / Hkv, ch, max_pages).units;
+  const Plan8 p = plan8(NS, Hkv, Hq / Hkv, ch, false, max_pages);
+  return (double)p.units;
 }
 
 template <int F, int D, int NQ, int QP, int PP, bool CHUNK>
@@ -677,14 +457,7 @@ static void launch8(const Args8& a, bool cut, hipStream_t st) {
     TimedLaunch t(HK_TK_ATTN8, st);
     hipLaunchKernelGGL((attn8_kernel<F, D, NQ, QP, PP, CHUNK>), dim3(groups), dim3(A8_NT), 0, st, a);
   }
-  if (cut) {
-    TimedLaunch t(HK_TK_ATTN8_MERGE, st);
-    // rows of many parts, where there are few
-    const bool few = a.n_units * 32 <= A8_GROUPS<D>;
-    const uint32_t rows = (uint32_t)a.n_units * (few ? a.cap : (a.cap + A8_NW - 1) / A8_NW);
-    const auto merge = few ? attn8_merge_kernel<D, 16 * NQ, PP, CHUNK, A8_NW> : attn8_merge_kernel<D, 16 * NQ, PP, CHUNK, 1>;
-    hipLaunchKernelGGL(merge, dim3(rows), dim3(A8_NT), 0, st, a, (int)groups);
-  }
+  if (cut) merge8<D, 16 * NQ, PP, CHUNK>(a, groups, st);
 }
 template <int F, int D, int NQ>
 static void launch8_t(const Args8& a, bool chunk, bool bf, bool cut, hipStream_t st) {
@@ -701,7 +474,8 @@ hipError_t hk_launch_attn8(int NS, int Hq, int Hkv, int D, const hk_paged_kv8* k
                            hk_dtype dtype, const void* q, int64_t q_row, float sm_scale, void* o, float* lse,
                            void* ws, hipStream_t st) {
   const hk_paged_kv& kv = kv8->kv;
-  const Plan8 p = plan8(NS, Hkv, Hq / Hkv, ch, kv.max_pages);
+  const bool bf = dtype == HK_BF16;
+  const Plan8 p = plan8(NS, Hkv, Hq / Hkv, ch, bf, kv.max_pages);
   Args8 a{};
   a.q = q;
   a.q_row = q_row;
@@ -715,11 +489,6 @@ hipError_t hk_launch_attn8(int NS, int Hq, int Hkv, int D, const hk_paged_kv8* k
   a.start = ch ? ch->start : nullptr;
   a.o = o;
   a.lse = lse;
-  char* at = static_cast<char*>(ws);
-  a.first = p.planned ? reinterpret_cast<int32_t*>(at) : nullptr;
-  at += align_up(kFirst8);
-  a.part_o = reinterpret_cast<float*>(at);
-  a.part_ml = reinterpret_cast<float*>(at + align_up(states8(D, p.cap) * D * 4));
   a.Hq = Hq;
   a.Hkv = Hkv;
   a.G = Hq / Hkv;
@@ -731,9 +500,13 @@ hipError_t hk_launch_attn8(int NS, int Hq, int Hkv, int D, const hk_paged_kv8* k
   a.n_units = (int)p.units;
   a.cap = p.cap;
   a.one_tile = p.one_tile;
+  a.rows_from = 1;
+  a.rows_to = p.tiles ? A8_ROWS : INT32_MAX;
   a.c2 = sm_scale * kLog2e;
-  const bool bf = dtype == HK_BF16;
+  carve8(a, p.planned, D, ws);
   if (kv.dtype == HK_I8) launch8_f<HK_I8>(a, D, p.nq, ch != nullptr, bf, p.cut, st);
   else launch8_f<HK_E4M3>(a, D, p.nq, ch != nullptr, bf, p.cut, st);
+  // (the launches follow one another: one workspace serves both)
+  if (p.tiles) hk_launch_attn8_tile(a, kv.dtype, D, ws, st);
   return hipGetLastError();
 }

@@ -1,0 +1,306 @@
+// 8-bit cache: attention of long chunks, bf16 queries (gfx950).
+//
+// A unit is TILE8_ROWS folded rows (see hk_attn8.hip) of a sequence and KV head: four waves of 32 rows
+// against the same keys, 32 at a time.  The codes of a tile are converted once for all waves, by all of
+// them, and lie in LDS as bf16: K by rows, V by dims, in the order of keys that the scores' registers
+// have, so that both kinds of fragment are 16 bytes in a row.  While tile t is computed, t + 1 is converted
+// into the other buffer and t + 2 is on its way into registers.
+//
+// Per wave and tile, 32x32x16 MFMAs: C[key][row] = K Q^T, then O^T[dim][row] += V^T P^T with P in two
+// bf16 parts, to 2^-16 of a term.  Lane l holds row l % 32 and half hi = l / 32 of the contraction; register
+// r of a score tile is key (r & 3) + 8 (r >> 2) + 4 hi.
+#include <type_traits>
+
+#include "hk_attn8.h"
+
+namespace hk {
+
+constexpr int TILE8_ROWS = 128;
+
+template <int F, int D>
+__global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
+#pragma clang fp contract(off)
+  constexpr int KS = D / 16, DT = D / 32;
+  constexpr int K_ROW = 2 * D + 16, V_ROW = 80;               // bytes; padded: no bank twice among 16 lanes
+  constexpr int KW = D / 16;                                  // words of codes of a thread that brings K
+  constexpr int K_TILE = 32 * K_ROW, TILE = K_TILE + D * V_ROW;
+  __shared__ __align__(16) char s_tile[2][TILE];
+  __shared__ __align__(16) float s_scale[2][64];              // K's times c2, V's times 2^-bias
+  __shared__ int s_sums[A8_NW];
+  const int lane = threadIdx.x & 63, row32 = lane & 31, hi = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool is_v = wave >= 2;
+  // what the thread brings of a tile: K: a quarter of row t / 4; V: dims 4 c .. 4 c + 3 of the eight keys of
+  // group t % 4 (of 16 (g / 2) + 4 (g % 2) + {0 .. 3, 8 .. 11}); D 64: c up to 16, by wave 2 alone
+  const int t = threadIdx.x & 127, grp = t & 3, c = t >> 2;
+  const bool brings = !is_v || c < D / 4;
+  const int page_of = is_v ? grp >> 1 : t >> 6;
+  const int from = is_v ? (grp & 1) * 4 * D + 4 * c : (c & 15) * D + grp * (D / 4);
+  const int to = is_v ? 4 * c * V_ROW + grp * 16 : c * K_ROW + grp * (D / 2);
+
+  int u = a.n_units - 1 - (int)blockIdx.x, skip = 0, left = 1 << 30;
+  if (a.first) {
+    int* first = reinterpret_cast<int*>(s_tile);
+    static_assert(sizeof(s_tile) >= (A8_UNITS + 1) * sizeof(int));
+    plan_units<TILE8_ROWS, true>(a, first, s_sums);
+    const int total = __builtin_amdgcn_readfirstlane(first[a.n_units]), n = min((int)gridDim.x, total);
+    if ((int)blockIdx.x >= n) return;
+    const int x = run_of(blockIdx.x, n, total);
+    left = run_of(blockIdx.x + 1, n, total) - x;
+    u = 0;
+    for (int h = a.n_units; h - u > 1;) {
+      const int mid = (u + h) / 2;
+      if (first[mid] <= x) u = mid;
+      else h = mid;
+    }
+    u = __builtin_amdgcn_readfirstlane(u);
+    skip = __builtin_amdgcn_readfirstlane(x - first[u]);
+    __syncthreads();
+  }
+  for (; left > 0 && u < a.n_units; ++u) {
+    const Unit w = unit_of<TILE8_ROWS, true>(a, u);
+    if (w.rows == 0) {
+      if (!a.first) return;
+      continue;
+    }
+    const int steps = steps_of(w), take = min(steps - skip, left);
+    const int p0 = skip * A8_STEP, p1 = min(p0 + take * A8_STEP, w.pages);
+    const int64_t state = take == steps ? -1 : (int64_t)(2 * blockIdx.x + (skip == 0)) * a.cap;
+    left = a.first ? left - take : 0;
+    skip = 0;
+    const int32_t* trow = a.table + (size_t)w.h * a.max_pages;
+    const uint16_t* mrow = a.masks + (size_t)w.h * a.max_pages;
+
+    // rows past the chunk repeat its last one; they are not stored
+    const int w0 = w.r0 + wave * 32, r = min(w0 + row32, w.rows - 1), tok = r / a.G, g = r - tok * a.G;
+    const int seen = w.off + tok;                             // keys before this one are seen by the lane's row,
+    const int seen_all = w.off + min(w0, w.rows - 1) / a.G;   // by every row of the wave,
+    const int seen_any = w.off + (min(w0 + 32, w.rows) - 1) / a.G;   // by any of them
+    bf16x8 qf[KS];
+    {
+      const uint16_t* q = static_cast<const uint16_t*>(a.q) + (int64_t)(w.c.first + tok) * a.q_row + (w.kv * a.G + g) * D;
+#pragma unroll
+      for (int s = 0; s < KS; ++s) qf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(q + 16 * s + 8 * hi));
+    }
+    const int bias = (int)A8_SLACK + 33 - __clz(max(p1 - p0, 1) * HK_PAGE);
+    const float down = __uint_as_float((uint32_t)(127 - bias) << 23), back = __uint_as_float((uint32_t)(127 + bias) << 23);
+    float m = -INFINITY, l = 0.f;
+    f32x16 acc[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[d][e] = 0.f;
+
+    // Ids and masks come 32 tiles at a time: lane i holds those of page i % 2 of tile i / 2.
+    const int tiles = p1 > p0 ? (p1 - p0 + 1) / 2 : 0;
+    int ids = 0, masks = 0;
+    uint32_t code[8];                                         // K: KW words; V: word of eight keys
+    float scale = 0.f;
+    uint32_t mask = 0, next_mask = 0;                         // of the tile computed, and of the one converted
+    auto load = [&](int i) {                                  // (past the last tile: its pages again)
+      if ((i & 31) == 0) {
+        const int page = p0 + 2 * i + lane;
+        ids = min(max(trow[min(page, p1 - 1)], 0), a.num_pages - 1);
+        masks = page < p1 ? mrow[page] : 0;
+      }
+      const int e = 2 * (i & 31);
+      const int id0 = __builtin_amdgcn_readlane(ids, e), id1 = __builtin_amdgcn_readlane(ids, e + 1);
+      next_mask = (uint32_t)__builtin_amdgcn_readlane(masks, e) | (uint32_t)__builtin_amdgcn_readlane(masks, e + 1) << 16;
+      const size_t at = (size_t)(uint32_t)(page_of ? id1 : id0) * (HK_PAGE * D) + from;
+      if (!is_v) {
+#pragma unroll
+        for (int k = 0; k < KW / 4; ++k)
+          *reinterpret_cast<u32x4*>(&code[4 * k]) = *reinterpret_cast<const u32x4*>(a.k_pool + at + 16 * k);
+      } else if (brings) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          code[j] = *reinterpret_cast<const uint32_t*>(a.v_pool + at + (8 * (j >> 2) + (j & 3)) * D);
+      }
+      if (wave == 0) {
+        const int id = (lane >> 4) & 1 ? id1 : id0;
+        scale = (lane >> 5 ? a.v_scale : a.k_scale)[(size_t)(uint32_t)id * HK_PAGE + (lane & 15)];
+      }
+    };
+    auto convert = [&](int buf, uint32_t mk) {
+      if (!is_v) {
+        char* at = s_tile[buf] + to;
+#pragma unroll
+        for (int k = 0; k < KW / 2; ++k)
+          *reinterpret_cast<u32x4*>(at + 16 * k) =
+              u32x4{Code<F>::template pair<0>(code[2 * k]), Code<F>::template pair<1>(code[2 * k]),
+                    Code<F>::template pair<0>(code[2 * k + 1]), Code<F>::template pair<1>(code[2 * k + 1])};
+      } else if (brings) {
+        if (F == HK_E4M3 && mk != 0xffffffffu) {
+          // a slot that is not valid may hold codes that stand for NaN
+          const uint32_t bits = mk >> (16 * (grp >> 1) + 4 * (grp & 1));
+#pragma unroll
+          for (int j = 0; j < 8; ++j) code[j] = (bits >> (8 * (j >> 2) + (j & 3))) & 1u ? code[j] : 0u;
+        }
+        char* at = s_tile[buf] + K_TILE + to;
+        u32x4 x[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t p = code[2 * k], q = code[2 * k + 1];
+          if constexpr (F == HK_I8) {
+            x[0][k] = high_halves(Code<F>::template value<0>(p), Code<F>::template value<0>(q));
+            x[1][k] = high_halves(Code<F>::template value<1>(p), Code<F>::template value<1>(q));
+            x[2][k] = high_halves(Code<F>::template value<2>(p), Code<F>::template value<2>(q));
+            x[3][k] = high_halves(Code<F>::template value<3>(p), Code<F>::template value<3>(q));
+          } else {
+            const uint32_t p0 = Code<F>::template pair<0>(p), q0 = Code<F>::template pair<0>(q);
+            const uint32_t p1 = Code<F>::template pair<1>(p), q1 = Code<F>::template pair<1>(q);
+            x[0][k] = __builtin_amdgcn_perm(q0, p0, 0x05040100u);
+            x[1][k] = __builtin_amdgcn_perm(q0, p0, 0x07060302u);
+            x[2][k] = __builtin_amdgcn_perm(q1, p1, 0x05040100u);
+            x[3][k] = __builtin_amdgcn_perm(q1, p1, 0x07060302u);
+          }
+        }
+#pragma unroll
+        for (int d = 0; d < 4; ++d) *reinterpret_cast<u32x4*>(at + d * V_ROW) = x[d];
+      }
+      if (wave == 0) s_scale[buf][lane] = scale * (lane >> 5 ? down : a.c2);
+    };
+    auto compute = [&](int buf, int key, uint32_t valid, auto is_full) {
+      constexpr bool FULL = decltype(is_full)::value;
+      f32x16 z = {};
+      const char* k = s_tile[buf] + row32 * K_ROW + hi * 16;
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+        z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(k + 32 * s)),
+                                                    qf[s], z, 0, 0, 0);
+      const float* sc = s_scale[buf] + 4 * hi;
+      uint32_t vis = 0xffffffffu;
+      if (!FULL) {
+        const int n = seen - key;
+        vis = (valid & (n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u)) >> (4 * hi);
+      }
+      float zm = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4 ks = *reinterpret_cast<const f32x4*>(sc + 8 * i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float x = z[4 * i + j] * ks[j];
+          if (!FULL) x = (vis >> (8 * i + j)) & 1u ? x : -INFINITY;
+          z[4 * i + j] = x;
+          zm = fmaxf(zm, x);
+        }
+      }
+      if (__any(zm > m + A8_SLACK)) {
+        zm = fmaxf(zm, __shfl_xor(zm, 32, 64));
+        const float mn = fmaxf(m, ceilf(zm));
+        const float alpha = m == -INFINITY ? 0.f : fast_exp2(m - mn);
+        m = mn;
+        l *= alpha;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) acc[d] *= alpha;
+      }
+      const float off = m == -INFINITY ? 0.f : m;
+      float sum[2] = {0.f, 0.f};
+      u32x4 pf[2][2];                                         // [half of the keys][part]
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4 vs = *reinterpret_cast<const f32x4*>(sc + 32 + 8 * i);
+        float x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          x[j] = fast_exp2(z[4 * i + j] - off);
+          sum[j & 1] += x[j];
+          x[j] *= vs[j];
+          if (!FULL) x[j] = (vis >> (8 * i + j)) & 1u ? x[j] : 0.f;   // (whatever the slot's scale is)
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          uint32_t part[2];
+          split_pair<2>(x[2 * j], x[2 * j + 1], part);
+          pf[i >> 1][0][2 * (i & 1) + j] = part[0];
+          pf[i >> 1][1][2 * (i & 1) + j] = part[1];
+        }
+      }
+      l += sum[0] + sum[1];
+      const char* v = s_tile[buf] + K_TILE + row32 * V_ROW + hi * 16;
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const bf16x8 vf = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(v + 32 * d * V_ROW + 32 * s));
+          acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, pf[s][1]), acc[d], 0, 0, 0);
+          acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, pf[s][0]), acc[d], 0, 0, 0);
+        }
+    };
+
+    if (tiles > 0) {
+      load(0);
+      convert(0, next_mask);
+      mask = next_mask;
+      if (tiles > 1) load(1);
+      __syncthreads();
+    }
+    for (int i = 0; i < tiles; ++i) {
+      const int buf = i & 1, key = (p0 + 2 * i) * HK_PAGE;
+      const uint32_t mk = next_mask;
+      if (i + 1 < tiles) {
+        convert(buf ^ 1, mk);
+        if (i + 2 < tiles) load(i + 2);
+      }
+      if (key < seen_any && w0 < w.rows) {
+        if (mask == 0xffffffffu && key + 32 <= seen_all) compute(buf, key, mask, std::true_type{});
+        else compute(buf, key, mask, std::false_type{});
+      }
+      mask = mk;
+      __syncthreads();
+    }
+
+    l += __shfl_xor(l, 32, 64);
+    if (w0 + row32 < w.rows) {
+      const float inv = l == 0.f ? 0.f : 1.f / l;             // (a NaN stays one)
+      const int64_t at = (int64_t)(w.c.first + tok) * a.Hq + w.kv * a.G + g, part = state + wave * 32 + row32;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int dim = 32 * d + 8 * j + 4 * hi;
+          float x[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) x[k] = acc[d][4 * j + k] * inv * back;
+          if (state >= 0) *reinterpret_cast<f32x4*>(a.part_o + part * D + dim) = f32x4{x[0], x[1], x[2], x[3]};
+          else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.o) + at * D + dim) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+        }
+      if (hi == 0) {
+        if (state >= 0) *reinterpret_cast<f32x2*>(a.part_ml + part * 2) = f32x2{l == 0.f ? -INFINITY : m, l};
+        else if (a.lse) a.lse[at] = lse8(m, l);
+      }
+    }
+  }
+}
+
+}  // namespace hk
+
+using namespace hk;
+
+int64_t hk_attn8_tile_units(int NS, int Hkv, int G, int n_tokens) {
+  return ((int64_t)n_tokens * G / TILE8_ROWS + NS) * Hkv;
+}
+size_t hk_attn8_tile_ws(int D) { return states8_bytes(D, TILE8_ROWS); }
+
+template <int F, int D>
+static void launch_tile(const Args8& a, hipStream_t st) {
+  const uint32_t groups = a.first ? A8_GROUPS<D> : (uint32_t)a.n_units;
+  {
+    TimedLaunch t(HK_TK_ATTN8, st);
+    hipLaunchKernelGGL((attn8_tile_kernel<F, D>), dim3(groups), dim3(A8_NT), 0, st, a);
+  }
+  if (a.first && a.max_pages > A8_STEP) merge8<D, TILE8_ROWS, 2, true>(a, groups, st);
+}
+
+void hk_launch_attn8_tile(Args8 a, hk_dtype format, int D, void* ws, hipStream_t st) {
+  const int64_t units = hk_attn8_tile_units(a.n_seq, a.Hkv, a.G, a.n_tokens);
+  a.n_units = (int)units;
+  a.cap = TILE8_ROWS;
+  a.one_tile = 0;
+  a.rows_from = A8_ROWS + 1;
+  a.rows_to = INT32_MAX;
+  carve8(a, planned8(units, a.max_pages), D, ws);
+  if (format == HK_I8) D == 128 ? launch_tile<HK_I8, 128>(a, st) : launch_tile<HK_I8, 64>(a, st);
+  else D == 128 ? launch_tile<HK_E4M3, 128>(a, st) : launch_tile<HK_E4M3, 64>(a, st);
+}
