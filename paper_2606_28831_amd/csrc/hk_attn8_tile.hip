@@ -9,8 +9,6 @@
 // Per wave and tile, 32x32x16 MFMAs: C[key][row] = K Q^T, then O^T[dim][row] += V^T P^T with P in two
 // bf16 parts, to 2^-16 of a term.  Lane l holds row l % 32 and half hi = l / 32 of the contraction; register
 // r of a score tile is key (r & 3) + 8 (r >> 2) + 4 hi.
-#include <type_traits>
-
 #include "hk_attn8.h"
 
 namespace hk {
@@ -26,17 +24,18 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
   constexpr int K_TILE = 32 * K_ROW, TILE = K_TILE + D * V_ROW;
   __shared__ __align__(16) char s_tile[2][TILE];
   __shared__ __align__(16) float s_scale[2][64];              // K's times c2, V's times 2^-bias
+  __shared__ int s_odd[2];                                    // whether one of V's scales is NaN or infinite
   __shared__ int s_sums[A8_NW];
   const int lane = threadIdx.x & 63, row32 = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool is_v = wave >= 2;
-  // what the thread brings of a tile: K: a quarter of row t / 4; V: dims 4 c .. 4 c + 3 of the eight keys of
-  // group t % 4 (of 16 (g / 2) + 4 (g % 2) + {0 .. 3, 8 .. 11}); D 64: c up to 16, by wave 2 alone
-  const int t = threadIdx.x & 127, grp = t & 3, c = t >> 2;
+  // Waves 0 and 1 bring a page of K each, 2 and 3 one of V.  A thread has of K a quarter of row lane / 4, of V
+  // dims 4 c .. 4 c + 3 of the eight keys 4 (lane % 2) + {0 .. 3, 8 .. 11}, c = lane / 2 (D 64: c below 16).
+  const int my = wave & 1, part4 = lane & 3, c = lane >> 1;
   const bool brings = !is_v || c < D / 4;
-  const int page_of = is_v ? grp >> 1 : t >> 6;
-  const int from = is_v ? (grp & 1) * 4 * D + 4 * c : (c & 15) * D + grp * (D / 4);
-  const int to = is_v ? 4 * c * V_ROW + grp * 16 : c * K_ROW + grp * (D / 2);
+  const uint32_t from = is_v ? (lane & 1) * 4 * D + 4 * c : (lane >> 2) * D + part4 * (D / 4);
+  const int to = is_v ? K_TILE + 4 * c * V_ROW + (2 * my + (lane & 1)) * 16
+                      : (16 * my + (lane >> 2)) * K_ROW + part4 * (D / 2);
 
   int u = a.n_units - 1 - (int)blockIdx.x, skip = 0, left = 1 << 30;
   if (a.first) {
@@ -84,7 +83,7 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
     }
     const int bias = (int)A8_SLACK + 33 - __clz(max(p1 - p0, 1) * HK_PAGE);
     const float down = __uint_as_float((uint32_t)(127 - bias) << 23), back = __uint_as_float((uint32_t)(127 + bias) << 23);
-    float m = -INFINITY, l = 0.f;
+    float m = -INFINITY, off = 0.f, l = 0.f;                  // off: m, or 0 while there is none
     f32x16 acc[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -106,15 +105,15 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
       const int e = 2 * (i & 31);
       const int id0 = __builtin_amdgcn_readlane(ids, e), id1 = __builtin_amdgcn_readlane(ids, e + 1);
       next_mask = (uint32_t)__builtin_amdgcn_readlane(masks, e) | (uint32_t)__builtin_amdgcn_readlane(masks, e + 1) << 16;
-      const size_t at = (size_t)(uint32_t)(page_of ? id1 : id0) * (HK_PAGE * D) + from;
+      const char* page = (is_v ? a.v_pool : a.k_pool) + (size_t)(uint32_t)(my ? id1 : id0) * (HK_PAGE * D);
       if (!is_v) {
 #pragma unroll
         for (int k = 0; k < KW / 4; ++k)
-          *reinterpret_cast<u32x4*>(&code[4 * k]) = *reinterpret_cast<const u32x4*>(a.k_pool + at + 16 * k);
+          *reinterpret_cast<u32x4*>(&code[4 * k]) = *reinterpret_cast<const u32x4*>(page + from + 16 * k);
       } else if (brings) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          code[j] = *reinterpret_cast<const uint32_t*>(a.v_pool + at + (8 * (j >> 2) + (j & 3)) * D);
+          code[j] = *reinterpret_cast<const uint32_t*>(page + from + (8 * (j >> 2) + (j & 3)) * D);
       }
       if (wave == 0) {
         const int id = (lane >> 4) & 1 ? id1 : id0;
@@ -132,11 +131,11 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
       } else if (brings) {
         if (F == HK_E4M3 && mk != 0xffffffffu) {
           // a slot that is not valid may hold codes that stand for NaN
-          const uint32_t bits = mk >> (16 * (grp >> 1) + 4 * (grp & 1));
+          const uint32_t bits = mk >> (16 * my + 4 * (lane & 1));
 #pragma unroll
           for (int j = 0; j < 8; ++j) code[j] = (bits >> (8 * (j >> 2) + (j & 3))) & 1u ? code[j] : 0u;
         }
-        char* at = s_tile[buf] + K_TILE + to;
+        char* at = s_tile[buf] + to;
         u32x4 x[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -158,10 +157,13 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
 #pragma unroll
         for (int d = 0; d < 4; ++d) *reinterpret_cast<u32x4*>(at + d * V_ROW) = x[d];
       }
-      if (wave == 0) s_scale[buf][lane] = scale * (lane >> 5 ? down : a.c2);
+      if (wave == 0) {
+        s_scale[buf][lane] = scale * (lane >> 5 ? down : a.c2);
+        const bool odd = __any(lane >= 32 && !(fabsf(scale) < INFINITY));
+        if (lane == 0) s_odd[buf] = odd;
+      }
     };
-    auto compute = [&](int buf, int key, uint32_t valid, auto is_full) {
-      constexpr bool FULL = decltype(is_full)::value;
+    auto compute = [&](int buf, int key, uint32_t valid, bool full) {
       f32x16 z = {};
       const char* k = s_tile[buf] + row32 * K_ROW + hi * 16;
 #pragma unroll
@@ -169,55 +171,61 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
         z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(k + 32 * s)),
                                                     qf[s], z, 0, 0, 0);
       const float* sc = s_scale[buf] + 4 * hi;
-      uint32_t vis = 0xffffffffu;
-      if (!FULL) {
-        const int n = seen - key;
-        vis = (valid & (n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u)) >> (4 * hi);
-      }
-      float zm = -INFINITY;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const f32x4 ks = *reinterpret_cast<const f32x4*>(sc + 8 * i);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float x = z[4 * i + j] * ks[j];
-          if (!FULL) x = (vis >> (8 * i + j)) & 1u ? x : -INFINITY;
-          z[4 * i + j] = x;
-          zm = fmaxf(zm, x);
-        }
+        for (int j = 0; j < 4; ++j) z[4 * i + j] *= ks[j];
       }
-      if (__any(zm > m + A8_SLACK)) {
+      const int n = seen - key;
+      uint32_t vis = (valid & (n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u)) >> (4 * hi);
+      if (!full) {
+        asm volatile("" : "+v"(vis));         // (a branch, not selects in every tile)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) z[e] = (vis >> ((e & 3) + 8 * (e >> 2))) & 1u ? z[e] : -INFINITY;
+      }
+      float zm = z[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) zm = fmaxf(zm, z[e]);
+      if (__builtin_expect(__any(zm > m + A8_SLACK), 0)) {
         zm = fmaxf(zm, __shfl_xor(zm, 32, 64));
         const float mn = fmaxf(m, ceilf(zm));
         const float alpha = m == -INFINITY ? 0.f : fast_exp2(m - mn);
         m = mn;
+        off = mn == -INFINITY ? 0.f : mn;
         l *= alpha;
 #pragma unroll
-        for (int d = 0; d < DT; ++d) acc[d] *= alpha;
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[d][e] *= alpha;
       }
-      const float off = m == -INFINITY ? 0.f : m;
       float sum[2] = {0.f, 0.f};
-      u32x4 pf[2][2];                                         // [half of the keys][part]
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        z[e] = fast_exp2(z[e] - off);
+        sum[e & 1] += z[e];
+      }
+      l += sum[0] + sum[1];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const f32x4 vs = *reinterpret_cast<const f32x4*>(sc + 32 + 8 * i);
-        float x[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          x[j] = fast_exp2(z[4 * i + j] - off);
-          sum[j & 1] += x[j];
-          x[j] *= vs[j];
-          if (!FULL) x[j] = (vis >> (8 * i + j)) & 1u ? x[j] : 0.f;   // (whatever the slot's scale is)
-        }
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          uint32_t part[2];
-          split_pair<2>(x[2 * j], x[2 * j + 1], part);
-          pf[i >> 1][0][2 * (i & 1) + j] = part[0];
-          pf[i >> 1][1][2 * (i & 1) + j] = part[1];
-        }
+        for (int j = 0; j < 4; ++j) z[4 * i + j] *= vs[j];
       }
-      l += sum[0] + sum[1];
+      if (!full && s_odd[buf]) {
+        // a probability of 0 times a scale of NaN, or of a slot that holds anything
+        asm volatile("" : "+v"(vis));
+#pragma unroll
+        for (int e = 0; e < 16; ++e) z[e] = (vis >> ((e & 3) + 8 * (e >> 2))) & 1u ? z[e] : 0.f;
+      }
+      u32x4 pf[2][2];                                         // [half of the keys][part]
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        uint32_t part[2];
+        split_pair<2>(z[2 * e], z[2 * e + 1], part);
+        pf[e >> 2][0][e & 3] = part[0];
+        pf[e >> 2][1][e & 3] = part[1];
+      }
       const char* v = s_tile[buf] + K_TILE + row32 * V_ROW + hi * 16;
 #pragma unroll
       for (int s = 0; s < 2; ++s)
@@ -244,8 +252,7 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
         if (i + 2 < tiles) load(i + 2);
       }
       if (key < seen_any && w0 < w.rows) {
-        if (mask == 0xffffffffu && key + 32 <= seen_all) compute(buf, key, mask, std::true_type{});
-        else compute(buf, key, mask, std::false_type{});
+        compute(buf, key, mask, mask == 0xffffffffu && key + 32 <= seen_all);
       }
       mask = mk;
       __syncthreads();
