@@ -142,6 +142,13 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_kernel(Args8 a) {
       }
     }
   }
+  // (waited for here, or every block's first product would wait for all loads, those of the blocks to come too)
+#pragma unroll
+  for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+    for (int i = 0; i < QP; ++i)
+#pragma unroll
+      for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qf[nq][i][s]));
   const int seen_all = w.off + w.r0 / a.G;    // by every row of the workgroup
   const int bias = (int)A8_SLACK + 33 - __clz(max(p1 - p0, 1) * HK_PAGE);
   const float down = __uint_as_float((uint32_t)(127 - bias) << 23), back = __uint_as_float((uint32_t)(127 + bias) << 23);

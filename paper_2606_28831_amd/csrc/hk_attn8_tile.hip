@@ -80,6 +80,9 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
       const uint16_t* q = static_cast<const uint16_t*>(a.q) + (int64_t)(w.c.first + tok) * a.q_row + (w.kv * a.G + g) * D;
 #pragma unroll
       for (int s = 0; s < KS; ++s) qf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(q + 16 * s + 8 * hi));
+      // (waited for here, or every tile's first product would wait for all loads, those of the tiles to come too)
+#pragma unroll
+      for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qf[s]));
     }
     const int bias = (int)A8_SLACK + 33 - __clz(max(p1 - p0, 1) * HK_PAGE);
     const float down = __uint_as_float((uint32_t)(127 - bias) << 23), back = __uint_as_float((uint32_t)(127 + bias) << 23);
