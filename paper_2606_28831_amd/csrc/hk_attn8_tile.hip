@@ -6,9 +6,16 @@
 // have, so that both kinds of fragment are 16 bytes in a row.  While tile t is computed, t + 1 is converted
 // into the other buffer and t + 2 is on its way into registers.
 //
-// Per wave and tile, 32x32x16 MFMAs: C[key][row] = K Q^T, then O^T[dim][row] += V^T P^T with P in two
-// bf16 parts, to 2^-16 of a term.  Lane l holds row l % 32 and half hi = l / 32 of the contraction; register
-// r of a score tile is key (r & 3) + 8 (r >> 2) + 4 hi.
+// Per wave and tile, 32x32x16 MFMAs: C[key][row] = K Q^T in bf16, then O^T[dim][row] += V^T P^T in fp16,
+// which holds V's codes exactly and P to 2^-11 of a term.  Lane l holds row l % 32 and half hi = l / 32 of the
+// contraction; register r of a score tile is key (r & 3) + 8 (r >> 2) + 4 hi.
+//
+// For P to be in fp16's range whatever V's scales are, the reference m follows what enters the product: with
+// V's scale s = f 2^e, f in [1/2, 1), and y = x + e, P = exp2(y - m) f 2^10 is at most 2^14, and smaller terms
+// keep their bits down to 2^-24 of the largest.  The softmax's sum takes exp2(y - m) 2^-e.  e is counted
+// from that of the unit's first keys, so that y is about x; of scales below 2^-90 it counts as 0 (their V is
+// below 2^-81, next to nothing).  Between bf16 in two parts, 24 products a tile, and this, 16: 8 prompts of
+// 4096 tokens 1930 us and 1673.
 #include "hk_attn8.h"
 
 namespace hk {
@@ -23,8 +30,9 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
   constexpr int KW = D / 16;                                  // words of codes of a thread that brings K
   constexpr int K_TILE = 32 * K_ROW, TILE = K_TILE + D * V_ROW;
   __shared__ __align__(16) char s_tile[2][TILE];
-  __shared__ __align__(16) float s_scale[2][64];              // K's times c2, V's times 2^-bias
-  __shared__ int s_odd[2];                                    // whether one of V's scales is NaN or infinite
+  __shared__ __align__(16) float s_scale[2][4][32];           // K's scales times c2; V's: e, f 2^10, 2^-e
+  __shared__ int s_base;                                      // what e is counted from
+  __shared__ int s_odd[2];                                    // whether an f is NaN or infinite
   __shared__ int s_sums[A8_NW];
   const int lane = threadIdx.x & 63, row32 = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -84,8 +92,6 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
 #pragma unroll
       for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qf[s]));
     }
-    const int bias = (int)A8_SLACK + 33 - __clz(max(p1 - p0, 1) * HK_PAGE);
-    const float down = __uint_as_float((uint32_t)(127 - bias) << 23), back = __uint_as_float((uint32_t)(127 + bias) << 23);
     float m = -INFINITY, off = 0.f, l = 0.f;                  // off: m, or 0 while there is none
     f32x16 acc[DT];
 #pragma unroll
@@ -98,6 +104,7 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
     int ids = 0, masks = 0;
     uint32_t code[8];                                         // K: KW words; V: word of eight keys
     float scale = 0.f;
+    int base = 0;
     uint32_t mask = 0, next_mask = 0;                         // of the tile computed, and of the one converted
     auto load = [&](int i) {                                  // (past the last tile: its pages again)
       if ((i & 31) == 0) {
@@ -142,27 +149,25 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
         u32x4 x[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const uint32_t p = code[2 * k], q = code[2 * k + 1];
-          if constexpr (F == HK_I8) {
-            x[0][k] = high_halves(Code<F>::template value<0>(p), Code<F>::template value<0>(q));
-            x[1][k] = high_halves(Code<F>::template value<1>(p), Code<F>::template value<1>(q));
-            x[2][k] = high_halves(Code<F>::template value<2>(p), Code<F>::template value<2>(q));
-            x[3][k] = high_halves(Code<F>::template value<3>(p), Code<F>::template value<3>(q));
-          } else {
-            const uint32_t p0 = Code<F>::template pair<0>(p), q0 = Code<F>::template pair<0>(q);
-            const uint32_t p1 = Code<F>::template pair<1>(p), q1 = Code<F>::template pair<1>(q);
-            x[0][k] = __builtin_amdgcn_perm(q0, p0, 0x05040100u);
-            x[1][k] = __builtin_amdgcn_perm(q0, p0, 0x07060302u);
-            x[2][k] = __builtin_amdgcn_perm(q1, p1, 0x05040100u);
-            x[3][k] = __builtin_amdgcn_perm(q1, p1, 0x07060302u);
-          }
+          x[0][k] = Code<F>::template halves<0>(code[2 * k], code[2 * k + 1]);
+          x[1][k] = Code<F>::template halves<1>(code[2 * k], code[2 * k + 1]);
+          x[2][k] = Code<F>::template halves<2>(code[2 * k], code[2 * k + 1]);
+          x[3][k] = Code<F>::template halves<3>(code[2 * k], code[2 * k + 1]);
         }
 #pragma unroll
         for (int d = 0; d < 4; ++d) *reinterpret_cast<u32x4*>(at + d * V_ROW) = x[d];
       }
       if (wave == 0) {
-        s_scale[buf][lane] = scale * (lane >> 5 ? down : a.c2);
-        const bool odd = __any(lane >= 32 && !(fabsf(scale) < INFINITY));
+        const int top = __builtin_amdgcn_frexp_expf(scale), e = top < -90 ? 0 : min(max(top - base, -126), 126);
+        const float f = __builtin_amdgcn_ldexpf(scale, 10 - (e + base));
+        if (lane < 32) {
+          s_scale[buf][0][lane] = scale * a.c2;
+        } else {
+          s_scale[buf][1][lane - 32] = (float)e;
+          s_scale[buf][2][lane - 32] = f;
+          s_scale[buf][3][lane - 32] = __builtin_amdgcn_ldexpf(1.f, -e);
+        }
+        const bool odd = __any(lane >= 32 && !(fabsf(f) < INFINITY));
         if (lane == 0) s_odd[buf] = odd;
       }
     };
@@ -173,12 +178,12 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
       for (int s = 0; s < KS; ++s)
         z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(k + 32 * s)),
                                                     qf[s], z, 0, 0, 0);
-      const float* sc = s_scale[buf] + 4 * hi;
+      const float* sc = s_scale[buf][0] + 4 * hi;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const f32x4 ks = *reinterpret_cast<const f32x4*>(sc + 8 * i);
+        const f32x4 ks = *reinterpret_cast<const f32x4*>(sc + 8 * i), ev = *reinterpret_cast<const f32x4*>(sc + 32 + 8 * i);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) z[4 * i + j] *= ks[j];
+        for (int j = 0; j < 4; ++j) z[4 * i + j] = fmaf(z[4 * i + j], ks[j], ev[j]);
       }
       const int n = seen - key;
       uint32_t vis = (valid & (n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u)) >> (4 * hi);
@@ -204,48 +209,49 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
       }
       float sum[2] = {0.f, 0.f};
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        z[e] = fast_exp2(z[e] - off);
-        sum[e & 1] += z[e];
+      for (int i = 0; i < 4; ++i) {
+        const f32x4 f = *reinterpret_cast<const f32x4*>(sc + 64 + 8 * i), up = *reinterpret_cast<const f32x4*>(sc + 96 + 8 * i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float p = fast_exp2(z[4 * i + j] - off);
+          sum[j & 1] = fmaf(p, up[j], sum[j & 1]);
+          z[4 * i + j] = p * f[j];
+        }
       }
       l += sum[0] + sum[1];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const f32x4 vs = *reinterpret_cast<const f32x4*>(sc + 32 + 8 * i);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) z[4 * i + j] *= vs[j];
-      }
       if (!full && s_odd[buf]) {
         // a probability of 0 times a scale of NaN, or of a slot that holds anything
         asm volatile("" : "+v"(vis));
 #pragma unroll
         for (int e = 0; e < 16; ++e) z[e] = (vis >> ((e & 3) + 8 * (e >> 2))) & 1u ? z[e] : 0.f;
       }
-      u32x4 pf[2][2];                                         // [half of the keys][part]
+      u32x4 pf[2];                                            // halves of the keys
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        uint32_t part[2];
-        split_pair<2>(z[2 * e], z[2 * e + 1], part);
-        pf[e >> 2][0][e & 3] = part[0];
-        pf[e >> 2][1][e & 3] = part[1];
-      }
+      for (int e = 0; e < 8; ++e)
+        pf[e >> 2][e & 3] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{z[2 * e], z[2 * e + 1]}), f16x2));
       const char* v = s_tile[buf] + K_TILE + row32 * V_ROW + hi * 16;
 #pragma unroll
       for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          const bf16x8 vf = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(v + 32 * d * V_ROW + 32 * s));
-          acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, pf[s][1]), acc[d], 0, 0, 0);
-          acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, pf[s][0]), acc[d], 0, 0, 0);
+          const f16x8 vf = __builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4*>(v + 32 * d * V_ROW + 32 * s));
+          acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, __builtin_bit_cast(f16x8, pf[s]), acc[d], 0, 0, 0);
         }
     };
 
     if (tiles > 0) {
       load(0);
+      if (wave == 0) {
+        const int e = lane >= 32 && (next_mask >> (lane - 32)) & 1u ? __builtin_amdgcn_frexp_expf(scale) : -1000;
+        base = (int)wave_max((float)e);
+        if (base < -90) base = 0;
+        if (lane == 0) s_base = base;
+      }
       convert(0, next_mask);
       mask = next_mask;
       if (tiles > 1) load(1);
       __syncthreads();
+      base = s_base;
     }
     for (int i = 0; i < tiles; ++i) {
       const int buf = i & 1, key = (p0 + 2 * i) * HK_PAGE;
@@ -263,6 +269,10 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
 
     l += __shfl_xor(l, 32, 64);
     if (w0 + row32 < w.rows) {
+      // l is brought to [1/2, 1): scales far apart leave sums far apart
+      const int up = __builtin_amdgcn_frexp_expf(l), down = base + Code<F>::F16_DOWN - 10 - up;
+      l = __builtin_amdgcn_frexp_mantf(l);
+      m += (float)up;
       const float inv = l == 0.f ? 0.f : 1.f / l;             // (a NaN stays one)
       const int64_t at = (int64_t)(w.c.first + tok) * a.Hq + w.kv * a.G + g, part = state + wave * 32 + row32;
 #pragma unroll
@@ -272,7 +282,7 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
           const int dim = 32 * d + 8 * j + 4 * hi;
           float x[4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) x[k] = acc[d][4 * j + k] * inv * back;
+          for (int k = 0; k < 4; ++k) x[k] = __builtin_amdgcn_ldexpf(acc[d][4 * j + k] * inv, down);
           if (state >= 0) *reinterpret_cast<f32x4*>(a.part_o + part * D + dim) = f32x4{x[0], x[1], x[2], x[3]};
           else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.o) + at * D + dim) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
         }

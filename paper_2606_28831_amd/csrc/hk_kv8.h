@@ -8,12 +8,14 @@ namespace hk {
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 // A row x of D values is held as D codes and one fp32 scale:
 //   a = max(max |x|, LEAST),  scale = a / MOST,  code = round(x (MOST / a)),
 // every step rounded to fp32, codes to the nearest with ties to even; a row with an infinite value
 // or NaN has codes 0 and the scale NaN.  Below LEAST the steps stay those of LEAST: neither quotient
-// leaves the normal numbers.  Both kinds of code are exact in bf16.
+// leaves the normal numbers.  Both kinds of code are exact in bf16 and in fp16.
 constexpr float KV8_LEAST = 0x1p-100f;
 template <int F>
 struct Code;
@@ -34,6 +36,15 @@ struct Code<HK_I8> {
   __device__ static __forceinline__ uint32_t pair(uint32_t w) {
     return __builtin_amdgcn_perm(__float_as_uint(value<2 * I + 1>(w)), __float_as_uint(value<2 * I>(w)), 0x07060302u);
   }
+  // Codes I of a and of b as two fp16 times 2^-F16_DOWN.  A byte c + 128 alone in a half is the subnormal
+  // (c + 128) 2^-24, so that one fma a pair brings codes to c 2^-9, exactly.
+  static constexpr int F16_DOWN = 9;
+  template <int I>
+  __device__ static __forceinline__ uint32_t halves(uint32_t a, uint32_t b) {
+    const uint32_t x = __builtin_amdgcn_perm(b ^ 0x80808080u, a ^ 0x80808080u, 0x0c040c00u + 0x00010001u * I);
+    const f16x2 up = {(_Float16)32768.f, (_Float16)32768.f}, less = {(_Float16)-0.25f, (_Float16)-0.25f};
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(f16x2, x), up, less));
+  }
 };
 template <>
 struct Code<HK_E4M3> {
@@ -51,6 +62,13 @@ struct Code<HK_E4M3> {
   template <int I>
   __device__ static __forceinline__ uint32_t pair(uint32_t w) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, I != 0));
+  }
+  static constexpr int F16_DOWN = 0;
+  template <int I>
+  __device__ static __forceinline__ uint32_t halves(uint32_t a, uint32_t b) {
+    const uint32_t x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, I >= 2));
+    const uint32_t y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, I >= 2));
+    return __builtin_amdgcn_perm(y, x, I & 1 ? 0x07060302u : 0x05040100u);
   }
 };
 

@@ -101,18 +101,24 @@ def _bound(dtype, parts, n_keys, lse, zabs, absv, o, D):
                dz = (1.01 D + 8) 2^-23 max sum |q k|;
       sums     probabilities off by 2 dz each and a few steps of the exponential, the running sum's n
                additions over 64 lanes at least, the states' joins: (n / 32 + 64) 2^-23;
-      parts    P enters the product with V rounded: to bf16 once (1: 2^-8 of every term), in two bf16
+      parts    P enters the product with V rounded: to fp16 once (1: 2^-11 of every term), in two bf16
                parts (2: 2^-16) or in three (3: 2^-23);
       dtype    of o: half a step, bf16 2^-8, fp32 2^-24;
       floor    p scale 2^-bias and its parts count as 0 below 2^-126: at most three such losses a term,
                each of 2^(bias - 126) times the code (448 at most), beside a largest p of at least a half,
-               with bias at most 6 + log2 of the keys (the slack of 4 and two roundings up)."""
+               with bias at most 6 + log2 of the keys (the slack of 4 and two roundings up).  fp16 (1) has
+               the step 2^-24 for small P: a term is off by 2^-25 at most, where the row's largest P is
+               at least 2^8 (2^10, times a reference's rounding up, times a scale's fraction, a half each),
+               which stands for no more than the largest p |v| of the row, and so of its sum p |v|:
+               2^-33 of that a key."""
     dz = (1.01 * D + 8) * 2.0 ** -23 * zabs
     rest = (n_keys / 32 + 64) * 2.0 ** -23
     half = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
-    p = {1: 2.0 ** -8, 2: 2.0 ** -16, 3: 2.0 ** -23}[parts]
+    p = {1: 2.0 ** -11, 2: 2.0 ** -16, 3: 2.0 ** -23}[parts]
     bo = half * np.abs(o) * 1.01 + (p + 2 * dz[..., None] + 2 * rest) * 1.05 * absv
     bo += 6 * n_keys * 448 * 2.0 ** (6 + math.log2(max(n_keys, 16)) - 126)
+    if parts == 1:
+        bo += n_keys * 2.0 ** -33 * absv.max(-1, keepdims=True)
     return bo, dz + rest + 2.0 ** -22 * np.maximum(1.0, np.abs(np.where(np.isfinite(lse), lse, 0.0)))
 
 
