@@ -589,20 +589,23 @@ def _run(name: str, t, tensors, stream, *args):
     for x in tensors:
         if x is not None and x.get_device() != dev:
             raise HardKVError(f"{name}: tensors on different devices")
-    here = torch.cuda.current_device()
+    # (a tensor is on the GPU, so that torch's own wrappers have nothing left to set up: the raw device and
+    # stream are a microsecond faster)
+    here = torch._C._cuda_getDevice()
     if dev != here:
         with torch.cuda.device(t.device):
             _check(getattr(lib(), name)(*args, _stream(stream)), name)
         return
-    # (the raw handle: torch's stream object takes longer than a launch)
     raw = torch._C._cuda_getCurrentRawStream(here) if stream is None else stream.cuda_stream
-    _check(getattr(lib(), name)(*args, C.c_void_p(raw)), name)
+    code = getattr(_lib or lib(), name)(*args, raw)
+    if code:
+        _check(code, name)
 
 
 def _vector(t, n: int, dtype, what: str):
     if t.dtype != dtype or not t.is_contiguous() or t.numel() < n:
         raise HardKVError(f"{what} must be a contiguous {dtype} tensor of at least {n} entries")
-    return C.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _token_rows(t, n_tokens: int, heads: int, D: int, dtype, what: str):
@@ -613,7 +616,7 @@ def _token_rows(t, n_tokens: int, heads: int, D: int, dtype, what: str):
         raise HardKVError(f"{what} must be [tokens, {heads}, {D}] in {dtype}")
     if stride[-1] != 1 or (heads > 1 and stride[-2] != D):
         raise HardKVError(f"{what}: the heads of a token must be contiguous")
-    return C.c_void_p(t.data_ptr()), stride[-3] if n_tokens > 1 else max(stride[-3], heads * D)
+    return t.data_ptr(), stride[-3] if n_tokens > 1 else max(stride[-3], heads * D)
 
 
 def hk_reserve_slots(d: hk_dims, kv: PagedKV, chunks: Chunks, alloc: Allocator, ws, slot_map=None,
@@ -715,16 +718,21 @@ def _row_dtype(t, what: str) -> int:
 
 
 def _rows8(name, d, kv, n_tokens, slot_map, k, v, stream):
-    _need(k.dim() in (3, 4) and (v is None or v.dim() == k.dim()), "rows must be 3- or 4-d")
+    nd, dtype, Hkv, D = k.dim(), k.dtype, d.Hkv, d.D
+    _need(nd in (3, 4) and (v is None or v.dim() == nd), "rows must be 3- or 4-d")
     _fits(d, _kv8(kv), 0)
-    layers = k.shape[0] if k.dim() == 4 else 1
-    _need(v is None or v.dim() == 3 or v.shape[0] == layers, "K and V differ in layers")
+    layers, kl, vl, vp, vr = 1, 0, 0, None, 0
     dt = _row_dtype(k, "rows")
-    kp, kr = _token_rows(k, n_tokens, d.Hkv, d.D, k.dtype, "K rows")
-    vp, vr = (None, 0) if v is None else _token_rows(v, n_tokens, d.Hkv, d.D, k.dtype, "V rows")
-    _run(name, kv.k_pool, (slot_map, k, v), stream, C.byref(d), C.byref(kv.desc8), layers, int(n_tokens),
-         _vector(slot_map, layers * n_tokens * d.Hkv, torch.int64, "slot_map"), dt, kp,
-         k.stride(0) if layers > 1 else 0, kr, vp, v.stride(0) if v is not None and layers > 1 else 0, vr)
+    kp, kr = _token_rows(k, n_tokens, Hkv, D, dtype, "K rows")
+    if v is not None:
+        vp, vr = _token_rows(v, n_tokens, Hkv, D, dtype, "V rows")
+    if nd == 4:
+        layers = k.shape[0]
+        _need(v is None or v.shape[0] == layers, "K and V differ in layers")
+        if layers > 1:
+            kl, vl = k.stride(0), 0 if v is None else v.stride(0)
+    _run(name, kv.k_pool, (slot_map, k, v), stream, d, kv.desc8, layers, n_tokens,
+         _vector(slot_map, layers * n_tokens * Hkv, torch.int64, "slot_map"), dt, kp, kl, kr, vp, vl, vr)
 
 
 def hk_write_kv8(d: hk_dims, kv: PagedKV8, n_tokens: int, slot_map, k_new, v_new, stream=None):
@@ -742,8 +750,8 @@ def hk_decode_attn8(d: hk_dims, q, kv: PagedKV8, sm_scale: float, o, lse, ws, st
     """q [NS, Hq, D] in float32 or bfloat16, o [NS, Hq, D] and lse [NS, Hq] (or None) in float32."""
     _fits(d, _kv8(kv), d.NS * d.Hkv)
     n = d.NS * d.Hq
-    _run("hk_decode_attn8", kv.k_pool, (q, o, lse, ws), stream, C.byref(d), _row_dtype(q, "q"),
-         _vector(q, n * d.D, q.dtype, "q"), C.byref(kv.desc8), float(sm_scale),
+    _run("hk_decode_attn8", kv.k_pool, (q, o, lse, ws), stream, d, _row_dtype(q, "q"),
+         _vector(q, n * d.D, q.dtype, "q"), kv.desc8, float(sm_scale),
          _vector(o, n * d.D, torch.float32, "o"), None if lse is None else _vector(lse, n, torch.float32, "lse"),
          _ptr(ws), ws.numel())
 
@@ -764,8 +772,8 @@ def hk_chunk_attn8(d: hk_dims, kv: PagedKV8, chunks: Chunks, q, sm_scale: float,
     dt = _row_dtype(q, "q")
     qp, qr = _token_rows(q, T, d.Hq, d.D, q.dtype, "q")
     _need(q.dim() == 3, "q must be 3-d")
-    _run("hk_chunk_attn8", kv.k_pool, (chunks.start, q, o, lse, ws), stream, C.byref(d), C.byref(kv.desc8),
-         C.byref(chunks.desc), dt, qp, qr, float(sm_scale), _vector(o, T * d.Hq * d.D, q.dtype, "o"),
+    _run("hk_chunk_attn8", kv.k_pool, (chunks.start, q, o, lse, ws), stream, d, kv.desc8,
+         chunks.desc, dt, qp, qr, float(sm_scale), _vector(o, T * d.Hq * d.D, q.dtype, "o"),
          None if lse is None else _vector(lse, T * d.Hq, torch.float32, "lse"), _ptr(ws), ws.numel())
 
 
@@ -774,9 +782,9 @@ def hk_compact8(d: hk_dims, kv: PagedKV8, sel_bits, L_dense: int, L_sparse: int,
     """hk_compact of an 8-bit cache, or with head_mode hk_compact_modes."""
     H = d.NS * d.Hkv
     _fits(d, _kv8(kv), H, alloc)
-    _run("hk_compact8", kv.k_pool, (sel_bits, head_mode, status, ws), stream, C.byref(d), C.byref(kv.desc8),
+    _run("hk_compact8", kv.k_pool, (sel_bits, head_mode, status, ws), stream, d, kv.desc8,
          _vector(sel_bits, H * (kv.max_pages // 2), torch.int32, "sel_bits"), int(L_dense), int(L_sparse),
-         None if head_mode is None else _vector(head_mode, H, torch.int32, "head_mode"), C.byref(alloc.desc),
+         None if head_mode is None else _vector(head_mode, H, torch.int32, "head_mode"), alloc.desc,
          _status(status), _ptr(ws), ws.numel())
 
 
