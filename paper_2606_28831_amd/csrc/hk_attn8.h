@@ -89,6 +89,19 @@ __device__ __forceinline__ int steps_of(const Unit& w) {
 __device__ __forceinline__ int run_of(int b, int n, int total) { return (int)((int64_t)total * b / n); }
 __device__ __forceinline__ int group_of(int x, int n, int total) { return (int)(((int64_t)(x + 1) * n - 1) / total); }
 
+// Of up to 64 units whose steps lane i holds for unit i: those before it, and the total.
+__device__ __forceinline__ int scan_units(int steps, int* before) {
+  const int lane = threadIdx.x & 63;
+  int x = steps;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o, 64);
+    if (lane >= o) x += y;
+  }
+  *before = x - steps;
+  return __builtin_amdgcn_readlane(x, 63);
+}
+
 // Steps before every unit into first (LDS), the total at first[n_units]; the last workgroup leaves them
 // for the merge.
 template <int ROWS, bool CHUNK>
@@ -121,6 +134,47 @@ __device__ __forceinline__ void plan_units(const Args8& a, int* first, int* sums
   __syncthreads();
   if (blockIdx.x == gridDim.x - 1)
     for (int u = threadIdx.x; u <= a.n_units; u += A8_NT) a.first[u] = first[u];
+}
+
+// A workgroup's run: its first unit, the steps of it that are another workgroup's, and its own steps (0: none).
+struct Run {
+  int unit, skip, left;
+};
+template <int ROWS, bool CHUNK>
+__device__ __forceinline__ Run run_of_group(const Args8& a, int* first, int* sums) {
+  Run r{0, 0, 0};
+  if (a.n_units <= 64) {
+    // every wave by itself (a launch of few units is short: with the list in LDS it took a microsecond more)
+    const int lane = threadIdx.x & 63;
+    int before;
+    const int total = scan_units(lane < a.n_units ? steps_of(unit_of<ROWS, CHUNK>(a, lane)) : 0, &before);
+    if (blockIdx.x == gridDim.x - 1 && threadIdx.x < 64) {
+      if (lane < a.n_units) a.first[lane] = before;
+      if (lane == 0) a.first[a.n_units] = total;
+    }
+    const int n = min((int)gridDim.x, total);
+    if ((int)blockIdx.x >= n) return r;
+    const int x = run_of(blockIdx.x, n, total);
+    r.left = run_of(blockIdx.x + 1, n, total) - x;
+    r.unit = 63 - __clzll(__ballot(lane < a.n_units && before <= x));
+    r.skip = x - __builtin_amdgcn_readlane(before, r.unit);
+    return r;
+  }
+  plan_units<ROWS, CHUNK>(a, first, sums);
+  const int total = __builtin_amdgcn_readfirstlane(first[a.n_units]), n = min((int)gridDim.x, total);
+  if ((int)blockIdx.x >= n) return r;
+  const int x = run_of(blockIdx.x, n, total);
+  r.left = run_of(blockIdx.x + 1, n, total) - x;
+  int u = 0;                                  // the last unit that begins at or before x
+  for (int hi = a.n_units; hi - u > 1;) {
+    const int mid = (u + hi) / 2;
+    if (first[mid] <= x) u = mid;
+    else hi = mid;
+  }
+  r.unit = __builtin_amdgcn_readfirstlane(u);
+  r.skip = __builtin_amdgcn_readfirstlane(x - first[u]);
+  __syncthreads();                            // (the tiles take first's place)
+  return r;
 }
 
 // log of l 2^m; the powers of two of both cancel as whole numbers
@@ -166,27 +220,34 @@ __global__ __launch_bounds__(A8_NT) void attn8_merge_kernel(Args8 a, int n_group
   const int per = (used + WAVES - 1) / WAVES, i0 = wave % WAVES * per, i1 = min(i0 + per, used);
   const auto state = [&](int i) { return (int64_t)(2 * (b0 + i) + (i == 0)) * a.cap + row; };
   const f32x2* ml = reinterpret_cast<const f32x2*>(a.part_ml);
-  float m = -INFINITY, l = 0.f;
-  for (int i = i0 + lane; i < i1; i += 64) m = fmaxf(m, ml[state(i)][0]);
+  // lane i has the weight of part i of 64; the first 64 (often all) are loaded once
+  const auto load = [&](int i) { return i < i1 ? ml[state(i)] : f32x2{-INFINITY, 0.f}; };
+  const f32x2 mine = load(i0 + lane);
+  float m = mine[0], l = 0.f;
+  for (int i = i0 + 64 + lane; i < i1; i += 64) m = fmaxf(m, load(i)[0]);
   m = wave_max(m);
-  const auto weight = [&](int i) {
-    const f32x2 x = ml[state(i)];
-    return x[0] == -INFINITY ? 0.f : x[1] * fast_exp2(x[0] - m);
-  };
-  for (int i = i0 + lane; i < i1; i += 64) l += weight(i);
+  const auto weight = [&](f32x2 x) { return x[0] == -INFINITY ? 0.f : x[1] * fast_exp2(x[0] - m); };
+  l = weight(mine);
+  for (int i = i0 + 64 + lane; i < i1; i += 64) l += weight(load(i));
   l = wave_sum(l);
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const int side = lane / LPR, at = lane % LPR;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   for (int from = i0; from < i1; from += 64) {
-    const float f = from + lane < i1 ? weight(from + lane) * inv : 0.f;
+    const float f = weight(from == i0 ? mine : load(from + lane)) * inv;
     const int most = min(i1 - from, 64);
-#pragma unroll 4
-    for (int j = 0; j < most; j += SIDE) {
-      const int i = min(j + side, most - 1);
-      const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_o + state(from + i) * D + 4 * at);
-      const float g = __shfl(f, j + side, 64);
-      if (j + side < most) o += g * x;
+    // four at a time on their way
+    for (int j = 0; j < most; j += 4 * SIDE) {
+      f32x4 x[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        x[k] = *reinterpret_cast<const f32x4*>(a.part_o + state(from + min(j + k * SIDE + side, most - 1)) * D + 4 * at);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int i = j + k * SIDE + side;
+        const float g = __shfl(f, i & 63, 64);
+        if (i < most) o += g * x[k];          // (what is past the last one holds anything)
+      }
     }
   }
 #pragma unroll

@@ -87,22 +87,11 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_kernel(Args8 a) {
 
   int u = blockIdx.x, skip = 0, left = 1 << 30;   // unit, its steps that are another's, steps of the run
   if (a.first) {
-    int* first = reinterpret_cast<int*>(s_tiles);
     static_assert(sizeof(s_tiles) >= (A8_UNITS + 1) * sizeof(int));
-    plan_units<ROWS, CHUNK>(a, first, reinterpret_cast<int*>(s_m));
-    const int total = __builtin_amdgcn_readfirstlane(first[a.n_units]), n = min((int)gridDim.x, total);
-    if ((int)blockIdx.x >= n) return;
-    const int x = run_of(blockIdx.x, n, total);
-    left = run_of(blockIdx.x + 1, n, total) - x;
-    u = 0;                                    // the last unit that begins at or before x
-    for (int hi = a.n_units; hi - u > 1;) {
-      const int mid = (u + hi) / 2;
-      if (first[mid] <= x) u = mid;
-      else hi = mid;
-    }
-    u = __builtin_amdgcn_readfirstlane(u);
-    skip = __builtin_amdgcn_readfirstlane(x - first[u]);
-    __syncthreads();                          // (the tiles take first's place)
+    const Run r = run_of_group<ROWS, CHUNK>(a, reinterpret_cast<int*>(s_tiles), reinterpret_cast<int*>(s_m));
+    u = r.unit;
+    skip = r.skip;
+    left = r.left;
   }
   for (; left > 0 && u < a.n_units; ++u) {
   const Unit w = unit_of<ROWS, CHUNK>(a, u);

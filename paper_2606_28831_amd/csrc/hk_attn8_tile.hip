@@ -47,22 +47,11 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
 
   int u = a.n_units - 1 - (int)blockIdx.x, skip = 0, left = 1 << 30;
   if (a.first) {
-    int* first = reinterpret_cast<int*>(s_tile);
     static_assert(sizeof(s_tile) >= (A8_UNITS + 1) * sizeof(int));
-    plan_units<TILE8_ROWS, true>(a, first, s_sums);
-    const int total = __builtin_amdgcn_readfirstlane(first[a.n_units]), n = min((int)gridDim.x, total);
-    if ((int)blockIdx.x >= n) return;
-    const int x = run_of(blockIdx.x, n, total);
-    left = run_of(blockIdx.x + 1, n, total) - x;
-    u = 0;
-    for (int h = a.n_units; h - u > 1;) {
-      const int mid = (u + h) / 2;
-      if (first[mid] <= x) u = mid;
-      else h = mid;
-    }
-    u = __builtin_amdgcn_readfirstlane(u);
-    skip = __builtin_amdgcn_readfirstlane(x - first[u]);
-    __syncthreads();
+    const Run r = run_of_group<TILE8_ROWS, true>(a, reinterpret_cast<int*>(s_tile), s_sums);
+    u = r.unit;
+    skip = r.skip;
+    left = r.left;
   }
   for (; left > 0 && u < a.n_units; ++u) {
     const Unit w = unit_of<TILE8_ROWS, true>(a, u);
