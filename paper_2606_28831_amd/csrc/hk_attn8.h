@@ -183,20 +183,20 @@ __device__ __forceinline__ float lse8(float m, float l) {
   return (m + (float)__builtin_amdgcn_frexp_expf(l) + __log2f(__builtin_amdgcn_frexp_mantf(l))) * kLn2;
 }
 
-// fp32 in N bf16 parts, of two values a word: N 1: exact ones, 2: to 2^-16, 3: all of its bits
+// fp32 in N bf16 parts, of two values a word: N 1: exact ones, 2: to 2^-16, 3: all of its bits but the last.
+// What a part leaves is formed by one dot product a value (with 0 for the other of the word), exactly.
 template <int N>
 __device__ __forceinline__ void split_pair(float x, float y, uint32_t (&out)[N]) {
-  if constexpr (N == 1) {
-    out[0] = pack_bf16(x, y);
-  } else if constexpr (N == 2) {
-    out[0] = pack_bf16(x, y);
-    out[1] = pack_bf16(x - bf16_lo(out[0]), y - bf16_hi(out[0]));
-  } else {
+  uint32_t minus_lo = 0x0000bf80u, minus_hi = 0xbf800000u;      // -1 and 0
+  asm("" : "+s"(minus_lo), "+s"(minus_hi));   // (in registers: as a literal the pair is not what it says)
+  const bf16x2 less_lo = __builtin_bit_cast(bf16x2, minus_lo), less_hi = __builtin_bit_cast(bf16x2, minus_hi);
 #pragma unroll
-    for (int i = 0; i < 3; ++i) {
-      out[i] = high_halves(x, y);
-      x -= bf16_lo(out[i]);
-      y -= bf16_hi(out[i]);
+  for (int i = 0; i < N; ++i) {
+    out[i] = pack_bf16(x, y);
+    if (i + 1 < N) {
+      const bf16x2 part = __builtin_bit_cast(bf16x2, out[i]);
+      x = __builtin_amdgcn_fdot2_f32_bf16(part, less_lo, x, false);
+      y = __builtin_amdgcn_fdot2_f32_bf16(part, less_hi, y, false);
     }
   }
 }

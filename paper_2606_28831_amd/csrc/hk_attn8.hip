@@ -203,7 +203,13 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_kernel(Args8 a) {
     }
     const float* scales = reinterpret_cast<const float*>(b + L::SCALES) + 4 * qd;
     const f32x4 ks[2] = {*reinterpret_cast<const f32x4*>(scales), *reinterpret_cast<const f32x4*>(scales + 16)};
-    const f32x4 vs[2] = {*reinterpret_cast<const f32x4*>(scales + 32), *reinterpret_cast<const f32x4*>(scales + 48)};
+    f32x4 vs[2] = {*reinterpret_cast<const f32x4*>(scales + 32), *reinterpret_cast<const f32x4*>(scales + 48)};
+    if (!full) {
+      uint32_t w = valid;
+      asm volatile("" : "+v"(w));             // (here and below: a branch, not selects in every block)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) vs[i >> 2][i & 3] = (w >> i) & 1u ? vs[i >> 2][i & 3] : 0.f;
+    }
     u32x4 pf[NQ][PP];
 #pragma unroll
     for (int nq = 0; nq < NQ; ++nq) {
@@ -220,9 +226,14 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_kernel(Args8 a) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         x[i] = z[nq][i >> 2][i & 3] * (ks[i >> 2][i & 3] * a.c2);
-        if (!full) x[i] = (vis >> i) & 1u ? x[i] : -INFINITY;
-        zm = fmaxf(zm, x[i]);
       }
+      if (!full) {
+        asm volatile("" : "+v"(vis));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = (vis >> i) & 1u ? x[i] : -INFINITY;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) zm = fmaxf(zm, x[i]);
       if (__any(zm > m[nq] + A8_SLACK)) {
         zm = fmaxf(zm, __shfl_xor(zm, 16, 64));
         zm = fmaxf(zm, __shfl_xor(zm, 32, 64));
@@ -240,7 +251,17 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_kernel(Args8 a) {
         x[i] = fast_exp2(x[i] - off);
         sum[i & 1] += x[i];
         x[i] *= vs[i >> 2][i & 3] * down;
-        if (!full) x[i] = (vis >> i) & 1u ? x[i] : 0.f;         // (whatever the slot's scale is)
+      }
+      if (CHUNK && !full) {
+        // a later token's scale may be NaN, and its product with a probability of 0
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) odd |= x[i] != x[i];
+        if (__any(odd)) {
+          asm volatile("" : "+v"(vis));
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = (vis >> i) & 1u ? x[i] : 0.f;
+        }
       }
       l[nq] += sum[0] + sum[1];
 #pragma unroll
