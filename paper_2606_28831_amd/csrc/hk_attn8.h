@@ -201,91 +201,109 @@ __device__ __forceinline__ void split_pair(float x, float y, uint32_t (&out)[N])
   }
 }
 
-// The states of a cut unit's parts (means of V, references, sums) to the row's: a wave takes a row, or
-// WAVES of them share a row's parts.  D / 4 lanes load a state; a wave has 256 / D of them on their way at once.
-template <int D, int ROWS, int PP, bool CHUNK, int WAVES>
+// The states of a cut unit's parts (means of V, references, sums) to the row's: a wave takes R rows, whose
+// loads are on their way at once, or WAVES of them share a row's parts.  D / 4 lanes load a state; 256 / D of
+// them lie side by side.  512 units, up to 32 rows: a row a wave 10.7 us, four 8.6; 4 rows 5.0 and 5.9.
+template <int D, int ROWS, int PP, bool CHUNK, int WAVES, int R>
 __global__ __launch_bounds__(A8_NT) void attn8_merge_kernel(Args8 a, int n_groups) {
-  constexpr int LPR = D / 4, SIDE = 64 / LPR, PER = A8_NW / WAVES;
+  constexpr int LPR = D / 4, SIDE = 64 / LPR, PER = R * A8_NW / WAVES;
   __shared__ float s_m[A8_NW], s_l[A8_NW];
   __shared__ f32x4 s_o[A8_NW][LPR];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int per_unit = (a.cap + PER - 1) / PER, u = blockIdx.x / per_unit;
-  const int row = (blockIdx.x - u * per_unit) * PER + wave / WAVES;
+  const int row = (blockIdx.x - u * per_unit) * PER + wave / WAVES * R;
   const Unit w = unit_of<ROWS, CHUNK>(a, u);
-  // (the waves of a row leave together)
-  if (w.rows == 0 || row >= a.cap || w.r0 + row >= w.rows) return;
+  const int rows = min(min(a.cap, w.rows - w.r0) - row, R);      // of the wave
+  if (w.rows == 0 || rows <= 0) return;       // (the waves of a row leave together)
   const int total = a.first[a.n_units], x0 = a.first[u], x1 = a.first[u + 1];
   const int n = min(n_groups, total), b0 = group_of(x0, n, total), used = group_of(x1 - 1, n, total) - b0 + 1;
   if (used < 2) return;                       // not cut
   const int per = (used + WAVES - 1) / WAVES, i0 = wave % WAVES * per, i1 = min(i0 + per, used);
-  const auto state = [&](int i) { return (int64_t)(2 * (b0 + i) + (i == 0)) * a.cap + row; };
+  const auto state = [&](int i, int k) { return (int64_t)(2 * (b0 + i) + (i == 0)) * a.cap + row + min(k, rows - 1); };
   const f32x2* ml = reinterpret_cast<const f32x2*>(a.part_ml);
   // lane i has the weight of part i of 64; the first 64 (often all) are loaded once
-  const auto load = [&](int i) { return i < i1 ? ml[state(i)] : f32x2{-INFINITY, 0.f}; };
-  const f32x2 mine = load(i0 + lane);
-  float m = mine[0], l = 0.f;
-  for (int i = i0 + 64 + lane; i < i1; i += 64) m = fmaxf(m, load(i)[0]);
-  m = wave_max(m);
-  const auto weight = [&](f32x2 x) { return x[0] == -INFINITY ? 0.f : x[1] * fast_exp2(x[0] - m); };
-  l = weight(mine);
-  for (int i = i0 + 64 + lane; i < i1; i += 64) l += weight(load(i));
-  l = wave_sum(l);
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const auto load = [&](int i, int k) { return i < i1 ? ml[state(i, k)] : f32x2{-INFINITY, 0.f}; };
+  f32x2 mine[R];
+  float m[R], l[R];
+  f32x4 o[R];
+#pragma unroll
+  for (int k = 0; k < R; ++k) mine[k] = load(i0 + lane, k);
+  const auto weight = [&](f32x2 x, int k) { return x[0] == -INFINITY ? 0.f : x[1] * fast_exp2(x[0] - m[k]); };
+#pragma unroll
+  for (int k = 0; k < R; ++k) {
+    m[k] = mine[k][0];
+    for (int i = i0 + 64 + lane; i < i1; i += 64) m[k] = fmaxf(m[k], load(i, k)[0]);
+    m[k] = wave_max(m[k]);
+    l[k] = weight(mine[k], k);
+    for (int i = i0 + 64 + lane; i < i1; i += 64) l[k] += weight(load(i, k), k);
+    l[k] = wave_sum(l[k]);
+    o[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
   const int side = lane / LPR, at = lane % LPR;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
   for (int from = i0; from < i1; from += 64) {
-    const float f = weight(from == i0 ? mine : load(from + lane)) * inv;
     const int most = min(i1 - from, 64);
-    // four at a time on their way
-    for (int j = 0; j < most; j += 4 * SIDE) {
-      f32x4 x[4];
+    float f[R];
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        x[k] = *reinterpret_cast<const f32x4*>(a.part_o + state(from + min(j + k * SIDE + side, most - 1)) * D + 4 * at);
+    for (int k = 0; k < R; ++k) f[k] = weight(from == i0 ? mine[k] : load(from + lane, k), k) * (l[k] == 0.f ? 0.f : 1.f / l[k]);
+    constexpr int U = 4 / R;                  // four loads on their way
+    for (int j = 0; j < most; j += U * SIDE) {
+      f32x4 x[R][U];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int i = j + k * SIDE + side;
-        const float g = __shfl(f, i & 63, 64);
-        if (i < most) o += g * x[k];          // (what is past the last one holds anything)
-      }
+      for (int k = 0; k < R; ++k)
+#pragma unroll
+        for (int v = 0; v < U; ++v)
+          x[k][v] = *reinterpret_cast<const f32x4*>(a.part_o + state(from + min(j + v * SIDE + side, most - 1), k) * D + 4 * at);
+#pragma unroll
+      for (int k = 0; k < R; ++k)
+#pragma unroll
+        for (int v = 0; v < U; ++v) {
+          const int i = j + v * SIDE + side;
+          const float g = __shfl(f[k], i & 63, 64);
+          if (i < most) o[k] += g * x[k][v];
+        }
     }
   }
 #pragma unroll
-  for (int d = LPR; d < 64; d <<= 1)
+  for (int k = 0; k < R; ++k)
 #pragma unroll
-    for (int k = 0; k < 4; ++k) o[k] += __shfl_xor(o[k], d, 64);
+    for (int d = LPR; d < 64; d <<= 1)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[k][e] += __shfl_xor(o[k][e], d, 64);
   if constexpr (WAVES > 1) {
     if (lane == 0) {
-      s_m[wave] = m;
-      s_l[wave] = l;
+      s_m[wave] = m[0];
+      s_l[wave] = l[0];
     }
-    if (lane < LPR) s_o[wave][lane] = o;
+    if (lane < LPR) s_o[wave][lane] = o[0];
     __syncthreads();
     if (wave != 0) return;
-    float mt = -INFINITY;
+    float mt = -INFINITY, lt = 0.f, part[WAVES];
 #pragma unroll
     for (int i = 0; i < WAVES; ++i) mt = fmaxf(mt, s_m[i]);
-    l = 0.f;
-    float part[WAVES];
 #pragma unroll
     for (int i = 0; i < WAVES; ++i) {
       part[i] = s_m[i] == -INFINITY ? 0.f : s_l[i] * fast_exp2(s_m[i] - mt);
-      l += part[i];
+      lt += part[i];
     }
-    m = mt;
-    const float back = l == 0.f ? 0.f : 1.f / l;
-    o = f32x4{0.f, 0.f, 0.f, 0.f};
+    m[0] = mt;
+    l[0] = lt;
+    const float back = lt == 0.f ? 0.f : 1.f / lt;
+    o[0] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (lane < LPR)
 #pragma unroll
-      for (int i = 0; i < WAVES; ++i) o += part[i] * back * s_o[i][lane];
+      for (int i = 0; i < WAVES; ++i) o[0] += part[i] * back * s_o[i][lane];
   }
-  const int r = w.r0 + row, tok = r / a.G, g = r - tok * a.G;
-  const int64_t to = (int64_t)(w.c.first + tok) * a.Hq + w.kv * a.G + g;
-  if (lane < LPR) {
-    if constexpr (PP == 3) *reinterpret_cast<f32x4*>(static_cast<float*>(a.o) + to * D + 4 * lane) = o;
-    else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.o) + to * D + 4 * lane) = u32x2{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
+#pragma unroll
+  for (int k = 0; k < R; ++k) {
+    if (k >= rows) break;
+    const int r = w.r0 + row + k, tok = r / a.G, g = r - tok * a.G;
+    const int64_t to = (int64_t)(w.c.first + tok) * a.Hq + w.kv * a.G + g;
+    if (lane < LPR) {
+      if constexpr (PP == 3) *reinterpret_cast<f32x4*>(static_cast<float*>(a.o) + to * D + 4 * lane) = o[k];
+      else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.o) + to * D + 4 * lane) = u32x2{pack_bf16(o[k][0], o[k][1]), pack_bf16(o[k][2], o[k][3])};
+    }
+    if (lane == 0 && a.lse) a.lse[to] = lse8(m[k], l[k]);
   }
-  if (lane == 0 && a.lse) a.lse[to] = lse8(m, l);
 }
 
 inline size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -309,10 +327,12 @@ inline void carve8(Args8& a, bool planned, int D, void* ws) {
 template <int D, int ROWS, int PP, bool CHUNK>
 inline void merge8(const Args8& a, uint32_t groups, hipStream_t st) {
   TimedLaunch t(HK_TK_ATTN8_MERGE, st);
-  // rows of many parts, where there are few
-  const bool few = a.n_units * 32 <= A8_GROUPS<D>;
-  const uint32_t rows = (uint32_t)a.n_units * (few ? a.cap : (a.cap + A8_NW - 1) / A8_NW);
-  const auto merge = few ? attn8_merge_kernel<D, ROWS, PP, CHUNK, A8_NW> : attn8_merge_kernel<D, ROWS, PP, CHUNK, 1>;
+  const bool few = a.n_units * 32 <= A8_GROUPS<D>, many = a.cap > 16;   // units, of many parts; rows
+  const int per = few ? 1 : many ? 4 * A8_NW : A8_NW;
+  const uint32_t rows = (uint32_t)a.n_units * ((a.cap + per - 1) / per);
+  const auto merge = few    ? attn8_merge_kernel<D, ROWS, PP, CHUNK, A8_NW, 1>
+                     : many ? attn8_merge_kernel<D, ROWS, PP, CHUNK, 1, 4>
+                            : attn8_merge_kernel<D, ROWS, PP, CHUNK, 1, 1>;
   hipLaunchKernelGGL(merge, dim3(rows), dim3(A8_NT), 0, st, a, (int)groups);
 }
 
