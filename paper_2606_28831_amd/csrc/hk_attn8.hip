@@ -445,7 +445,7 @@ inline Plan8 plan8(int NS, int Hkv, int G, const hk_chunks* ch, bool bf, int max
   const int64_t tiles = !ch ? (int64_t)NS * ((G + rows - 1) / rows)
                             : p.one_tile ? NS : (int64_t)ch->n_tokens * G / rows + NS;
   p.units = tiles * Hkv;
-  p.planned = planned8(p.units, max_pages);
+  p.planned = planned8(p.units, !p.one_tile, max_pages);
   p.cut = p.planned && max_pages > A8_STEP;
   return p;
 }

@@ -309,7 +309,7 @@ void hk_launch_attn8_tile(Args8 a, hk_dtype format, int D, void* ws, hipStream_t
   a.one_tile = 0;
   a.rows_from = A8_ROWS + 1;
   a.rows_to = INT32_MAX;
-  carve8(a, planned8(units, a.max_pages), D, ws);
+  carve8(a, planned8(units, true, a.max_pages), D, ws);
   if (format == HK_I8) D == 128 ? launch_tile<HK_I8, 128>(a, st) : launch_tile<HK_I8, 64>(a, st);
   else D == 128 ? launch_tile<HK_E4M3, 128>(a, st) : launch_tile<HK_E4M3, 64>(a, st);
 }
