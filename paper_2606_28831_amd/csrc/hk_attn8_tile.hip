@@ -3,8 +3,9 @@
 // A unit is TILE8_ROWS folded rows (see hk_attn8.hip) of a sequence and KV head: four waves of 32 rows
 // against the same keys, 32 at a time.  The codes of a tile are converted once for all waves, by all of
 // them, and lie in LDS as bf16: K by rows, V by dims, in the order of keys that the scores' registers
-// have, so that both kinds of fragment are 16 bytes in a row.  While tile t is computed, t + 1 is converted
-// into the other buffer and t + 2 is on its way into registers.
+// have, so that both kinds of fragment are 16 bytes in a row.  While two tiles are computed, the next two are
+// converted into the other buffers and two more are on their way into registers.  One tile a barrier took 1673
+// us where two take 1575; converting between the two computations 1660 to 1720.
 //
 // Per wave and tile, 32x32x16 MFMAs: C[key][row] = K Q^T in bf16, then O^T[dim][row] += V^T P^T in fp16,
 // which holds V's codes exactly and P to 2^-11 of a term.  Lane l holds row l % 32 and half hi = l / 32 of the
@@ -14,8 +15,14 @@
 // V's scale s = f 2^e, f in [1/2, 1), and y = x + e, P = exp2(y - m) f 2^10 is at most 2^14, and smaller terms
 // keep their bits down to 2^-24 of the largest.  The softmax's sum takes exp2(y - m) 2^-e.  e is counted
 // from that of the unit's first keys, so that y is about x; of scales below 2^-90 it counts as 0 (their V is
-// below 2^-81, next to nothing).  Between bf16 in two parts, 24 products a tile, and this, 16: 8 prompts of
-// 4096 tokens 1930 us and 1673.
+// below 2^-81, next to nothing).  Against P in two parts of bf16, 24 products a tile instead of 16: 1930 us and
+// 1673.
+//
+// Measured: 8 prompts of 4096 tokens of 32 query heads, 8 KV heads of 128 dims, causal, 1570 to 1625
+// us, 677 to 700 TFLOP/s; a
+// bf16 matrix product of 8192^3 reaches 1231.  The matrix units work a quarter to a third of the time: a wave's
+// chain of scores, softmax and values has waits that two waves a SIMD fill only in part, and 231 registers
+// leave no room for a third.
 #include "hk_attn8.h"
 
 namespace hk {
@@ -29,10 +36,11 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
   constexpr int K_ROW = 2 * D + 16, V_ROW = 80;               // bytes; padded: no bank twice among 16 lanes
   constexpr int KW = D / 16;                                  // words of codes of a thread that brings K
   constexpr int K_TILE = 32 * K_ROW, TILE = K_TILE + D * V_ROW;
-  __shared__ __align__(16) char s_tile[2][TILE];
-  __shared__ __align__(16) float s_scale[2][4][32];           // K's scales times c2; V's: e, f 2^10, 2^-e
+  constexpr int NT = 4;                                       // tiles in LDS: two computed, two converted
+  __shared__ __align__(16) char s_tile[NT][TILE];
+  __shared__ __align__(16) float s_scale[NT][4][32];          // K's scales times c2; V's: e, f 2^10, 2^-e
   __shared__ int s_base;                                      // what e is counted from
-  __shared__ int s_odd[2];                                    // whether an f is NaN or infinite
+  __shared__ int s_odd[NT];                                   // whether an f is NaN or infinite
   __shared__ int s_sums[A8_NW];
   const int lane = threadIdx.x & 63, row32 = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -91,11 +99,11 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
     // Ids and masks come 32 tiles at a time: lane i holds those of page i % 2 of tile i / 2.
     const int tiles = p1 > p0 ? (p1 - p0 + 1) / 2 : 0;
     int ids = 0, masks = 0;
-    uint32_t code[8];                                         // K: KW words; V: word of eight keys
-    float scale = 0.f;
+    uint32_t code[2][8];                                      // of two tiles; K: KW words; V: word of eight keys
+    float scale[2] = {0.f, 0.f};
     int base = 0;
-    uint32_t mask = 0, next_mask = 0;                         // of the tile computed, and of the one converted
-    auto load = [&](int i) {                                  // (past the last tile: its pages again)
+    uint32_t mask[2] = {0, 0}, next_mask[2] = {0, 0};         // of the tiles computed, and of those converted
+    auto load = [&](int x, int i) {                           // (past the last tile: its pages again)
       if ((i & 31) == 0) {
         const int page = p0 + 2 * i + lane;
         ids = min(max(trow[min(page, p1 - 1)], 0), a.num_pages - 1);
@@ -103,54 +111,54 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
       }
       const int e = 2 * (i & 31);
       const int id0 = __builtin_amdgcn_readlane(ids, e), id1 = __builtin_amdgcn_readlane(ids, e + 1);
-      next_mask = (uint32_t)__builtin_amdgcn_readlane(masks, e) | (uint32_t)__builtin_amdgcn_readlane(masks, e + 1) << 16;
+      next_mask[x] = (uint32_t)__builtin_amdgcn_readlane(masks, e) | (uint32_t)__builtin_amdgcn_readlane(masks, e + 1) << 16;
       const char* page = (is_v ? a.v_pool : a.k_pool) + (size_t)(uint32_t)(my ? id1 : id0) * (HK_PAGE * D);
       if (!is_v) {
 #pragma unroll
         for (int k = 0; k < KW / 4; ++k)
-          *reinterpret_cast<u32x4*>(&code[4 * k]) = *reinterpret_cast<const u32x4*>(page + from + 16 * k);
+          *reinterpret_cast<u32x4*>(&code[x][4 * k]) = *reinterpret_cast<const u32x4*>(page + from + 16 * k);
       } else if (brings) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          code[j] = *reinterpret_cast<const uint32_t*>(page + from + (8 * (j >> 2) + (j & 3)) * D);
+          code[x][j] = *reinterpret_cast<const uint32_t*>(page + from + (8 * (j >> 2) + (j & 3)) * D);
       }
       if (wave == 0) {
         const int id = (lane >> 4) & 1 ? id1 : id0;
-        scale = (lane >> 5 ? a.v_scale : a.k_scale)[(size_t)(uint32_t)id * HK_PAGE + (lane & 15)];
+        scale[x] = (lane >> 5 ? a.v_scale : a.k_scale)[(size_t)(uint32_t)id * HK_PAGE + (lane & 15)];
       }
     };
-    auto convert = [&](int buf, uint32_t mk) {
+    auto convert = [&](int which, int buf, uint32_t mk) {
       if (!is_v) {
         char* at = s_tile[buf] + to;
 #pragma unroll
         for (int k = 0; k < KW / 2; ++k)
           *reinterpret_cast<u32x4*>(at + 16 * k) =
-              u32x4{Code<F>::template pair<0>(code[2 * k]), Code<F>::template pair<1>(code[2 * k]),
-                    Code<F>::template pair<0>(code[2 * k + 1]), Code<F>::template pair<1>(code[2 * k + 1])};
+              u32x4{Code<F>::template pair<0>(code[which][2 * k]), Code<F>::template pair<1>(code[which][2 * k]),
+                    Code<F>::template pair<0>(code[which][2 * k + 1]), Code<F>::template pair<1>(code[which][2 * k + 1])};
       } else if (brings) {
         if (F == HK_E4M3 && mk != 0xffffffffu) {
           // a slot that is not valid may hold codes that stand for NaN
           const uint32_t bits = mk >> (16 * my + 4 * (lane & 1));
 #pragma unroll
-          for (int j = 0; j < 8; ++j) code[j] = (bits >> (8 * (j >> 2) + (j & 3))) & 1u ? code[j] : 0u;
+          for (int j = 0; j < 8; ++j) code[which][j] = (bits >> (8 * (j >> 2) + (j & 3))) & 1u ? code[which][j] : 0u;
         }
         char* at = s_tile[buf] + to;
         u32x4 x[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          x[0][k] = Code<F>::template halves<0>(code[2 * k], code[2 * k + 1]);
-          x[1][k] = Code<F>::template halves<1>(code[2 * k], code[2 * k + 1]);
-          x[2][k] = Code<F>::template halves<2>(code[2 * k], code[2 * k + 1]);
-          x[3][k] = Code<F>::template halves<3>(code[2 * k], code[2 * k + 1]);
+          x[0][k] = Code<F>::template halves<0>(code[which][2 * k], code[which][2 * k + 1]);
+          x[1][k] = Code<F>::template halves<1>(code[which][2 * k], code[which][2 * k + 1]);
+          x[2][k] = Code<F>::template halves<2>(code[which][2 * k], code[which][2 * k + 1]);
+          x[3][k] = Code<F>::template halves<3>(code[which][2 * k], code[which][2 * k + 1]);
         }
 #pragma unroll
         for (int d = 0; d < 4; ++d) *reinterpret_cast<u32x4*>(at + d * V_ROW) = x[d];
       }
       if (wave == 0) {
-        const int top = __builtin_amdgcn_frexp_expf(scale), e = top < -90 ? 0 : min(max(top - base, -126), 126);
-        const float f = __builtin_amdgcn_ldexpf(scale, 10 - (e + base));
+        const int top = __builtin_amdgcn_frexp_expf(scale[which]), e = top < -90 ? 0 : min(max(top - base, -126), 126);
+        const float f = __builtin_amdgcn_ldexpf(scale[which], 10 - (e + base));
         if (lane < 32) {
-          s_scale[buf][0][lane] = scale * a.c2;
+          s_scale[buf][0][lane] = scale[which] * a.c2;
         } else {
           s_scale[buf][1][lane - 32] = (float)e;
           s_scale[buf][2][lane - 32] = f;
@@ -229,30 +237,41 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
     };
 
     if (tiles > 0) {
-      load(0);
+      load(0, 0);
+      if (tiles > 1) load(1, 1);
       if (wave == 0) {
-        const int e = lane >= 32 && (next_mask >> (lane - 32)) & 1u ? __builtin_amdgcn_frexp_expf(scale) : -1000;
+        const int e = lane >= 32 && (next_mask[0] >> (lane - 32)) & 1u ? __builtin_amdgcn_frexp_expf(scale[0]) : -1000;
         base = (int)wave_max((float)e);
         if (base < -90) base = 0;
         if (lane == 0) s_base = base;
       }
-      convert(0, next_mask);
-      mask = next_mask;
-      if (tiles > 1) load(1);
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        if (x < tiles) convert(x, x, next_mask[x]);
+        mask[x] = next_mask[x];
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+        if (2 + x < tiles) load(x, 2 + x);
       __syncthreads();
       base = s_base;
     }
-    for (int i = 0; i < tiles; ++i) {
-      const int buf = i & 1, key = (p0 + 2 * i) * HK_PAGE;
-      const uint32_t mk = next_mask;
-      if (i + 1 < tiles) {
-        convert(buf ^ 1, mk);
-        if (i + 2 < tiles) load(i + 2);
+    for (int i = 0; i < tiles; i += 2) {
+      const int buf = i & 2;
+      const uint32_t mk[2] = {next_mask[0], next_mask[1]};
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+        if (i + 2 + x < tiles) convert(x, (buf ^ 2) + x, mk[x]);
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+        if (i + 4 + x < tiles) load(x, i + 4 + x);
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int key = (p0 + 2 * (i + x)) * HK_PAGE;
+        if (i + x < tiles && key < seen_any && w0 < w.rows)
+          compute(buf + x, key, mask[x], mask[x] == 0xffffffffu && key + 32 <= seen_all);
+        mask[x] = mk[x];
       }
-      if (key < seen_any && w0 < w.rows) {
-        compute(buf, key, mask, mask == 0xffffffffu && key + 32 <= seen_all);
-      }
-      mask = mk;
       __syncthreads();
     }
 
