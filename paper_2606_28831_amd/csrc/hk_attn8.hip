@@ -419,7 +419,9 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_kernel(Args8 a) {
         put(DT * k + j, value(0), value(1), value(2), value(3));
       }
     if (qd == 0) {
-      if (state >= 0) *reinterpret_cast<f32x2*>(a.part_ml + (state + row) * 2) = f32x2{lt[nq] == 0.f ? -INFINITY : mt[nq], lt[nq]};
+      // (NaN keys alone leave a sum of NaN and no reference)
+      const float ref = lt[nq] == 0.f ? -INFINITY : mt[nq] == -INFINITY ? 0.f : mt[nq];
+      if (state >= 0) *reinterpret_cast<f32x2*>(a.part_ml + (state + row) * 2) = f32x2{ref, lt[nq]};
       else if (a.lse) a.lse[at] = lse8(mt[nq], lt[nq]);
     }
   }

@@ -19,10 +19,9 @@
 // 1673.
 //
 // Measured: 8 prompts of 4096 tokens of 32 query heads, 8 KV heads of 128 dims, causal, 1570 to 1625
-// us, 677 to 700 TFLOP/s; a
-// bf16 matrix product of 8192^3 reaches 1231.  The matrix units work a quarter to a third of the time: a wave's
-// chain of scores, softmax and values has waits that two waves a SIMD fill only in part, and 231 registers
-// leave no room for a third.
+// us, 677 to 700 TFLOP/s; a bf16 matrix product of 8192^3 reaches 1236.  The matrix units work 29% of the
+// cycles and the vector units 53%, 13.6 vector instructions a product of 32 cycles: conversions, scales,
+// softmax.  A wave waits 33% of its time, and 231 registers leave no room for a third a SIMD.
 #include "hk_attn8.h"
 
 namespace hk {
@@ -280,7 +279,7 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
       // l is brought to [1/2, 1): scales far apart leave sums far apart
       const int up = __builtin_amdgcn_frexp_expf(l), down = base + Code<F>::F16_DOWN - 10 - up;
       l = __builtin_amdgcn_frexp_mantf(l);
-      m += (float)up;
+      m = off + (float)up;                                    // (NaN keys alone leave a sum of NaN and no reference)
       const float inv = l == 0.f ? 0.f : 1.f / l;             // (a NaN stays one)
       const int64_t at = (int64_t)(w.c.first + tok) * a.Hq + w.kv * a.G + g, part = state + wave * 32 + row32;
 #pragma unroll

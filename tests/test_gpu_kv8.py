@@ -392,6 +392,47 @@ def test_nan_rows_reach_who_sees_them_alone(fmt):
             assert torch.isnan(o).all()
 
 
+@pytest.mark.parametrize("fmt", ["i8", "e4m3"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_nan_row_that_is_alone_in_its_part(fmt, dtype):
+    """A long row is cut into parts of eight pages; in one of them the only valid slot is a NaN row."""
+    c = Cache8([700], 128, fmt, seed=3, width=64)
+    row = int(c.t[0, 11]) * 16 + 5
+    c.k_scale.view(-1)[row] = float("nan")
+    _bytes(c.k_pool).view(-1, 128)[row] = 0
+    c.page_mask[0, 8:16] = 0
+    c.page_mask[0, 11] = 1 << 5
+    for _, o, lse in (_decode(c, 1, 1, 2, dtype, check=False), _attend(c, [6], 1, 2, dtype, check=False),
+                      _attend(c, [70], 1, 2, dtype, check=False)):
+        assert torch.isnan(o).all() and torch.isnan(lse).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_masks_that_leave_nothing(D):
+    """A head all of whose slots are masked, one with a single slot at the far end, one of plain rows."""
+    c = Cache8([900, 900, 900], D, "i8", seed=3, width=64)
+    c.m[0] = 0
+    c.m[1] = 0
+    c.m[1, 56] = 1 << 3
+    c.page_mask.copy_(torch.tensor(c.m, device=DEV).to(torch.int16))
+    _, o, lse = _decode(c, 1, 3, 4, "bf16")
+    assert (o[0, :4] == 0).all() and torch.isneginf(lse[0, :4]).all()
+    _attend(c, [1], 3, 4, "bf16")
+
+
+def test_decode_of_more_heads_than_are_planned():
+    NS, Hkv = 520, 8
+    c = Cache8([(7 * i) % 45 for i in range(NS * Hkv)], 64, "e4m3", width=40, seed=4)
+    _decode(c, NS, Hkv, 2, "f32", heads=list(range(0, NS * Hkv, 331)) + [NS * Hkv - 1])
+
+
+@pytest.mark.parametrize("fmt,dtype,lens", [("i8", "bf16", [1100, 1040]), ("e4m3", "f32", [301, 260])])
+def test_more_tiles_than_are_planned(fmt, dtype, lens):
+    Hkv, G = 8, 8
+    c = Cache8([n + 20 - k for n in lens for k in range(Hkv)], 64, fmt, seed=4, keep_last=2000)
+    _attend(c, lens, Hkv, G, dtype, pad=2, heads=[0, 5, 15])
+
+
 # ------------------------------------------------------------------ chunks
 ATTN = [
     ("bf16", 128, 2, 4, [5], [37]),
@@ -735,6 +776,42 @@ def test_captured_and_replayed_on_another_stream():
         for a, b in zip(outs, want[i]):
             assert torch.equal(a.nan_to_num(9.0), b.nan_to_num(9.0))
     assert int(status) == 0 and int(chd.status) == 0 and int(dec.status) == 0
+
+
+@pytest.mark.parametrize("fmt", ["i8", "e4m3"])
+def test_a_captured_segment_of_a_loop(fmt):
+    """Steps and their compression through DecodeLoop in one graph, replayed between eager work: the same as eager."""
+    from paper_2606_28831_amd.pipeline import DecodeLoop
+    L, B, Hq, Hkv, D, W = 2, 2, 4, 2, 64, 6
+    H, loops = L * B * Hkv, []
+    for _ in range(2):
+        kv, al = _empty(H, D, fmt, 40, 400)
+        loops.append(DecodeLoop(L, B, Hq, Hkv, D, W, kv, al, 0.9, 32))
+    q, k, v = (torch.empty(W, L * B, h, D, dtype=torch.bfloat16, device=DEV) for h in (Hq, Hkv, Hkv))
+    lse = torch.empty(W, L * B, Hq, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(8)
+
+    def fill():
+        for t in (q, k, v):
+            t.copy_(torch.randn(t.shape, generator=g, device=DEV))
+
+    fill()
+    loops[0].segment(q, k, v, lse)
+    loops[1].segment(q, k, v, lse)
+    graph = loops[1].capture_segment(q, k, v, lse)
+    for _ in range(12):
+        fill()
+        loops[0].segment(q, k, v, lse)
+        torch.cuda.synchronize()
+        want = lse.clone(), loops[0].o.clone()
+        lse.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(lse, want[0]) and torch.equal(loops[1].o, want[1])
+        for name in ("page_table", "page_mask", "n_pages"):
+            assert torch.equal(getattr(loops[0].kv, name), getattr(loops[1].kv, name)), name
+    assert all(int(x.status) == 0 and int(x.comp.buf.status) == 0 for x in loops)
+    assert int(loops[0].kv.n_pages.max()) > 2
 
 
 def test_calls_on_a_stream_of_their_own():
