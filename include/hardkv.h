@@ -649,7 +649,8 @@ hk_status hk_write_kv8(const hk_dims* dims, const hk_paged_kv8* kv8, int32_t n_l
 
 /* Its inverse: pool rows read back, code * scale rounded to fp32 and then to `dtype`, into rows of
  * k_out and v_out laid out as hk_write_kv8's are (v_out NULL: K alone).  Rows whose entry lies outside
- * [0, 16 * num_pages) are left as they are; several rows may have one slot.
+ * [0, 16 * num_pages) are left as they are; several rows may have one slot.  k_out and v_out must not
+ * overlap.
  */
 hk_status hk_read_kv8(const hk_dims* dims, const hk_paged_kv8* kv8, int32_t n_layers,
                       int32_t n_tokens, const int64_t* slot_map, hk_dtype dtype, void* k_out,
@@ -662,9 +663,11 @@ hk_status hk_read_kv8(const hk_dims* dims, const hk_paged_kv8* kv8, int32_t n_la
  * slots past the row's end hold is not read into the result.  Sums stay finite to the top of the fp32
  * range; values below 2^-80 (1e-24) lose bits.  A valid slot must not hold an e4m3 code of NaN (0x7f,
  * 0xff): hk_write_kv8 writes none, and what the sequence's results then are is not said.
- * The ranges that a row is split into follow from the sizes of the call alone; the same row's last bits
- * can change with them.
- * Hq / Hkv at most 64 (HK_ERR_SHAPE); all pointers 16-byte aligned but the tables' and lse, of their
+ * How rows are split over workgroups follows from the lengths of all rows of the call, so the last bits
+ * of o and lse can change with the batch; the same call gives the same bits.  q times a row's codes has
+ * to stay in the fp32 range.
+ * Hq / Hkv at most 64, NS Hkv (twice that where Hq / Hkv is above 32) below 2^24 (HK_ERR_SHAPE); all
+ * pointers 16-byte aligned but the tables' and lse, of their
  * types' alignment; workspace: >= hk_workspace_size(HK_OP_DECODE8) bytes, 256-byte aligned; calls that
  * overlap on one workspace race.
  */
@@ -673,7 +676,12 @@ hk_status hk_decode_attn8(const hk_dims* dims, hk_dtype dtype, const void* q,
                           void* workspace, size_t ws_bytes, hipStream_t stream);
 
 /* hk_chunk_attn over an 8-bit cache: q and o in `dtype` (HK_F32 or HK_BF16), the meaning, layouts,
- * strides and limits of hk_chunk_attn otherwise; range and codes as for hk_decode_attn8.
+ * strides and limits of hk_chunk_attn otherwise; range, codes and bits as for hk_decode_attn8.
+ * Precision: fp32 rows keep all of P's bits.  With bf16 rows P enters the product with V to 2^-16 of a
+ * term in chunks of up to 32 queries of a KV head; in longer ones to 2^-11, and terms below 2^-33 of a
+ * query's largest can be lost.  These longer ones want the V scales of a head within 2^100 of one another.
+ * Where chunks can have more than 32 queries of a KV head, (n_tokens G / 32 + n_seq) Hkv has to stay below
+ * 2^24 (HK_ERR_SHAPE).
  * workspace: >= hk_chunk_attn8_workspace_size(dims, chunks, kv8->kv.max_pages) bytes, 256-byte aligned
  * (never 0 for sizes that are accepted); calls that overlap on one workspace race.
  */

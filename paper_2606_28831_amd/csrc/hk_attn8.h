@@ -314,7 +314,8 @@ inline size_t states8_bytes(int D, int cap) {
   return align_up(kFirst8) + align_up(states8(D, cap) * D * 4) + align_up(states8(D, cap) * 8);
 }
 // Units of tiles cost a search in the starts each, and every workgroup plans them all: past four a thread a
-// workgroup for each unit is sooner done (7 fp32 prompts of 504 tokens, 2670 units: 210 us planned, 116 not; 14 of 1016 in bf16, 2700 tiles: 321, 214).
+// workgroup for each unit is sooner done (7 fp32 prompts of 504 tokens, 2670 units: 210 us planned, 116 not;
+// 14 of 1016 in bf16, 2700 tiles: 321 and 214).
 inline bool planned8(int64_t units, bool tiles, int max_pages) {
   return units <= (tiles ? 4 * A8_NT : A8_UNITS) && units * (((int64_t)max_pages + A8_STEP - 1) / A8_STEP) < (1ll << 31);
 }
