@@ -683,7 +683,9 @@ hk_status hk_decode_attn8(const hk_dims* dims, hk_dtype dtype, const void* q,
  * Where chunks can have more than 32 queries of a KV head, (n_tokens G / 32 + n_seq) Hkv has to stay below
  * 2^24 (HK_ERR_SHAPE).
  * workspace: >= hk_chunk_attn8_workspace_size(dims, chunks, kv8->kv.max_pages) bytes, 256-byte aligned
- * (never 0 for sizes that are accepted); calls that overlap on one workspace race.
+ * (never 0 for sizes that are accepted; more tokens, longer chunks or wider tables need no less, but that
+ * up to 512 MB of converted pages are asked for only where they suffice and max_len Hq / Hkv is at least
+ * 4096); calls that overlap on one workspace race.
  */
 size_t hk_chunk_attn8_workspace_size(const hk_dims* dims, const hk_chunks* chunks,
                                      int32_t max_pages);
@@ -737,7 +739,7 @@ enum {
   HK_TK_TRIM = 22,         /* hk_trim_slots: count + write, timed together               */
   HK_TK_WRITE_KV8 = 23,    /* hk_write_kv8                                               */
   HK_TK_READ_KV8 = 24,     /* hk_read_kv8                                                */
-  HK_TK_ATTN8 = 25,        /* hk_decode_attn8, hk_chunk_attn8: attention of rows and ranges */
+  HK_TK_ATTN8 = 25,        /* hk_decode_attn8, hk_chunk_attn8: attention, tiles converted before it */
   HK_TK_ATTN8_MERGE = 26,  /* hk_decode_attn8, hk_chunk_attn8: merge of the ranges' states */
   HK_TK_COUNT = 27
 };

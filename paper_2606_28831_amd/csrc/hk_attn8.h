@@ -23,6 +23,7 @@ struct Args8 {
   const uint16_t* masks;
   void* o;
   float *lse, *part_o, *part_ml;              // states: of workgroup b's first unit at 2 b, of its last at 2 b + 1
+  char* ready;                                // tiles converted beforehand, or NULL
   int32_t* first;                             // step that a unit begins at, and the number of steps; NULL: not planned
   int Hq, Hkv, G, max_pages, num_pages, n_seq, n_tokens, max_len;
   int n_units, cap;                           // cap: rows of a unit in the workspace
@@ -343,5 +344,6 @@ inline void merge8(const Args8& a, uint32_t groups, hipStream_t st) {
 
 // bf16 chunks of more than A8_ROWS rows of a KV head: units, workspace, launch
 int64_t hk_attn8_tile_units(int NS, int Hkv, int G, int n_tokens);
-size_t hk_attn8_tile_ws(int D);
-void hk_launch_attn8_tile(hk::Args8 a, hk_dtype format, int D, void* ws, hipStream_t st);
+// (heads * max_pages: of the tables; most: rows of a chunk at most)
+size_t hk_attn8_tile_ws(int D, int64_t heads, int max_pages, int64_t most);
+void hk_launch_attn8_tile(hk::Args8 a, hk_dtype format, int D, int64_t most, void* ws, hipStream_t st);

@@ -1,11 +1,11 @@
 // 8-bit cache: attention of long chunks, bf16 queries (gfx950).
 //
 // A unit is TILE8_ROWS folded rows (see hk_attn8.hip) of a sequence and KV head: four waves of 32 rows
-// against the same keys, 32 at a time.  The codes of a tile are converted once for all waves, by all of
-// them, and lie in LDS as bf16: K by rows, V by dims, in the order of keys that the scores' registers
-// have, so that both kinds of fragment are 16 bytes in a row.  While two tiles are computed, the next two are
-// converted into the other buffers and two more are on their way into registers.  One tile a barrier took 1673
-// us where two take 1575; converting between the two computations 1660 to 1720.
+// against the same keys, 32 at a time.  The codes of a tile lie in LDS as bf16 (K, by rows) and fp16 (V, by dims,
+// in the order of keys that the scores' registers have), so that both kinds of fragment are 16 bytes in a row.
+// They are converted by all waves for all of them: while two tiles are computed, the next two are converted into
+// the other buffers and two more are on their way into registers.  Or, for long chunks (READY), a launch
+// before has converted every tile of a head once, and it goes from memory straight into LDS.
 //
 // Per wave and tile, 32x32x16 MFMAs: C[key][row] = K Q^T in bf16, then O^T[dim][row] += V^T P^T in fp16,
 // which holds V's codes exactly and P to 2^-11 of a term.  Lane l holds row l % 32 and half hi = l / 32 of the
@@ -14,32 +14,130 @@
 // For P to be in fp16's range whatever V's scales are, the reference m follows what enters the product: with
 // V's scale s = f 2^e, f in [1/2, 1), and y = x + e, P = exp2(y - m) f 2^10 is at most 2^14, and smaller terms
 // keep their bits down to 2^-24 of the largest.  The softmax's sum takes exp2(y - m) 2^-e.  e is counted
-// from that of the unit's first keys, so that y is about x; of scales below 2^-90 it counts as 0 (their V is
-// below 2^-81, next to nothing).  Against P in two parts of bf16, 24 products a tile instead of 16: 1930 us and
-// 1673.
+// from that of the unit's first keys (READY: the head's), so that y is about x; of scales below 2^-90 it counts as 0
+// (their V is below 2^-81, next to nothing).
 //
-// Measured: 8 prompts of 4096 tokens of 32 query heads, 8 KV heads of 128 dims, causal, 1570 to 1625
-// us, 677 to 700 TFLOP/s; a bf16 matrix product of 8192^3 reaches 1236.  The matrix units work 29% of the
-// cycles and the vector units 53%, 13.6 vector instructions a product of 32 cycles: conversions, scales,
-// softmax.  A wave waits 33% of its time, and 231 registers leave no room for a third a SIMD.
+// Measured on 8 prompts of 4096 tokens of 32 query heads, 8 KV heads of 128 dims, causal: 1403 to 1458 us, 755 to 784
+// TFLOP/s, of which the conversion is 38; 1570 to 1625 with every unit converting its tiles, and 1136 without conversions and
+// loads at all.  A bf16 matrix product of 8192^3 reaches 1236 TFLOP/s.  What bounds it is vector work beside
+// MFMA: the matrix units are busy for 34% of the cycles and the vector units for 51% (29 and 53 with every unit
+// converting), waves wait for 34% of theirs, at two a SIMD.  P in two parts of bf16, 24 products a tile instead of 16: 1930 us for 1673; one tile a barrier 1673 for
+// 1575; converting between the computations of two tiles 1660 to 1720; two tiles in one softmax spill (1767); 64 rows
+// a wave, at one wave a SIMD, 2745; eight waves of 256 rows 1629 to 1675.
 #include "hk_attn8.h"
 
 namespace hk {
 
 constexpr int TILE8_ROWS = 128;
 
+// A converted tile: K by rows and V by dims, whose 16-byte pieces lie in turned orders so that 16 lanes of
+// a fragment's read meet no bank twice; K's scales times c2, V's e, f 2^10 and 2^-e; `odd` and what e is counted from.
+template <int D>
+struct Ready8 {
+  static constexpr int V = 64 * D, SCALES = 2 * V, ODD = SCALES + 512, BASE = ODD + 4, BYTES = SCALES + 1024;
+  __device__ static __forceinline__ int k_at(int row, int piece) {
+    return row * 2 * D + (piece ^ (D == 128 ? row & 15 : row >> 1 & 7)) * 16;
+  }
+  // rows of one dim % 4 lie side by side
+  __device__ static __forceinline__ int v_at(int dim, int piece) {
+    return V + ((dim & 3) * (D / 4) + (dim >> 2)) * 64 + ((piece ^ dim ^ (dim >> 2 & 2)) & 3) * 16;
+  }
+};
+// V's scale as e, f 2^10 (see above)
+__device__ __forceinline__ int v_exponent(float scale, int base) {
+  const int top = __builtin_amdgcn_frexp_expf(scale);
+  return top < -90 ? 0 : min(max(top - base, -126), 126);
+}
+// of 32 keys, in lanes 32 .. 63
+__device__ __forceinline__ int v_base(float scale, uint32_t mask) {
+  const int lane = threadIdx.x & 63;
+  const int e = lane >= 32 && (mask >> (lane - 32)) & 1u ? __builtin_amdgcn_frexp_expf(scale) : -1000;
+  const int base = (int)wave_max((float)e);
+  return base < -90 ? 0 : base;
+}
+
+// A tile a workgroup, of the heads whose chunks the tile kernel takes.
 template <int F, int D>
+__global__ __launch_bounds__(A8_NT) void attn8_convert_kernel(Args8 a) {
+  using L = Ready8<D>;
+  const int per = a.max_pages / 2, h = blockIdx.x / per, t = blockIdx.x - h * per;
+  const int len = chunk_of(a.start, h / a.Hkv, a.n_tokens, a.max_len).len, n = min(max(a.n_pages[h], 0), a.max_pages);
+  if (len * a.G < a.rows_from || 2 * t >= n) return;
+  const int32_t* trow = a.table + (size_t)h * a.max_pages;
+  const uint16_t* mrow = a.masks + (size_t)h * a.max_pages;
+  const auto page = [&](int p) { return min(max(trow[min(p, n - 1)], 0), a.num_pages - 1); };
+  const auto valid = [&](int p) { return p < n ? (uint32_t)mrow[p] : 0u; };
+  const int id[2] = {page(2 * t), page(2 * t + 1)};
+  const uint32_t mask = valid(2 * t) | valid(2 * t + 1) << 16;
+  char* to = a.ready + (size_t)blockIdx.x * L::BYTES;
+  const int i = threadIdx.x;
+  if (i < 2 * D) {
+    const int key = i / (D / 16), piece = i % (D / 16);
+    const u32x4 w = *reinterpret_cast<const u32x4*>(a.k_pool + ((size_t)(uint32_t)id[key >> 4] * HK_PAGE + (key & 15)) * D + piece * 16);
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      *reinterpret_cast<u32x4*>(to + L::k_at(key, 2 * piece + k)) =
+          u32x4{Code<F>::template pair<0>(w[2 * k]), Code<F>::template pair<1>(w[2 * k]),
+                Code<F>::template pair<0>(w[2 * k + 1]), Code<F>::template pair<1>(w[2 * k + 1])};
+  }
+  if (i < D) {
+    // dims 4 c .. of the eight keys of piece p: 16 (p / 2) + 4 (p % 2) + {0 .. 3, 8 .. 11}
+    const int c = i >> 2, p = i & 3, first = 4 * (p & 1);
+    const char* from = a.v_pool + ((size_t)(uint32_t)id[p >> 1] * HK_PAGE + first) * D + 4 * c;
+    const uint32_t bits = mask >> (16 * (p >> 1) + first);
+    uint32_t code[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int key = 8 * (j >> 2) + (j & 3);
+      code[j] = *reinterpret_cast<const uint32_t*>(from + key * D);
+      // a slot that is not valid may hold codes that stand for NaN
+      if (F == HK_E4M3) code[j] = (bits >> key) & 1u ? code[j] : 0u;
+    }
+    u32x4 x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      x[0][k] = Code<F>::template halves<0>(code[2 * k], code[2 * k + 1]);
+      x[1][k] = Code<F>::template halves<1>(code[2 * k], code[2 * k + 1]);
+      x[2][k] = Code<F>::template halves<2>(code[2 * k], code[2 * k + 1]);
+      x[3][k] = Code<F>::template halves<3>(code[2 * k], code[2 * k + 1]);
+    }
+#pragma unroll
+    for (int d = 0; d < 4; ++d) *reinterpret_cast<u32x4*>(to + L::v_at(4 * c + d, p)) = x[d];
+  }
+  if (i >= A8_NT - 64) {
+    const int lane = i & 63, slot = lane & 15;
+    const bool second = lane & 16;
+    const size_t begin = (size_t)(uint32_t)(second ? page(1) : page(0)) * HK_PAGE + slot;
+    const int base = v_base(a.v_scale[begin], valid(0) | valid(1) << 16);
+    const float scale = (lane >> 5 ? a.v_scale : a.k_scale)[(size_t)(uint32_t)id[second] * HK_PAGE + slot];
+    const int e = v_exponent(scale, base);
+    const float f = __builtin_amdgcn_ldexpf(scale, 10 - (e + base));
+    float* out = reinterpret_cast<float*>(to + L::SCALES) + (lane & 31);
+    if (lane < 32) {
+      out[0] = scale * a.c2;
+    } else {
+      out[32] = (float)e;
+      out[64] = f;
+      out[96] = __builtin_amdgcn_ldexpf(1.f, -e);
+    }
+    const bool odd = __any(lane >= 32 && !(fabsf(f) < INFINITY));
+    if (lane == 0) *reinterpret_cast<u32x2*>(to + L::ODD) = u32x2{odd ? 1u : 0u, (uint32_t)base};
+  }
+}
+
+template <int F, int D, bool READY>
 __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
 #pragma clang fp contract(off)
+  using L = Ready8<D>;
   constexpr int KS = D / 16, DT = D / 32;
   constexpr int K_ROW = 2 * D + 16, V_ROW = 80;               // bytes; padded: no bank twice among 16 lanes
   constexpr int KW = D / 16;                                  // words of codes of a thread that brings K
-  constexpr int K_TILE = 32 * K_ROW, TILE = K_TILE + D * V_ROW;
+  constexpr int K_TILE = 32 * K_ROW, TILE = READY ? L::BYTES : K_TILE + D * V_ROW;
   constexpr int NT = 4;                                       // tiles in LDS: two computed, two converted
   __shared__ __align__(16) char s_tile[NT][TILE];
-  __shared__ __align__(16) float s_scale[NT][4][32];          // K's scales times c2; V's: e, f 2^10, 2^-e
+  __shared__ __align__(16) float s_scale[READY ? 1 : NT][4][32];   // K's scales times c2; V's: e, f 2^10, 2^-e
   __shared__ int s_base;                                      // what e is counted from
-  __shared__ int s_odd[NT];                                   // whether an f is NaN or infinite
+  __shared__ int s_odd[READY ? 1 : NT];                       // whether an f is NaN or infinite
   __shared__ int s_sums[A8_NW];
   const int lane = threadIdx.x & 63, row32 = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -51,6 +149,12 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
   const uint32_t from = is_v ? (lane & 1) * 4 * D + 4 * c : (lane >> 2) * D + part4 * (D / 4);
   const int to = is_v ? K_TILE + 4 * c * V_ROW + (2 * my + (lane & 1)) * 16
                       : (16 * my + (lane >> 2)) * K_ROW + part4 * (D / 2);
+
+  // the lane's fragments: of K, dims 16 s + 8 hi on of row row32; of V, the keys of piece 2 s + hi of dim 32 d + row32
+  const auto k_at = [&](int s) { return READY ? L::k_at(row32, 2 * s + hi) : row32 * K_ROW + hi * 16 + 32 * s; };
+  const auto v_at = [&](int d, int s) {
+    return READY ? L::v_at(32 * d + row32, 2 * s + hi) : K_TILE + (32 * d + row32) * V_ROW + hi * 16 + 32 * s;
+  };
 
   int u = a.n_units - 1 - (int)blockIdx.x, skip = 0, left = 1 << 30;
   if (a.first) {
@@ -154,27 +258,27 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
         for (int d = 0; d < 4; ++d) *reinterpret_cast<u32x4*>(at + d * V_ROW) = x[d];
       }
       if (wave == 0) {
-        const int top = __builtin_amdgcn_frexp_expf(scale[which]), e = top < -90 ? 0 : min(max(top - base, -126), 126);
+        const int e = v_exponent(scale[which], base);
         const float f = __builtin_amdgcn_ldexpf(scale[which], 10 - (e + base));
         if (lane < 32) {
-          s_scale[buf][0][lane] = scale[which] * a.c2;
+          s_scale[READY ? 0 : buf][0][lane] = scale[which] * a.c2;
         } else {
-          s_scale[buf][1][lane - 32] = (float)e;
-          s_scale[buf][2][lane - 32] = f;
-          s_scale[buf][3][lane - 32] = __builtin_amdgcn_ldexpf(1.f, -e);
+          s_scale[READY ? 0 : buf][1][lane - 32] = (float)e;
+          s_scale[READY ? 0 : buf][2][lane - 32] = f;
+          s_scale[READY ? 0 : buf][3][lane - 32] = __builtin_amdgcn_ldexpf(1.f, -e);
         }
         const bool odd = __any(lane >= 32 && !(fabsf(f) < INFINITY));
-        if (lane == 0) s_odd[buf] = odd;
+        if (lane == 0) s_odd[READY ? 0 : buf] = odd;
       }
     };
     auto compute = [&](int buf, int key, uint32_t valid, bool full) {
       f32x16 z = {};
-      const char* k = s_tile[buf] + row32 * K_ROW + hi * 16;
+      const char* tile = s_tile[buf];
 #pragma unroll
       for (int s = 0; s < KS; ++s)
-        z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(k + 32 * s)),
+        z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(tile + k_at(s))),
                                                     qf[s], z, 0, 0, 0);
-      const float* sc = s_scale[buf][0] + 4 * hi;
+      const float* sc = (READY ? reinterpret_cast<const float*>(tile + L::SCALES) : s_scale[READY ? 0 : buf][0]) + 4 * hi;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const f32x4 ks = *reinterpret_cast<const f32x4*>(sc + 8 * i), ev = *reinterpret_cast<const f32x4*>(sc + 32 + 8 * i);
@@ -215,7 +319,7 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
         }
       }
       l += sum[0] + sum[1];
-      if (!full && s_odd[buf]) {
+      if (!full && (READY ? *reinterpret_cast<const int*>(tile + L::ODD) : s_odd[READY ? 0 : buf])) {
         // a probability of 0 times a scale of NaN, or of a slot that holds anything
         asm volatile("" : "+v"(vis));
 #pragma unroll
@@ -225,53 +329,92 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
         pf[e >> 2][e & 3] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{z[2 * e], z[2 * e + 1]}), f16x2));
-      const char* v = s_tile[buf] + K_TILE + row32 * V_ROW + hi * 16;
 #pragma unroll
       for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          const f16x8 vf = __builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4*>(v + 32 * d * V_ROW + 32 * s));
+          const f16x8 vf = __builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4*>(tile + v_at(d, s)));
           acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, __builtin_bit_cast(f16x8, pf[s]), acc[d], 0, 0, 0);
         }
     };
 
-    if (tiles > 0) {
-      load(0, 0);
-      if (tiles > 1) load(1, 1);
-      if (wave == 0) {
-        const int e = lane >= 32 && (next_mask[0] >> (lane - 32)) & 1u ? __builtin_amdgcn_frexp_expf(scale[0]) : -1000;
-        base = (int)wave_max((float)e);
-        if (base < -90) base = 0;
-        if (lane == 0) s_base = base;
+    // a tile converted beforehand, straight into LDS
+    const char* ready = nullptr;
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)s_tile[0];
+    if constexpr (READY) ready = a.ready + ((size_t)w.h * (a.max_pages / 2) + p0 / 2) * L::BYTES + lane * 16;
+    auto request = [&](int x, int i, int buf) {
+      if ((i & 31) == 0) {
+        const int page = p0 + 2 * i + lane;
+        masks = page < p1 ? mrow[page] : 0;
       }
+      const int e = 2 * (i & 31);
+      next_mask[x] = (uint32_t)__builtin_amdgcn_readlane(masks, e) | (uint32_t)__builtin_amdgcn_readlane(masks, e + 1) << 16;
+      for (int j = wave; j < L::BYTES / 1024; j += A8_NW)
+        direct_load(ready + (size_t)i * L::BYTES + j * 1024, lds + buf * L::BYTES + j * 1024);
+    };
+    if constexpr (READY) {
+      if (tiles > 0) {
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        if (x < tiles) convert(x, x, next_mask[x]);
-        mask[x] = next_mask[x];
+        for (int x = 0; x < 2; ++x) {
+          if (x < tiles) request(x, x, x);
+          mask[x] = next_mask[x];
+        }
+        direct_wait<0>();
+        __syncthreads();
+        base = *reinterpret_cast<const int*>(s_tile[0] + L::BASE);
       }
+      for (int i = 0; i < tiles; i += 2) {
+        const int buf = i & 2;
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
-        if (2 + x < tiles) load(x, 2 + x);
-      __syncthreads();
-      base = s_base;
-    }
-    for (int i = 0; i < tiles; i += 2) {
-      const int buf = i & 2;
-      const uint32_t mk[2] = {next_mask[0], next_mask[1]};
+        for (int x = 0; x < 2; ++x)
+          if (i + 2 + x < tiles) request(x, i + 2 + x, (buf ^ 2) + x);
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
-        if (i + 2 + x < tiles) convert(x, (buf ^ 2) + x, mk[x]);
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-        if (i + 4 + x < tiles) load(x, i + 4 + x);
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int key = (p0 + 2 * (i + x)) * HK_PAGE;
-        if (i + x < tiles && key < seen_any && w0 < w.rows)
-          compute(buf + x, key, mask[x], mask[x] == 0xffffffffu && key + 32 <= seen_all);
-        mask[x] = mk[x];
+        for (int x = 0; x < 2; ++x) {
+          const int key = (p0 + 2 * (i + x)) * HK_PAGE;
+          if (i + x < tiles && key < seen_any && w0 < w.rows)
+            compute(buf + x, key, mask[x], mask[x] == 0xffffffffu && key + 32 <= seen_all);
+          mask[x] = next_mask[x];
+        }
+        direct_wait<0>();
+        __syncthreads();
       }
-      __syncthreads();
+    } else {
+      if (tiles > 0) {
+        load(0, 0);
+        if (tiles > 1) load(1, 1);
+        if (wave == 0) {
+          base = v_base(scale[0], next_mask[0]);
+          if (lane == 0) s_base = base;
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          if (x < tiles) convert(x, x, next_mask[x]);
+          mask[x] = next_mask[x];
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          if (2 + x < tiles) load(x, 2 + x);
+        __syncthreads();
+        base = s_base;
+      }
+      for (int i = 0; i < tiles; i += 2) {
+        const int buf = i & 2;
+        const uint32_t mk[2] = {next_mask[0], next_mask[1]};
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          if (i + 2 + x < tiles) convert(x, (buf ^ 2) + x, mk[x]);
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          if (i + 4 + x < tiles) load(x, i + 4 + x);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int key = (p0 + 2 * (i + x)) * HK_PAGE;
+          if (i + x < tiles && key < seen_any && w0 < w.rows)
+            compute(buf + x, key, mask[x], mask[x] == 0xffffffffu && key + 32 <= seen_all);
+          mask[x] = mk[x];
+        }
+        __syncthreads();
+      }
     }
 
     l += __shfl_xor(l, 32, 64);
@@ -308,19 +451,37 @@ using namespace hk;
 int64_t hk_attn8_tile_units(int NS, int Hkv, int G, int n_tokens) {
   return ((int64_t)n_tokens * G / TILE8_ROWS + NS) * Hkv;
 }
-size_t hk_attn8_tile_ws(int D) { return states8_bytes(D, TILE8_ROWS); }
+// Where chunks may be long, a launch before converts every tile once for all of its head's units, into the
+// workspace.  (32 / 8 heads of 128, without and with it: 8 prompts of 4096 tokens 1590 and 1403 us, of 1024 150 and
+// 143, of 512 62 and 62, of 256 55 and 59; chunks of 1024 tokens over 32000 1501 and 1482, of 512 760 and 770, of 128
+// 216 and 267: the tile kernel then reads twice the bytes.)
+constexpr int64_t READY_ROWS = 4096;
+constexpr size_t READY_MOST = (size_t)1 << 29;   // bytes of tiles at most
+static size_t ready_bytes(int D, int64_t heads, int max_pages, int64_t most) {
+  const size_t all = (size_t)heads * (max_pages / 2) * (D == 128 ? Ready8<128>::BYTES : Ready8<64>::BYTES);
+  return most >= READY_ROWS && all <= READY_MOST ? all : 0;
+}
+size_t hk_attn8_tile_ws(int D, int64_t heads, int max_pages, int64_t most) {
+  return states8_bytes(D, TILE8_ROWS) + ready_bytes(D, heads, max_pages, most);
+}
 
 template <int F, int D>
 static void launch_tile(const Args8& a, hipStream_t st) {
   const uint32_t groups = a.first ? A8_GROUPS<D> : (uint32_t)a.n_units;
   {
     TimedLaunch t(HK_TK_ATTN8, st);
-    hipLaunchKernelGGL((attn8_tile_kernel<F, D>), dim3(groups), dim3(A8_NT), 0, st, a);
+    if (a.ready) {
+      const uint32_t tiles = (uint32_t)((int64_t)a.n_seq * a.Hkv * (a.max_pages / 2));
+      hipLaunchKernelGGL((attn8_convert_kernel<F, D>), dim3(tiles), dim3(A8_NT), 0, st, a);
+      hipLaunchKernelGGL((attn8_tile_kernel<F, D, true>), dim3(groups), dim3(A8_NT), 0, st, a);
+    } else {
+      hipLaunchKernelGGL((attn8_tile_kernel<F, D, false>), dim3(groups), dim3(A8_NT), 0, st, a);
+    }
   }
   if (a.first && a.max_pages > A8_STEP) merge8<D, TILE8_ROWS, 2, true>(a, groups, st);
 }
 
-void hk_launch_attn8_tile(Args8 a, hk_dtype format, int D, void* ws, hipStream_t st) {
+void hk_launch_attn8_tile(Args8 a, hk_dtype format, int D, int64_t most, void* ws, hipStream_t st) {
   const int64_t units = hk_attn8_tile_units(a.n_seq, a.Hkv, a.G, a.n_tokens);
   a.n_units = (int)units;
   a.cap = TILE8_ROWS;
@@ -328,6 +489,7 @@ void hk_launch_attn8_tile(Args8 a, hk_dtype format, int D, void* ws, hipStream_t
   a.rows_from = A8_ROWS + 1;
   a.rows_to = INT32_MAX;
   carve8(a, planned8(units, true, a.max_pages), D, ws);
+  if (ready_bytes(D, (int64_t)a.n_seq * a.Hkv, a.max_pages, most)) a.ready = static_cast<char*>(ws) + states8_bytes(D, TILE8_ROWS);
   if (format == HK_I8) D == 128 ? launch_tile<HK_I8, 128>(a, st) : launch_tile<HK_I8, 64>(a, st);
   else D == 128 ? launch_tile<HK_E4M3, 128>(a, st) : launch_tile<HK_E4M3, 64>(a, st);
 }

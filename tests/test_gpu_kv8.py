@@ -433,6 +433,46 @@ def test_more_tiles_than_are_planned(fmt, dtype, lens):
     _attend(c, lens, Hkv, G, dtype, pad=2, heads=[0, 5, 15])
 
 
+LONG = [("i8", 128, 4, [1030, 40, 3, 0], [700, 33, 900, 50]), ("e4m3", 128, 8, [515, 17], [1, 2000]),
+        ("e4m3", 64, 4, [9, 1025, 31], [300, 0, 15]), ("i8", 64, 16, [257, 1, 2, 60], [16, 700, 0, 31])]
+
+
+@pytest.mark.parametrize("holes", [0.0, 0.35])
+@pytest.mark.parametrize("fmt,D,G,lens,ctx", LONG)
+def test_long_chunks_beside_short_ones(fmt, D, G, lens, ctx, holes):
+    """Chunks of 4096 query rows of a KV head and more, whose tiles are converted beforehand."""
+    rows = [ctx[s] - min(ctx[s], 3 * kv) + lens[s] for s in range(len(lens)) for kv in range(2)]
+    c = Cache8(rows, D, fmt, holes=holes, seed=G, keep_last=max(lens), width=256)
+    _attend(c, lens, 2, G, "bf16", pad=3, lead=2)
+
+
+@pytest.mark.parametrize("fmt", ["i8", "e4m3"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_chunks_that_may_be_long(fmt, D):
+    """The same with a short chunk where a long one was promised: sharp scores, scales near the range's ends, heads
+    without pages, NaN rows."""
+    most = dict(max_len=2048)
+    for q_scale in (40.0, 0.0):
+        _attend(Cache8([1500, 90, 0], D, fmt, seed=21, holes=0.1, keep_last=70), [40, 70, 0], 1, 2, "bf16", q_scale=q_scale, **most)
+    for size in (1e30, 1e-20):
+        _attend(Cache8([500], D, fmt, seed=2, v_scale=size), [40], 1, 4, "bf16", **most)
+    for which in ("k", "v"):
+        c = Cache8([100], D, fmt, seed=3)
+        row = int(c.t[0, 97 // 16]) * 16 + 97 % 16
+        getattr(c, which + "_scale").view(-1)[row] = float("nan")
+        _bytes(getattr(c, which + "_pool")).view(-1, D)[row] = 0
+        _, o, lse = _attend(c, [70], 1, 2, "bf16", check=False, **most)
+        assert torch.isfinite(o[:67]).all() and torch.isfinite(lse[:67]).all()
+        assert torch.isnan(o[67:]).all() and torch.isnan(lse[67:]).all() == (which == "k")
+    # V scales far apart in a head, within 2^100 of one another
+    c = Cache8([600], D, fmt, seed=3)
+    far = torch.pow(2.0, -(torch.arange(c.v_scale.numel(), device=DEV) % 7) * 9.0).view_as(c.v_scale)
+    c.v_scale.mul_(far)
+    c.v_sc[:] = c.v_scale.view(-1).cpu().numpy()
+    for long in (most, {}):
+        _attend(c, [70], 1, 2, "bf16", **long)
+
+
 # ------------------------------------------------------------------ chunks
 ATTN = [
     ("bf16", 128, 2, 4, [5], [37]),
