@@ -684,8 +684,8 @@ hk_status hk_decode_attn8(const hk_dims* dims, hk_dtype dtype, const void* q,
  * 2^24 (HK_ERR_SHAPE).
  * workspace: >= hk_chunk_attn8_workspace_size(dims, chunks, kv8->kv.max_pages) bytes, 256-byte aligned
  * (never 0 for sizes that are accepted; more tokens, longer chunks or wider tables need no less, but that
- * up to 512 MB of converted pages are asked for only where they suffice and max_len Hq / Hkv is at least
- * 4096); calls that overlap on one workspace race.
+ * up to 512 MB of converted pages are asked for only where they suffice and the smaller of max_len and
+ * n_tokens, times Hq / Hkv, is at least 4096); calls that overlap on one workspace race.
  */
 size_t hk_chunk_attn8_workspace_size(const hk_dims* dims, const hk_chunks* chunks,
                                      int32_t max_pages);

@@ -463,12 +463,15 @@ inline Plan8 plan8(int NS, int Hkv, int G, const hk_chunks* ch, bool bf, int max
 
 using namespace hk;
 
+// tokens of a chunk at most
+static int64_t longest(const hk_chunks& ch) { return std::min(ch.max_len, ch.n_tokens); }
+
 // (any chunks of no more tokens, and none longer, take no more)
 size_t hk_attn8_ws(int NS, int Hq, int Hkv, int D, const hk_chunks* ch, int max_pages) {
   const int G = Hq / Hkv;
   const bool long_ones = ch && (int64_t)ch->max_len * G > A8_ROWS;
   const size_t most = states8_bytes(D, plan8(NS, Hkv, G, ch, false, max_pages).cap);
-  return long_ones ? std::max(most, hk_attn8_tile_ws(D, (int64_t)NS * Hkv, max_pages, (int64_t)ch->max_len * G)) : most;
+  return long_ones ? std::max(most, hk_attn8_tile_ws(D, (int64_t)NS * Hkv, max_pages, longest(*ch) * G)) : most;
 }
 
 double hk_attn8_groups(int NS, int Hq, int Hkv, const hk_chunks* ch, int max_pages) {
@@ -533,6 +536,6 @@ hipError_t hk_launch_attn8(int NS, int Hq, int Hkv, int D, const hk_paged_kv8* k
   if (kv.dtype == HK_I8) launch8_f<HK_I8>(a, D, p.nq, ch != nullptr, bf, p.cut, st);
   else launch8_f<HK_E4M3>(a, D, p.nq, ch != nullptr, bf, p.cut, st);
   // (the launches follow one another: one workspace serves both)
-  if (p.tiles) hk_launch_attn8_tile(a, kv.dtype, D, (int64_t)ch->max_len * a.G, ws, st);
+  if (p.tiles) hk_launch_attn8_tile(a, kv.dtype, D, longest(*ch) * a.G, ws, st);
   return hipGetLastError();
 }
