@@ -17,13 +17,14 @@
 // from that of the unit's first keys (READY: the head's), so that y is about x; of scales below 2^-90 it counts as 0
 // (their V is below 2^-81, next to nothing).
 //
-// Measured on 8 prompts of 4096 tokens of 32 query heads, 8 KV heads of 128 dims, causal: 1403 to 1458 us, 755 to 784
-// TFLOP/s, of which the conversion is 38; 1570 to 1625 with every unit converting its tiles, and 1136 without conversions and
-// loads at all.  A bf16 matrix product of 8192^3 reaches 1236 TFLOP/s.  What bounds it is vector work beside
-// MFMA: the matrix units are busy for 34% of the cycles and the vector units for 51% (29 and 53 with every unit
-// converting), waves wait for 34% of theirs, at two a SIMD.  P in two parts of bf16, 24 products a tile instead of 16: 1930 us for 1673; one tile a barrier 1673 for
-// 1575; converting between the computations of two tiles 1660 to 1720; two tiles in one softmax spill (1767); 64 rows
-// a wave, at one wave a SIMD, 2745; eight waves of 256 rows 1629 to 1675.
+// Measured on 8 prompts of 4096 tokens of 32 query heads, 8 KV heads of 128 dims, causal: 1403 to 1458 us, 755 to
+// 784 TFLOP/s, of which the conversion is 38; 1570 to 1625 with every unit converting its tiles, and 1136 without
+// conversions and loads at all.  A bf16 matrix product of 8192^3 reaches 1236 TFLOP/s.  What bounds it is vector
+// work beside MFMA: the matrix units are busy for 34% of the cycles and the vector units for 51% (29 and 53 with
+// every unit converting), waves wait for 34% of theirs, at two a SIMD.  P in two parts of bf16, 24 products a tile
+// instead of 16: 1930 us for 1673; one tile a barrier 1673 for 1575; converting between the computations of two
+// tiles 1660 to 1720; two tiles in one softmax spill (1767); 64 rows a wave, at one wave a SIMD, 2745; eight waves
+// of 256 rows 1629 to 1675.
 #include "hk_attn8.h"
 
 namespace hk {
