@@ -661,8 +661,9 @@ hk_status hk_read_kv8(const hk_dims* dims, const hk_paged_kv8* kv8, int32_t n_la
  * fp32, lse [NS][Hq] fp32 or NULL.  Codes enter the products exactly; q, scores, probabilities, sums
  * and outputs keep fp32.  A head with no valid slot gives o = 0, lse = -inf.  What masked slots and
  * slots past the row's end hold is not read into the result.  Sums stay finite to the top of the fp32
- * range; values below 2^-80 (1e-24) lose bits.  A valid slot must not hold an e4m3 code of NaN (0x7f,
- * 0xff): hk_write_kv8 writes none, and what the sequence's results then are is not said.
+ * range; values below 2^-80 (1e-24) lose bits, probabilities below 2^-125 may count as 0.  A valid slot
+ * must not hold an e4m3 code of NaN (0x7f, 0xff): hk_write_kv8 writes none, and what the sequence's
+ * results then are is not said.
  * How rows are split over workgroups follows from the lengths of all rows of the call, so the last bits
  * of o and lse can change with the batch; the same call gives the same bits.  q times a row's codes has
  * to stay in the fp32 range.
@@ -679,7 +680,7 @@ hk_status hk_decode_attn8(const hk_dims* dims, hk_dtype dtype, const void* q,
  * strides and limits of hk_chunk_attn otherwise; range, codes and bits as for hk_decode_attn8.
  * Precision: fp32 rows keep all of P's bits.  With bf16 rows P enters the product with V to 2^-16 of a
  * term in chunks of up to 32 queries of a KV head; in longer ones to 2^-11, and terms below 2^-33 of a
- * query's largest can be lost.  These longer ones want the V scales of a head within 2^100 of one another.
+ * query's largest can be lost, whatever the sizes of a head's V rows.
  * Where chunks can have more than 32 queries of a KV head, (n_tokens G / 32 + n_seq) Hkv has to stay below
  * 2^24 (HK_ERR_SHAPE).
  * workspace: >= hk_chunk_attn8_workspace_size(dims, chunks, kv8->kv.max_pages) bytes, 256-byte aligned

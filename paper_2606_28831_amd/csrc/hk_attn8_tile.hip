@@ -15,7 +15,10 @@
 // V's scale s = f 2^e, f in [1/2, 1), and y = x + e, P = exp2(y - m) f 2^10 is at most 2^14, and smaller terms
 // keep their bits down to 2^-24 of the largest.  The softmax's sum takes exp2(y - m) 2^-e.  e is counted
 // from that of the unit's first keys (READY: the head's), so that y is about x; of scales below 2^-90 it counts as 0
-// (their V is below 2^-81, next to nothing).
+// (their V is below 2^-81, next to nothing).  Where a valid key has an e past FAR8 in size, that sum could leave the
+// range, or lose keys whose V is small: 2^-e is NaN there, and a unit that finds its sum to be NaN is computed again
+// with a reference of the sum's own, which follows x (a check in every tile instead: 1435 to 1495 us for 1400 to
+// 1460 of the prompts below).
 //
 // Measured on 8 prompts of 4096 tokens of 32 query heads, 8 KV heads of 128 dims, causal: 1403 to 1458 us, 755 to
 // 784 TFLOP/s, of which the conversion is 38; 1570 to 1625 with every unit converting its tiles, and 1136 without
@@ -25,11 +28,16 @@
 // instead of 16: 1930 us for 1673; one tile a barrier 1673 for 1575; converting between the computations of two
 // tiles 1660 to 1720; two tiles in one softmax spill (1767); 64 rows a wave, at one wave a SIMD, 2745; eight waves
 // of 256 rows 1629 to 1675.
+#include <type_traits>
+
 #include "hk_attn8.h"
 
 namespace hk {
 
 constexpr int TILE8_ROWS = 128;
+// Where every e is within it, a key of 2^-58 and more of the sum is in the range of exp2(y - m): y is at least
+// m - SLACK - 2 FAR8 - 58.
+constexpr int FAR8 = 32;
 
 // A converted tile: K by rows and V by dims, whose 16-byte pieces lie in turned orders so that 16 lanes of
 // a fragment's read meet no bank twice; K's scales times c2, V's e, f 2^10 and 2^-e; `odd` and what e is counted from.
@@ -47,7 +55,13 @@ struct Ready8 {
 // V's scale as e, f 2^10 (see above)
 __device__ __forceinline__ int v_exponent(float scale, int base) {
   const int top = __builtin_amdgcn_frexp_expf(scale);
-  return top < -90 ? 0 : min(max(top - base, -126), 126);
+  return top < -90 ? 0 : top - base;
+}
+// 2^-e of key i, NaN past FAR8; of a slot that is not valid, whose scale may be anything, in range: its p is 0
+__device__ __forceinline__ float v_back(int e, int i, uint32_t mask) {
+  float back = __builtin_amdgcn_ldexpf(1.f, -e);
+  if (__builtin_expect(__any(fabsf((float)e) > FAR8), 0) && abs(e) > FAR8) back = (mask >> i) & 1u ? __builtin_nanf("") : 1.f;
+  return back;
 }
 // of 32 keys, in lanes 32 .. 63
 __device__ __forceinline__ int v_base(float scale, uint32_t mask) {
@@ -119,7 +133,7 @@ __global__ __launch_bounds__(A8_NT) void attn8_convert_kernel(Args8 a) {
     } else {
       out[32] = (float)e;
       out[64] = f;
-      out[96] = __builtin_amdgcn_ldexpf(1.f, -e);
+      out[96] = v_back(e, lane & 31, mask);
     }
     const bool odd = __any(lane >= 32 && !(fabsf(f) < INFINITY));
     if (lane == 0) *reinterpret_cast<u32x2*>(to + L::ODD) = u32x2{odd ? 1u : 0u, (uint32_t)base};
@@ -140,6 +154,7 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
   __shared__ int s_base;                                      // what e is counted from
   __shared__ int s_odd[READY ? 1 : NT];                       // whether an f is NaN or infinite
   __shared__ int s_sums[A8_NW];
+  __shared__ int s_again;                                     // the last unit with a sum of NaN
   const int lane = threadIdx.x & 63, row32 = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool is_v = wave >= 2;
@@ -158,6 +173,7 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
   };
 
   int u = a.n_units - 1 - (int)blockIdx.x, skip = 0, left = 1 << 30;
+  if (threadIdx.x == 0) s_again = -1;
   if (a.first) {
     static_assert(sizeof(s_tile) >= (A8_UNITS + 1) * sizeof(int));
     const Run r = run_of_group<TILE8_ROWS, true>(a, reinterpret_cast<int*>(s_tile), s_sums);
@@ -194,6 +210,7 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
       for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qf[s]));
     }
     float m = -INFINITY, off = 0.f, l = 0.f;                  // off: m, or 0 while there is none
+    float ahead = 0.f;                                        // l's reference is off plus this whole number
     f32x16 acc[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -266,19 +283,28 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
         } else {
           s_scale[READY ? 0 : buf][1][lane - 32] = (float)e;
           s_scale[READY ? 0 : buf][2][lane - 32] = f;
-          s_scale[READY ? 0 : buf][3][lane - 32] = __builtin_amdgcn_ldexpf(1.f, -e);
+          s_scale[READY ? 0 : buf][3][lane - 32] = v_back(e, lane - 32, mk);
         }
         const bool odd = __any(lane >= 32 && !(fabsf(f) < INFINITY));
         if (lane == 0) s_odd[READY ? 0 : buf] = odd;
       }
     };
-    auto compute = [&](int buf, int key, uint32_t valid, bool full) {
+    auto compute = [&](auto far, int buf, int key, uint32_t valid, bool full) {
       f32x16 z = {};
       const char* tile = s_tile[buf];
 #pragma unroll
       for (int s = 0; s < KS; ++s)
         z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(tile + k_at(s))),
                                                     qf[s], z, 0, 0, 0);
+      if constexpr (!READY) {
+        // reads ahead of the products (left to the compiler, each waits for its own: 4 to 5% slower)
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+          if (s < KS - 2) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+      }
       const float* sc = (READY ? reinterpret_cast<const float*>(tile + L::SCALES) : s_scale[READY ? 0 : buf][0]) + 4 * hi;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -296,17 +322,38 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
       float zm = z[0];
 #pragma unroll
       for (int e = 1; e < 16; ++e) zm = fmaxf(zm, z[e]);
-      if (__builtin_expect(__any(zm > m + A8_SLACK), 0)) {
+      if (far.value || __builtin_expect(__any(zm > m + A8_SLACK), 0)) {
         zm = fmaxf(zm, __shfl_xor(zm, 32, 64));
         const float mn = fmaxf(m, ceilf(zm));
         const float alpha = m == -INFINITY ? 0.f : fast_exp2(m - mn);
+        const float to = mn == -INFINITY ? 0.f : mn;
+        if constexpr (far.value) ahead += off - to;
+        else l *= alpha;
         m = mn;
-        off = mn == -INFINITY ? 0.f : mn;
-        l *= alpha;
+        off = to;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
           for (int e = 0; e < 16; ++e) acc[d][e] *= alpha;
+      }
+      if constexpr (far.value) {
+        // (y - off - e, in this order: of scores past 2^24 the first difference is exact, and P and l agree)
+        const auto x = [&](int e) { return z[e] - off - sc[32 + (e & 3) + 8 * (e >> 2)]; };
+        float zx = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          zx = fmaxf(zx, x(e));
+          if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        }
+        zx = fmaxf(zx, __shfl_xor(zx, 32, 64));
+        const float an = fmaxf(ahead, ceilf(zx)), less = an == -INFINITY ? 0.f : an;
+        l *= ahead == -INFINITY ? 0.f : fast_exp2(ahead - an);      // (a sum of NaN stays one)
+        ahead = an;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          l += fast_exp2(x(e) - less);
+          if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        }
       }
       float sum[2] = {0.f, 0.f};
 #pragma unroll
@@ -319,7 +366,7 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
           z[4 * i + j] = p * f[j];
         }
       }
-      l += sum[0] + sum[1];
+      if constexpr (!far.value) l += sum[0] + sum[1];
       if (!full && (READY ? *reinterpret_cast<const int*>(tile + L::ODD) : s_odd[READY ? 0 : buf])) {
         // a probability of 0 times a scale of NaN, or of a slot that holds anything
         asm volatile("" : "+v"(vis));
@@ -373,7 +420,7 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
         for (int x = 0; x < 2; ++x) {
           const int key = (p0 + 2 * (i + x)) * HK_PAGE;
           if (i + x < tiles && key < seen_any && w0 < w.rows)
-            compute(buf + x, key, mask[x], mask[x] == 0xffffffffu && key + 32 <= seen_all);
+            compute(std::false_type{}, buf + x, key, mask[x], mask[x] == 0xffffffffu && key + 32 <= seen_all);
           mask[x] = next_mask[x];
         }
         direct_wait<0>();
@@ -411,9 +458,38 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
         for (int x = 0; x < 2; ++x) {
           const int key = (p0 + 2 * (i + x)) * HK_PAGE;
           if (i + x < tiles && key < seen_any && w0 < w.rows)
-            compute(buf + x, key, mask[x], mask[x] == 0xffffffffu && key + 32 <= seen_all);
+            compute(std::false_type{}, buf + x, key, mask[x], mask[x] == 0xffffffffu && key + 32 <= seen_all);
           mask[x] = mk[x];
         }
+        __syncthreads();
+      }
+    }
+
+    // (a unit's waves read s_again before the barriers of the next one that could write it)
+    if (tiles > 0) {
+      if (__any(l != l) && lane == 0) s_again = u;
+      __syncthreads();
+    }
+    if (tiles > 0 && __builtin_amdgcn_readfirstlane(s_again) == u) {
+      m = -INFINITY;
+      off = 0.f;
+      l = 0.f;
+      ahead = -INFINITY;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[d][e] = 0.f;
+      for (int i = 0; i < tiles; ++i) {
+        if constexpr (READY) {
+          request(0, i, 0);
+          direct_wait<0>();
+        } else {
+          load(0, i);
+          convert(0, 0, next_mask[0]);
+        }
+        __syncthreads();
+        const int key = (p0 + 2 * i) * HK_PAGE;
+        compute(std::true_type{}, 0, key, next_mask[0], false);
         __syncthreads();
       }
     }
@@ -421,7 +497,8 @@ __global__ __launch_bounds__(A8_NT, 2) void attn8_tile_kernel(Args8 a) {
     l += __shfl_xor(l, 32, 64);
     if (w0 + row32 < w.rows) {
       // l is brought to [1/2, 1): scales far apart leave sums far apart
-      const int up = __builtin_amdgcn_frexp_expf(l), down = base + Code<F>::F16_DOWN - 10 - up;
+      const int up = __builtin_amdgcn_frexp_expf(l) + (ahead == -INFINITY ? 0 : (int)ahead);
+      const int down = base + Code<F>::F16_DOWN - 10 - up;
       l = __builtin_amdgcn_frexp_mantf(l);
       m = off + (float)up;                                    // (NaN keys alone leave a sum of NaN and no reference)
       const float inv = l == 0.f ? 0.f : 1.f / l;             // (a NaN stays one)
