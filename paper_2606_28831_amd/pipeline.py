@@ -62,8 +62,15 @@ class ScoringCopy:
         self.lse = torch.empty(W * n * Hq, dtype=torch.float32, device=dev)
         self.ws = workspace(OP_SCORE, dims(n, Hq, Hkv, D, W), P, dev)
 
+    def takes(self, q_obs):
+        """Refuse window queries that a copy in score_dtype would round."""
+        dtype = self.k.dtype
+        if q_obs.dtype != dtype and (q_obs.dtype, dtype) != (torch.bfloat16, torch.float32):
+            raise HardKVError(f"window queries of {q_obs.dtype} over K read back in {dtype}: give their type as score_dtype")
+
     def groups(self, q_obs, stream=None):
         """For every few sequences: (their dims, first head, heads, sequences as a slice, queries, K)."""
+        self.takes(q_obs)
         for s0 in range(0, self.NS, self.n):
             ns = min(self.n, self.NS - s0)
             h0, H, sl = s0 * self.Hkv, ns * self.Hkv, slice(s0, s0 + ns)
@@ -94,8 +101,9 @@ def _compact(d, kv, sel_bits, L_dense, L_sparse, alloc, status, ws, stream):
 class Compressor:
     """One compression step over every head of a paged cache.
 
-    An 8-bit cache (PagedKV8) is scored on copies of its K, read back in score_dtype, the type of its
-    window queries, and rewritten as it lies.
+    An 8-bit cache (PagedKV8) is scored on copies of its K, read back in score_dtype, and rewritten as it
+    lies.  score_dtype is the type of the window queries, or float32 for bfloat16 ones, whose K is then not
+    rounded; others are refused.
 
     metric "attn": attention mass over the window, calibrated with T = 1.
     metric "attn+red": attention mass and key redundancy, each calibrated (the
@@ -215,7 +223,8 @@ class BudgetCompressor:
 
     rank_by_c: break ties in the votes by the window's calibrated mean attention (adds the
     attention-mass pass and the calibration); otherwise by recency.  The per-row
-    probabilities take n_heads * G * W * S_max * 4 bytes (buf["a_rows"]).
+    probabilities take n_heads * G * W * S_max * 4 bytes (buf["a_rows"]).  8-bit caches and score_dtype
+    as for Compressor.
     """
 
     def __init__(self, NS, Hq, Hkv, D, W, kv: PagedKV, alloc: Allocator, p: float,
@@ -266,6 +275,8 @@ class BudgetCompressor:
                 b["row_lse"][:, sl].copy_(lse)
 
     def select(self, q_obs, stream=None):
+        if self.copy is not None:
+            self.copy.takes(q_obs)
         b, H, S, pm = self.buf, self.n_heads, self.S_max, self.kv.page_mask
         hk_budget_plan(self.d, self.kv, self.L_dense, self.L_lower, self.L_upper, b["head_mode"],
                        b["k_cap"], stream=stream)
@@ -432,7 +443,8 @@ class DecodeLoop:
                 every layer.  After an extend() whose slots were refused (status) it takes
                 nothing back and draws no token (-1): the cache stays as it was.
     Heads are ordered (layer, sequence, KV head); sequence index = layer * B + b.
-    An 8-bit cache (PagedKV8) takes queries, K and V in bf16 (score_dtype), and so o of extend().
+    An 8-bit cache (PagedKV8) takes queries, K and V in bf16 or fp32, and o of extend() in the queries'
+    type; compress() takes window queries as Compressor does (fp32 ones: score_dtype=torch.float32).
     """
 
     def __init__(self, L, B, Hq, Hkv, D, W, kv: PagedKV, alloc: Allocator, p: float,
@@ -498,6 +510,8 @@ class DecodeLoop:
     def segment(self, q_seg, k_seg, v_seg, lse_seg, stream=None):
         """len(q_seg) decode steps, then one compression over the last W steps' queries
         and their decode LSEs (Sec. 3.1 Steps 1-3)."""
+        if self.bits8:
+            self.comp.copy.takes(q_seg)
         T = q_seg.shape[0]
         for t in range(T):
             self.step(q_seg[t], k_seg[t], v_seg[t], lse_seg[t], stream=stream)

@@ -1,0 +1,72 @@
+"""Scores and selections of an 8-bit cache, in groups of sequences, against those of a cache that holds what its
+rows read back as: the same kernels over the same numbers, so the same bits."""
+import numpy as np
+import pytest
+import torch
+
+import oracle.kv8_oracle as O8
+from test_gpu_kv8 import DEV, DT, I32, Cache8
+
+pytestmark = pytest.mark.gpu
+NS, HKV, G, D, W = 5, 2, 2, 64, 4
+
+
+def _caches(dtype, fmt="i8"):
+    """An 8-bit cache and one of its rows in `dtype`, with their allocators."""
+    import paper_2606_28831_amd as hk
+    c = Cache8([100 + 37 * i for i in range(NS * HKV)], D, fmt, holes=0.1, seed=6, spare=400)
+    pools = []
+    for codes, s in ((c.k_codes, c.k_sc), (c.v_codes, c.v_sc)):
+        x = torch.tensor(O8.values(codes, fmt) * s.astype(np.float64)[:, None]).float().to(DT[dtype])
+        pools.append(x.to(DEV).view(-1, 16, D))
+    plain = hk.PagedKV(pools[0], pools[1], c.page_table.clone(), c.page_mask.clone(), c.n_pages.clone())
+    return c, plain, hk.Allocator(c.free_ids.clone(), c.free_top.clone())
+
+
+def _queries(dtype, seed=1):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    return torch.randn(W, NS, HKV * G, D, generator=g, device=DEV).to(DT[dtype])
+
+
+def _in_groups(x, c, dtype):
+    """The compressor's copies made small: groups of 2, 2 and 1 sequences."""
+    from paper_2606_28831_amd.pipeline import ScoringCopy
+    small = ScoringCopy(NS, HKV * G, HKV, D, W, c.kv, DT[dtype], max_bytes=2 * HKV * c.width * 16 * D * DT[dtype].itemsize)
+    assert small.n == 2
+    x.copy = small
+    if isinstance(x.buf, dict):
+        x.buf["ws_score"] = small.ws
+    else:
+        x.buf.ws_score = small.ws
+    return x
+
+
+def _same(a, b, names, c, plain, al):
+    torch.cuda.synchronize()
+    a, b = (m if isinstance(m, dict) else vars(m) for m in (a.buf, b.buf))
+    assert int(a["status"]) == 0 and int(b["status"]) == 0
+    for name in names:
+        assert torch.equal(a[name], b[name]), name
+    for x, y in ((c.page_mask, plain.page_mask), (c.n_pages, plain.n_pages), (c.page_table, plain.page_table),
+                 (c.free_ids, al.free_ids), (c.free_top, al.free_top)):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("fmt", ["i8", "e4m3"])
+@pytest.mark.parametrize("budget", [False, True])
+@pytest.mark.parametrize("q_dtype", ["f32", "bf16"])
+def test_scores_in_fp32(q_dtype, budget, fmt):
+    """K read back in fp32, with fp32 queries or bf16 ones widened."""
+    from paper_2606_28831_amd.pipeline import BudgetCompressor, Compressor
+    c, plain, al = _caches("f32", fmt)
+    q = _queries(q_dtype)
+    made = []
+    for kv, alloc, more in ((c.kv, c.alloc, dict(score_dtype=torch.float32)), (plain, al, {})):
+        if budget:
+            x = BudgetCompressor(NS, HKV * G, HKV, D, W, kv, alloc, 0.8, 100, 200, L_dense=32, n_sink=4, rank_by_c=True, **more)
+        else:
+            x = Compressor(NS, HKV * G, HKV, D, W, kv, alloc, 0.8, L_dense=32, **more)
+        made.append(x)
+    _in_groups(made[0], c, "f32").step(q)
+    made[1].step(q.float())
+    _same(made[0], made[1], ("cand_len", "row_lse", "s_attn", "sel_bits", "k") + (("votes", "head_mode") if budget else ()), c, plain, al)

@@ -1,0 +1,58 @@
+"""What the compressors refuse of the window queries of an 8-bit cache, without a GPU."""
+import pytest
+import torch
+
+BF, F32, I32 = torch.bfloat16, torch.float32, torch.int32
+NS, HKV, G, D, W = 5, 2, 2, 64, 4
+
+
+@pytest.fixture(scope="module")
+def hk():
+    import paper_2606_28831_amd as m
+    m.lib()
+    return m
+
+
+def _cache(hk, heads=NS * HKV, pages=20, width=4):
+    z = lambda *s, dt=torch.uint8: torch.zeros(*s, dtype=dt)  # noqa: E731
+    kv = hk.PagedKV8(z(pages, 16, D).view(torch.int8), z(pages, 16, D).view(torch.int8), z(pages, 16, dt=F32),
+                     z(pages, 16, dt=F32), z(heads, width, dt=I32), z(heads, width, dt=torch.int16), z(heads, dt=I32))
+    return kv, hk.Allocator(z(pages, dt=I32), z(1, dt=I32))
+
+
+def _compressor(hk, **more):
+    from paper_2606_28831_amd.pipeline import Compressor
+    kv, al = _cache(hk)
+    return Compressor(NS, HKV * G, HKV, D, W, kv, al, 0.8, **more)
+
+
+def _q(dtype, *shape):
+    return torch.zeros(*(shape or (W, NS, HKV * G, D)), dtype=dtype)
+
+
+def test_queries_are_not_rounded_without_a_word(hk):
+    from paper_2606_28831_amd.pipeline import BudgetCompressor, DecodeLoop
+    comp = _compressor(hk)
+    for dtype in (F32, torch.float16, torch.float64):
+        for call in (comp.score, comp.step):
+            with pytest.raises(hk.HardKVError, match="score_dtype"):
+                call(_q(dtype))
+    kv, al = _cache(hk)
+    budget = BudgetCompressor(NS, HKV * G, HKV, D, W, kv, al, 0.8, 100, 200)
+    for call in (budget.select, budget.step):
+        with pytest.raises(hk.HardKVError, match="score_dtype"):
+            call(_q(F32))
+    loop = DecodeLoop(1, NS, HKV * G, HKV, D, W, kv, al, 0.8, 16)
+    with pytest.raises(hk.HardKVError, match="score_dtype"):
+        loop.compress(_q(F32), torch.zeros(W, NS, HKV * G))
+    with pytest.raises(hk.HardKVError, match="score_dtype"):     # (before a step of the segment is taken)
+        loop.segment(_q(F32), _q(F32, W, NS, HKV, D), _q(F32, W, NS, HKV, D), torch.zeros(W, NS, HKV * G))
+    with pytest.raises(hk.HardKVError, match="score_dtype"):
+        _compressor(hk, score_dtype=F32).score(_q(torch.float64))
+
+
+def test_queries_of_the_type_or_widened_go_on(hk):
+    """(to the call that wants a GPU)"""
+    for dtype, to in ((BF, BF), (F32, F32), (BF, F32)):
+        with pytest.raises(hk.HardKVError, match="outside the GPU"):
+            _compressor(hk, score_dtype=to).score(_q(dtype))
