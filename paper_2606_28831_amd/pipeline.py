@@ -42,6 +42,17 @@ class CompressBuffers:
     ws_select: torch.Tensor
 
 
+def _shaped(t, shape, dtype, what: str):
+    """t in a shape that can be cut by head or sequence: a contiguous one may come in any other."""
+    if t.dtype != dtype:
+        raise HardKVError(f"{what} must be {dtype}")
+    if tuple(t.shape) == shape:
+        return t
+    if t.numel() != math.prod(shape) or not t.is_contiguous():
+        raise HardKVError(f"{what} must be {list(shape)}")
+    return t.view(shape)
+
+
 class ScoringCopy:
     """K of an 8-bit cache read back in bf16 or fp32, a few sequences at a time, as the score passes
     take it: a paged cache of its own whose rows lie one after the other, at most max_bytes of it."""
@@ -71,6 +82,7 @@ class ScoringCopy:
     def groups(self, q_obs, stream=None):
         """For every few sequences: (their dims, first head, heads, sequences as a slice, queries, K)."""
         self.takes(q_obs)
+        q_obs = _shaped(q_obs, (self.W, self.NS, self.Hq, self.D), q_obs.dtype, "window queries")
         for s0 in range(0, self.NS, self.n):
             ns = min(self.n, self.NS - s0)
             h0, H, sl = s0 * self.Hkv, ns * self.Hkv, slice(s0, s0 + ns)
@@ -159,6 +171,10 @@ class Compressor:
     def score(self, q_obs, ref_slots=None, row_lse_in=None, stream=None):
         b = self.buf
         if self.copy is not None:
+            if ref_slots is not None:
+                ref_slots = _shaped(ref_slots, (self.n_heads, self.n_ref), torch.int32, "ref_slots")
+            if row_lse_in is not None:
+                row_lse_in = _shaped(row_lse_in, tuple(b.row_lse.shape), torch.float32, "row_lse_in")
             for d, h0, H, sl, q, kv in self.copy.groups(q_obs, stream):
                 heads, lse = slice(h0, h0 + H), self.copy.group_lse(sl)
                 if row_lse_in is not None:

@@ -70,3 +70,26 @@ def test_scores_in_fp32(q_dtype, budget, fmt):
     _in_groups(made[0], c, "f32").step(q)
     made[1].step(q.float())
     _same(made[0], made[1], ("cand_len", "row_lse", "s_attn", "sel_bits", "k") + (("votes", "head_mode") if budget else ()), c, plain, al)
+
+
+@pytest.mark.parametrize("flat", [False, True])
+@pytest.mark.parametrize("red", [False, True])
+@pytest.mark.parametrize("given", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_references_and_given_lses_in_groups(dtype, given, red, flat):
+    """Redundancy and row LSEs of the caller's, cut for groups of sequences; in another shape too."""
+    from paper_2606_28831_amd.pipeline import Compressor
+    c, plain, al = _caches(dtype)
+    q, H = _queries(dtype), NS * HKV
+    more = dict(metric="attn+red", n_ref=6) if red else {}
+    x = Compressor(NS, HKV * G, HKV, D, W, c.kv, c.alloc, 0.8, L_dense=32, score_dtype=DT[dtype], **more)
+    y = Compressor(NS, HKV * G, HKV, D, W, plain, al, 0.8, L_dense=32, **more)
+    rng = np.random.default_rng(5)
+    ref = torch.tensor(np.array([rng.choice(c.slots(h), 6, replace=False) for h in range(H)]), dtype=I32, device=DEV) if red else None
+    lse = torch.randn(W, NS, HKV * G, device=DEV, generator=torch.Generator(device=DEV).manual_seed(3)) + 4.0 if given else None
+    shaped = lambda t, *s: t if t is None or not flat else t.view(*s)  # noqa: E731
+    _in_groups(x, c, dtype).step(shaped(q, W, NS, HKV, G, D), ref_slots=shaped(ref, NS, HKV, 6),
+                                 row_lse_in=shaped(lse, W * NS, HKV * G))
+    y.step(q, ref_slots=ref, row_lse_in=lse)
+    _same(x, y, ("cand_len", "s_attn", "sel_bits", "k") + (() if given else ("row_lse",)) +
+          (("x_red", "T_red") if red else ()), c, plain, al)

@@ -56,3 +56,31 @@ def test_queries_of_the_type_or_widened_go_on(hk):
     for dtype, to in ((BF, BF), (F32, F32), (BF, F32)):
         with pytest.raises(hk.HardKVError, match="outside the GPU"):
             _compressor(hk, score_dtype=to).score(_q(dtype))
+
+
+def test_arguments_are_cut_by_sequence_only_where_they_fit(hk):
+    """References, LSEs and queries go to the score pass a few sequences at a time: what does not hold one entry for
+    each head or row would be read past its end, or spread over rows it is not of."""
+    comp, q = _compressor(hk, metric="attn+red", n_ref=3), _q(BF)
+    H, Hq = NS * HKV, HKV * G
+    ref = torch.zeros(H, 3, dtype=I32)
+    for bad in (ref[:7], ref[:, :2].contiguous(), ref.long(), torch.zeros(H, 4, dtype=I32), torch.zeros(H * 3 - 1, dtype=I32)):
+        with pytest.raises(hk.HardKVError, match="ref_slots"):
+            comp.score(q, ref_slots=bad)
+    for bad in (torch.zeros(W, 1, Hq), torch.zeros(1, NS, Hq), torch.zeros(W, NS), torch.zeros(W, NS, Hq, dtype=BF),
+                torch.zeros(W, Hq, NS).transpose(1, 2)[:, :, :1], torch.zeros(NS, W, Hq).transpose(0, 1)[:2]):
+        with pytest.raises(hk.HardKVError, match="row_lse_in"):
+            comp.score(q, row_lse_in=bad)
+    for bad in (_q(BF, 1, NS, Hq, D), _q(BF, W, 1, Hq, D), _q(BF, W, NS, Hq, 1), _q(BF, W, NS, Hq), _q(BF, W, NS, Hq, D + 64)):
+        with pytest.raises(hk.HardKVError, match="window queries"):
+            comp.score(bad)
+
+
+def test_arguments_of_another_shape_with_as_many_entries_go_on(hk):
+    """(to the call that wants a GPU: contiguous ones are one buffer in any shape)"""
+    comp, Hq = _compressor(hk, metric="attn+red", n_ref=3), HKV * G
+    for q, ref, lse in ((_q(BF, W, NS, HKV, G, D), torch.zeros(NS, HKV, 3, dtype=I32), torch.zeros(W, NS * Hq)),
+                        (_q(BF, W * NS * Hq * D), torch.zeros(NS * HKV * 3, dtype=I32), torch.zeros(W * NS * Hq)),
+                        (_q(BF, NS, W, Hq, D).transpose(0, 1), None, torch.zeros(NS, W, Hq).transpose(0, 1))):
+        with pytest.raises(hk.HardKVError, match="outside the GPU"):
+            comp.score(q, ref_slots=ref, row_lse_in=lse)
