@@ -629,7 +629,10 @@ hk_status hk_compact_modes(const hk_dims* dims, const hk_paged_kv* kv, const uin
  * back as NaN, and so do the results of the queries that see it.
  * Tables, masks, allocator and slot maps are those of hk_paged_kv: hk_reserve_slots, hk_trim_slots and
  * hk_budget_plan take &kv8->kv as it is.  hk_score and hk_score_rows take K read back (hk_read_kv8);
- * the selection then goes to hk_compact8.
+ * the selection then goes to hk_compact8.  Read back in fp32 K is what the hk_*_attn8 calls see (to fp32
+ * rounding); in bf16 it is rounded once more, by 2^-9 of each value, which moves a score by up to
+ * 2^-9 sm_scale sum_d |q_d k_d|: row LSEs of hk_decode_attn8 given to hk_score as row_lse_in then are not
+ * quite those of the scores, and a row's probabilities sum to 1 within e^ that.
  */
 typedef struct {
   hk_paged_kv kv;        /* pools of codes, [num_pages][16][D] bytes; kv.dtype HK_I8 or HK_E4M3 */

@@ -115,7 +115,8 @@ class Compressor:
 
     An 8-bit cache (PagedKV8) is scored on copies of its K, read back in score_dtype, and rewritten as it
     lies.  score_dtype is the type of the window queries, or float32 for bfloat16 ones, whose K is then not
-    rounded; others are refused.
+    rounded; others are refused.  K in bfloat16 moves a score by up to 2^-9 sm_scale sum |q k| against what
+    hk_decode_attn8 sees: rows scored under its LSEs (row_lse_in) sum to 1 within e^ that.
 
     metric "attn": attention mass over the window, calibrated with T = 1.
     metric "attn+red": attention mass and key redundancy, each calibrated (the

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import oracle.kv8_oracle as O8
+from hk_testlib import np64
 from test_gpu_kv8 import DEV, DT, I32, Cache8
 
 pytestmark = pytest.mark.gpu
@@ -41,15 +42,17 @@ def _in_groups(x, c, dtype):
     return x
 
 
-def _same(a, b, names, c, plain, al):
+def _same(a, b, names):
     torch.cuda.synchronize()
+    kvs, als = (a.kv, b.kv), (a.alloc, b.alloc)
     a, b = (m if isinstance(m, dict) else vars(m) for m in (a.buf, b.buf))
     assert int(a["status"]) == 0 and int(b["status"]) == 0
     for name in names:
         assert torch.equal(a[name], b[name]), name
-    for x, y in ((c.page_mask, plain.page_mask), (c.n_pages, plain.n_pages), (c.page_table, plain.page_table),
-                 (c.free_ids, al.free_ids), (c.free_top, al.free_top)):
-        assert torch.equal(x, y)
+    for what in ("page_mask", "n_pages", "page_table"):
+        assert torch.equal(getattr(kvs[0], what), getattr(kvs[1], what)), what
+    for what in ("free_ids", "free_top"):
+        assert torch.equal(getattr(als[0], what), getattr(als[1], what)), what
 
 
 @pytest.mark.parametrize("fmt", ["i8", "e4m3"])
@@ -69,7 +72,7 @@ def test_scores_in_fp32(q_dtype, budget, fmt):
         made.append(x)
     _in_groups(made[0], c, "f32").step(q)
     made[1].step(q.float())
-    _same(made[0], made[1], ("cand_len", "row_lse", "s_attn", "sel_bits", "k") + (("votes", "head_mode") if budget else ()), c, plain, al)
+    _same(made[0], made[1], ("cand_len", "row_lse", "s_attn", "sel_bits", "k") + (("votes", "head_mode") if budget else ()))
 
 
 @pytest.mark.parametrize("flat", [False, True])
@@ -92,4 +95,64 @@ def test_references_and_given_lses_in_groups(dtype, given, red, flat):
                                  row_lse_in=shaped(lse, W * NS, HKV * G))
     y.step(q, ref_slots=ref, row_lse_in=lse)
     _same(x, y, ("cand_len", "s_attn", "sel_bits", "k") + (() if given else ("row_lse",)) +
-          (("x_red", "T_red") if red else ()), c, plain, al)
+          (("x_red", "T_red") if red else ()))
+
+
+def _read_back(loop_kv, dtype):
+    """A cache of the rows' values in `dtype`, every valid slot read back (the others 0), with the same tables."""
+    import paper_2606_28831_amd as hk
+    pages, _, d = loop_kv.k_pool.shape
+    pools = []
+    for codes, s in ((loop_kv.k_pool, loop_kv.k_scale), (loop_kv.v_pool, loop_kv.v_scale)):
+        x = (codes.float() * s[..., None]).nan_to_num(0.0)
+        pools.append(x.to(DT[dtype]).contiguous())
+    return hk.PagedKV(pools[0], pools[1], loop_kv.page_table.clone(), loop_kv.page_mask.clone(), loop_kv.n_pages.clone())
+
+
+@pytest.mark.parametrize("score", ["bf16", "f32"])
+@pytest.mark.parametrize("fmt", ["i8", "e4m3"])
+def test_a_loop_selects_by_its_rows_as_they_read_back(fmt, score):
+    """The selection of DecodeLoop.compress, from the steps' own LSEs over the codes, is that of a compressor over
+    the rows read back, given the same LSEs."""
+    import paper_2606_28831_amd as hk
+    from paper_2606_28831_amd.pipeline import Compressor, DecodeLoop
+    from test_gpu_kv8 import _empty
+    L, B = 2, 3
+    kv, al = _empty(L * B * HKV, D, fmt, 20, 400)
+    loop = DecodeLoop(L, B, HKV * G, HKV, D, W, kv, al, 0.7, 16, score_dtype=DT[score])
+    g = torch.Generator(device=DEV).manual_seed(8)
+    rnd = lambda *s: torch.randn(*s, generator=g, device=DEV).to(torch.bfloat16)  # noqa: E731
+    for i in range(3):
+        n = 40 if i == 0 else W
+        q, k, v = rnd(n, L * B, HKV * G, D), rnd(n, L * B, HKV, D), rnd(n, L * B, HKV, D)
+        lse = torch.empty(n, L * B, HKV * G, device=DEV)
+        for t in range(n):
+            loop.step(q[t], k[t], v[t], lse[t])
+        plain = _read_back(kv, score)
+        comp = Compressor(L * B, HKV * G, HKV, D, W, plain, hk.Allocator(al.free_ids.clone(), al.free_top.clone()), 0.7, L_dense=16)
+        loop.compress(q[n - W:], lse[n - W:])
+        comp.step(q[n - W:].to(DT[score]), row_lse_in=lse[n - W:].contiguous())
+        _same(loop.comp, comp, ("cand_len", "s_attn", "sel_bits", "k"))
+        assert int(loop.status) == 0 and 0 < int(loop.comp.buf.k.sum()) < int(loop.comp.buf.cand_len.sum())
+
+
+@pytest.mark.parametrize("score", ["bf16", "f32"])
+@pytest.mark.parametrize("fmt", ["i8", "e4m3"])
+def test_how_far_given_lses_are_from_the_scores(fmt, score):
+    """A row's probabilities under hk_decode_attn8's own LSE: with K rounded to bf16 for the scores every score is
+    off by 2^-9 sum |q k| / sqrt(D) at most, and so the sum over the row by that factor; with fp32 copies they sum
+    to 1 within the score pass's own tolerance (1e-5; bf16 2e-3) and the LSE's."""
+    from paper_2606_28831_amd.pipeline import Compressor, Decoder
+    c, _, _ = _caches("f32", fmt)
+    q = _queries("bf16")[:1]
+    o, lse = torch.empty(NS, HKV * G, D, device=DEV), torch.empty(1, NS, HKV * G, device=DEV)
+    Decoder(NS, HKV * G, HKV, D, c.kv, c.alloc).attend(q[0], o, lse[0])
+    comp = Compressor(NS, HKV * G, HKV, D, 1, c.kv, c.alloc, 0.8, score_dtype=DT[score])
+    comp.score(q, row_lse_in=lse)
+    total = np.exp(np64(comp.buf.s_attn)).sum(1)                      # mean over the G rows of a head
+    for h in range(NS * HKV):
+        s, kv = divmod(h, HKV)
+        k, _, valid, _ = c.head(h)
+        zabs = (np.abs(np64(q[0, s, kv * G:kv * G + G])) @ np.abs(k[valid]).T).max() / np.sqrt(D)
+        bound = 3e-5 if score == "f32" else np.expm1(1.01 * 2.0 ** -9 * zabs) + 2e-3
+        assert abs(total[h] - 1) <= bound, (h, total[h], bound)
