@@ -20,10 +20,10 @@
 // with a reference of the sum's own, which follows x (a check in every tile instead: 1435 to 1495 us for 1400 to
 // 1460 of the prompts below).
 //
-// Measured on 8 prompts of 4096 tokens of 32 query heads, 8 KV heads of 128 dims, causal: 1403 to 1458 us, 755 to
-// 784 TFLOP/s, of which the conversion is 38; 1570 to 1625 with every unit converting its tiles, and 1136 without
+// Measured on 8 prompts of 4096 tokens of 32 query heads, 8 KV heads of 128 dims, causal: 1390 to 1510 us, 728 to
+// 791 TFLOP/s, of which the conversion is 38; 1570 to 1625 with every unit converting its tiles, and 1136 without
 // conversions and loads at all.  A bf16 matrix product of 8192^3 reaches 1236 TFLOP/s.  What bounds it is vector
-// work beside MFMA: the matrix units are busy for 34% of the cycles and the vector units for 51% (29 and 53 with
+// work beside MFMA: the matrix units are busy for 34% of the cycles and the vector units for 51% (28 and 52 with
 // every unit converting), waves wait for 34% of theirs, at two a SIMD.  P in two parts of bf16, 24 products a tile
 // instead of 16: 1930 us for 1673; one tile a barrier 1673 for 1575; converting between the computations of two
 // tiles 1660 to 1720; two tiles in one softmax spill (1767); 64 rows a wave, at one wave a SIMD, 2745; eight waves
@@ -530,9 +530,9 @@ int64_t hk_attn8_tile_units(int NS, int Hkv, int G, int n_tokens) {
   return ((int64_t)n_tokens * G / TILE8_ROWS + NS) * Hkv;
 }
 // Where chunks may be long, a launch before converts every tile once for all of its head's units, into the
-// workspace.  (32 / 8 heads of 128, without and with it: 8 prompts of 4096 tokens 1590 and 1403 us, of 1024 150 and
-// 143, of 512 62 and 62, of 256 55 and 59; chunks of 1024 tokens over 32000 1501 and 1482, of 512 760 and 770, of 128
-// 216 and 267: the tile kernel then reads twice the bytes.)
+// workspace.  (32 / 8 heads of 128, without and with it: 8 prompts of 4096 tokens 1613 and 1438 us, of 1024 153 and
+// 142, of 512 65 and 63, of 256 55 and 59; 2 chunks of 1024 tokens over 32000 1546 and 1502, of 512 781 and 775, of 128
+// 221 and 269; 8 of 64 over 4000 81 and 113: the tile kernel then reads twice the bytes.)
 constexpr int64_t READY_ROWS = 4096;
 constexpr size_t READY_MOST = (size_t)1 << 29;   // bytes of tiles at most
 static size_t ready_bytes(int D, int64_t heads, int max_pages, int64_t most) {
