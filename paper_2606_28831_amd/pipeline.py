@@ -13,7 +13,7 @@ from dataclasses import dataclass
 import torch
 
 from . import (Allocator, Chunks, PagedKV, PagedKV8, OP_APPEND, OP_DECODE8, OP_COMPACT, OP_DECODE, OP_RESERVE, OP_SCORE, OP_TRIM,
-               HardKVError, chunk_attn8_workspace, chunk_attn_workspace, dims, hk_chunk_attn8, hk_compact8,
+               HardKVError, _fits, chunk_attn8_workspace, chunk_attn_workspace, dims, hk_chunk_attn8, hk_compact8,
                hk_decode_attn8, hk_read_kv8, hk_write_kv8, hk_append_kv, hk_chunk_attn, hk_reserve_slots,
                hk_trim_slots, hk_verify_draft, hk_write_kv, verify_workspace,
                hk_budget_plan, hk_budget_select, hk_calibrate, hk_calibrate_solve_T,
@@ -58,6 +58,7 @@ class ScoringCopy:
     take it: a paged cache of its own whose rows lie one after the other, at most max_bytes of it."""
 
     def __init__(self, NS, Hq, Hkv, D, W, kv: PagedKV8, dtype=torch.bfloat16, max_bytes: int = 1 << 30):
+        _fits(dims(NS, Hq, Hkv, D, W), kv, NS * Hkv)
         dev, P = kv.k_pool.device, kv.max_pages
         row = P * 16 * D * dtype.itemsize * Hkv
         self.n = n = max(1, min(NS, max_bytes // row))

@@ -84,3 +84,17 @@ def test_arguments_of_another_shape_with_as_many_entries_go_on(hk):
                         (_q(BF, NS, W, Hq, D).transpose(0, 1), None, torch.zeros(NS, W, Hq).transpose(0, 1))):
         with pytest.raises(hk.HardKVError, match="outside the GPU"):
             comp.score(q, ref_slots=ref, row_lse_in=lse)
+
+
+def test_caches_of_fewer_rows_than_heads_are_refused(hk):
+    """(a row of tables alone would be spread over all heads)"""
+    from paper_2606_28831_amd.pipeline import BudgetCompressor, Compressor
+    for heads in (1, NS * HKV - 1):
+        kv, al = _cache(hk, heads=heads)
+        with pytest.raises(hk.HardKVError, match="fewer rows"):
+            Compressor(NS, HKV * G, HKV, D, W, kv, al, 0.8).score(_q(BF))
+        with pytest.raises(hk.HardKVError, match="fewer rows"):
+            BudgetCompressor(NS, HKV * G, HKV, D, W, kv, al, 0.8, 100, 200).select(_q(BF))
+    kv, al = _cache(hk)
+    with pytest.raises(hk.HardKVError, match="head size"):
+        Compressor(NS, HKV * G, HKV, 128, W, kv, al, 0.8).score(_q(BF, W, NS, HKV * G, 128))
